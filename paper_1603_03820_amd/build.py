@@ -34,14 +34,18 @@ def hipcc() -> str:
     return "hipcc"
 
 
+# the operators that answer with a trained model (include/als_serve.h): a library of its own
+SERVE_SRC = os.path.join(PKG, "csrc", "serve.hip")
+SERVE_LIB = os.path.join(PKG, "libals_serve.so")
 PEAKS_SRC = os.path.join(PKG, "csrc", "peaks.hip")
 PEAKS_LIB = os.path.join(PKG, "libpeaks.so")
 
 
 def build(verbose: bool = False) -> str:
-    """Compile libals.so and the bench's peak microbenchmarks (libpeaks.so) unconditionally (the
-    build check compiles every time); return the libals.so path."""
+    """Compile libals.so, libals_serve.so and the bench's peak microbenchmarks (libpeaks.so) unconditionally
+    (the build check compiles every time); return the libals.so path."""
     _compile(PEAKS_SRC, PEAKS_LIB, verbose)
+    _compile(SERVE_SRC, SERVE_LIB, verbose)
     return _compile(SRC, LIB, verbose)
 
 

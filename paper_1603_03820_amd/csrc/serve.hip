@@ -1,0 +1,711 @@
+// Answering with a trained factor model on gfx950 (MI355X): the C ABI of include/als_serve.h plus its kernels.
+//
+//   k_quantize   rows to 8-bit integers with one scale a row
+//   k_score      scores of users against items from 8-bit rows (integer matrix instructions)
+//   k_sample     one column a row from its scores: temperature, top-k, top-p, min-p, columns left out
+#include <hip/hip_bf16.h>
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <mutex>
+#include <new>
+
+#include "als_serve.h"
+
+namespace {
+
+typedef int i4 __attribute__((ext_vector_type(4)));
+
+constexpr int kWave = 64;
+
+struct F16 { uint16_t bits; };
+struct BF16 { uint16_t bits; };
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(F16 v) {
+    return (float)__builtin_bit_cast(_Float16, v.bits);
+}
+__device__ __forceinline__ float to_float(BF16 v) {
+    return __builtin_bit_cast(float, (uint32_t)v.bits << 16);
+}
+// The nearest value of the type, ties to even.
+__device__ __forceinline__ void from_float(float v, float* out) { *out = v; }
+__device__ __forceinline__ void from_float(float v, F16* out) {
+    *out = F16{__builtin_bit_cast(uint16_t, (_Float16)v)};
+}
+__device__ __forceinline__ void from_float(float v, BF16* out) {
+    *out = BF16{__builtin_bit_cast(uint16_t, (__bf16)v)};
+}
+
+// ------------------------------------------------------------------------------ quantize --
+
+constexpr int kQuantThreads = 256;
+
+// A wave a row: the largest magnitude, then the quotients, the row's second read from the cache.
+template <typename T>
+__global__ __launch_bounds__(kQuantThreads) void k_quantize(const T* __restrict__ x, int64_t of, int64_t ldx,
+                                                            const int32_t* __restrict__ users, int64_t rows,
+                                                            int f, int8_t* __restrict__ q, int64_t ldq,
+                                                            float* __restrict__ scale) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int64_t row = (int64_t)blockIdx.x * (kQuantThreads / kWave) + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    const int64_t src = users ? (int64_t)users[row] : row;
+    const bool there = src >= 0 && src < of;
+    const T* xr = x + (there ? src : 0) * ldx;
+    float a = 0.f;
+    bool finite = there;
+    if (there)
+        for (int k = lane; k < f; k += kWave) {
+            const float v = fabsf(to_float(xr[k]));
+            finite = finite && v < INFINITY;
+            a = fmaxf(a, v);
+        }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) a = fmaxf(a, __shfl_xor(a, d));
+    finite = __all(finite);
+    // 127 x past the largest float: a power of two off both sides changes no quotient
+    const float down = a > 1e36f ? 0x1p-8f : 1.f;
+    const float div = a * down;
+    int8_t* qr = q + row * ldq;
+    const int64_t pad = ((int64_t)f + 15) / 16 * 16;
+    const int end = (int)(pad < ldq ? pad : ldq);
+    for (int k = lane; k < end; k += kWave) {
+        float v = 0.f;
+        if (finite && a > 0.f && k < f) v = rintf((to_float(xr[k]) * down) * 127.f / div);
+        qr[k] = (int8_t)v;
+    }
+    if (lane == 0) scale[row] = finite ? a * (1.f / 127.f) : NAN;
+}
+
+// --------------------------------------------------------------------------------- score --
+
+// Sixteen values of a row from column k on, zeros past column f (any alignment).
+__device__ __forceinline__ i4 load16(const int8_t* row, int k, int f) {
+    i4 v = {0, 0, 0, 0};
+    if (k + 16 <= f) {
+        __builtin_memcpy(&v, row + k, 16);
+    } else if (k < f) {
+        uint32_t w[4] = {0, 0, 0, 0};
+        for (int b = 0; b < 16; ++b)
+            if (k + b < f) w[b >> 2] |= (uint32_t)(uint8_t)row[k + b] << (8 * (b & 3));
+        v = i4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+    }
+    return v;
+}
+
+constexpr int kScoreThreads = 256;
+constexpr int kScoreTiles = 4;                                   // 16-item tiles of a wave
+constexpr int kScoreItems = 16 * kScoreTiles * (kScoreThreads / kWave);
+
+// A wave: 16 users x 64 items by v_mfma_i32_16x16x64_i8, the items as the first operand, so that a lane
+// holds four neighbouring items of one user (C layout: column l & 15, rows 4 (l >> 4) + r).
+template <typename T>
+__global__ __launch_bounds__(kScoreThreads) void k_score(const int8_t* __restrict__ xq, int64_t ldx,
+                                                         const float* __restrict__ xs, int64_t m,
+                                                         const int8_t* __restrict__ tq, int64_t ldt,
+                                                         const float* __restrict__ ts, int64_t n, int f,
+                                                         T* __restrict__ out, int64_t ldo, int64_t item_blocks) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int64_t i0 = (int64_t)blockIdx.x / item_blocks * 16;
+    const int64_t j0 = (int64_t)blockIdx.x % item_blocks * kScoreItems + (threadIdx.x >> 6) * (16 * kScoreTiles);
+    const int64_t i = i0 + (lane & 15);
+    i4 acc[kScoreTiles];
+#pragma unroll
+    for (int t = 0; t < kScoreTiles; ++t) acc[t] = i4{0, 0, 0, 0};
+    for (int k = 16 * (lane >> 4); k < (f + 63) / 64 * 64; k += 64) {
+        const i4 b = i < m ? load16(xq + i * ldx, k, f) : i4{0, 0, 0, 0};
+#pragma unroll
+        for (int t = 0; t < kScoreTiles; ++t) {
+            const int64_t j = j0 + 16 * t + (lane & 15);
+            const i4 a = j < n ? load16(tq + j * ldt, k, f) : i4{0, 0, 0, 0};
+            acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, acc[t], 0, 0, 0);
+        }
+    }
+    if (i >= m) return;
+    const float s = xs[i];
+#pragma unroll
+    for (int t = 0; t < kScoreTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t j = j0 + 16 * t + 4 * (lane >> 4) + r;
+            if (j < n) from_float((float)acc[t][r] * s * ts[j], out + i * ldo + j);
+        }
+}
+
+// -------------------------------------------------------------------------------- sample --
+
+constexpr int kSampleThreads = 1024;
+constexpr int kSampleWaves = kSampleThreads / kWave;
+constexpr int kBins = 2048;
+constexpr int kList = 1024;              // candidates that are ranked one against another
+constexpr int kChunk = 1 << 19;          // columns whose left-out bits are held at a time (64 KB)
+
+struct Limits {
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    float temperature_all;
+    int32_t top_k_all;
+    float top_p_all;
+    float min_p_all;
+};
+
+// Larger scores have larger keys; -0 has +0's.
+__device__ __forceinline__ uint32_t key_of(float z) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, z + 0.f);
+    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float score_of(uint32_t key) {
+    const uint32_t b = key & 0x80000000u ? key ^ 0x80000000u : ~key;
+    return __builtin_bit_cast(float, b);
+}
+
+// floor(2^40 e), 0 <= e <= 1; NaN gives 0.
+__device__ __forceinline__ uint64_t fixed40(float e) {
+    if (!(e > 0.f)) return 0;
+    const uint32_t b = __builtin_bit_cast(uint32_t, e);
+    const uint64_t mant = (b & 0x7FFFFFu) | 0x800000u;
+    const int shift = (int)(b >> 23) - 110;
+    return shift >= 0 ? mant << shift : (shift > -32 ? mant >> -shift : 0);
+}
+
+// floor(total part / 2^24), part <= 2^24, total < 2^62.
+__device__ __forceinline__ uint64_t share_of(uint64_t total, uint32_t part) {
+    return (total >> 24) * part + (((total & 0xFFFFFFu) * part) >> 24);
+}
+
+__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) {
+    const uint32_t lo = __shfl_up((uint32_t)v, d), hi = __shfl_up((uint32_t)(v >> 32), d);
+    return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t shfl64(uint64_t v, int lane) {
+    const uint32_t lo = __shfl((uint32_t)v, lane), hi = __shfl((uint32_t)(v >> 32), lane);
+    return (uint64_t)hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t scan64(uint64_t v) {   // inclusive, over the wave
+    const int lane = threadIdx.x & (kWave - 1);
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const uint64_t o = shfl_up64(v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+struct SampleShared {
+    uint64_t mass[kBins];
+    uint32_t count[kBins];
+    uint32_t list_d[kList];
+    uint32_t list_i[kList];
+    uint64_t wave64[kSampleWaves + 1];
+    uint32_t wave_a[kSampleWaves], wave_b[kSampleWaves], wave_c[kSampleWaves];
+    uint32_t found_bin, found_count, listed;
+    uint64_t found_before;
+    uint32_t cut_d, cut_i;
+    uint64_t before;
+    uint32_t bits[1];   // the columns left out, one bit each
+};
+
+// One row in the hands of one workgroup.
+template <typename T>
+struct Row {
+    const T* z;
+    int64_t n;
+    const int32_t* rated;
+    int64_t rated_count;
+    SampleShared* sh;
+    uint32_t best;      // the largest key
+    float top, inv_t;
+    bool one_chunk;
+
+    // Marks the left-out columns of [c0, c1).
+    __device__ void mark(int64_t c0, int64_t c1) {
+        __syncthreads();
+        for (int64_t w = threadIdx.x; w < (c1 - c0 + 31) / 32; w += kSampleThreads) sh->bits[w] = 0;
+        __syncthreads();
+        for (int64_t k = threadIdx.x; k < rated_count; k += kSampleThreads) {
+            const int64_t c = rated[k];
+            if (c >= c0 && c < c1) atomicOr(&sh->bits[(c - c0) >> 5], 1u << ((c - c0) & 31));
+        }
+        __syncthreads();
+    }
+
+    // fn(column, key) for every allowed column.
+    template <typename Fn>
+    __device__ void each(Fn fn) {
+        for (int64_t c0 = 0; c0 < n; c0 += kChunk) {
+            const int64_t c1 = c0 + kChunk < n ? c0 + kChunk : n;
+            if (rated_count > 0 && !one_chunk) mark(c0, c1);
+            for (int64_t c = c0 + threadIdx.x; c < c1; c += kSampleThreads) {
+                const float v = to_float(z[c]);
+                if (!(v > -INFINITY)) continue;
+                if (rated_count > 0 && (sh->bits[(c - c0) >> 5] >> ((c - c0) & 31) & 1)) continue;
+                fn(c, key_of(v));
+            }
+        }
+    }
+
+    __device__ float exp_of(uint32_t d) const {
+        const float v = score_of(best - d);
+        const float x = d == 0 ? 0.f : (v - top) * inv_t;
+        return expf(x);
+    }
+    __device__ uint64_t weight_of(uint32_t d) const { return fixed40(exp_of(d)); }
+};
+
+// Sums over the workgroup, to every thread.
+__device__ uint64_t block_sum(uint64_t v, SampleShared* sh) {
+    const uint64_t s = scan64(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) sh->wave64[threadIdx.x >> 6] = s;
+    __syncthreads();
+    uint64_t total = 0;
+    for (int w = 0; w < kSampleWaves; ++w) total += sh->wave64[w];
+    return total;
+}
+
+// A place in the order (score descending, column ascending): columns up to and with (d, column).
+struct Cut {
+    uint32_t d;
+    uint32_t column;
+    __device__ bool keeps(uint32_t dd, int64_t c) const {
+        return dd < d || (dd == d && (uint32_t)c <= column);
+    }
+};
+
+// The first column, by column number, at which the running sum of measure(column, d) exceeds t (the sum
+// over all columns does).
+template <typename T, typename Fn>
+__device__ uint32_t find_column(Row<T>& row, uint64_t t, Fn measure) {
+    SampleShared* sh = row.sh;
+    uint64_t before = 0;
+    for (int64_t c0 = 0; c0 < row.n; c0 += kChunk) {
+        const int64_t c1 = c0 + kChunk < row.n ? c0 + kChunk : row.n;
+        if (row.rated_count > 0 && !row.one_chunk) row.mark(c0, c1);
+        for (int64_t b0 = c0; b0 < c1; b0 += kSampleThreads) {
+            const int64_t c = b0 + threadIdx.x;
+            uint64_t v = 0;
+            if (c < c1) {
+                const float z = to_float(row.z[c]);
+                if (z > -INFINITY &&
+                    !(row.rated_count > 0 && (sh->bits[(c - c0) >> 5] >> ((c - c0) & 31) & 1)))
+                    v = measure(c, row.best - key_of(z));
+            }
+            const uint64_t s = scan64(v);
+            __syncthreads();
+            if ((threadIdx.x & 63) == 63) sh->wave64[threadIdx.x >> 6] = s;
+            if (threadIdx.x == 0) sh->cut_i = 0xFFFFFFFFu;
+            __syncthreads();
+            uint64_t mine = before;
+            for (int w = 0; w < kSampleWaves; ++w) {
+                if (w == (int)(threadIdx.x >> 6)) mine = before;
+                before += sh->wave64[w];
+            }
+            if (v > 0 && mine + s > t && mine + s - v <= t) sh->cut_i = (uint32_t)c;
+            __syncthreads();
+            if (sh->cut_i != 0xFFFFFFFFu) return sh->cut_i;
+        }
+    }
+    return 0xFFFFFFFFu;
+}
+
+// The last column, in the order, with less than `target` of the measure before it; among the columns that
+// `within` keeps.  BY_MASS: the measure is the weight, else 1.  target >= 1 and at most the sum.
+template <bool BY_MASS, typename T>
+__device__ Cut select_cut(Row<T>& row, Cut within, uint32_t widest, uint64_t target) {
+    SampleShared* sh = row.sh;
+    uint64_t before = 0;                       // measure in front of the range
+    uint32_t lo = 0, hi = widest;              // the range of distances
+    for (;;) {
+        int shift = 0;
+        while (((hi - lo) >> shift) >= kBins) ++shift;
+        __syncthreads();
+        for (int b = threadIdx.x; b < kBins; b += kSampleThreads) { sh->mass[b] = 0; sh->count[b] = 0; }
+        __syncthreads();
+        row.each([&](int64_t c, uint32_t key) {
+            const uint32_t d = row.best - key;
+            if (d < lo || d > hi || !within.keeps(d, c)) return;
+            const uint32_t b = (d - lo) >> shift;
+            atomicAdd(&sh->count[b], 1u);
+            if (BY_MASS) {
+                const uint64_t w = row.weight_of(d);
+                if (w) atomicAdd((unsigned long long*)&sh->mass[b], (unsigned long long)w);
+            }
+        });
+        __syncthreads();
+        // the bin in which the measure reaches the target: two bins a thread
+        const int b = 2 * threadIdx.x;
+        const uint64_t v0 = BY_MASS ? sh->mass[b] : sh->count[b], v1 = BY_MASS ? sh->mass[b + 1] : sh->count[b + 1];
+        const uint64_t s = scan64(v0 + v1);
+        if ((threadIdx.x & 63) == 63) sh->wave64[threadIdx.x >> 6] = s;
+        __syncthreads();
+        uint64_t at = before;
+        for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) at += sh->wave64[w];
+        at += s - (v0 + v1);
+        if (at < target && target <= at + v0) {
+            sh->found_bin = b; sh->found_before = at; sh->found_count = sh->count[b];
+        } else if (at + v0 < target && target <= at + v0 + v1) {
+            sh->found_bin = b + 1; sh->found_before = at + v0; sh->found_count = sh->count[b + 1];
+        }
+        if (threadIdx.x == 0) sh->listed = 0;
+        __syncthreads();
+        before = sh->found_before;
+        lo = lo + (sh->found_bin << shift);
+        const uint32_t end = shift ? lo + ((1u << shift) - 1) : lo;
+        hi = end < hi && end >= lo ? end : hi;
+        const uint32_t count = sh->found_count;
+        if (count <= kList) {
+            row.each([&](int64_t c, uint32_t key) {
+                const uint32_t d = row.best - key;
+                if (d < lo || d > hi || !within.keeps(d, c)) return;
+                const uint32_t at = atomicAdd(&sh->listed, 1u);
+                sh->list_d[at] = d;
+                sh->list_i[at] = (uint32_t)c;
+            });
+            __syncthreads();
+            if (threadIdx.x < count) {
+                const uint32_t d = sh->list_d[threadIdx.x], i = sh->list_i[threadIdx.x];
+                uint64_t front = before;
+                for (uint32_t k = 0; k < count; ++k) {
+                    const uint32_t dk = sh->list_d[k];
+                    if (dk < d || (dk == d && sh->list_i[k] < i)) front += BY_MASS ? row.weight_of(dk) : 1;
+                }
+                const uint64_t own = BY_MASS ? row.weight_of(d) : 1;
+                if (front < target && target <= front + own) { sh->cut_d = d; sh->cut_i = i; }
+            }
+            __syncthreads();
+            const Cut cut{sh->cut_d, sh->cut_i};
+            __syncthreads();
+            return cut;
+        }
+        if (lo == hi) {    // equal scores: as many of them, by column, as reach the target
+            const uint64_t own = BY_MASS ? row.weight_of(lo) : 1;
+            const uint64_t keep = (target - before + own - 1) / own;
+            const uint32_t d = lo;
+            const uint32_t c = find_column(row, keep - 1, [&](int64_t cc, uint32_t dd) -> uint64_t {
+                return dd == d && within.keeps(dd, cc) ? 1 : 0;
+            });
+            __syncthreads();
+            return Cut{d, c};
+        }
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kSampleThreads) void k_sample(const T* __restrict__ z, int64_t rows, int64_t n,
+                                                           int64_t ldz, Limits lim, const float* __restrict__ u,
+                                                           const int64_t* __restrict__ rated_ptr,
+                                                           const int32_t* __restrict__ rated_idx,
+                                                           const int32_t* __restrict__ users, int64_t of,
+                                                           int32_t* __restrict__ index, float* __restrict__ log) {
+    extern __shared__ unsigned char shared[];
+    SampleShared* sh = (SampleShared*)shared;
+    const int64_t r = blockIdx.x;
+    Row<T> row;
+    row.z = z + r * ldz;
+    row.n = n;
+    row.sh = sh;
+    row.rated = nullptr;
+    row.rated_count = 0;
+    row.one_chunk = n <= kChunk;
+    if (rated_ptr) {
+        const int64_t src = users ? (int64_t)users[r] : r;
+        if (src < 0 || src >= of) {
+            if (threadIdx.x == 0) { index[r] = -1; if (log) log[r] = NAN; }
+            return;
+        }
+        row.rated = rated_idx + rated_ptr[src];
+        row.rated_count = rated_ptr[src + 1] - rated_ptr[src];
+        if (row.rated_count > 0 && row.one_chunk) row.mark(0, n);
+    }
+    // the largest and the least key, and the number of allowed columns
+    uint32_t hi = 0, lo = 0xFFFFFFFFu, count = 0;
+    row.each([&](int64_t, uint32_t key) { hi = max(hi, key); lo = min(lo, key); ++count; });
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        hi = max(hi, (uint32_t)__shfl_xor(hi, d));
+        lo = min(lo, (uint32_t)__shfl_xor(lo, d));
+        count += __shfl_xor(count, d);
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+        const int w = threadIdx.x >> 6;
+        sh->wave_a[w] = hi; sh->wave_b[w] = lo; sh->wave_c[w] = count;
+    }
+    __syncthreads();
+    hi = 0; lo = 0xFFFFFFFFu; count = 0;
+    for (int w = 0; w < kSampleWaves; ++w) {
+        hi = max(hi, sh->wave_a[w]); lo = min(lo, sh->wave_b[w]); count += sh->wave_c[w];
+    }
+    if (count == 0) {
+        if (threadIdx.x == 0) { index[r] = -1; if (log) log[r] = -INFINITY; }
+        return;
+    }
+    const float t = lim.temperature ? lim.temperature[r] : lim.temperature_all;
+    const bool greedy = !(t > 0.f);
+    row.best = hi;
+    row.top = score_of(hi);
+    row.inv_t = greedy ? 1.f : 1.f / t;
+    const int k = lim.top_k ? lim.top_k[r] : lim.top_k_all;
+    const float p = lim.top_p ? lim.top_p[r] : lim.top_p_all;
+    const float least = lim.min_p ? lim.min_p[r] : lim.min_p_all;
+    const float least_e = least > 0.f ? fminf(least, 1.f) : 0.f;
+    const uint32_t widest = hi - lo;
+    Cut cut{widest, 0xFFFFFFFFu};
+    if (greedy) {
+        const uint32_t c = find_column(row, 0, [](int64_t, uint32_t d) -> uint64_t { return d == 0; });
+        if (threadIdx.x == 0) { index[r] = (int32_t)c; if (log) log[r] = 0.f; }
+        return;
+    }
+    if (k > 0 && (uint32_t)k < count) cut = select_cut<false>(row, cut, cut.d, (uint64_t)k);
+    if (p < 1.f) {
+        uint64_t sum = 0;
+        row.each([&](int64_t c, uint32_t key) {
+            if (cut.keeps(hi - key, c)) sum += row.weight_of(hi - key);
+        });
+        sum = block_sum(sum, sh);
+        const uint32_t part = p > 0.f ? (uint32_t)(p * 0x1p24f) : 0;
+        uint64_t target = share_of(sum, part);
+        if (target < 1) target = 1;
+        cut = select_cut<true>(row, cut, cut.d, target);
+    }
+    auto weight = [&](int64_t c, uint32_t d) -> uint64_t {
+        if (!cut.keeps(d, c)) return 0;
+        const float e = row.exp_of(d);
+        return e >= least_e ? fixed40(e) : 0;
+    };
+    uint64_t sum = 0;
+    row.each([&](int64_t c, uint32_t key) { sum += weight(c, hi - key); });
+    sum = block_sum(sum, sh);
+    float uu = u[r];
+    uu = uu > 0.f ? fminf(uu, 1.f - 0x1p-24f) : 0.f;
+    const uint32_t c = find_column(row, share_of(sum, (uint32_t)(uu * 0x1p24f)), weight);
+    if (threadIdx.x == 0) {
+        index[r] = (int32_t)c;
+        if (log) {
+            const float v = to_float(row.z[c]);
+            const uint32_t d = hi - key_of(v);
+            const float x = d == 0 ? 0.f : (v - row.top) * row.inv_t;
+            log[r] = x - logf((float)sum * 0x1p-40f);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------- host --
+
+bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+size_t type_bytes(int dtype) { return dtype == ALS_F32 ? 4 : 2; }
+
+// Bytes from the first element of a strided matrix to past its last.
+uint64_t span_of(int64_t rows, int64_t cols, int64_t ld, size_t bytes) {
+    return rows <= 0 || cols <= 0 ? 0 : ((uint64_t)(rows - 1) * (uint64_t)ld + (uint64_t)cols) * bytes;
+}
+
+bool overlap(const void* a, uint64_t an, const void* b, uint64_t bn) {
+    if (!a || !b || an == 0 || bn == 0) return false;
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y + bn && y < x + an;
+}
+
+struct DeviceGuard {
+    int prev = -1;
+    bool ok = false;
+    explicit DeviceGuard(int dev) {
+        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+        ok = (prev == dev) || hipSetDevice(dev) == hipSuccess;
+    }
+    ~DeviceGuard() {
+        int cur = -1;
+        if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
+    }
+};
+
+// What a device is: asked for once per device and process.
+constexpr int kMaxDevices = 64;
+struct DeviceInfo {
+    std::mutex mu;
+    bool known = false;
+    int cus = 0;
+};
+DeviceInfo g_device[kMaxDevices];
+
+int query_device(int device, int* cus) {
+    int count = 0;
+    if (hipGetDeviceCount(&count) != hipSuccess || device < 0 || device >= count || device >= kMaxDevices)
+        return ALS_ERR_DEVICE;
+    DeviceInfo& d = g_device[device];
+    std::lock_guard<std::mutex> lock(d.mu);
+    if (!d.known) {
+        hipDeviceProp_t prop;
+        if (hipGetDeviceProperties(&prop, device) != hipSuccess) return ALS_ERR_DEVICE;
+        if (strncmp(prop.gcnArchName, "gfx950", 6) != 0) return ALS_ERR_DEVICE;
+        d.cus = prop.multiProcessorCount;
+        d.known = true;
+    }
+    *cus = d.cus;
+    return ALS_OK;
+}
+
+constexpr size_t kWorkspaceBytes = 64u << 20;
+
+}  // namespace
+
+struct als_serve_ctx {
+    int device;
+    int cus;
+    unsigned char* ws;
+    size_t ws_bytes;
+    int last_hip;
+};
+
+namespace {
+
+int finish(als_serve_ctx* ctx) {
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return ALS_OK;
+    ctx->last_hip = (int)e;
+    return ALS_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t als_serve_workspace_bytes(int device) {
+    int cus = 0;
+    return query_device(device, &cus) == ALS_OK ? kWorkspaceBytes : 0;
+}
+
+int als_serve_init(als_serve_ctx** out, int device, void* workspace, size_t workspace_bytes) {
+    if (!out) return ALS_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!workspace) return ALS_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return ALS_ERR_ALIGN;
+    int cus = 0;
+    if (const int rc = query_device(device, &cus); rc != ALS_OK) return rc;
+    if (workspace_bytes < kWorkspaceBytes) return ALS_ERR_WORKSPACE;
+    als_serve_ctx* ctx = new (std::nothrow) als_serve_ctx();
+    if (!ctx) return ALS_ERR_INVALID_ARG;
+    ctx->device = device;
+    ctx->cus = cus;
+    ctx->ws = (unsigned char*)workspace;
+    ctx->ws_bytes = workspace_bytes;
+    ctx->last_hip = 0;
+    *out = ctx;
+    return ALS_OK;
+}
+
+int als_serve_destroy(als_serve_ctx* ctx) {
+    delete ctx;
+    return ALS_OK;
+}
+
+int als_serve_last_hip_error(const als_serve_ctx* ctx) { return ctx ? ctx->last_hip : 0; }
+
+int als_quantize(als_serve_ctx* ctx, const void* x, int32_t dtype, int64_t of, int64_t ldx, const int32_t* users,
+                 int64_t rows, int32_t f, int8_t* q, int64_t ldq, float* scale, void* stream) {
+    if (!ctx || of < 0 || rows < 0 || dtype < ALS_F32 || dtype > ALS_BF16) return ALS_ERR_INVALID_ARG;
+    if (f < 1 || f > ALS_SERVE_F_MAX) return ALS_ERR_UNSUPPORTED_F;
+    if (ldx < f || ldq < f || (!users && rows > of)) return ALS_ERR_INVALID_ARG;
+    if (rows == 0) return ALS_OK;
+    if (!q || !scale || (of > 0 && !x)) return ALS_ERR_INVALID_ARG;
+    if (!aligned(x, type_bytes(dtype)) || !aligned(users, 4) || !aligned(scale, 4)) return ALS_ERR_ALIGN;
+    const int64_t pad = ((int64_t)f + 15) / 16 * 16;
+    const uint64_t xn = span_of(of, f, ldx, type_bytes(dtype));
+    const uint64_t qn = span_of(rows, pad < ldq ? pad : ldq, ldq, 1), sn = (uint64_t)rows * 4;
+    if (overlap(q, qn, x, xn) || overlap(scale, sn, x, xn) || overlap(q, qn, scale, sn) ||
+        overlap(q, qn, users, sn) || overlap(scale, sn, users, sn))
+        return ALS_ERR_ALIAS;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return ALS_ERR_DEVICE;
+    const int64_t per = kQuantThreads / kWave, blocks = (rows + per - 1) / per;
+    if (blocks > INT32_MAX) return ALS_ERR_INVALID_ARG;
+    const auto launch = [&](auto* p) {
+        using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
+        hipLaunchKernelGGL(k_quantize<T>, dim3((unsigned)blocks), dim3(kQuantThreads), 0, (hipStream_t)stream, p,
+                           of, ldx, users, rows, f, q, ldq, scale);
+    };
+    if (dtype == ALS_F32) launch((const float*)x);
+    else if (dtype == ALS_F16) launch((const F16*)x);
+    else launch((const BF16*)x);
+    return finish(ctx);
+}
+
+int als_score(als_serve_ctx* ctx, const int8_t* xq, int64_t ldx, const float* xs, int64_t m, const int8_t* tq,
+              int64_t ldt, const float* ts, int64_t n, int32_t f, void* out, int32_t dtype, int64_t ldo,
+              void* stream) {
+    if (!ctx || m < 0 || n < 0 || dtype < ALS_F32 || dtype > ALS_BF16) return ALS_ERR_INVALID_ARG;
+    if (f < 1 || f > ALS_SERVE_F_MAX) return ALS_ERR_UNSUPPORTED_F;
+    if (ldx < f || ldt < f || ldo < n) return ALS_ERR_INVALID_ARG;
+    if (m == 0 || n == 0) return ALS_OK;
+    if (!xq || !xs || !tq || !ts || !out) return ALS_ERR_INVALID_ARG;
+    if (!aligned(xs, 4) || !aligned(ts, 4) || !aligned(out, type_bytes(dtype))) return ALS_ERR_ALIGN;
+    const uint64_t on = span_of(m, n, ldo, type_bytes(dtype));
+    if (overlap(out, on, xq, span_of(m, f, ldx, 1)) || overlap(out, on, tq, span_of(n, f, ldt, 1)) ||
+        overlap(out, on, xs, (uint64_t)m * 4) || overlap(out, on, ts, (uint64_t)n * 4))
+        return ALS_ERR_ALIAS;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return ALS_ERR_DEVICE;
+    const int64_t item_blocks = (n + kScoreItems - 1) / kScoreItems, user_blocks = (m + 15) / 16;
+    if (item_blocks > INT32_MAX / user_blocks) return ALS_ERR_INVALID_ARG;
+    const auto launch = [&](auto* p) {
+        using T = std::remove_pointer_t<decltype(p)>;
+        hipLaunchKernelGGL(k_score<T>, dim3((unsigned)(item_blocks * user_blocks)), dim3(kScoreThreads), 0,
+                           (hipStream_t)stream, xq, ldx, xs, m, tq, ldt, ts, n, f, p, ldo, item_blocks);
+    };
+    if (dtype == ALS_F32) launch((float*)out);
+    else if (dtype == ALS_F16) launch((F16*)out);
+    else launch((BF16*)out);
+    return finish(ctx);
+}
+
+int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, int64_t n, int64_t ldz,
+               const als_sample_limits* limits, const float* u, const int64_t* rated_ptr,
+               const int32_t* rated_idx, const int32_t* users, int64_t of, int32_t* index, float* log,
+               void* stream) {
+    if (!ctx || !limits || rows < 0 || n < 0 || n > ALS_SERVE_N_MAX || dtype < ALS_F32 || dtype > ALS_BF16 ||
+        ldz < n || of < 0)
+        return ALS_ERR_INVALID_ARG;
+    if (rows == 0) return ALS_OK;
+    if (!u || !index || (n > 0 && !z) || rows > INT32_MAX) return ALS_ERR_INVALID_ARG;
+    if (!rated_ptr != !rated_idx || (users && !rated_ptr) || (rated_ptr && !users && of < rows))
+        return ALS_ERR_INVALID_ARG;
+    const als_sample_limits& l = *limits;
+    if (!aligned(z, type_bytes(dtype)) || !aligned(u, 4) || !aligned(rated_ptr, 8) || !aligned(rated_idx, 4) ||
+        !aligned(users, 4) || !aligned(index, 4) || !aligned(log, 4) || !aligned(l.temperature, 4) ||
+        !aligned(l.top_k, 4) || !aligned(l.top_p, 4) || !aligned(l.min_p, 4))
+        return ALS_ERR_ALIGN;
+    const uint64_t rn = (uint64_t)rows * 4;
+    const void* outs[2] = {index, log};
+    for (const void* o : outs)
+        if (overlap(o, rn, z, span_of(rows, n, ldz, type_bytes(dtype))) || overlap(o, rn, u, rn) ||
+            overlap(o, rn, rated_ptr, ((uint64_t)of + 1) * 8) || overlap(o, rn, users, rn) ||
+            overlap(o, rn, l.temperature, rn) || overlap(o, rn, l.top_k, rn) || overlap(o, rn, l.top_p, rn) ||
+            overlap(o, rn, l.min_p, rn))
+            return ALS_ERR_ALIAS;
+    if (overlap(index, rn, log, rn)) return ALS_ERR_ALIAS;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return ALS_ERR_DEVICE;
+    const Limits lim{l.temperature, l.top_k, l.top_p, l.min_p, l.temperature_all, l.top_k_all, l.top_p_all,
+                     l.min_p_all};
+    const int64_t bits = rated_ptr ? (n < kChunk ? n : kChunk) : 0;
+    const size_t lds = sizeof(SampleShared) + (size_t)((bits + 31) / 32) * 4;
+    const auto launch = [&](auto* p) {
+        using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
+        (void)hipFuncSetAttribute((const void*)k_sample<T>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        hipLaunchKernelGGL(k_sample<T>, dim3((unsigned)rows), dim3(kSampleThreads), lds, (hipStream_t)stream, p,
+                           rows, n, ldz, lim, u, rated_ptr, rated_idx, users, of, index, log);
+    };
+    if (dtype == ALS_F32) launch((const float*)z);
+    else if (dtype == ALS_F16) launch((const F16*)z);
+    else launch((const BF16*)z);
+    return finish(ctx);
+}
+
+}  // extern "C"
