@@ -12,6 +12,7 @@
 #include <cstring>
 #include <mutex>
 #include <new>
+#include <type_traits>
 
 #include "als_serve.h"
 
@@ -134,6 +135,180 @@ __global__ __launch_bounds__(kScoreThreads) void k_score(const int8_t* __restric
             const int64_t j = j0 + 16 * t + 4 * (lane >> 4) + r;
             if (j < n) from_float((float)acc[t][r] * s * ts[j], out + i * ldo + j);
         }
+}
+
+// The product in tiles: a workgroup of WU x WI waves holds a tile of users x items, each wave FU x FI
+// fragments of 16 x 16, and walks f in steps of 128.  A step's rows of both sides lie in LDS, 128 bytes a row, while
+// the next step's arrive straight from memory in the other half (buffer_load ... lds: no registers, no
+// instructions but the load).  The 16-byte group c of row r lies in slot c ^ (r / 2 % 8), so that the 16 rows of
+// one operand read spread over all banks.
+constexpr int kStep = 128;
+constexpr int64_t kTileStride = 1 << 22;        // row strides below it keep a tile's offsets below 2^30 ...
+constexpr uint32_t kPastEnd = 0x7FFFFFF0u;      // ... and this past every tile's end
+
+template <int WU, int WI, int FU, int FI>
+struct Tiles {
+    static constexpr int kWaves = WU * WI;
+    static constexpr int kUsers = WU * FU * 16, kItems = WI * FI * 16;
+    static constexpr int kRows = kUsers + kItems;
+    static constexpr int kLoads = kRows / 8 / kWaves;      // 1 KB loads of a wave and step
+    static constexpr int kStage = kRows * kStep;           // bytes
+    static_assert(kRows % (8 * kWaves) == 0 && (kUsers / 8) % kLoads == 0, "a load has rows of one side");
+};
+
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+// A buffer of `bytes` bytes from `base` on (both the same in every lane).
+__device__ __forceinline__ i4 buffer_of(const void* base, uint32_t bytes) {
+    const uint64_t b = (uint64_t)base;
+    i4 r;
+    r[0] = __builtin_amdgcn_readfirstlane((uint32_t)b);
+    r[1] = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32) & 0xFFFFu);
+    r[2] = __builtin_amdgcn_readfirstlane(bytes);
+    r[3] = 0x00020000;
+    return r;
+}
+
+// 16 bytes a lane from buffer + voffset + soffset to LDS at `lds` + 16 lane.  Inline assembly: the compiler would
+// wait for every load to LDS before any LDS read.  It has no result register; the caller waits
+// (settle) before the data are read.  M0 needs one wait state.
+__device__ __forceinline__ void load_to_lds(i4 buffer, uint32_t voffset, uint32_t soffset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+                 :
+                 : "v"(voffset), "s"(buffer), "s"(soffset), "s"(lds)
+                 : "memory");
+}
+// All of this wave's loads have arrived and its LDS reads are done.
+__device__ __forceinline__ void settle() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
+// The bytes of the group at k that lie before f.
+__device__ __forceinline__ i4 keep_bytes(i4 v, int k, int f) {
+    const int left = f - k;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        const int bytes = left - 4 * d;
+        v[d] &= bytes >= 4 ? -1 : (bytes > 0 ? (1 << (8 * bytes)) - 1 : 0);
+    }
+    return v;
+}
+
+// Tile t of a grid of tu x ti: the eight dies take workgroups in turn, so each gets a run of tiles of its own, and
+// runs go down eight tiles of users before the next of items (their rows stay in the die's L2).
+__device__ __forceinline__ void tile_of(uint32_t t, uint32_t tu, uint32_t ti, uint32_t* u, uint32_t* i) {
+    const uint32_t total = tu * ti, per = total / 8;
+    if (t < per * 8) t = (t % 8) * per + t / 8;
+    const uint32_t band = 8 * ti, b = t / band, left = t % band;
+    const uint32_t high = tu - 8 * b < 8 ? tu - 8 * b : 8;
+    *u = 8 * b + left % high;
+    *i = left / high;
+}
+
+template <typename T, int WU, int WI, int FU, int FI>
+__global__ __launch_bounds__(64 * WU * WI) void k_score_tiles(
+    const int8_t* __restrict__ xq, int64_t ldx, const float* __restrict__ xs, int64_t m,
+    const int8_t* __restrict__ tq, int64_t ldt, const float* __restrict__ ts, int64_t n, int f,
+    T* __restrict__ out, int64_t ldo, uint32_t tu, uint32_t ti) {
+    using C = Tiles<WU, WI, FU, FI>;
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t tile_u, tile_i;
+    tile_of(blockIdx.x, tu, ti, &tile_u, &tile_i);
+    const int64_t u0 = (int64_t)tile_u * C::kUsers, i0 = (int64_t)tile_i * C::kItems;
+
+    // this wave's loads are of one side: rows first .. first + 8 kLoads - 1 of the stage
+    const int first = wave * C::kLoads * 8;
+    const bool of_users = first < C::kUsers;
+    const int64_t ld = of_users ? ldx : ldt;
+    const int64_t left = of_users ? m - u0 : n - i0;
+    const int64_t span = (left < (of_users ? C::kUsers : C::kItems) ? left : (of_users ? C::kUsers : C::kItems)) * ld;
+    const i4 buffer = buffer_of((of_users ? xq + u0 * ldx : tq + i0 * ldt),
+                                (uint32_t)(span - ld + (f + 15) / 16 * 16));
+    uint32_t voffset[C::kLoads];
+#pragma unroll
+    for (int l = 0; l < C::kLoads; ++l) {
+        const int r = first + 8 * l + (lane >> 3);
+        voffset[l] = (uint32_t)((r - (of_users ? 0 : C::kUsers)) * ld) + 16 * ((lane & 7) ^ (r >> 1 & 7));
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+    const int steps = (f + kStep - 1) / kStep;
+    const auto fetch = [&](int step) {
+        const uint32_t to = lds0 + (step & 1) * C::kStage + first * kStep;
+        if (step + 1 < steps) {
+#pragma unroll
+            for (int l = 0; l < C::kLoads; ++l)
+                load_to_lds(buffer, voffset[l], step * kStep, __builtin_amdgcn_readfirstlane(to + l * 1024));
+        } else {   // groups past f are not read: their offset is past the buffer's end
+#pragma unroll
+            for (int l = 0; l < C::kLoads; ++l) {
+                const int r = first + 8 * l + (lane >> 3);
+                const bool in = step * kStep + 16 * ((lane & 7) ^ (r >> 1 & 7)) < f;
+                load_to_lds(buffer, in ? voffset[l] : kPastEnd, step * kStep,
+                            __builtin_amdgcn_readfirstlane(to + l * 1024));
+            }
+        }
+    };
+
+    const int wu = wave / WI, wi = wave % WI;
+    const int row = lane & 15, group = lane >> 4;
+    i4 acc[FU][FI];
+#pragma unroll
+    for (int u = 0; u < FU; ++u)
+#pragma unroll
+        for (int i = 0; i < FI; ++i) acc[u][i] = i4{0, 0, 0, 0};
+
+    const auto multiply = [&](int step, auto tail) {
+        const unsigned char* at = lds + (step & 1) * C::kStage;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int slot = 16 * ((4 * h + group) ^ (row >> 1 & 7));
+            i4 a[FI], b[FU];
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+                a[i] = *(const i4*)(at + (C::kUsers + (wi * FI + i) * 16 + row) * kStep + slot);
+#pragma unroll
+            for (int u = 0; u < FU; ++u) {
+                b[u] = *(const i4*)(at + ((wu * FU + u) * 16 + row) * kStep + slot);
+                if (tail.value) b[u] = keep_bytes(b[u], step * kStep + 64 * h + 16 * group, f);
+            }
+#pragma unroll
+            for (int u = 0; u < FU; ++u)
+#pragma unroll
+                for (int i = 0; i < FI; ++i)
+                    acc[u][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[u], acc[u][i], 0, 0, 0);
+        }
+    };
+
+    fetch(0);
+    settle();
+    __builtin_amdgcn_s_barrier();
+    for (int step = 0; step + 1 < steps; ++step) {
+        fetch(step + 1);
+        multiply(step, std::false_type());
+        settle();
+        __builtin_amdgcn_s_barrier();
+    }
+    multiply(steps - 1, std::true_type());
+
+#pragma unroll
+    for (int u = 0; u < FU; ++u) {
+        const int64_t user = u0 + (wu * FU + u) * 16 + row;
+        if (user >= m) continue;
+        const float s = xs[user];
+        T* o = out + user * ldo;
+#pragma unroll
+        for (int i = 0; i < FI; ++i) {
+            const int64_t item = i0 + (wi * FI + i) * 16 + 4 * group;
+            if (item + 4 <= n) {
+                T v[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) from_float((float)acc[u][i][r] * s * ts[item + r], &v[r]);
+                __builtin_memcpy(o + item, v, sizeof v);
+            } else {
+                for (int r = 0; r < 4; ++r)
+                    if (item + r < n) from_float((float)acc[u][i][r] * s * ts[item + r], o + item + r);
+            }
+        }
+    }
 }
 
 // -------------------------------------------------------------------------------- sample --
@@ -652,6 +827,24 @@ int als_score(als_serve_ctx* ctx, const int8_t* xq, int64_t ldx, const float* xs
         return ALS_ERR_ALIAS;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return ALS_ERR_DEVICE;
+    if (aligned(xq, 16) && aligned(tq, 16) && ldx % 16 == 0 && ldt % 16 == 0 && f > 128 && m > 128 &&
+        ldx < kTileStride && ldt < kTileStride) {
+        using C = Tiles<2, 4, 8, 4>;
+        const int64_t tu = (m + C::kUsers - 1) / C::kUsers, ti = (n + C::kItems - 1) / C::kItems;
+        if (tu * ti > INT32_MAX) return ALS_ERR_INVALID_ARG;
+        const auto launch = [&](auto* p) {
+            using T = std::remove_pointer_t<decltype(p)>;
+            (void)hipFuncSetAttribute((const void*)k_score_tiles<T, 2, 4, 8, 4>,
+                                      hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+            hipLaunchKernelGGL((k_score_tiles<T, 2, 4, 8, 4>), dim3((unsigned)(tu * ti)), dim3(64 * C::kWaves),
+                               2 * C::kStage, (hipStream_t)stream, xq, ldx, xs, m, tq, ldt, ts, n, f, p, ldo,
+                               (uint32_t)tu, (uint32_t)ti);
+        };
+        if (dtype == ALS_F32) launch((float*)out);
+        else if (dtype == ALS_F16) launch((F16*)out);
+        else launch((BF16*)out);
+        return finish(ctx);
+    }
     const int64_t item_blocks = (n + kScoreItems - 1) / kScoreItems, user_blocks = (m + 15) / 16;
     if (item_blocks > INT32_MAX / user_blocks) return ALS_ERR_INVALID_ARG;
     const auto launch = [&](auto* p) {
