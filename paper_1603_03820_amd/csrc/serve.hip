@@ -151,12 +151,10 @@ struct Tiles {
     static constexpr int kWaves = WU * WI;
     static constexpr int kUsers = WU * FU * 16, kItems = WI * FI * 16;
     static constexpr int kRows = kUsers + kItems;
-    static constexpr int kLoads = kRows / 8 / kWaves;      // 1 KB loads of a wave and step
+    static constexpr int kUserLoads = kUsers / 8 / kWaves, kItemLoads = kItems / 8 / kWaves;   // 1 KB, a wave and step
     static constexpr int kStage = kRows * kStep;           // bytes
-    static_assert(kRows % (8 * kWaves) == 0 && (kUsers / 8) % kLoads == 0, "a load has rows of one side");
+    static_assert(kUsers % (8 * kWaves) == 0 && kItems % (8 * kWaves) == 0, "whole loads");
 };
-
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 // A buffer of `bytes` bytes from `base` on (both the same in every lane).
 __device__ __forceinline__ i4 buffer_of(const void* base, uint32_t bytes) {
@@ -215,37 +213,40 @@ __global__ __launch_bounds__(64 * WU * WI) void k_score_tiles(
     tile_of(blockIdx.x, tu, ti, &tile_u, &tile_i);
     const int64_t u0 = (int64_t)tile_u * C::kUsers, i0 = (int64_t)tile_i * C::kItems;
 
-    // this wave's loads are of one side: rows first .. first + 8 kLoads - 1 of the stage
-    const int first = wave * C::kLoads * 8;
-    const bool of_users = first < C::kUsers;
-    const int64_t ld = of_users ? ldx : ldt;
-    const int64_t left = of_users ? m - u0 : n - i0;
-    const int64_t span = (left < (of_users ? C::kUsers : C::kItems) ? left : (of_users ? C::kUsers : C::kItems)) * ld;
-    const i4 buffer = buffer_of((of_users ? xq + u0 * ldx : tq + i0 * ldt),
-                                (uint32_t)(span - ld + (f + 15) / 16 * 16));
-    uint32_t voffset[C::kLoads];
+    // what the buffers hold: the tile's rows, the last up to the end of its last group
+    const int64_t users = m - u0 < C::kUsers ? m - u0 : C::kUsers, items = n - i0 < C::kItems ? n - i0 : C::kItems;
+    const int whole = (f + 15) / 16 * 16;
+    const i4 from_u = buffer_of(xq + u0 * ldx, (uint32_t)((users - 1) * ldx + whole));
+    const i4 from_i = buffer_of(tq + i0 * ldt, (uint32_t)((items - 1) * ldt + whole));
+    const int first_u = wave * C::kUserLoads * 8, first_i = wave * C::kItemLoads * 8;   // this wave's rows
+    const auto group_of = [&](int r) { return 16 * ((lane & 7) ^ (r >> 1 & 7)); };
+    uint32_t of_u[C::kUserLoads], of_i[C::kItemLoads];
 #pragma unroll
-    for (int l = 0; l < C::kLoads; ++l) {
-        const int r = first + 8 * l + (lane >> 3);
-        voffset[l] = (uint32_t)((r - (of_users ? 0 : C::kUsers)) * ld) + 16 * ((lane & 7) ^ (r >> 1 & 7));
+    for (int l = 0; l < C::kUserLoads; ++l) {
+        const int r = first_u + 8 * l + (lane >> 3);
+        of_u[l] = (uint32_t)(r * ldx) + group_of(r);
+    }
+#pragma unroll
+    for (int l = 0; l < C::kItemLoads; ++l) {
+        const int r = first_i + 8 * l + (lane >> 3);
+        of_i[l] = (uint32_t)(r * ldt) + group_of(r);
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
     const int steps = (f + kStep - 1) / kStep;
-    const auto fetch = [&](int step) {
-        const uint32_t to = lds0 + (step & 1) * C::kStage + first * kStep;
-        if (step + 1 < steps) {
+    // groups past f are not read: their offset is past the buffer's end
+    const auto fetch = [&](int step, auto tail) {
+        const uint32_t to = lds0 + (step & 1) * C::kStage;
+        const auto at = [&](uint32_t offset, int r) {
+            return !tail.value || step * kStep + group_of(r) < f ? offset : kPastEnd;
+        };
 #pragma unroll
-            for (int l = 0; l < C::kLoads; ++l)
-                load_to_lds(buffer, voffset[l], step * kStep, __builtin_amdgcn_readfirstlane(to + l * 1024));
-        } else {   // groups past f are not read: their offset is past the buffer's end
+        for (int l = 0; l < C::kUserLoads; ++l)
+            load_to_lds(from_u, at(of_u[l], first_u + 8 * l + (lane >> 3)), step * kStep,
+                        __builtin_amdgcn_readfirstlane(to + (first_u + 8 * l) * kStep));
 #pragma unroll
-            for (int l = 0; l < C::kLoads; ++l) {
-                const int r = first + 8 * l + (lane >> 3);
-                const bool in = step * kStep + 16 * ((lane & 7) ^ (r >> 1 & 7)) < f;
-                load_to_lds(buffer, in ? voffset[l] : kPastEnd, step * kStep,
-                            __builtin_amdgcn_readfirstlane(to + l * 1024));
-            }
-        }
+        for (int l = 0; l < C::kItemLoads; ++l)
+            load_to_lds(from_i, at(of_i[l], first_i + 8 * l + (lane >> 3)), step * kStep,
+                        __builtin_amdgcn_readfirstlane(to + (C::kUsers + first_i + 8 * l) * kStep));
     };
 
     const int wu = wave / WI, wi = wave % WI;
@@ -278,12 +279,19 @@ __global__ __launch_bounds__(64 * WU * WI) void k_score_tiles(
         }
     };
 
-    fetch(0);
+    if (steps > 1) fetch(0, std::false_type());
+    else fetch(0, std::true_type());
     settle();
     __builtin_amdgcn_s_barrier();
-    for (int step = 0; step + 1 < steps; ++step) {
-        fetch(step + 1);
+    for (int step = 0; step + 2 < steps; ++step) {
+        fetch(step + 1, std::false_type());
         multiply(step, std::false_type());
+        settle();
+        __builtin_amdgcn_s_barrier();
+    }
+    if (steps > 1) {
+        fetch(steps - 1, std::true_type());
+        multiply(steps - 2, std::false_type());
         settle();
         __builtin_amdgcn_s_barrier();
     }
@@ -340,6 +348,10 @@ __device__ __forceinline__ float score_of(uint32_t key) {
     return __builtin_bit_cast(float, b);
 }
 
+// 0 for a column that may not be drawn; every other key is at least 0x00800000.
+__device__ __forceinline__ uint32_t allowed_key(float z) { return z > -INFINITY ? key_of(z) : 0; }
+__device__ __forceinline__ float unit_of(float u) { return u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f; }
+
 // floor(2^40 e), 0 <= e <= 1; NaN gives 0.
 __device__ __forceinline__ uint64_t fixed40(float e) {
     if (!(e > 0.f)) return 0;
@@ -354,22 +366,495 @@ __device__ __forceinline__ uint64_t share_of(uint64_t total, uint32_t part) {
     return (total >> 24) * part + (((total & 0xFFFFFFu) * part) >> 24);
 }
 
-__device__ __forceinline__ uint64_t shfl_up64(uint64_t v, int d) {
-    const uint32_t lo = __shfl_up((uint32_t)v, d), hi = __shfl_up((uint32_t)(v >> 32), d);
+// One of the wave's DPP moves of a 64-bit value: lanes without a source get 0.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t dpp64(uint64_t v) {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
     return (uint64_t)hi << 32 | lo;
 }
-__device__ __forceinline__ uint64_t shfl64(uint64_t v, int lane) {
-    const uint32_t lo = __shfl((uint32_t)v, lane), hi = __shfl((uint32_t)(v >> 32), lane);
-    return (uint64_t)hi << 32 | lo;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp32(uint32_t v) {
+    return __builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
 }
-__device__ __forceinline__ uint64_t scan64(uint64_t v) {   // inclusive, over the wave
-    const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const uint64_t o = shfl_up64(v, d);
-        if (lane >= d) v += o;
-    }
+// Inclusive sums over the wave: within rows of 16 lanes, then across rows.
+__device__ __forceinline__ uint64_t scan64(uint64_t v) {
+    v += dpp64<0x111, 0xF>(v);   // row_shr:1, 2, 4, 8
+    v += dpp64<0x112, 0xF>(v);
+    v += dpp64<0x114, 0xF>(v);
+    v += dpp64<0x118, 0xF>(v);
+    v += dpp64<0x142, 0xA>(v);   // row_bcast:15 into rows 1 and 3
+    v += dpp64<0x143, 0xC>(v);   // row_bcast:31 into rows 2 and 3
     return v;
+}
+__device__ __forceinline__ uint32_t scan32(uint32_t v) {
+    v += dpp32<0x111, 0xF>(v);
+    v += dpp32<0x112, 0xF>(v);
+    v += dpp32<0x114, 0xF>(v);
+    v += dpp32<0x118, 0xF>(v);
+    v += dpp32<0x142, 0xA>(v);
+    v += dpp32<0x143, 0xC>(v);
+    return v;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    v = max(v, dpp32<0x111, 0xF>(v));
+    v = max(v, dpp32<0x112, 0xF>(v));
+    v = max(v, dpp32<0x114, 0xF>(v));
+    v = max(v, dpp32<0x118, 0xF>(v));
+    v = max(v, dpp32<0x142, 0xA>(v));
+    v = max(v, dpp32<0x143, 0xC>(v));
+    return __builtin_amdgcn_readlane(v, 63);
+}
+__device__ __forceinline__ uint64_t last64(uint64_t v) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), 63) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((uint32_t)v, 63);
+}
+
+// What a row asks for, and its best score: all that a weight depends on.
+struct Asked {
+    uint32_t best;      // the largest key
+    float top, inv_t;   // its score, 1 / T
+    float least_e;      // min_p
+
+    __device__ __forceinline__ float exp_of(uint32_t key) const {
+        return expf(key == best ? 0.f : (score_of(key) - top) * inv_t);
+    }
+    __device__ __forceinline__ uint64_t weight_of(uint32_t key) const { return fixed40(exp_of(key)); }
+};
+
+// A place in the order (score descending, position ascending): what stands up to it, itself included, stays.
+struct Cut {
+    uint32_t key = 1;      // every allowed key is larger
+    uint32_t position = 0;
+    __device__ __forceinline__ bool keeps(uint32_t k, uint32_t p) const {
+        return k > key || (k == key && p <= position);
+    }
+};
+
+// One row in the registers of a workgroup of NT threads: 4 R keys a thread (0: not allowed), a wave's
+// positions in one run.  Bins and list are LDS: a cut is found by a histogram over the scores, then by
+// ranking the columns of the one bin in which it falls.  LDS sums are of integers, so their order does not matter.
+template <int NT, int R>
+struct Held {
+    static constexpr int kThreads = NT, kWaves = NT / kWave, kBins = 4 * NT, kList = 2 * NT;
+    static constexpr int kColumns = NT * R * 4;
+    struct Shared {
+        uint64_t bin[kBins];
+        uint32_t list_key[kList], list_position[kList];
+        uint64_t wave_sum[kWaves];
+        uint32_t wave_a[kWaves], wave_b[kWaves], wave_c[kWaves];
+        uint64_t found_before;
+        uint32_t found_bin, listed;
+        uint32_t cut_key, cut_position;
+        uint32_t low, high;
+    };
+    uint32_t key[R * 4];
+    Shared* sh;
+
+    static __device__ __forceinline__ int lane() { return threadIdx.x & (kWave - 1); }
+    static __device__ __forceinline__ int wave() { return threadIdx.x / kWave; }
+    // of the first of a thread's four keys v
+    static __device__ __forceinline__ uint32_t position(int v) {
+        return (uint32_t)(wave() * R + v) * (4 * kWave) + 4 * lane();
+    }
+    static __device__ __forceinline__ void sync() {
+        if (NT > kWave) __syncthreads();
+        else __builtin_amdgcn_wave_barrier();
+    }
+    // fn(key, position) for every held key.  Four at a time, and each key through an empty statement that hides its
+    // value: left alone, the compiler interleaves all of a thread's exponentials and keeps the weights of one pass for
+    // the next, in the registers of three more waves or in scratch.
+    template <typename Fn>
+    __device__ __forceinline__ void each(Fn fn) const {
+        uint32_t first = position(0);
+        asm volatile("" : "+v"(first));
+#pragma unroll
+        for (int v = 0; v < R; ++v) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t k = key[4 * v + c];
+                asm volatile("" : "+v"(k));
+                fn(k, first + 4 * kWave * v + c);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+
+    // Of the waves' sums: their sum, and the sum of those before this wave's.
+    __device__ __forceinline__ uint64_t sum(uint64_t mine, uint64_t* before_wave) {
+        sync();
+        if (lane() == 0) sh->wave_sum[wave()] = mine;
+        sync();
+        uint64_t total = 0;
+        *before_wave = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w == wave()) *before_wave = total;
+            total += sh->wave_sum[w];
+        }
+        return total;
+    }
+
+    // Largest and least allowed key, and how many there are.
+    __device__ __forceinline__ void range(uint32_t* best, uint32_t* least, uint32_t* count) {
+        uint32_t hi = 0, lo = 0, n = 0;    // lo: the complement's largest
+#pragma unroll
+        for (int j = 0; j < 4 * R; ++j) {
+            hi = max(hi, key[j]);
+            lo = max(lo, key[j] ? ~key[j] : 0u);
+            n += key[j] != 0;
+        }
+        hi = wave_max(hi);
+        lo = wave_max(lo);
+        n = __builtin_amdgcn_readlane(scan32(n), 63);
+        if (kWaves > 1) {
+            if (lane() == 0) { sh->wave_a[wave()] = hi; sh->wave_b[wave()] = lo; sh->wave_c[wave()] = n; }
+            sync();
+            hi = lo = n = 0;
+            for (int w = 0; w < kWaves; ++w) {
+                hi = max(hi, sh->wave_a[w]);
+                lo = max(lo, sh->wave_b[w]);
+                n += sh->wave_c[w];
+            }
+        }
+        *best = hi;
+        *least = ~lo;
+        *count = n;
+    }
+
+    // The first position at which the running sum of measure(key, position) exceeds t (the sum over all does).
+    template <typename Fn>
+    __device__ __forceinline__ uint32_t find(uint64_t t, uint64_t mine, uint64_t before_wave, Fn measure) {
+        // `mine`: this wave's sum; exactly one wave holds the place
+        if (t >= before_wave && t - before_wave < mine) {
+            uint64_t left = t - before_wave;
+            bool open = true;
+            uint32_t first = position(0);
+            asm volatile("" : "+v"(first));
+#pragma unroll
+            for (int v = 0; v < R; ++v) {
+                if (open) {
+                    uint64_t w[4], s = 0;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t k = key[4 * v + c];
+                        asm volatile("" : "+v"(k));
+                        w[c] = measure(k, first + 4 * kWave * v + c);
+                        s += w[c];
+                    }
+                    const uint64_t upto = scan64(s), all = last64(upto);
+                    if (left < all) {
+                        uint64_t at = upto - s;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            if (left >= at && left < at + w[c]) sh->cut_position = first + 4 * kWave * v + c;
+                            at += w[c];
+                        }
+                        open = false;
+                    } else {
+                        left -= all;
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        sync();
+        const uint32_t p = sh->cut_position;
+        sync();
+        return p;
+    }
+
+    // The bin of a key: linear in the score from the best one down, the last bin for all that is `range` or more
+    // below it.
+    struct Scale { float top, per; uint32_t best; };
+    __device__ __forceinline__ int bin_of(uint32_t k, const Scale& c) const {
+        const float x = (c.top - score_of(k)) * c.per;
+        return k == c.best ? 0 : (x < (float)(kBins - 1) ? (int)x : kBins - 1);
+    }
+
+    // Adds up the bins in their order: the first at which the sum reaches the target (found_bin,
+    // found_before).  target(total) is asked once the total is known.
+    template <typename Fn>
+    __device__ __forceinline__ void search_bins(Fn target) {
+        sync();
+        uint64_t v[4], s = 0, before;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) { v[b] = sh->bin[4 * threadIdx.x + b]; s += v[b]; }
+        const uint64_t upto = scan64(s);
+        sync();
+        if (lane() == 63) sh->wave_sum[wave()] = upto;
+        if (threadIdx.x == 0) sh->listed = 0;
+        sync();
+        uint64_t total = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w == wave()) before = total;
+            total += sh->wave_sum[w];
+        }
+        uint64_t at = before + upto - s;
+        const uint64_t goal = target(total);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            if (at < goal && goal <= at + v[b]) {
+                sh->found_bin = 4 * threadIdx.x + b;
+                sh->found_before = at;
+            }
+            at += v[b];
+        }
+        sync();
+    }
+
+    // Among the listed columns, the last with less than `goal` of the measure before it.
+    __device__ __forceinline__ Cut rank_list(bool by_mass, uint32_t count, uint64_t before, uint64_t goal,
+                                             const Asked& ask) {
+        for (uint32_t i = threadIdx.x; i < count; i += NT) {
+            const uint32_t k = sh->list_key[i], p = sh->list_position[i];
+            uint64_t front = before;
+            for (uint32_t j = 0; j < count; ++j) {
+                const uint32_t kj = sh->list_key[j];
+                if (kj > k || (kj == k && sh->list_position[j] < p)) front += by_mass ? ask.weight_of(kj) : 1;
+            }
+            const uint64_t own = by_mass ? ask.weight_of(k) : 1;
+            if (front < goal && goal <= front + own) { sh->cut_key = k; sh->cut_position = p; }
+        }
+        sync();
+        Cut cut;
+        cut.key = sh->cut_key;
+        cut.position = sh->cut_position;
+        sync();
+        return cut;
+    }
+
+    // The columns that `take` picks, on the list as far as it holds them; how many there are.
+    template <typename Fn>
+    __device__ __forceinline__ uint32_t make_list(Fn take) {
+        each([&](uint32_t k, uint32_t p) {
+            if (take(k, p)) {
+                const uint32_t at = atomicAdd(&sh->listed, 1u);
+                if (at < (uint32_t)kList) { sh->list_key[at] = k; sh->list_position[at] = p; }
+            }
+        });
+        sync();
+        return sh->listed;
+    }
+
+    // The last column, in the order, with less than the target of the measure before it, among the columns
+    // that `within` keeps.  by_mass: the measure is the weight and the target share_of(its sum, part), at least 1;
+    // else the target is `part` columns (fewer than there are).
+    __device__ __forceinline__ Cut select(bool by_mass, Cut within, uint32_t least, float t, uint32_t part,
+                                          const Asked& ask) {
+        sync();
+        for (int b = threadIdx.x; b < kBins; b += NT) sh->bin[b] = 0;
+        sync();
+        // past 28 T below the best, a weight is 0
+        const float all = ask.top - score_of(least);
+        const bool clipped = all > 28.f * t;
+        const float range = clipped ? 28.f * t : all;
+        const Scale scale{ask.top, range > 0.f ? (float)(kBins - 1) / range : 0.f, ask.best};
+        each([&](uint32_t k, uint32_t p) {
+            if (within.keeps(k, p)) {
+                const uint64_t w = by_mass ? ask.weight_of(k) : 1;
+                if (w) atomicAdd((unsigned long long*)&sh->bin[bin_of(k, scale)], (unsigned long long)w);
+            }
+        });
+        uint64_t goal;
+        search_bins([&](uint64_t total) {
+            goal = by_mass ? share_of(total, part) : part;
+            if (goal < 1) goal = 1;
+            return goal;
+        });
+        const int bin = sh->found_bin;
+        uint64_t before = sh->found_before;
+        if (!by_mass && clipped && bin == kBins - 1) return within;   // what would go has no weight
+        uint32_t listed = make_list([&](uint32_t k, uint32_t p) { return within.keeps(k, p) && bin_of(k, scale) == bin; });
+        if (listed <= (uint32_t)kList) return rank_list(by_mass, listed, before, goal, ask);
+
+        // Many columns crowd one bin (equal scores, or some far from the others): bins of keys, narrowed until
+        // the rest can be ranked or is one key.
+        before = 0;
+        uint32_t lo = 0, hi = 0xFFFFFFFFu;     // distances of keys from the best
+        for (;;) {
+            const auto in = [&](uint32_t k, uint32_t p) {
+                const uint32_t d = ask.best - k;
+                return d >= lo && d <= hi && within.keeps(k, p);
+            };
+            uint32_t far = 0, near = 0;        // the largest distance, the least one's complement
+            each([&](uint32_t k, uint32_t p) {
+                if (in(k, p)) { far = max(far, ask.best - k); near = max(near, ~(ask.best - k)); }
+            });
+            far = wave_max(far);
+            near = wave_max(near);
+            sync();
+            if (threadIdx.x == 0) { sh->high = 0; sh->low = 0; }
+            for (int b = threadIdx.x; b < kBins; b += NT) sh->bin[b] = 0;
+            sync();
+            if (lane() == 0) { atomicMax(&sh->high, far); atomicMax(&sh->low, near); }
+            sync();
+            lo = ~sh->low;
+            hi = sh->high;
+            int shift = 0;
+            while (((hi - lo) >> shift) >= (uint32_t)kBins) ++shift;
+            each([&](uint32_t k, uint32_t p) {
+                if (in(k, p)) {
+                    const uint64_t w = by_mass ? ask.weight_of(k) : 1;
+                    if (w) atomicAdd((unsigned long long*)&sh->bin[(ask.best - k - lo) >> shift], (unsigned long long)w);
+                }
+            });
+            search_bins([&](uint64_t) { return goal - before; });
+            before += sh->found_before;
+            lo += sh->found_bin << shift;
+            const uint32_t end = lo + ((1u << shift) - 1);
+            hi = end < hi ? end : hi;
+            if (lo == hi) {     // equal scores: as many of them, by position, as reach the goal
+                Cut cut;
+                cut.key = ask.best - lo;
+                const uint64_t own = by_mass ? ask.weight_of(cut.key) : 1;
+                const uint64_t more = (goal - before + own - 1) / own;
+                const auto same = [&](uint32_t k, uint32_t p) -> uint64_t { return k == cut.key && within.keeps(k, p); };
+                uint64_t mine = 0, before_wave;
+                each([&](uint32_t k, uint32_t p) { mine += same(k, p); });
+                mine = last64(scan64(mine));
+                sum(mine, &before_wave);
+                cut.position = find(more - 1, mine, before_wave, same);
+                return cut;
+            }
+            listed = make_list(in);
+            if (listed <= (uint32_t)kList) return rank_list(by_mass, listed, before, goal, ask);
+        }
+    }
+
+    // The draw: the position, and the logarithm of its probability (to every thread).
+    struct Drawn { uint32_t position; float log; };
+    __device__ __forceinline__ Drawn draw(uint32_t least, uint32_t count, float t, int top_k, float top_p, float u,
+                                          const Asked& ask) {
+        Cut cut;
+#pragma nounroll
+        for (int by_mass = 0; by_mass < 2; ++by_mass) {     // one copy of the code for both cuts
+            if (by_mass ? !(top_p < 1.f) : top_k <= 0 || (uint32_t)top_k >= count) continue;
+            const uint32_t part = by_mass ? (top_p > 0.f ? (uint32_t)(top_p * 0x1p24f) : 0) : (uint32_t)top_k;
+            cut = select(by_mass != 0, cut, least, t, part, ask);
+        }
+        const auto weight = [&](uint32_t k, uint32_t p) -> uint64_t {
+            if (!cut.keeps(k, p)) return 0;
+            const float e = ask.exp_of(k);
+            return e >= ask.least_e ? fixed40(e) : 0;
+        };
+        uint64_t mine = 0, before_wave;
+        each([&](uint32_t k, uint32_t p) { mine += weight(k, p); });
+        mine = last64(scan64(mine));
+        const uint64_t total = sum(mine, &before_wave);
+        const uint32_t p = find(share_of(total, (uint32_t)(u * 0x1p24f)), mine, before_wave, weight);
+        each([&](uint32_t k, uint32_t at) { if (at == p) sh->cut_key = k; });
+        sync();
+        const uint32_t k = sh->cut_key;
+        const float x = k == ask.best ? 0.f : (score_of(k) - ask.top) * ask.inv_t;
+        return Drawn{p, x - logf((float)total * 0x1p-40f)};
+    }
+
+    // The first position of the best key.
+    __device__ __forceinline__ uint32_t first_of(uint32_t best) {
+        uint32_t p = 0;
+#pragma unroll
+        for (int j = 0; j < 4 * R; ++j)
+            if (key[j] == best) p = max(p, ~(position(j / 4) + j % 4));
+        p = wave_max(p);
+        if (kWaves > 1) {
+            sync();
+            if (lane() == 0) sh->wave_a[wave()] = p;
+            sync();
+            for (int w = 0; w < kWaves; ++w) p = max(p, sh->wave_a[w]);
+        }
+        return ~p;
+    }
+};
+
+__device__ __forceinline__ float limit_of(const float* each, float all, int64_t r) { return each ? each[r] : all; }
+
+// A row's CSR row of columns to leave out.
+struct Rated {
+    const int64_t* ptr;
+    const int32_t* idx;
+    const int32_t* users;
+    int64_t of;
+    // false: the row's user does not exist
+    __device__ __forceinline__ bool row(int64_t r, const int32_t** list, int64_t* count) const {
+        *list = nullptr;
+        *count = 0;
+        if (!ptr) return true;
+        const int64_t u = users ? (int64_t)users[r] : r;
+        if (u < 0 || u >= of) return false;
+        const int64_t first = ptr[u];
+        *list = idx + first;
+        *count = ptr[u + 1] - first;
+        return true;
+    }
+};
+
+// Four keys from column c on; columns from n on get 0.
+template <typename T>
+__device__ __forceinline__ void load_keys(const T* z, uint32_t c, uint32_t n, uint32_t* key) {
+    T v[4];
+    if (c + 4 <= n) {
+        __builtin_memcpy(v, z + c, sizeof v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) key[i] = allowed_key(to_float(v[i]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) key[i] = c + i < n ? allowed_key(to_float(z[c + i])) : 0;
+    }
+}
+
+// A workgroup a row, the row in registers from its one read on.
+template <int NT, int R, typename T>
+__global__ __launch_bounds__(NT) void k_sample(const T* __restrict__ z, int64_t rows, uint32_t n, int64_t ldz,
+                                               Limits lim, const float* __restrict__ u, Rated rated,
+                                               int32_t* __restrict__ index, float* __restrict__ log) {
+    using H = Held<NT, R>;
+    extern __shared__ __align__(16) unsigned char shared[];
+    H h;
+    h.sh = (typename H::Shared*)shared;
+    uint32_t* bits = (uint32_t*)(shared + sizeof(typename H::Shared));   // the columns left out, one bit each
+    const int64_t r = blockIdx.x;
+    const int32_t* list;
+    int64_t listed;
+    if (!rated.row(r, &list, &listed)) {
+        if (threadIdx.x == 0) { index[r] = -1; if (log) log[r] = NAN; }
+        return;
+    }
+    const T* zr = z + r * ldz;
+#pragma unroll
+    for (int v = 0; v < R; ++v) load_keys(zr, h.position(v), n, &h.key[4 * v]);
+    if (listed > 0) {
+        for (uint32_t w = threadIdx.x; w < (n + 31) / 32; w += NT) bits[w] = 0;
+        H::sync();
+        for (int64_t k = threadIdx.x; k < listed; k += NT) {
+            const uint32_t c = (uint32_t)list[k];
+            if (c < n) atomicOr(&bits[c >> 5], 1u << (c & 31));
+        }
+        H::sync();
+#pragma unroll
+        for (int v = 0; v < R; ++v) {
+            const uint32_t c = h.position(v);
+            const uint32_t four = c < n ? bits[c >> 5] >> (c & 31) : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h.key[4 * v + i] = four >> i & 1 ? 0 : h.key[4 * v + i];
+        }
+    }
+    uint32_t best, least, count;
+    h.range(&best, &least, &count);
+    if (count == 0) {
+        if (threadIdx.x == 0) { index[r] = -1; if (log) log[r] = -INFINITY; }
+        return;
+    }
+    const float t = limit_of(lim.temperature, lim.temperature_all, r);
+    if (!(t > 0.f)) {
+        const uint32_t p = h.first_of(best);
+        if (threadIdx.x == 0) { index[r] = (int32_t)p; if (log) log[r] = 0.f; }
+        return;
+    }
+    const float min_p = limit_of(lim.min_p, lim.min_p_all, r);
+    const Asked ask{best, score_of(best), 1.f / t, min_p > 0.f ? fminf(min_p, 1.f) : 0.f};
+    const auto d = h.draw(least, count, t, lim.top_k ? lim.top_k[r] : lim.top_k_all,
+                          limit_of(lim.top_p, lim.top_p_all, r), unit_of(u[r]), ask);
+    if (threadIdx.x == 0) { index[r] = (int32_t)d.position; if (log) log[r] = d.log; }
 }
 
 struct SampleShared {
@@ -445,7 +930,7 @@ __device__ uint64_t block_sum(uint64_t v, SampleShared* sh) {
 }
 
 // A place in the order (score descending, column ascending): columns up to and with (d, column).
-struct Cut {
+struct LongCut {
     uint32_t d;
     uint32_t column;
     __device__ bool keeps(uint32_t dd, int64_t c) const {
@@ -492,7 +977,7 @@ __device__ uint32_t find_column(Row<T>& row, uint64_t t, Fn measure) {
 // The last column, in the order, with less than `target` of the measure before it; among the columns that
 // `within` keeps.  BY_MASS: the measure is the weight, else 1.  target >= 1 and at most the sum.
 template <bool BY_MASS, typename T>
-__device__ Cut select_cut(Row<T>& row, Cut within, uint32_t widest, uint64_t target) {
+__device__ LongCut select_cut(Row<T>& row, LongCut within, uint32_t widest, uint64_t target) {
     SampleShared* sh = row.sh;
     uint64_t before = 0;                       // measure in front of the range
     uint32_t lo = 0, hi = widest;              // the range of distances
@@ -554,7 +1039,7 @@ __device__ Cut select_cut(Row<T>& row, Cut within, uint32_t widest, uint64_t tar
                 if (front < target && target <= front + own) { sh->cut_d = d; sh->cut_i = i; }
             }
             __syncthreads();
-            const Cut cut{sh->cut_d, sh->cut_i};
+            const LongCut cut{sh->cut_d, sh->cut_i};
             __syncthreads();
             return cut;
         }
@@ -566,13 +1051,13 @@ __device__ Cut select_cut(Row<T>& row, Cut within, uint32_t widest, uint64_t tar
                 return dd == d && within.keeps(dd, cc) ? 1 : 0;
             });
             __syncthreads();
-            return Cut{d, c};
+            return LongCut{d, c};
         }
     }
 }
 
 template <typename T>
-__global__ __launch_bounds__(kSampleThreads) void k_sample(const T* __restrict__ z, int64_t rows, int64_t n,
+__global__ __launch_bounds__(kSampleThreads) void k_sample_long(const T* __restrict__ z, int64_t rows, int64_t n,
                                                            int64_t ldz, Limits lim, const float* __restrict__ u,
                                                            const int64_t* __restrict__ rated_ptr,
                                                            const int32_t* __restrict__ rated_idx,
@@ -631,7 +1116,7 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample(const T* __restrict__
     const float least = lim.min_p ? lim.min_p[r] : lim.min_p_all;
     const float least_e = least > 0.f ? fminf(least, 1.f) : 0.f;
     const uint32_t widest = hi - lo;
-    Cut cut{widest, 0xFFFFFFFFu};
+    LongCut cut{widest, 0xFFFFFFFFu};
     if (greedy) {
         const uint32_t c = find_column(row, 0, [](int64_t, uint32_t d) -> uint64_t { return d == 0; });
         if (threadIdx.x == 0) { index[r] = (int32_t)c; if (log) log[r] = 0.f; }
@@ -887,12 +1372,30 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
     if (!guard.ok) return ALS_ERR_DEVICE;
     const Limits lim{l.temperature, l.top_k, l.top_p, l.min_p, l.temperature_all, l.top_k_all, l.top_p_all,
                      l.min_p_all};
-    const int64_t bits = rated_ptr ? (n < kChunk ? n : kChunk) : 0;
-    const size_t lds = sizeof(SampleShared) + (size_t)((bits + 31) / 32) * 4;
+    const Rated rated{rated_ptr, rated_idx, users, of};
+    const auto held = [&](auto h, auto* p) {
+        using H = decltype(h);
+        using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
+        auto* kernel = k_sample<H::kThreads, H::kColumns / H::kThreads / 4, T>;
+        const size_t lds = sizeof(typename H::Shared) + (rated_ptr ? (size_t)(n + 31) / 32 * 4 : 0);
+        (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(H::kThreads), lds, (hipStream_t)stream, p, rows,
+                           (uint32_t)n, ldz, lim, u, rated, index, log);
+    };
     const auto launch = [&](auto* p) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
-        (void)hipFuncSetAttribute((const void*)k_sample<T>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        hipLaunchKernelGGL(k_sample<T>, dim3((unsigned)rows), dim3(kSampleThreads), lds, (hipStream_t)stream, p,
+        if (n <= 256) return held(Held<64, 1>(), p);
+        if (n <= 1024) return held(Held<64, 4>(), p);
+        if (n <= 4096) return held(Held<256, 4>(), p);
+        if (n <= 8192) return held(Held<256, 8>(), p);
+        if (n <= 12288) return held(Held<512, 6>(), p);
+        if (n <= 20480) return held(Held<512, 10>(), p);
+        if (n <= 32768) return held(Held<512, 16>(), p);
+        if (n <= 65536) return held(Held<1024, 16>(), p);
+        const int64_t bits = rated_ptr ? (n < kChunk ? n : kChunk) : 0;
+        const size_t lds = sizeof(SampleShared) + (size_t)((bits + 31) / 32) * 4;
+        (void)hipFuncSetAttribute((const void*)k_sample_long<T>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        hipLaunchKernelGGL(k_sample_long<T>, dim3((unsigned)rows), dim3(kSampleThreads), lds, (hipStream_t)stream, p,
                            rows, n, ldz, lim, u, rated_ptr, rated_idx, users, of, index, log);
     };
     if (dtype == ALS_F32) launch((const float*)z);
