@@ -348,8 +348,6 @@ __device__ __forceinline__ float score_of(uint32_t key) {
     return __builtin_bit_cast(float, b);
 }
 
-// 0 for a column that may not be drawn; every other key is at least 0x00800000.
-__device__ __forceinline__ uint32_t allowed_key(float z) { return z > -INFINITY ? key_of(z) : 0; }
 __device__ __forceinline__ float unit_of(float u) { return u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f; }
 
 // floor(2^40 e), 0 <= e <= 1; NaN gives 0.
@@ -405,6 +403,20 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
     v = max(v, dpp32<0x143, 0xC>(v));
     return __builtin_amdgcn_readlane(v, 63);
 }
+__device__ __forceinline__ float wave_max(float v) {      // NaN-free
+    const uint32_t least = __builtin_bit_cast(uint32_t, -INFINITY);
+#define ALS_STEP(CTRL, ROWS)                                                                                        \
+    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(                                             \
+                     (int)least, (int)__builtin_bit_cast(uint32_t, v), CTRL, ROWS, 0xF, false)))
+    ALS_STEP(0x111, 0xF);
+    ALS_STEP(0x112, 0xF);
+    ALS_STEP(0x114, 0xF);
+    ALS_STEP(0x118, 0xF);
+    ALS_STEP(0x142, 0xA);
+    ALS_STEP(0x143, 0xC);
+#undef ALS_STEP
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
 __device__ __forceinline__ uint64_t last64(uint64_t v) {
     return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), 63) << 32 |
            (uint32_t)__builtin_amdgcn_readlane((uint32_t)v, 63);
@@ -412,71 +424,92 @@ __device__ __forceinline__ uint64_t last64(uint64_t v) {
 
 // What a row asks for, and its best score: all that a weight depends on.
 struct Asked {
-    uint32_t best;      // the largest key
-    float top, inv_t;   // its score, 1 / T
-    float least_e;      // min_p
+    float top, inv_t;   // the best score, 1 / T
+    float least;        // 2^40 min_p
 
-    __device__ __forceinline__ float exp_of(uint32_t key) const {
-        return expf(key == best ? 0.f : (score_of(key) - top) * inv_t);
+    // 2^40 exp((z - top) / T), z <= top, of the exponential rounded to fp32: 2 to the nearest whole number of
+    // x log2(e), held in two parts, times 2 to the rest.  Where that is 1 or more it equals 2^40 expf(x) in every bit
+    // (tested over all such x) at half the instructions: x ends at -64, where no weight is left, so that nothing
+    // overflows.  No product may be fused into a sum here but the two that are written so.
+    __device__ __forceinline__ float scaled(float z) const {
+#pragma clang fp contract(off)
+        const float x = fmaxf((z - top) * inv_t, -64.f);    // -64 also where a difference or product is not a number
+        const float high = x * 0x1.715476p+0f;
+        const float low = fmaf(x, 0x1.4ae0cp-26f, fmaf(x, 0x1.715476p+0f, -high));
+        const float whole = rintf(high);
+        const float e = ldexpf(__builtin_amdgcn_exp2f((high - whole) + low), (int)whole + 40);
+        return z == top ? 0x1p40f : e;
     }
-    __device__ __forceinline__ uint64_t weight_of(uint32_t key) const { return fixed40(exp_of(key)); }
+    // The weight, a whole number of at most 24 significant bits.
+    __device__ __forceinline__ float weight_of(float z) const { return floorf(scaled(z)); }
 };
+
+__device__ __forceinline__ uint64_t whole_of(float w) {      // of a weight
+    const uint32_t high = (uint32_t)(w * 0x1p-20f);
+    return ((uint64_t)high << 20) + (uint32_t)fmaf((float)high, -0x1p20f, w);
+}
+// 53 bits hold the sum of a thread's weights.
+__device__ __forceinline__ uint64_t whole_of(double w) {
+    const uint32_t high = (uint32_t)(w * 0x1p-32);
+    return ((uint64_t)high << 32) + (uint32_t)fma((double)high, -0x1p32, w);
+}
 
 // A place in the order (score descending, position ascending): what stands up to it, itself included, stays.
 struct Cut {
-    uint32_t key = 1;      // every allowed key is larger
-    uint32_t position = 0;
-    __device__ __forceinline__ bool keeps(uint32_t k, uint32_t p) const {
-        return k > key || (k == key && p <= position);
+    float z = -INFINITY;        // every allowed score is larger
+    int position = -1;
+    __device__ __forceinline__ bool keeps(float v, uint32_t p) const {
+        return v > z || (v == z && (int)p <= position);
     }
 };
 
-// One row in the registers of a workgroup of NT threads: 4 R keys a thread (0: not allowed), a wave's
-// positions in one run.  Bins and list are LDS: a cut is found by a histogram over the scores, then by
-// ranking the columns of the one bin in which it falls.  LDS sums are of integers, so their order does not matter.
-template <int NT, int R>
+// One row in the registers of a workgroup: K scores a thread (-inf: not allowed), four neighbours at a time, a
+// wave's positions in one run.  The loops over them stay loops (a register is picked by a uniform index): unrolled,
+// a row's passes are one long run of code that no instruction cache holds, at four times the time.
+// Bins and list are LDS: a cut is found by a histogram over the scores, then by ranking the columns of the one bin
+// in which it falls.  LDS sums are of integers, so their order does not matter.
+template <int K, int BINS>
 struct Held {
-    static constexpr int kThreads = NT, kWaves = NT / kWave, kBins = 4 * NT, kList = 2 * NT;
-    static constexpr int kColumns = NT * R * 4;
+    static constexpr int kScores = K, kBins = BINS, kList = BINS / 2, kMaxWaves = 16;
+    typedef float Scores __attribute__((ext_vector_type(K < 32 ? K : 32)));
+    static_assert(K % 4 == 0 && K <= 64, "scores a thread");    // (its weights add up below 2^53)
     struct Shared {
         uint64_t bin[kBins];
-        uint32_t list_key[kList], list_position[kList];
-        uint64_t wave_sum[kWaves];
-        uint32_t wave_a[kWaves], wave_b[kWaves], wave_c[kWaves];
+        float list_z[kList];
+        uint32_t list_position[kList];
+        uint64_t wave_sum[kMaxWaves];
+        float wave_a[kMaxWaves], wave_b[kMaxWaves];
+        uint32_t wave_c[kMaxWaves];
         uint64_t found_before;
         uint32_t found_bin, listed;
-        uint32_t cut_key, cut_position;
+        float cut_z;
+        uint32_t cut_position;
         uint32_t low, high;
     };
-    uint32_t key[R * 4];
+    Scores z[(K + 31) / 32];
     Shared* sh;
+    int threads, waves;      // of the workgroup
 
     static __device__ __forceinline__ int lane() { return threadIdx.x & (kWave - 1); }
-    static __device__ __forceinline__ int wave() { return threadIdx.x / kWave; }
-    // of the first of a thread's four keys v
+    static __device__ __forceinline__ int wave() { return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave); }
+    // of the first of a thread's four scores v
     static __device__ __forceinline__ uint32_t position(int v) {
-        return (uint32_t)(wave() * R + v) * (4 * kWave) + 4 * lane();
+        return (uint32_t)(wave() * (K / 4) + v) * (4 * kWave) + 4 * lane();
     }
-    static __device__ __forceinline__ void sync() {
-        if (NT > kWave) __syncthreads();
-        else __builtin_amdgcn_wave_barrier();
+    __device__ __forceinline__ void sync() const {
+        if (waves > 1) __syncthreads();
+        else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    // fn(key, position) for every held key.  Four at a time, and each key through an empty statement that hides its
-    // value: left alone, the compiler interleaves all of a thread's exponentials and keeps the weights of one pass for
-    // the next, in the registers of three more waves or in scratch.
+    // fn(score, position) for every held score.
     template <typename Fn>
     __device__ __forceinline__ void each(Fn fn) const {
-        uint32_t first = position(0);
-        asm volatile("" : "+v"(first));
 #pragma unroll
-        for (int v = 0; v < R; ++v) {
+        for (int h = 0; h < (K + 31) / 32; ++h) {
+            uint32_t p = position(8 * h);
+#pragma nounroll
+            for (int v = 0; v < (K < 32 ? K : 32); v += 4, p += 4 * kWave)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t k = key[4 * v + c];
-                asm volatile("" : "+v"(k));
-                fn(k, first + 4 * kWave * v + c);
-            }
-            __builtin_amdgcn_sched_barrier(0);
+                for (int c = 0; c < 4; ++c) fn(z[h][v + c], p + c);
         }
     }
 
@@ -487,58 +520,132 @@ struct Held {
         sync();
         uint64_t total = 0;
         *before_wave = 0;
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < waves; ++w) {
             if (w == wave()) *before_wave = total;
             total += sh->wave_sum[w];
         }
         return total;
     }
 
-    // Largest and least allowed key, and how many there are.
-    __device__ __forceinline__ void range(uint32_t* best, uint32_t* least, uint32_t* count) {
-        uint32_t hi = 0, lo = 0, n = 0;    // lo: the complement's largest
-#pragma unroll
-        for (int j = 0; j < 4 * R; ++j) {
-            hi = max(hi, key[j]);
-            lo = max(lo, key[j] ? ~key[j] : 0u);
-            n += key[j] != 0;
+    // A thread's largest score, and the workgroup's.
+    __device__ __forceinline__ float largest(float* best) {
+        float mine = -INFINITY;
+        each([&](float k, uint32_t) { mine = fmaxf(mine, k); });
+        float hi = wave_max(mine);
+        if (waves > 1) {
+            if (lane() == 0) sh->wave_a[wave()] = hi;
+            sync();
+            for (int w = 0; w < waves; ++w) hi = fmaxf(hi, sh->wave_a[w]);
         }
-        hi = wave_max(hi);
+        *best = hi;
+        return mine;
+    }
+    // The least allowed score, and how many there are.
+    __device__ __forceinline__ void spread(float* least, uint32_t* count) {
+        float lo = -INFINITY;    // the least one's negative
+        uint32_t n = 0;
+        each([&](float k, uint32_t) {
+            lo = fmaxf(lo, k > -INFINITY ? -k : -INFINITY);
+            n += k > -INFINITY;
+        });
         lo = wave_max(lo);
         n = __builtin_amdgcn_readlane(scan32(n), 63);
-        if (kWaves > 1) {
-            if (lane() == 0) { sh->wave_a[wave()] = hi; sh->wave_b[wave()] = lo; sh->wave_c[wave()] = n; }
+        if (waves > 1) {
+            if (lane() == 0) { sh->wave_b[wave()] = lo; sh->wave_c[wave()] = n; }
             sync();
-            hi = lo = n = 0;
-            for (int w = 0; w < kWaves; ++w) {
-                hi = max(hi, sh->wave_a[w]);
-                lo = max(lo, sh->wave_b[w]);
+            lo = -INFINITY;
+            n = 0;
+            for (int w = 0; w < waves; ++w) {
+                lo = fmaxf(lo, sh->wave_b[w]);
                 n += sh->wave_c[w];
             }
         }
-        *best = hi;
-        *least = ~lo;
+        *least = -lo;
         *count = n;
     }
 
-    // The first position at which the running sum of measure(key, position) exceeds t (the sum over all does).
+    // A score that at least k columns reach (and few more, where scores lie in no order): the k-th largest of the
+    // threads' largest ones, as near below it as bins tell.  -inf: fewer than k threads hold a column.
+    __device__ __forceinline__ float reached_by(uint32_t k, float mine, float best) {
+        float low = wave_max(mine > -INFINITY ? -mine : -INFINITY);     // the least one's negative
+        if (lane() == 0) sh->wave_b[wave()] = low;
+        for (int b = threadIdx.x; b < kBins; b += threads) sh->bin[b] = 0;
+        sync();
+        for (int w = 0; w < waves; ++w) low = fmaxf(low, sh->wave_b[w]);
+        const Scale scale{best, best + low > 0.f ? (float)(kBins - 1) / (best + low) : 0.f};
+        const int bin = mine > -INFINITY ? bin_of(mine, scale) : kBins;
+        if (bin < kBins) atomicAdd((unsigned long long*)&sh->bin[bin], 1ull);
+        if (threadIdx.x == 0) sh->found_bin = kBins;
+        search_bins([&](uint64_t) { return (uint64_t)k; });
+        const int found = (int)sh->found_bin;
+        if (found == kBins) return -INFINITY;
+        low = wave_max(bin <= found ? -mine : -INFINITY);
+        if (lane() == 0) sh->wave_b[wave()] = low;
+        sync();
+        for (int w = 0; w < waves; ++w) low = fmaxf(low, sh->wave_b[w]);
+        sync();
+        return -low;
+    }
+
+    // The columns with a score of `least` or more on the list, by position; how many there are (if the list
+    // does not hold them, it is not written).
+    __device__ __forceinline__ uint32_t collect(float least) {
+        uint32_t mine = 0;
+        each([&](float k, uint32_t) { mine += (uint32_t)__popcll(__ballot(k >= least)); });
+        if (lane() == 0) sh->wave_c[wave()] = mine;
+        sync();
+        uint32_t total = 0, at = 0;
+        for (int w = 0; w < waves; ++w) {
+            if (w == wave()) at = total;
+            total += sh->wave_c[w];
+        }
+        if (total > (uint32_t)kList) { sync(); return total; }
+        const uint64_t below = (1ull << lane()) - 1;
+#pragma unroll
+        for (int h = 0; h < (K + 31) / 32; ++h) {
+            uint32_t p = position(8 * h);
+#pragma nounroll
+            for (int v = 0; v < (K < 32 ? K : 32); v += 4, p += 4 * kWave) {
+                uint64_t takes[4];
+                uint32_t mine = at, all = 0;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    takes[c] = __ballot(z[h][v + c] >= least);
+                    mine += __popcll(takes[c] & below);
+                    all += __popcll(takes[c]);
+                }
+                if (all) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (takes[c] >> lane() & 1) {
+                            sh->list_z[mine] = z[h][v + c];
+                            sh->list_position[mine++] = p + c;
+                        }
+                    at += all;
+                }
+            }
+        }
+        sync();
+        return total;
+    }
+
+    // The first position at which the running sum of measure(score, position), a whole number, exceeds t (the
+    // sum over all does).
     template <typename Fn>
     __device__ __forceinline__ uint32_t find(uint64_t t, uint64_t mine, uint64_t before_wave, Fn measure) {
         // `mine`: this wave's sum; exactly one wave holds the place
         if (t >= before_wave && t - before_wave < mine) {
             uint64_t left = t - before_wave;
             bool open = true;
-            uint32_t first = position(0);
-            asm volatile("" : "+v"(first));
 #pragma unroll
-            for (int v = 0; v < R; ++v) {
-                if (open) {
+            for (int h = 0; h < (K + 31) / 32; ++h) {
+                uint32_t p = position(8 * h);
+#pragma nounroll
+                for (int v = 0; open && v < (K < 32 ? K : 32); v += 4, p += 4 * kWave) {
                     uint64_t w[4], s = 0;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        uint32_t k = key[4 * v + c];
-                        asm volatile("" : "+v"(k));
-                        w[c] = measure(k, first + 4 * kWave * v + c);
+                        w[c] = whole_of(measure(z[h][v + c], p + c));
                         s += w[c];
                     }
                     const uint64_t upto = scan64(s), all = last64(upto);
@@ -546,7 +653,7 @@ struct Held {
                         uint64_t at = upto - s;
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
-                            if (left >= at && left < at + w[c]) sh->cut_position = first + 4 * kWave * v + c;
+                            if (left >= at && left < at + w[c]) sh->cut_position = p + c;
                             at += w[c];
                         }
                         open = false;
@@ -554,7 +661,6 @@ struct Held {
                         left -= all;
                     }
                 }
-                __builtin_amdgcn_sched_barrier(0);
             }
         }
         sync();
@@ -563,12 +669,15 @@ struct Held {
         return p;
     }
 
-    // The bin of a key: linear in the score from the best one down, the last bin for all that is `range` or more
-    // below it.
-    struct Scale { float top, per; uint32_t best; };
-    __device__ __forceinline__ int bin_of(uint32_t k, const Scale& c) const {
-        const float x = (c.top - score_of(k)) * c.per;
-        return k == c.best ? 0 : (x < (float)(kBins - 1) ? (int)x : kBins - 1);
+    // The bin of a score: linear from the best one down, the last bin for all that is the range or more below it.
+    struct Scale { float top, per; };
+    __device__ __forceinline__ int bin_of(float k, const Scale& c) const {
+        const float x = (c.top - k) * c.per;
+        return k == c.top ? 0 : (x < (float)(kBins - 1) ? (int)x : kBins - 1);
+    }
+    __device__ __forceinline__ void add_to_bin(uint32_t bin, bool by_mass, float k, const Asked& ask) {
+        const uint64_t w = by_mass ? whole_of(ask.weight_of(k)) : 1;
+        if (w) atomicAdd((unsigned long long*)&sh->bin[bin], (unsigned long long)w);
     }
 
     // Adds up the bins in their order: the first at which the sum reaches the target (found_bin,
@@ -576,49 +685,55 @@ struct Held {
     template <typename Fn>
     __device__ __forceinline__ void search_bins(Fn target) {
         sync();
-        uint64_t v[4], s = 0, before;
-#pragma unroll
-        for (int b = 0; b < 4; ++b) { v[b] = sh->bin[4 * threadIdx.x + b]; s += v[b]; }
+        const int per = (kBins + threads - 1) / threads, first = per * threadIdx.x;
+        const int end = first + per < kBins ? first + per : kBins;
+        uint64_t s = 0, before;
+        for (int b = first; b < end; ++b) s += sh->bin[b];
         const uint64_t upto = scan64(s);
-        sync();
         if (lane() == 63) sh->wave_sum[wave()] = upto;
         if (threadIdx.x == 0) sh->listed = 0;
         sync();
         uint64_t total = 0;
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < waves; ++w) {
             if (w == wave()) before = total;
             total += sh->wave_sum[w];
         }
         uint64_t at = before + upto - s;
         const uint64_t goal = target(total);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            if (at < goal && goal <= at + v[b]) {
-                sh->found_bin = 4 * threadIdx.x + b;
-                sh->found_before = at;
+        if (at < goal && goal <= at + s)
+            for (int b = first; b < end; ++b) {
+                const uint64_t v = sh->bin[b];
+                if (at < goal && goal <= at + v) {
+                    sh->found_bin = b;
+                    sh->found_before = at;
+                }
+                at += v;
             }
-            at += v[b];
-        }
         sync();
     }
 
-    // Among the listed columns, the last with less than `goal` of the measure before it.
+    // Among the listed columns, the last with less than `goal` of the measure before it.  The bins, done with,
+    // take the listed columns' measures.
     __device__ __forceinline__ Cut rank_list(bool by_mass, uint32_t count, uint64_t before, uint64_t goal,
                                              const Asked& ask) {
-        for (uint32_t i = threadIdx.x; i < count; i += NT) {
-            const uint32_t k = sh->list_key[i], p = sh->list_position[i];
+        for (uint32_t i = threadIdx.x; i < count; i += threads)
+            sh->bin[i] = by_mass ? whole_of(ask.weight_of(sh->list_z[i])) : 1;
+        sync();
+        for (uint32_t i = threadIdx.x; i < count; i += threads) {
+            const float k = sh->list_z[i];
+            const uint32_t p = sh->list_position[i];
             uint64_t front = before;
             for (uint32_t j = 0; j < count; ++j) {
-                const uint32_t kj = sh->list_key[j];
-                if (kj > k || (kj == k && sh->list_position[j] < p)) front += by_mass ? ask.weight_of(kj) : 1;
+                const float kj = sh->list_z[j];
+                if (kj > k || (kj == k && sh->list_position[j] < p)) front += sh->bin[j];
             }
-            const uint64_t own = by_mass ? ask.weight_of(k) : 1;
-            if (front < goal && goal <= front + own) { sh->cut_key = k; sh->cut_position = p; }
+            const uint64_t own = sh->bin[i];
+            if (front < goal && goal <= front + own) { sh->cut_z = k; sh->cut_position = p; }
         }
         sync();
         Cut cut;
-        cut.key = sh->cut_key;
-        cut.position = sh->cut_position;
+        cut.z = sh->cut_z;
+        cut.position = (int)sh->cut_position;
         sync();
         return cut;
     }
@@ -626,10 +741,10 @@ struct Held {
     // The columns that `take` picks, on the list as far as it holds them; how many there are.
     template <typename Fn>
     __device__ __forceinline__ uint32_t make_list(Fn take) {
-        each([&](uint32_t k, uint32_t p) {
+        each([&](float k, uint32_t p) {
             if (take(k, p)) {
                 const uint32_t at = atomicAdd(&sh->listed, 1u);
-                if (at < (uint32_t)kList) { sh->list_key[at] = k; sh->list_position[at] = p; }
+                if (at < (uint32_t)kList) { sh->list_z[at] = k; sh->list_position[at] = p; }
             }
         });
         sync();
@@ -639,21 +754,18 @@ struct Held {
     // The last column, in the order, with less than the target of the measure before it, among the columns
     // that `within` keeps.  by_mass: the measure is the weight and the target share_of(its sum, part), at least 1;
     // else the target is `part` columns (fewer than there are).
-    __device__ __forceinline__ Cut select(bool by_mass, Cut within, uint32_t least, float t, uint32_t part,
+    __device__ __forceinline__ Cut select(bool by_mass, Cut within, float least, float t, uint32_t part,
                                           const Asked& ask) {
         sync();
-        for (int b = threadIdx.x; b < kBins; b += NT) sh->bin[b] = 0;
+        for (int b = threadIdx.x; b < kBins; b += threads) sh->bin[b] = 0;
         sync();
         // past 28 T below the best, a weight is 0
-        const float all = ask.top - score_of(least);
+        const float all = ask.top - least;
         const bool clipped = all > 28.f * t;
         const float range = clipped ? 28.f * t : all;
-        const Scale scale{ask.top, range > 0.f ? (float)(kBins - 1) / range : 0.f, ask.best};
-        each([&](uint32_t k, uint32_t p) {
-            if (within.keeps(k, p)) {
-                const uint64_t w = by_mass ? ask.weight_of(k) : 1;
-                if (w) atomicAdd((unsigned long long*)&sh->bin[bin_of(k, scale)], (unsigned long long)w);
-            }
+        const Scale scale{ask.top, range > 0.f ? (float)(kBins - 1) / range : 0.f};
+        each([&](float k, uint32_t p) {
+            if (within.keeps(k, p)) add_to_bin(bin_of(k, scale), by_mass, k, ask);
         });
         uint64_t goal;
         search_bins([&](uint64_t total) {
@@ -664,27 +776,29 @@ struct Held {
         const int bin = sh->found_bin;
         uint64_t before = sh->found_before;
         if (!by_mass && clipped && bin == kBins - 1) return within;   // what would go has no weight
-        uint32_t listed = make_list([&](uint32_t k, uint32_t p) { return within.keeps(k, p) && bin_of(k, scale) == bin; });
+        uint32_t listed = make_list([&](float k, uint32_t p) { return within.keeps(k, p) && bin_of(k, scale) == bin; });
         if (listed <= (uint32_t)kList) return rank_list(by_mass, listed, before, goal, ask);
 
         // Many columns crowd one bin (equal scores, or some far from the others): bins of keys, narrowed until
-        // the rest can be ranked or is one key.
+        // the rest can be ranked or is one score.
         before = 0;
+        const uint32_t best = key_of(ask.top);
         uint32_t lo = 0, hi = 0xFFFFFFFFu;     // distances of keys from the best
         for (;;) {
-            const auto in = [&](uint32_t k, uint32_t p) {
-                const uint32_t d = ask.best - k;
+            const auto in = [&](float k, uint32_t p) {
+                const uint32_t d = best - key_of(k);
                 return d >= lo && d <= hi && within.keeps(k, p);
             };
             uint32_t far = 0, near = 0;        // the largest distance, the least one's complement
-            each([&](uint32_t k, uint32_t p) {
-                if (in(k, p)) { far = max(far, ask.best - k); near = max(near, ~(ask.best - k)); }
+            each([&](float k, uint32_t p) {
+                const uint32_t d = best - key_of(k);
+                if (in(k, p)) { far = max(far, d); near = max(near, ~d); }
             });
             far = wave_max(far);
             near = wave_max(near);
             sync();
             if (threadIdx.x == 0) { sh->high = 0; sh->low = 0; }
-            for (int b = threadIdx.x; b < kBins; b += NT) sh->bin[b] = 0;
+            for (int b = threadIdx.x; b < kBins; b += threads) sh->bin[b] = 0;
             sync();
             if (lane() == 0) { atomicMax(&sh->high, far); atomicMax(&sh->low, near); }
             sync();
@@ -692,11 +806,8 @@ struct Held {
             hi = sh->high;
             int shift = 0;
             while (((hi - lo) >> shift) >= (uint32_t)kBins) ++shift;
-            each([&](uint32_t k, uint32_t p) {
-                if (in(k, p)) {
-                    const uint64_t w = by_mass ? ask.weight_of(k) : 1;
-                    if (w) atomicAdd((unsigned long long*)&sh->bin[(ask.best - k - lo) >> shift], (unsigned long long)w);
-                }
+            each([&](float k, uint32_t p) {
+                if (in(k, p)) add_to_bin((best - key_of(k) - lo) >> shift, by_mass, k, ask);
             });
             search_bins([&](uint64_t) { return goal - before; });
             before += sh->found_before;
@@ -705,15 +816,16 @@ struct Held {
             hi = end < hi ? end : hi;
             if (lo == hi) {     // equal scores: as many of them, by position, as reach the goal
                 Cut cut;
-                cut.key = ask.best - lo;
-                const uint64_t own = by_mass ? ask.weight_of(cut.key) : 1;
+                cut.z = score_of(best - lo);
+                const uint64_t own = by_mass ? whole_of(ask.weight_of(cut.z)) : 1;
                 const uint64_t more = (goal - before + own - 1) / own;
-                const auto same = [&](uint32_t k, uint32_t p) -> uint64_t { return k == cut.key && within.keeps(k, p); };
-                uint64_t mine = 0, before_wave;
-                each([&](uint32_t k, uint32_t p) { mine += same(k, p); });
-                mine = last64(scan64(mine));
+                const auto same = [&](float k, uint32_t p) { return k == cut.z && within.keeps(k, p) ? 1.f : 0.f; };
+                float count = 0.f;
+                each([&](float k, uint32_t p) { count += same(k, p); });
+                const uint64_t mine = last64(scan64((uint64_t)(uint32_t)count));
+                uint64_t before_wave;
                 sum(mine, &before_wave);
-                cut.position = find(more - 1, mine, before_wave, same);
+                cut.position = (int)find(more - 1, mine, before_wave, same);
                 return cut;
             }
             listed = make_list(in);
@@ -723,44 +835,44 @@ struct Held {
 
     // The draw: the position, and the logarithm of its probability (to every thread).
     struct Drawn { uint32_t position; float log; };
-    __device__ __forceinline__ Drawn draw(uint32_t least, uint32_t count, float t, int top_k, float top_p, float u,
-                                          const Asked& ask) {
+    __device__ __forceinline__ Drawn draw(float t, int top_k, float top_p, float u, const Asked& ask) {
         Cut cut;
+        float least = 0.f;
+        uint32_t count = 0;
+        if (top_k > 0 || top_p < 1.f) spread(&least, &count);
 #pragma nounroll
         for (int by_mass = 0; by_mass < 2; ++by_mass) {     // one copy of the code for both cuts
             if (by_mass ? !(top_p < 1.f) : top_k <= 0 || (uint32_t)top_k >= count) continue;
             const uint32_t part = by_mass ? (top_p > 0.f ? (uint32_t)(top_p * 0x1p24f) : 0) : (uint32_t)top_k;
             cut = select(by_mass != 0, cut, least, t, part, ask);
         }
-        const auto weight = [&](uint32_t k, uint32_t p) -> uint64_t {
-            if (!cut.keeps(k, p)) return 0;
-            const float e = ask.exp_of(k);
-            return e >= ask.least_e ? fixed40(e) : 0;
+        const auto weight = [&](float k, uint32_t p) {
+            const float e = ask.scaled(k);
+            return cut.keeps(k, p) && e >= ask.least ? floorf(e) : 0.f;
         };
-        uint64_t mine = 0, before_wave;
-        each([&](uint32_t k, uint32_t p) { mine += weight(k, p); });
-        mine = last64(scan64(mine));
+        double thread = 0.0;
+        each([&](float k, uint32_t p) { thread += (double)weight(k, p); });
+        const uint64_t mine = last64(scan64(whole_of(thread)));
+        uint64_t before_wave;
         const uint64_t total = sum(mine, &before_wave);
         const uint32_t p = find(share_of(total, (uint32_t)(u * 0x1p24f)), mine, before_wave, weight);
-        each([&](uint32_t k, uint32_t at) { if (at == p) sh->cut_key = k; });
+        each([&](float k, uint32_t at) { if (at == p) sh->cut_z = k; });
         sync();
-        const uint32_t k = sh->cut_key;
-        const float x = k == ask.best ? 0.f : (score_of(k) - ask.top) * ask.inv_t;
+        const float k = sh->cut_z;
+        const float x = k == ask.top ? 0.f : (k - ask.top) * ask.inv_t;
         return Drawn{p, x - logf((float)total * 0x1p-40f)};
     }
 
-    // The first position of the best key.
-    __device__ __forceinline__ uint32_t first_of(uint32_t best) {
+    // The first position of the best score.
+    __device__ __forceinline__ uint32_t first_of(float best) {
         uint32_t p = 0;
-#pragma unroll
-        for (int j = 0; j < 4 * R; ++j)
-            if (key[j] == best) p = max(p, ~(position(j / 4) + j % 4));
+        each([&](float k, uint32_t at) { if (k == best) p = max(p, ~at); });
         p = wave_max(p);
-        if (kWaves > 1) {
+        if (waves > 1) {
             sync();
-            if (lane() == 0) sh->wave_a[wave()] = p;
+            if (lane() == 0) sh->wave_c[wave()] = p;
             sync();
-            for (int w = 0; w < kWaves; ++w) p = max(p, sh->wave_a[w]);
+            for (int w = 0; w < waves; ++w) p = max(p, sh->wave_c[w]);
         }
         return ~p;
     }
@@ -788,59 +900,69 @@ struct Rated {
     }
 };
 
-// Four keys from column c on; columns from n on get 0.
+// Four scores from column c on, -inf for columns from n on and for what may not be drawn.
 template <typename T>
-__device__ __forceinline__ void load_keys(const T* z, uint32_t c, uint32_t n, uint32_t* key) {
+__device__ __forceinline__ void load_scores(const T* row, uint32_t c, uint32_t n, float* z) {
     T v[4];
     if (c + 4 <= n) {
-        __builtin_memcpy(v, z + c, sizeof v);
+        __builtin_memcpy(v, row + c, sizeof v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) key[i] = allowed_key(to_float(v[i]));
+        for (int i = 0; i < 4; ++i) z[i] = to_float(v[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) key[i] = c + i < n ? allowed_key(to_float(z[c + i])) : 0;
+        for (int i = 0; i < 4; ++i) z[i] = c + i < n ? to_float(row[c + i]) : -INFINITY;
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = z[i] > -INFINITY ? z[i] : -INFINITY;    // NaN
 }
 
 // A workgroup a row, the row in registers from its one read on.
-template <int NT, int R, typename T>
-__global__ __launch_bounds__(NT) void k_sample(const T* __restrict__ z, int64_t rows, uint32_t n, int64_t ldz,
-                                               Limits lim, const float* __restrict__ u, Rated rated,
-                                               int32_t* __restrict__ index, float* __restrict__ log) {
-    using H = Held<NT, R>;
+template <int K, int BINS, typename T>
+__global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 5 : 4)) void k_sample(const T* __restrict__ z, int64_t rows, uint32_t n, int64_t ldz,
+                                                 Limits lim, const float* __restrict__ u, Rated rated,
+                                                 int32_t* __restrict__ index, float* __restrict__ log) {
+    using H = Held<K, BINS>;
     extern __shared__ __align__(16) unsigned char shared[];
     H h;
     h.sh = (typename H::Shared*)shared;
+    h.threads = blockDim.x;
+    h.waves = blockDim.x / kWave;
     uint32_t* bits = (uint32_t*)(shared + sizeof(typename H::Shared));   // the columns left out, one bit each
     const int64_t r = blockIdx.x;
+    const T* zr = z + r * ldz;
+#pragma unroll
+    for (int v = 0; v < K / 4; ++v) {
+        float four[4];
+        load_scores(zr, h.position(v), n, four);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h.z[v / 8][v % 8 * 4 + i] = four[i];
+    }
     const int32_t* list;
     int64_t listed;
     if (!rated.row(r, &list, &listed)) {
         if (threadIdx.x == 0) { index[r] = -1; if (log) log[r] = NAN; }
         return;
     }
-    const T* zr = z + r * ldz;
-#pragma unroll
-    for (int v = 0; v < R; ++v) load_keys(zr, h.position(v), n, &h.key[4 * v]);
     if (listed > 0) {
-        for (uint32_t w = threadIdx.x; w < (n + 31) / 32; w += NT) bits[w] = 0;
-        H::sync();
-        for (int64_t k = threadIdx.x; k < listed; k += NT) {
+        for (uint32_t w = threadIdx.x; w < (n + 31) / 32; w += h.threads) bits[w] = 0;
+        h.sync();
+        for (int64_t k = threadIdx.x; k < listed; k += h.threads) {
             const uint32_t c = (uint32_t)list[k];
             if (c < n) atomicOr(&bits[c >> 5], 1u << (c & 31));
         }
-        H::sync();
+        h.sync();
 #pragma unroll
-        for (int v = 0; v < R; ++v) {
+        for (int v = 0; v < K / 4; ++v) {
             const uint32_t c = h.position(v);
             const uint32_t four = c < n ? bits[c >> 5] >> (c & 31) : 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) h.key[4 * v + i] = four >> i & 1 ? 0 : h.key[4 * v + i];
+            for (int i = 0; i < 4; ++i)
+                h.z[v / 8][v % 8 * 4 + i] = four >> i & 1 ? -INFINITY : h.z[v / 8][v % 8 * 4 + i];
         }
     }
-    uint32_t best, least, count;
-    h.range(&best, &least, &count);
-    if (count == 0) {
+    float best;
+    const float mine = h.largest(&best);
+    if (!(best > -INFINITY)) {
         if (threadIdx.x == 0) { index[r] = -1; if (log) log[r] = -INFINITY; }
         return;
     }
@@ -850,10 +972,39 @@ __global__ __launch_bounds__(NT) void k_sample(const T* __restrict__ z, int64_t 
         if (threadIdx.x == 0) { index[r] = (int32_t)p; if (log) log[r] = 0.f; }
         return;
     }
-    const float min_p = limit_of(lim.min_p, lim.min_p_all, r);
-    const Asked ask{best, score_of(best), 1.f / t, min_p > 0.f ? fminf(min_p, 1.f) : 0.f};
-    const auto d = h.draw(least, count, t, lim.top_k ? lim.top_k[r] : lim.top_k_all,
-                          limit_of(lim.top_p, lim.top_p_all, r), unit_of(u[r]), ask);
+    const float min_p = limit_of(lim.min_p, lim.min_p_all, r), top_p = limit_of(lim.top_p, lim.top_p_all, r);
+    const Asked ask{best, 1.f / t, min_p > 0.f ? fminf(min_p, 1.f) * 0x1p40f : 0.f};
+    const int top_k = lim.top_k ? lim.top_k[r] : lim.top_k_all;
+    // A few best columns are looked for among the few that reach a score which enough threads' largest ones reach:
+    // the passes over the row are then two comparisons a score, and all else is done on a list.
+    if (K > 4 && top_k > 0 && top_k <= h.threads * 3 / 4) {
+        const float reached = h.reached_by((uint32_t)top_k, mine, best);
+        const uint32_t count = reached > -INFINITY ? h.collect(reached) : H::kList + 1;
+        if (count <= (uint32_t)H::kList && count <= 4u * h.threads) {
+            Held<4, BINS> few;
+            few.sh = (typename Held<4, BINS>::Shared*)shared;
+            few.threads = h.threads;
+            few.waves = h.waves;
+            uint32_t column[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t at = 4 * threadIdx.x + i;
+                few.z[0][i] = at < count ? few.sh->list_z[at] : -INFINITY;
+                column[i] = at < count ? few.sh->list_position[at] : 0;
+            }
+            few.sync();
+            const auto d = few.draw(t, top_k, top_p, unit_of(u[r]), ask);
+            if (threadIdx.x == d.position / 4) {
+                uint32_t c = column[0];
+#pragma unroll
+                for (int i = 1; i < 4; ++i) c = d.position % 4 == (uint32_t)i ? column[i] : c;
+                index[r] = (int32_t)c;
+                if (log) log[r] = d.log;
+            }
+            return;
+        }
+    }
+    const auto d = h.draw(t, top_k, top_p, unit_of(u[r]), ask);
     if (threadIdx.x == 0) { index[r] = (int32_t)d.position; if (log) log[r] = d.log; }
 }
 
@@ -1376,22 +1527,19 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
     const auto held = [&](auto h, auto* p) {
         using H = decltype(h);
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
-        auto* kernel = k_sample<H::kThreads, H::kColumns / H::kThreads / 4, T>;
+        auto* kernel = k_sample<H::kScores, H::kBins, T>;
         const size_t lds = sizeof(typename H::Shared) + (rated_ptr ? (size_t)(n + 31) / 32 * 4 : 0);
         (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(H::kThreads), lds, (hipStream_t)stream, p, rows,
-                           (uint32_t)n, ldz, lim, u, rated, index, log);
+        const int64_t a_wave = kWave * H::kScores, waves = n < a_wave ? 1 : (n + a_wave - 1) / a_wave;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3((unsigned)(kWave * waves)), lds, (hipStream_t)stream, p,
+                           rows, (uint32_t)n, ldz, lim, u, rated, index, log);
     };
     const auto launch = [&](auto* p) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
-        if (n <= 256) return held(Held<64, 1>(), p);
-        if (n <= 1024) return held(Held<64, 4>(), p);
-        if (n <= 4096) return held(Held<256, 4>(), p);
-        if (n <= 8192) return held(Held<256, 8>(), p);
-        if (n <= 12288) return held(Held<512, 6>(), p);
-        if (n <= 20480) return held(Held<512, 10>(), p);
-        if (n <= 32768) return held(Held<512, 16>(), p);
-        if (n <= 65536) return held(Held<1024, 16>(), p);
+        if (n <= 512) return held(Held<8, 256>(), p);
+        if (n <= 4096) return held(Held<8, 1024>(), p);
+        if (n <= 32768) return held(Held<32, 2048>(), p);
+        if (n <= 65536) return held(Held<64, 4096>(), p);
         const int64_t bits = rated_ptr ? (n < kChunk ? n : kChunk) : 0;
         const size_t lds = sizeof(SampleShared) + (size_t)((bits + 31) / 32) * 4;
         (void)hipFuncSetAttribute((const void*)k_sample_long<T>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
