@@ -7,6 +7,7 @@
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
@@ -139,21 +140,26 @@ __global__ __launch_bounds__(kScoreThreads) void k_score(const int8_t* __restric
 
 // The product in tiles: a workgroup of WU x WI waves holds a tile of users x items, each wave FU x FI
 // fragments of 16 x 16, and walks f in steps of 128.  A step's rows of both sides lie in LDS, 128 bytes a row, while
-// the next step's arrive straight from memory in the other half (buffer_load ... lds: no registers, no
-// instructions but the load).  The 16-byte group c of row r lies in slot c ^ (r / 2 % 8), so that the 16 rows of
-// one operand read spread over all banks.
+// the next steps' (STAGES - 1 of them) arrive straight from memory beside them (buffer_load ... lds: no
+// registers, no instructions but the load).  The 16-byte group c of row r lies in slot c ^ s(r), so that the 16 rows of
+// one operand read spread over all banks: s is r / 2 % 8 where an operand's rows are neighbours.  For
+// outputs of 16 bits an item operand takes rows 0..3 of every 8 of 32, or 4..7 (so that a lane's four items of two
+// fragments are neighbours and go out as 16 bytes), and s is r / 2 % 2 + 2 (r / 8 % 4).
 constexpr int kStep = 128;
 constexpr int64_t kTileStride = 1 << 22;        // row strides below it keep a tile's offsets below 2^30 ...
 constexpr uint32_t kPastEnd = 0x7FFFFFF0u;      // ... and this past every tile's end
 
-template <int WU, int WI, int FU, int FI>
+template <int WU, int WI, int FU, int FI, int STAGES>
 struct Tiles {
     static constexpr int kWaves = WU * WI;
     static constexpr int kUsers = WU * FU * 16, kItems = WI * FI * 16;
     static constexpr int kRows = kUsers + kItems;
     static constexpr int kUserLoads = kUsers / 8 / kWaves, kItemLoads = kItems / 8 / kWaves;   // 1 KB, a wave and step
     static constexpr int kStage = kRows * kStep;           // bytes
+    static constexpr int kStages = STAGES;
     static_assert(kUsers % (8 * kWaves) == 0 && kItems % (8 * kWaves) == 0, "whole loads");
+    static_assert(FI % 2 == 0, "pairs of item fragments");
+    static_assert((STAGES - 2) * (kUserLoads + kItemLoads) < 64, "loads that can be counted");
 };
 
 // A buffer of `bytes` bytes from `base` on (both the same in every lane).
@@ -176,8 +182,11 @@ __device__ __forceinline__ void load_to_lds(i4 buffer, uint32_t voffset, uint32_
                  : "v"(voffset), "s"(buffer), "s"(soffset), "s"(lds)
                  : "memory");
 }
-// All of this wave's loads have arrived and its LDS reads are done.
-__device__ __forceinline__ void settle() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+// All of this wave's loads but the last LEFT have arrived, and its LDS reads are done.
+template <int LEFT>
+__device__ __forceinline__ void settle() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(LEFT) : "memory");
+}
 
 // The bytes of the group at k that lie before f.
 __device__ __forceinline__ i4 keep_bytes(i4 v, int k, int f) {
@@ -201,12 +210,13 @@ __device__ __forceinline__ void tile_of(uint32_t t, uint32_t tu, uint32_t ti, ui
     *i = left / high;
 }
 
-template <typename T, int WU, int WI, int FU, int FI>
+template <typename T, int WU, int WI, int FU, int FI, int STAGES>
 __global__ __launch_bounds__(64 * WU * WI) void k_score_tiles(
     const int8_t* __restrict__ xq, int64_t ldx, const float* __restrict__ xs, int64_t m,
     const int8_t* __restrict__ tq, int64_t ldt, const float* __restrict__ ts, int64_t n, int f,
     T* __restrict__ out, int64_t ldo, uint32_t tu, uint32_t ti) {
-    using C = Tiles<WU, WI, FU, FI>;
+    using C = Tiles<WU, WI, FU, FI, STAGES>;
+    constexpr bool kPairs = sizeof(T) == 2;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t tile_u, tile_i;
@@ -219,34 +229,44 @@ __global__ __launch_bounds__(64 * WU * WI) void k_score_tiles(
     const i4 from_u = buffer_of(xq + u0 * ldx, (uint32_t)((users - 1) * ldx + whole));
     const i4 from_i = buffer_of(tq + i0 * ldt, (uint32_t)((items - 1) * ldt + whole));
     const int first_u = wave * C::kUserLoads * 8, first_i = wave * C::kItemLoads * 8;   // this wave's rows
-    const auto group_of = [&](int r) { return 16 * ((lane & 7) ^ (r >> 1 & 7)); };
+    const auto spread_u = [](int r) { return r >> 1 & 7; };
+    const auto spread_i = [](int r) { return kPairs ? (r >> 1 & 1) | (r >> 3 & 3) << 1 : r >> 1 & 7; };
+    const auto group_u = [&](int r) { return 16 * ((lane & 7) ^ spread_u(r)); };
+    const auto group_i = [&](int r) { return 16 * ((lane & 7) ^ spread_i(r)); };
     uint32_t of_u[C::kUserLoads], of_i[C::kItemLoads];
 #pragma unroll
     for (int l = 0; l < C::kUserLoads; ++l) {
         const int r = first_u + 8 * l + (lane >> 3);
-        of_u[l] = (uint32_t)(r * ldx) + group_of(r);
+        of_u[l] = (uint32_t)(r * ldx) + group_u(r);
     }
 #pragma unroll
     for (int l = 0; l < C::kItemLoads; ++l) {
         const int r = first_i + 8 * l + (lane >> 3);
-        of_i[l] = (uint32_t)(r * ldt) + group_of(r);
+        of_i[l] = (uint32_t)(r * ldt) + group_i(r);
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
     const int steps = (f + kStep - 1) / kStep;
     // groups past f are not read: their offset is past the buffer's end
-    const auto fetch = [&](int step, auto tail) {
-        const uint32_t to = lds0 + (step & 1) * C::kStage;
-        const auto at = [&](uint32_t offset, int r) {
-            return !tail.value || step * kStep + group_of(r) < f ? offset : kPastEnd;
-        };
+    const auto fetch = [&](int step, int stage, auto tail) {
+        const uint32_t to = lds0 + stage * C::kStage;
 #pragma unroll
-        for (int l = 0; l < C::kUserLoads; ++l)
-            load_to_lds(from_u, at(of_u[l], first_u + 8 * l + (lane >> 3)), step * kStep,
-                        __builtin_amdgcn_readfirstlane(to + (first_u + 8 * l) * kStep));
+        for (int l = 0; l < C::kUserLoads; ++l) {
+            const int r = first_u + 8 * l;
+            const bool in = !tail.value || step * kStep + group_u(r + (lane >> 3)) < f;
+            load_to_lds(from_u, in ? of_u[l] : kPastEnd, step * kStep,
+                        __builtin_amdgcn_readfirstlane(to + r * kStep));
+        }
 #pragma unroll
-        for (int l = 0; l < C::kItemLoads; ++l)
-            load_to_lds(from_i, at(of_i[l], first_i + 8 * l + (lane >> 3)), step * kStep,
-                        __builtin_amdgcn_readfirstlane(to + (C::kUsers + first_i + 8 * l) * kStep));
+        for (int l = 0; l < C::kItemLoads; ++l) {
+            const int r = first_i + 8 * l;
+            const bool in = !tail.value || step * kStep + group_i(r + (lane >> 3)) < f;
+            load_to_lds(from_i, in ? of_i[l] : kPastEnd, step * kStep,
+                        __builtin_amdgcn_readfirstlane(to + (C::kUsers + r) * kStep));
+        }
+    };
+    const auto fetch_any = [&](int step, int stage) {
+        if (step + 1 < steps) fetch(step, stage, std::false_type());
+        else fetch(step, stage, std::true_type());
     };
 
     const int wu = wave / WI, wi = wave % WI;
@@ -257,18 +277,24 @@ __global__ __launch_bounds__(64 * WU * WI) void k_score_tiles(
 #pragma unroll
         for (int i = 0; i < FI; ++i) acc[u][i] = i4{0, 0, 0, 0};
 
-    const auto multiply = [&](int step, auto tail) {
-        const unsigned char* at = lds + (step & 1) * C::kStage;
+    // the first item of fragment i's rows 4 x (of a lane's results: 4 group), and the row of the operand's row x
+    const auto item_of = [&](int i, int x) {
+        return kPairs ? (wi * FI + (i & ~1)) * 16 + 8 * x + 4 * (i & 1) : (wi * FI + i) * 16 + 4 * x;
+    };
+    const auto multiply = [&](int step, int stage, auto tail) {
+        const unsigned char* at = lds + stage * C::kStage;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int slot = 16 * ((4 * h + group) ^ (row >> 1 & 7));
             i4 a[FI], b[FU];
 #pragma unroll
-            for (int i = 0; i < FI; ++i)
-                a[i] = *(const i4*)(at + (C::kUsers + (wi * FI + i) * 16 + row) * kStep + slot);
+            for (int i = 0; i < FI; ++i) {
+                const int r = item_of(i, row >> 2) + (row & 3);
+                a[i] = *(const i4*)(at + (C::kUsers + r) * kStep + 16 * ((4 * h + group) ^ spread_i(r)));
+            }
 #pragma unroll
             for (int u = 0; u < FU; ++u) {
-                b[u] = *(const i4*)(at + ((wu * FU + u) * 16 + row) * kStep + slot);
+                const int r = (wu * FU + u) * 16 + row;
+                b[u] = *(const i4*)(at + r * kStep + 16 * ((4 * h + group) ^ spread_u(r)));
                 if (tail.value) b[u] = keep_bytes(b[u], step * kStep + 64 * h + 16 * group, f);
             }
 #pragma unroll
@@ -279,44 +305,74 @@ __global__ __launch_bounds__(64 * WU * WI) void k_score_tiles(
         }
     };
 
-    if (steps > 1) fetch(0, std::false_type());
-    else fetch(0, std::true_type());
-    settle();
+#pragma unroll
+    for (int p = 0; p < STAGES - 1; ++p)
+        if (p < steps) fetch_any(p, p);
+    // the scales, here rather than where they are used: there, each load would be waited for
+    float s[FU], t[FI][4];
+#pragma unroll
+    for (int u = 0; u < FU; ++u) {
+        const int64_t user = u0 + (wu * FU + u) * 16 + row;
+        s[u] = xs[user < m ? user : m - 1];
+    }
+#pragma unroll
+    for (int i = 0; i < FI; ++i) {
+        const int64_t item = i0 + item_of(i, group);
+        if (item + 4 <= n) __builtin_memcpy(t[i], ts + item, 16);
+        else
+            for (int r = 0; r < 4; ++r) t[i][r] = ts[item + r < n ? item + r : n - 1];
+    }
+    // a step: its rows are there and the last step's are done with (one barrier for both), whose place the rows
+    // STAGES - 1 steps on take
+    int stage = 0;
+    const auto after = [](int x) { return x + 1 == STAGES ? 0 : x + 1; };
+    int step = 0;
+    for (; step + STAGES - 1 < steps; ++step) {
+        settle<(STAGES - 2) * (C::kUserLoads + C::kItemLoads)>();
+        __builtin_amdgcn_s_barrier();
+        fetch_any(step + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+        multiply(step, stage, std::false_type());
+        stage = after(stage);
+    }
+    settle<0>();
     __builtin_amdgcn_s_barrier();
-    for (int step = 0; step + 2 < steps; ++step) {
-        fetch(step + 1, std::false_type());
-        multiply(step, std::false_type());
-        settle();
-        __builtin_amdgcn_s_barrier();
+    for (; step + 1 < steps; ++step) {
+        multiply(step, stage, std::false_type());
+        stage = after(stage);
     }
-    if (steps > 1) {
-        fetch(steps - 1, std::true_type());
-        multiply(steps - 2, std::false_type());
-        settle();
-        __builtin_amdgcn_s_barrier();
-    }
-    multiply(steps - 1, std::true_type());
+    multiply(step, stage, std::true_type());
 
 #pragma unroll
     for (int u = 0; u < FU; ++u) {
         const int64_t user = u0 + (wu * FU + u) * 16 + row;
         if (user >= m) continue;
-        const float s = xs[user];
         T* o = out + user * ldo;
+        constexpr int kTogether = kPairs ? 2 : 1;
 #pragma unroll
-        for (int i = 0; i < FI; ++i) {
-            const int64_t item = i0 + (wi * FI + i) * 16 + 4 * group;
-            if (item + 4 <= n) {
-                T v[4];
+        for (int i = 0; i < FI; i += kTogether) {
+            const int64_t item = i0 + item_of(i, group);
+            T v[4 * kTogether];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) from_float((float)acc[u][i][r] * s * ts[item + r], &v[r]);
+            for (int r = 0; r < 4 * kTogether; ++r)
+                from_float((float)acc[u][i + r / 4][r % 4] * s[u] * t[i + r / 4][r % 4], &v[r]);
+            if (item + 4 * kTogether <= n) {
                 __builtin_memcpy(o + item, v, sizeof v);
             } else {
-                for (int r = 0; r < 4; ++r)
-                    if (item + r < n) from_float((float)acc[u][i][r] * s * ts[item + r], o + item + r);
+                for (int r = 0; r < 4 * kTogether; ++r)
+                    if (item + r < n) o[item + r] = v[r];
             }
         }
     }
+}
+
+// Rows of any stride and alignment to rows of a stride that is a multiple of 16, zeros past f.
+__global__ __launch_bounds__(256) void k_pack(const int8_t* __restrict__ from, int64_t ld, int64_t rows, int f,
+                                              int8_t* __restrict__ to, int64_t groups) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows * groups) return;
+    const int64_t r = i / groups;
+    const i4 v = load16(from + r * ld, (int)(i - r * groups) * 16, f);
+    *(i4*)(to + i * 16) = v;
 }
 
 // -------------------------------------------------------------------------------- sample --
@@ -1377,6 +1433,74 @@ struct als_serve_ctx {
 
 namespace {
 
+// Lets a kernel use all of a CU's LDS; once per kernel and device.
+template <typename Kernel>
+void whole_lds(Kernel kernel, int device, std::atomic<uint64_t>* done) {
+    if (done->load(std::memory_order_acquire) >> device & 1) return;
+    if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess)
+        done->fetch_or(1ull << device, std::memory_order_release);
+}
+
+struct ScoreArgs {
+    const int8_t* xq;
+    int64_t ldx;
+    const float* xs;
+    int64_t m;
+    const int8_t* tq;
+    int64_t ldt;
+    const float* ts;
+    int64_t n;
+    int f;
+    void* out;
+    int64_t ldo;
+    hipStream_t stream;
+    int device;
+};
+
+template <typename T, int WU, int WI, int FU, int FI, int STAGES>
+bool launch_tiles(const ScoreArgs& a) {
+    using C = Tiles<WU, WI, FU, FI, STAGES>;
+    static std::atomic<uint64_t> done{0};
+    auto* kernel = k_score_tiles<T, WU, WI, FU, FI, STAGES>;
+    const int64_t tu = (a.m + C::kUsers - 1) / C::kUsers, ti = (a.n + C::kItems - 1) / C::kItems;
+    if (tu > INT32_MAX / ti) return false;
+    const int steps = (a.f + kStep - 1) / kStep;
+    whole_lds(kernel, a.device, &done);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tu * ti)), dim3(64 * C::kWaves),
+                       (steps < STAGES ? steps : STAGES) * C::kStage, a.stream, a.xq, a.ldx, a.xs, a.m, a.tq, a.ldt,
+                       a.ts, a.n, a.f, (T*)a.out, a.ldo, (uint32_t)tu, (uint32_t)ti);
+    return true;
+}
+
+// The tile: the largest that still gives every CU enough of them.  A large tile reads the rows fewer times, which
+// counts where f is large; with few tiles, CUs stand idle (256 x 8,192 x 8,192, us: 256 x 256 tiles 90, 128 x 128
+// 42, 64 x 128 37, 64 x 64 in four stages 27).  Measured (us, users x items x f):
+//   8,192 x 8,192 x 8,192      256 x 256: 437    128 x 128: 492    64 x 128: 586
+//   1,024 x 8,192 x 8,192      256 x 256: 95     128 x 128: 63     64 x 128: 85
+//   2,048 x 2,048 x 1,024      128 x 128: 10.0   64 x 128: 8.9     64 x 64: 11.4
+//   512 x 512 x 4,096          64 x 128: 14.9    64 x 64: 10.8     16 x 64: 8.9
+//   5 x 8,192 x 8,192          64 x 128: 35      64 x 64: 18       16 x 64: 15
+// Up to f = 128 there is one step and the scores' way out counts: 4,096 x 40,000 x 128 to fp32 in 150 us by 128 x 128
+// tiles and 170 by 64 x 128; to 16 bits in 86 by 32 x 256 (half a line of memory a user and wave), 100 and 110.
+template <typename T>
+bool score_tiles(const ScoreArgs& a, int cus) {
+    const auto tiles = [&](int64_t users, int64_t items) {
+        return ((a.m + users - 1) / users) * ((a.n + items - 1) / items);
+    };
+    if (a.m > 16) {
+        if (a.f <= kStep) {
+            if (sizeof(T) == 2 && tiles(32, 256) >= 8 * cus) return launch_tiles<T, 1, 4, 2, 4, 2>(a);
+            if (sizeof(T) == 4 && tiles(128, 128) >= 8 * cus) return launch_tiles<T, 2, 2, 4, 4, 2>(a);
+        } else {
+            if (a.f >= 1024 && tiles(256, 256) >= cus) return launch_tiles<T, 2, 4, 8, 4, 2>(a);
+            if (tiles(128, 128) >= 2 * cus) return launch_tiles<T, 2, 2, 4, 4, 2>(a);
+        }
+        if (tiles(64, 128) >= 2 * cus) return launch_tiles<T, 2, 2, 2, 4, 2>(a);
+        if (tiles(64, 64) >= cus) return launch_tiles<T, 2, 2, 2, 2, 4>(a);
+    }
+    return launch_tiles<T, 1, 2, 1, 2, 4>(a);
+}
+
 int finish(als_serve_ctx* ctx) {
     const hipError_t e = hipGetLastError();
     if (e == hipSuccess) return ALS_OK;
@@ -1463,23 +1587,26 @@ int als_score(als_serve_ctx* ctx, const int8_t* xq, int64_t ldx, const float* xs
         return ALS_ERR_ALIAS;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return ALS_ERR_DEVICE;
-    if (aligned(xq, 16) && aligned(tq, 16) && ldx % 16 == 0 && ldt % 16 == 0 && f > 128 && m > 128 &&
-        ldx < kTileStride && ldt < kTileStride) {
-        using C = Tiles<2, 4, 8, 4>;
-        const int64_t tu = (m + C::kUsers - 1) / C::kUsers, ti = (n + C::kItems - 1) / C::kItems;
-        if (tu * ti > INT32_MAX) return ALS_ERR_INVALID_ARG;
-        const auto launch = [&](auto* p) {
-            using T = std::remove_pointer_t<decltype(p)>;
-            (void)hipFuncSetAttribute((const void*)k_score_tiles<T, 2, 4, 8, 4>,
-                                      hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-            hipLaunchKernelGGL((k_score_tiles<T, 2, 4, 8, 4>), dim3((unsigned)(tu * ti)), dim3(64 * C::kWaves),
-                               2 * C::kStage, (hipStream_t)stream, xq, ldx, xs, m, tq, ldt, ts, n, f, p, ldo,
-                               (uint32_t)tu, (uint32_t)ti);
+    const hipStream_t st = (hipStream_t)stream;
+    // rows that a tile's loads cannot take are first laid out anew, where the workspace holds them
+    const int64_t whole = ((int64_t)f + 15) / 16 * 16;
+    const auto direct = [](const int8_t* q, int64_t ld) { return aligned(q, 16) && ld % 16 == 0 && ld < kTileStride; };
+    const int64_t x_need = direct(xq, ldx) ? 0 : m * whole, t_need = direct(tq, ldt) ? 0 : n * whole;
+    if (m <= (int64_t)ctx->ws_bytes && n <= (int64_t)ctx->ws_bytes && x_need + t_need <= (int64_t)ctx->ws_bytes) {
+        const auto pack = [&](const int8_t*& q, int64_t& ld, int64_t rows, unsigned char* to) {
+            const int64_t groups = whole / 16, blocks = (rows * groups + 255) / 256;
+            hipLaunchKernelGGL(k_pack, dim3((unsigned)blocks), dim3(256), 0, st, q, ld, rows, f, (int8_t*)to, groups);
+            q = (const int8_t*)to;
+            ld = whole;
         };
-        if (dtype == ALS_F32) launch((float*)out);
-        else if (dtype == ALS_F16) launch((F16*)out);
-        else launch((BF16*)out);
-        return finish(ctx);
+        if (x_need) pack(xq, ldx, m, ctx->ws);
+        if (t_need) pack(tq, ldt, n, ctx->ws + x_need);
+        const ScoreArgs args{xq, ldx, xs, m, tq, ldt, ts, n, f, out, ldo, st, ctx->device};
+        bool ok = false;
+        if (dtype == ALS_F32) ok = score_tiles<float>(args, ctx->cus);
+        else if (dtype == ALS_F16) ok = score_tiles<F16>(args, ctx->cus);
+        else ok = score_tiles<BF16>(args, ctx->cus);
+        return ok ? finish(ctx) : ALS_ERR_INVALID_ARG;
     }
     const int64_t item_blocks = (n + kScoreItems - 1) / kScoreItems, user_blocks = (m + 15) / 16;
     if (item_blocks > INT32_MAX / user_blocks) return ALS_ERR_INVALID_ARG;
@@ -1529,7 +1656,8 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
         auto* kernel = k_sample<H::kScores, H::kBins, T>;
         const size_t lds = sizeof(typename H::Shared) + (rated_ptr ? (size_t)(n + 31) / 32 * 4 : 0);
-        (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        static std::atomic<uint64_t> done{0};
+        whole_lds(kernel, ctx->device, &done);
         const int64_t a_wave = kWave * H::kScores, waves = n < a_wave ? 1 : (n + a_wave - 1) / a_wave;
         hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3((unsigned)(kWave * waves)), lds, (hipStream_t)stream, p,
                            rows, (uint32_t)n, ldz, lim, u, rated, index, log);
@@ -1542,7 +1670,8 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
         if (n <= 65536) return held(Held<64, 4096>(), p);
         const int64_t bits = rated_ptr ? (n < kChunk ? n : kChunk) : 0;
         const size_t lds = sizeof(SampleShared) + (size_t)((bits + 31) / 32) * 4;
-        (void)hipFuncSetAttribute((const void*)k_sample_long<T>, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        static std::atomic<uint64_t> done{0};
+        whole_lds(k_sample_long<T>, ctx->device, &done);
         hipLaunchKernelGGL(k_sample_long<T>, dim3((unsigned)rows), dim3(kSampleThreads), lds, (hipStream_t)stream, p,
                            rows, n, ldz, lim, u, rated_ptr, rated_idx, users, of, index, log);
     };
