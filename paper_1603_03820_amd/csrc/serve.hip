@@ -46,41 +46,145 @@ __device__ __forceinline__ void from_float(float v, BF16* out) {
 
 constexpr int kQuantThreads = 256;
 
-// A wave a row: the largest magnitude, then the quotients, the row's second read from the cache.
-template <typename T>
+// A row's scale from the bits of its largest magnitude (NaN where the row is not finite).
+struct RowScale {
+    float largest, inverse;
+    bool finite, far;      // far: 127 x overflows, or the inverse does
+    __device__ __forceinline__ explicit RowScale(uint32_t bits) {
+        largest = __builtin_bit_cast(float, bits);
+        finite = bits < 0x7F800000u;
+        far = largest > 1e36f || largest < 1e-36f;
+        inverse = 1.f / largest;
+    }
+    __device__ __forceinline__ float scale() const { return finite ? largest * (1.f / 127.f) : NAN; }
+    // rint(127 x / a).  The product with 1 / a is within 2^-15 of the quotient, so it rounds to the same whole number
+    // unless it lies that near to a half; a division takes ten instructions, and about one wave in twenty takes it.
+    __device__ __forceinline__ int of(float x) const {
+        const float y = x * 127.f, p = y * inverse;
+        float r = rintf(p);
+        if (far || !(fabsf(fabsf(p - r) - 0.5f) > 0x1p-14f)) {
+            if (!finite || largest == 0.f) return 0;
+            // past the largest float: a power of two off both sides changes no quotient
+            const float down = largest > 1e36f ? 0x1p-8f : 1.f;
+            r = rintf((x * down) * 127.f / (largest * down));
+        }
+        return (int)r;
+    }
+};
+
+template <int N>
+__device__ __forceinline__ uint32_t max_of_lanes(uint32_t v) {     // over N neighbouring lanes, to each
+#pragma unroll
+    for (int d = N / 2; d > 0; d >>= 1) v = max(v, (uint32_t)__shfl_xor(v, d));
+    return v;
+}
+
+// `v` values of a row (of f) from k on as the bits of their magnitudes and as values, 0 past f.
+template <typename T, int V>
+__device__ __forceinline__ uint32_t load_row(const T* row, int k, int f, float (&x)[V]) {
+    T t[V];
+    if (k + V <= f) {
+        __builtin_memcpy(t, row + k, sizeof t);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = to_float(t[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = k + i < f ? to_float(row[k + i]) : 0.f;
+    }
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) most = max(most, __builtin_bit_cast(uint32_t, x[i]) & 0x7FFFFFFFu);
+    return most;
+}
+
+// The values' whole numbers at k, as far as `end` (f and its padding).
+template <int V>
+__device__ __forceinline__ void store_row(int8_t* row, int k, int end, const RowScale& s, const float (&x)[V]) {
+    if (k >= end) return;
+    int8_t v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (int8_t)s.of(x[i]);
+    if (k + V <= end) {
+        __builtin_memcpy(row + k, v, V);
+    } else {
+        for (int i = 0; i < V; ++i)
+            if (k + i < end) row[k + i] = v[i];
+    }
+}
+
+// G lanes a row (or, G = 256, a workgroup), 16 bytes a lane and load, E loads a row and ROWS rows at once, all of which
+// stay in registers between the largest magnitude and the quotients: each row is read once.
+template <typename T, int G, int E, int ROWS>
 __global__ __launch_bounds__(kQuantThreads) void k_quantize(const T* __restrict__ x, int64_t of, int64_t ldx,
                                                             const int32_t* __restrict__ users, int64_t rows,
                                                             int f, int8_t* __restrict__ q, int64_t ldq,
                                                             float* __restrict__ scale) {
-    const int lane = threadIdx.x & (kWave - 1);
-    const int64_t row = (int64_t)blockIdx.x * (kQuantThreads / kWave) + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const int64_t src = users ? (int64_t)users[row] : row;
-    const bool there = src >= 0 && src < of;
-    const T* xr = x + (there ? src : 0) * ldx;
-    float a = 0.f;
-    bool finite = there;
-    if (there)
-        for (int k = lane; k < f; k += kWave) {
-            const float v = fabsf(to_float(xr[k]));
-            finite = finite && v < INFINITY;
-            a = fmaxf(a, v);
-        }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) a = fmaxf(a, __shfl_xor(a, d));
-    finite = __all(finite);
-    // 127 x past the largest float: a power of two off both sides changes no quotient
-    const float down = a > 1e36f ? 0x1p-8f : 1.f;
-    const float div = a * down;
-    int8_t* qr = q + row * ldq;
+    constexpr int V = 16 / sizeof(T), kGroups = kQuantThreads / G;
+    static_assert(G < kQuantThreads || ROWS == 1, "a workgroup takes one row");
+    __shared__ uint32_t of_waves[kQuantThreads / kWave];
+    const int lane = threadIdx.x % G;
+    const int64_t first = ((int64_t)blockIdx.x * kGroups + threadIdx.x / G) * ROWS;
     const int64_t pad = ((int64_t)f + 15) / 16 * 16;
     const int end = (int)(pad < ldq ? pad : ldq);
-    for (int k = lane; k < end; k += kWave) {
-        float v = 0.f;
-        if (finite && a > 0.f && k < f) v = rintf((to_float(xr[k]) * down) * 127.f / div);
-        qr[k] = (int8_t)v;
+    float v[ROWS][E][V];
+    uint32_t most[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const int64_t row = first + r;
+        int64_t src = row;
+        if (users) src = row < rows ? (int64_t)users[row] : -1;
+        const bool there = row < rows && src >= 0 && src < of;
+        most[r] = there ? 0 : 0x7FC00000u;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            most[r] = max(most[r], load_row<T, V>(x + (there ? src * ldx : 0), (e * G + lane) * V, there ? f : 0, v[r][e]));
     }
-    if (lane == 0) scale[row] = finite ? a * (1.f / 127.f) : NAN;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const int64_t row = first + r;
+        uint32_t m = max_of_lanes<(G < kWave ? G : kWave)>(most[r]);
+        if (G == kQuantThreads) {
+            if (lane % kWave == 0) of_waves[lane / kWave] = m;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kQuantThreads / kWave; ++w) m = max(m, of_waves[w]);
+        }
+        if (row >= rows) continue;
+        const RowScale s(m);
+#pragma unroll
+        for (int e = 0; e < E; ++e) store_row<V>(q + row * ldq, (e * G + lane) * V, end, s, v[r][e]);
+        if (lane == 0) scale[row] = s.scale();
+    }
+}
+
+// Rows that no workgroup's registers hold: a workgroup a row, the second read from the cache.
+template <typename T>
+__global__ __launch_bounds__(kQuantThreads) void k_quantize_long(const T* __restrict__ x, int64_t of, int64_t ldx,
+                                                                 const int32_t* __restrict__ users, int64_t rows,
+                                                                 int f, int8_t* __restrict__ q, int64_t ldq,
+                                                                 float* __restrict__ scale) {
+    constexpr int V = 16 / sizeof(T);
+    __shared__ uint32_t of_waves[kQuantThreads / kWave];
+    const int64_t row = blockIdx.x;
+    const int64_t src = users ? (int64_t)users[row] : row;
+    const bool there = src >= 0 && src < of;
+    const T* xr = x + (there ? src * ldx : 0);
+    const int64_t pad = ((int64_t)f + 15) / 16 * 16;
+    const int end = (int)(pad < ldq ? pad : ldq);
+    uint32_t m = there ? 0 : 0x7FC00000u;
+    float v[V];
+    for (int k = threadIdx.x * V; k < f; k += kQuantThreads * V) m = max(m, load_row<T, V>(xr, k, there ? f : 0, v));
+    m = max_of_lanes<kWave>(m);
+    if (threadIdx.x % kWave == 0) of_waves[threadIdx.x / kWave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kQuantThreads / kWave; ++w) m = max(m, of_waves[w]);
+    const RowScale s(m);
+    for (int k = threadIdx.x * V; k < end; k += kQuantThreads * V) {
+        load_row<T, V>(xr, k, there ? f : 0, v);
+        store_row<V>(q + row * ldq, k, end, s, v);
+    }
+    if (threadIdx.x == 0) scale[row] = s.scale();
 }
 
 // --------------------------------------------------------------------------------- score --
@@ -1559,17 +1663,38 @@ int als_quantize(als_serve_ctx* ctx, const void* x, int32_t dtype, int64_t of, i
         return ALS_ERR_ALIAS;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return ALS_ERR_DEVICE;
-    const int64_t per = kQuantThreads / kWave, blocks = (rows + per - 1) / per;
-    if (blocks > INT32_MAX) return ALS_ERR_INVALID_ARG;
+    // as few lanes a row as hold it (a lane holds up to 8 x 16 bytes), several rows at once where they are short
+    const auto go = [&](auto* p, auto lanes, auto loads, auto at_once) {
+        using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
+        constexpr int G = decltype(lanes)::value, E = decltype(loads)::value, R = decltype(at_once)::value;
+        const int64_t per = kQuantThreads / G * R, blocks = (rows + per - 1) / per;
+        if (blocks > INT32_MAX) return false;
+        hipLaunchKernelGGL((k_quantize<T, G, E, R>), dim3((unsigned)blocks), dim3(kQuantThreads), 0,
+                           (hipStream_t)stream, p, of, ldx, users, rows, f, q, ldq, scale);
+        return true;
+    };
+    bool ok = true;
     const auto launch = [&](auto* p) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
-        hipLaunchKernelGGL(k_quantize<T>, dim3((unsigned)blocks), dim3(kQuantThreads), 0, (hipStream_t)stream, p,
-                           of, ldx, users, rows, f, q, ldq, scale);
+        using std::integral_constant;
+        const int groups = (int)((pad + 16 / sizeof(T) - 1) / (16 / sizeof(T)));      // loads of a row
+        if (groups <= 16) ok = go(p, integral_constant<int, 16>(), integral_constant<int, 1>(), integral_constant<int, 4>());
+        else if (groups <= 32) ok = go(p, integral_constant<int, 32>(), integral_constant<int, 1>(), integral_constant<int, 4>());
+        else if (groups <= 64) ok = go(p, integral_constant<int, 64>(), integral_constant<int, 1>(), integral_constant<int, 4>());
+        else if (groups <= 128) ok = go(p, integral_constant<int, 64>(), integral_constant<int, 2>(), integral_constant<int, 2>());
+        else if (groups <= 256) ok = go(p, integral_constant<int, 64>(), integral_constant<int, 4>(), integral_constant<int, 1>());
+        else if (groups <= 512) ok = go(p, integral_constant<int, 256>(), integral_constant<int, 2>(), integral_constant<int, 1>());
+        else if (groups <= 1024) ok = go(p, integral_constant<int, 256>(), integral_constant<int, 4>(), integral_constant<int, 1>());
+        else if (groups <= 2048) ok = go(p, integral_constant<int, 256>(), integral_constant<int, 8>(), integral_constant<int, 1>());
+        else if (rows > INT32_MAX) ok = false;
+        else
+            hipLaunchKernelGGL(k_quantize_long<T>, dim3((unsigned)rows), dim3(kQuantThreads), 0, (hipStream_t)stream,
+                               p, of, ldx, users, rows, f, q, ldq, scale);
     };
     if (dtype == ALS_F32) launch((const float*)x);
     else if (dtype == ALS_F16) launch((const F16*)x);
     else launch((const BF16*)x);
-    return finish(ctx);
+    return ok ? finish(ctx) : ALS_ERR_INVALID_ARG;
 }
 
 int als_score(als_serve_ctx* ctx, const int8_t* xq, int64_t ldx, const float* xs, int64_t m, const int8_t* tq,

@@ -67,6 +67,7 @@ class Context:
 
     def __init__(self, device: int = 0):
         self.device = torch.device("cuda", device)
+        self.index = device
         nbytes = als_serve_workspace_bytes(device)
         if nbytes == 0:
             raise RuntimeError(f"als_serve_workspace_bytes failed for device {device} (not gfx950?)")
@@ -75,6 +76,8 @@ class Context:
         _check("als_serve_init", _lib.als_serve_init(ctypes.byref(h), device,
                                                      ctypes.c_void_p(self.workspace.data_ptr()), nbytes))
         self.handle = h
+        self._limits = _Limits()
+        self._limits_ref = ctypes.byref(self._limits)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -88,94 +91,120 @@ class Context:
             pass
 
 
-class _Call:
-    """One call's stream and tensors.  A tensor that the call allocates is allocated on the call's stream, and
-    one that is used on another stream than the current one is recorded there, so that its memory is not handed
-    out again while the call may still run."""
+# A call's checks take as long as its launch where the work is small, so they read each property of a tensor
+# once and pass plain numbers on (an empty tensor's pointer is 0, which is NULL).
 
-    def __init__(self, ctx: Context, stream):
-        if not ctx.handle:
-            raise ValueError("the context is closed")
-        self.device = ctx.device
-        self.current = torch.cuda.current_stream(ctx.device)
-        self.torch_stream = self.current if stream is None else stream
-        self.other = self.torch_stream != self.current
-        self.stream = ctypes.c_void_p(self.torch_stream.cuda_stream)
 
-    def empty(self, shape, dtype):
-        if not self.other:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(self.torch_stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+def _stream(ctx: Context, stream):
+    """(handle, stream or None): the stream of a call, and the stream itself where it is not the current one."""
+    if not ctx.handle:
+        raise ValueError("the context is closed")
+    current = torch._C._cuda_getCurrentRawStream(ctx.index)
+    if stream is None:
+        return current, None
+    handle = stream.cuda_stream
+    return handle, stream if handle != current else None
 
-    def _use(self, t, name, dtypes):
-        if not isinstance(t, torch.Tensor) or not t.is_cuda:
-            raise TypeError(f"{name} must be a device tensor")
-        if t.device != self.device:
-            raise ValueError(f"{name} is on {t.device}, the context on {self.device}")
-        if t.dtype not in dtypes:
-            raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
-        if self.other:
-            t.record_stream(self.torch_stream)
-        return ctypes.c_void_p(t.data_ptr()) if t.numel() else None
 
-    def vector(self, t, name, dtype, length):
-        p = self._use(t, name, (dtype,))
-        if t.dim() != 1 or t.shape[0] != length:
-            raise ValueError(f"{name} must have {length} elements, has shape {tuple(t.shape)}")
-        if length > 1 and t.stride(0) != 1:
-            raise ValueError(f"{name} must be contiguous")
-        return p
+def _use(ctx: Context, t, name, dtypes, other):
+    """Checks a tensor's place and type.  One that is used on another stream than the current one is recorded
+    there, so that its memory is not handed out again while the call may still run."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.get_device() != ctx.index:
+        raise ValueError(f"{name} is on {t.device}, the context on {ctx.device}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
+    if other is not None:
+        t.record_stream(other)
 
-    def matrix(self, t, name, dtypes, rows=None, cols=None):
-        """(pointer, row stride) of a matrix whose rows are contiguous, at any distance."""
-        p = self._use(t, name, dtypes)
-        if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-            want = ("any" if rows is None else rows, "any" if cols is None else cols)
-            raise ValueError(f"{name} must be a matrix of {want[0]} x {want[1]}, has shape {tuple(t.shape)}")
-        if t.shape[1] > 1 and t.stride(1) != 1:
-            raise ValueError(f"the rows of {name} must be contiguous")
-        if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+
+def _empty(ctx: Context, shape, dtype, other):
+    """Allocated on the call's stream."""
+    if other is None:
+        return torch.empty(shape, dtype=dtype, device=ctx.device)
+    with torch.cuda.stream(other):
+        return torch.empty(shape, dtype=dtype, device=ctx.device)
+
+
+def _vector(ctx: Context, t, name, dtypes, length, other):
+    """Pointer of a contiguous vector of that length."""
+    _use(ctx, t, name, dtypes, other)
+    if t.dim() != 1 or t.numel() != length:
+        raise ValueError(f"{name} must have {length} elements, has shape {tuple(t.shape)}")
+    if length > 1 and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _matrix(ctx: Context, t, name, dtypes, rows, cols, other):
+    """(pointer, row stride, rows, columns) of a matrix whose rows are contiguous, at any distance."""
+    _use(ctx, t, name, dtypes, other)
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+        want = ("any" if rows is None else rows, "any" if cols is None else cols)
+        raise ValueError(f"{name} must be a matrix of {want[0]} x {want[1]}, has shape {tuple(shape)}")
+    rows, cols = shape
+    ld, one = t.stride()
+    if cols > 1 and one != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    if ld < cols:
+        if rows > 1:
             raise ValueError(f"the rows of {name} overlap")
-        return p, (t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0)))
+        ld = cols
+    return t.data_ptr(), ld, rows, cols
+
+
+_I8, _I32, _I64, _F32, _FLOATS = (torch.int8,), (torch.int32,), (torch.int64,), (torch.float32,), tuple(_DTYPES)
 
 
 def als_quantize(ctx: Context, x, users=None, q=None, scale=None, stream=None):
     """(q, scale): the rows of x (f32, f16 or bf16), or the rows `users` (int32) of it, as 8-bit integers
     with one scale each, x ~ scale q.  Without `q` the result is a view of rows whose stride is the next
     multiple of 16."""
-    call = _Call(ctx, stream)
-    px, ldx = call.matrix(x, "x", tuple(_DTYPES))
-    of, f = x.shape
-    rows = of if users is None else users.numel()
-    pu = None if users is None else call.vector(users, "users", torch.int32, rows)
+    handle, other = _stream(ctx, stream)
+    px, ldx, of, f = _matrix(ctx, x, "x", _FLOATS, None, None, other)
+    rows, pu = of, None
+    if users is not None:
+        rows = users.numel()
+        pu = _vector(ctx, users, "users", _I32, rows, other)
     if q is None:
-        q = call.empty((rows, (f + 15) // 16 * 16), torch.int8)[:, :f]
+        ldq = (f + 15) // 16 * 16
+        q = _empty(ctx, (rows, ldq), torch.int8, other)
+        pq = q.data_ptr()
+        if ldq != f:
+            q = q[:, :f]
+    else:
+        pq, ldq, _, _ = _matrix(ctx, q, "q", _I8, rows, f, other)
     if scale is None:
-        scale = call.empty((rows,), torch.float32)
-    pq, ldq = call.matrix(q, "q", (torch.int8,), rows, f)
-    ps = call.vector(scale, "scale", torch.float32, rows)
-    rc = _lib.als_quantize(ctx.handle, px, _DTYPES[x.dtype], of, ldx, pu, rows, f, pq, ldq, ps, call.stream)
-    _check("als_quantize", rc, ctx.handle)
+        scale = _empty(ctx, (rows,), torch.float32, other)
+        ps = scale.data_ptr()
+    else:
+        ps = _vector(ctx, scale, "scale", _F32, rows, other)
+    rc = _lib.als_quantize(ctx.handle, px, _DTYPES[x.dtype], of, ldx, pu, rows, f, pq, ldq, ps, handle)
+    if rc:
+        _check("als_quantize", rc, ctx.handle)
     return q, scale
 
 
 def als_score(ctx: Context, xq, xs, tq, ts, out=None, dtype=torch.float32, stream=None):
     """out[i, j] = xs_i ts_j sum_k xq_ik tq_jk for 8-bit rows with a scale each; out (f32, f16 or bf16, `dtype`
     where it is not given) may have any row stride."""
-    call = _Call(ctx, stream)
-    px, ldx = call.matrix(xq, "xq", (torch.int8,))
-    m, f = xq.shape
-    pt, ldt = call.matrix(tq, "tq", (torch.int8,), None, f)
-    n = tq.shape[0]
+    handle, other = _stream(ctx, stream)
+    px, ldx, m, f = _matrix(ctx, xq, "xq", _I8, None, None, other)
+    pt, ldt, n, _ = _matrix(ctx, tq, "tq", _I8, None, f, other)
     if out is None:
         if dtype not in _DTYPES:
             raise TypeError(f"dtype must be {' or '.join(map(str, _DTYPES))}, got {dtype}")
-        out = call.empty((m, n), dtype)
-    po, ldo = call.matrix(out, "out", tuple(_DTYPES), m, n)
-    rc = _lib.als_score(ctx.handle, px, ldx, call.vector(xs, "xs", torch.float32, m), m, pt, ldt,
-                        call.vector(ts, "ts", torch.float32, n), n, f, po, _DTYPES[out.dtype], ldo, call.stream)
-    _check("als_score", rc, ctx.handle)
+        out = _empty(ctx, (m, n), dtype, other)
+        po, ldo = out.data_ptr(), n
+    else:
+        dtype = out.dtype
+        po, ldo, _, _ = _matrix(ctx, out, "out", _FLOATS, m, n, other)
+    rc = _lib.als_score(ctx.handle, px, ldx, _vector(ctx, xs, "xs", _F32, m, other), m, pt, ldt,
+                        _vector(ctx, ts, "ts", _F32, n, other), n, f, po, _DTYPES[dtype], ldo, handle)
+    if rc:
+        _check("als_score", rc, ctx.handle)
     return out
 
 
@@ -185,40 +214,54 @@ def als_sample(ctx: Context, scores, u, temperature=1.0, top_k=0, top_p=1.0, min
     logarithm of its probability.  temperature, top_k, top_p and min_p are numbers, or tensors with one value
     a row (float32; top_k int32); `rated` = (rowptr, colidx) is a CSR of columns to leave out, row users[r] (int32)
     of it for row r, or row r.  See als_sample in include/als_serve.h for the definition."""
-    call = _Call(ctx, stream)
-    pz, ldz = call.matrix(scores, "scores", tuple(_DTYPES))
-    rows, n = scores.shape
-    lim = _Limits()
-    for name, value, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
-                               ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
-        if isinstance(value, torch.Tensor):
-            setattr(lim, name, call.vector(value, name, dtype, rows))
-        else:
-            setattr(lim, name + "_all", value)
+    handle, other = _stream(ctx, stream)
+    pz, ldz, rows, n = _matrix(ctx, scores, "scores", _FLOATS, None, None, other)
+    lim = ctx._limits
+    lim.temperature = lim.top_k = lim.top_p = lim.min_p = None
+    if isinstance(temperature, torch.Tensor):
+        lim.temperature = _vector(ctx, temperature, "temperature", _F32, rows, other)
+    else:
+        lim.temperature_all = temperature
+    if isinstance(top_k, torch.Tensor):
+        lim.top_k = _vector(ctx, top_k, "top_k", _I32, rows, other)
+    else:
+        lim.top_k_all = top_k
+    if isinstance(top_p, torch.Tensor):
+        lim.top_p = _vector(ctx, top_p, "top_p", _F32, rows, other)
+    else:
+        lim.top_p_all = top_p
+    if isinstance(min_p, torch.Tensor):
+        lim.min_p = _vector(ctx, min_p, "min_p", _F32, rows, other)
+    else:
+        lim.min_p_all = min_p
     pp = pi = pu = None
     of = 0
     if rated is not None:
         rowptr, colidx = rated
         of = rowptr.numel() - 1
-        pp = call.vector(rowptr, "rated[0]", torch.int64, of + 1)
-        pi = call.vector(colidx, "rated[1]", torch.int32, colidx.numel())
-        if pi is None:
-            pi = pp     # every row is empty: nothing is read
+        pp = _vector(ctx, rowptr, "rated[0]", _I64, of + 1, other)
+        # (of a CSR without entries nothing is read)
+        pi = _vector(ctx, colidx, "rated[1]", _I32, colidx.numel(), other) or pp
         if users is not None:
-            pu = call.vector(users, "users", torch.int32, rows)
+            pu = _vector(ctx, users, "users", _I32, rows, other)
         elif of < rows:
             raise ValueError(f"rated has {of} rows, scores {rows}")
     elif users is not None:
         raise ValueError("users without rated")
     if index is None:
-        index = call.empty((rows,), torch.int32)
+        index = _empty(ctx, (rows,), torch.int32, other)
+        p_index = index.data_ptr()
+    else:
+        p_index = _vector(ctx, index, "index", _I32, rows, other)
     if log is None:
-        log = call.empty((rows,), torch.float32)
-    rc = _lib.als_sample(ctx.handle, pz, _DTYPES[scores.dtype], rows, n, ldz, ctypes.byref(lim),
-                         call.vector(u, "u", torch.float32, rows), pp, pi, pu, of,
-                         call.vector(index, "index", torch.int32, rows), call.vector(log, "log", torch.float32, rows),
-                         call.stream)
-    _check("als_sample", rc, ctx.handle)
+        log = _empty(ctx, (rows,), torch.float32, other)
+        p_log = log.data_ptr()
+    else:
+        p_log = _vector(ctx, log, "log", _F32, rows, other)
+    rc = _lib.als_sample(ctx.handle, pz, _DTYPES[scores.dtype], rows, n, ldz, ctx._limits_ref,
+                         _vector(ctx, u, "u", _F32, rows, other), pp, pi, pu, of, p_index, p_log, handle)
+    if rc:
+        _check("als_sample", rc, ctx.handle)
     return index, log
 
 
