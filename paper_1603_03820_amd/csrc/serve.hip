@@ -112,49 +112,39 @@ __device__ __forceinline__ void store_row(int8_t* row, int k, int end, const Row
     }
 }
 
-// G lanes a row (or, G = 256, a workgroup), 16 bytes a lane and load, E loads a row and ROWS rows at once, all of which
-// stay in registers between the largest magnitude and the quotients: each row is read once.
-template <typename T, int G, int E, int ROWS>
+// G lanes a row (or, G = 256, a workgroup), 16 bytes a lane and load, E loads, all of which stay in registers between
+// the largest magnitude and the quotients: each row is read once.
+template <typename T, int G, int E>
 __global__ __launch_bounds__(kQuantThreads) void k_quantize(const T* __restrict__ x, int64_t of, int64_t ldx,
                                                             const int32_t* __restrict__ users, int64_t rows,
                                                             int f, int8_t* __restrict__ q, int64_t ldq,
                                                             float* __restrict__ scale) {
-    constexpr int V = 16 / sizeof(T), kGroups = kQuantThreads / G;
-    static_assert(G < kQuantThreads || ROWS == 1, "a workgroup takes one row");
+    constexpr int V = 16 / sizeof(T);
     __shared__ uint32_t of_waves[kQuantThreads / kWave];
     const int lane = threadIdx.x % G;
-    const int64_t first = ((int64_t)blockIdx.x * kGroups + threadIdx.x / G) * ROWS;
+    const int64_t row = (int64_t)blockIdx.x * (kQuantThreads / G) + threadIdx.x / G;
+    int64_t src = row;
+    if (users) src = row < rows ? (int64_t)users[row] : -1;
+    const bool there = row < rows && src >= 0 && src < of;
+    const T* xr = x + (there ? src * ldx : 0);
+    float v[E][V];
+    uint32_t most = there ? 0 : 0x7FC00000u;
+#pragma unroll
+    for (int e = 0; e < E; ++e) most = max(most, load_row<T, V>(xr, (e * G + lane) * V, there ? f : 0, v[e]));
+    most = max_of_lanes<(G < kWave ? G : kWave)>(most);
+    if (G == kQuantThreads) {
+        if (lane % kWave == 0) of_waves[lane / kWave] = most;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kQuantThreads / kWave; ++w) most = max(most, of_waves[w]);
+    }
+    if (row >= rows) return;
+    const RowScale s(most);
     const int64_t pad = ((int64_t)f + 15) / 16 * 16;
     const int end = (int)(pad < ldq ? pad : ldq);
-    float v[ROWS][E][V];
-    uint32_t most[ROWS];
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const int64_t row = first + r;
-        int64_t src = row;
-        if (users) src = row < rows ? (int64_t)users[row] : -1;
-        const bool there = row < rows && src >= 0 && src < of;
-        most[r] = there ? 0 : 0x7FC00000u;
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-            most[r] = max(most[r], load_row<T, V>(x + (there ? src * ldx : 0), (e * G + lane) * V, there ? f : 0, v[r][e]));
-    }
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const int64_t row = first + r;
-        uint32_t m = max_of_lanes<(G < kWave ? G : kWave)>(most[r]);
-        if (G == kQuantThreads) {
-            if (lane % kWave == 0) of_waves[lane / kWave] = m;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < kQuantThreads / kWave; ++w) m = max(m, of_waves[w]);
-        }
-        if (row >= rows) continue;
-        const RowScale s(m);
-#pragma unroll
-        for (int e = 0; e < E; ++e) store_row<V>(q + row * ldq, (e * G + lane) * V, end, s, v[r][e]);
-        if (lane == 0) scale[row] = s.scale();
-    }
+    for (int e = 0; e < E; ++e) store_row<V>(q + row * ldq, (e * G + lane) * V, end, s, v[e]);
+    if (lane == 0) scale[row] = s.scale();
 }
 
 // Rows that no workgroup's registers hold: a workgroup a row, the second read from the cache.
@@ -1663,29 +1653,33 @@ int als_quantize(als_serve_ctx* ctx, const void* x, int32_t dtype, int64_t of, i
         return ALS_ERR_ALIAS;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return ALS_ERR_DEVICE;
-    // as few lanes a row as hold it (a lane holds up to 8 x 16 bytes), several rows at once where they are short
-    const auto go = [&](auto* p, auto lanes, auto loads, auto at_once) {
+    const auto go = [&](auto* p, auto lanes, auto loads) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
-        constexpr int G = decltype(lanes)::value, E = decltype(loads)::value, R = decltype(at_once)::value;
-        const int64_t per = kQuantThreads / G * R, blocks = (rows + per - 1) / per;
+        constexpr int G = decltype(lanes)::value, E = decltype(loads)::value;
+        const int64_t per = kQuantThreads / G, blocks = (rows + per - 1) / per;
         if (blocks > INT32_MAX) return false;
-        hipLaunchKernelGGL((k_quantize<T, G, E, R>), dim3((unsigned)blocks), dim3(kQuantThreads), 0,
+        hipLaunchKernelGGL((k_quantize<T, G, E>), dim3((unsigned)blocks), dim3(kQuantThreads), 0,
                            (hipStream_t)stream, p, of, ldx, users, rows, f, q, ldq, scale);
         return true;
     };
+    // Two loads a lane and the fewest lanes that hold the row so, up to a wave; then more loads, then a workgroup.
+    // 625,000 x 100 fp32: 16 lanes of 2 loads 61 us, 8 of 4 65, 32 of 1 100, 32 of 2 94 (half the lanes idle);
+    // 200,000 x 256: 32 of 2 44, 16 of 4 49, 64 of 1 56; 1,000,000 x 16: 4 of 2 17, 8 of 1 30, 16 of 1 58.
     bool ok = true;
     const auto launch = [&](auto* p) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
         using std::integral_constant;
+        using Two = integral_constant<int, 2>;
         const int groups = (int)((pad + 16 / sizeof(T) - 1) / (16 / sizeof(T)));      // loads of a row
-        if (groups <= 16) ok = go(p, integral_constant<int, 16>(), integral_constant<int, 1>(), integral_constant<int, 4>());
-        else if (groups <= 32) ok = go(p, integral_constant<int, 32>(), integral_constant<int, 1>(), integral_constant<int, 4>());
-        else if (groups <= 64) ok = go(p, integral_constant<int, 64>(), integral_constant<int, 1>(), integral_constant<int, 4>());
-        else if (groups <= 128) ok = go(p, integral_constant<int, 64>(), integral_constant<int, 2>(), integral_constant<int, 2>());
-        else if (groups <= 256) ok = go(p, integral_constant<int, 64>(), integral_constant<int, 4>(), integral_constant<int, 1>());
-        else if (groups <= 512) ok = go(p, integral_constant<int, 256>(), integral_constant<int, 2>(), integral_constant<int, 1>());
-        else if (groups <= 1024) ok = go(p, integral_constant<int, 256>(), integral_constant<int, 4>(), integral_constant<int, 1>());
-        else if (groups <= 2048) ok = go(p, integral_constant<int, 256>(), integral_constant<int, 8>(), integral_constant<int, 1>());
+        if (groups <= 8) ok = go(p, integral_constant<int, 4>(), Two());
+        else if (groups <= 16) ok = go(p, integral_constant<int, 8>(), Two());
+        else if (groups <= 32) ok = go(p, integral_constant<int, 16>(), Two());
+        else if (groups <= 64) ok = go(p, integral_constant<int, 32>(), Two());
+        else if (groups <= 128) ok = go(p, integral_constant<int, 64>(), Two());
+        else if (groups <= 256) ok = go(p, integral_constant<int, 64>(), integral_constant<int, 4>());
+        else if (groups <= 512) ok = go(p, integral_constant<int, 256>(), Two());
+        else if (groups <= 1024) ok = go(p, integral_constant<int, 256>(), integral_constant<int, 4>());
+        else if (groups <= 2048) ok = go(p, integral_constant<int, 256>(), integral_constant<int, 8>());
         else if (rows > INT32_MAX) ok = false;
         else
             hipLaunchKernelGGL(k_quantize_long<T>, dim3((unsigned)rows), dim3(kQuantThreads), 0, (hipStream_t)stream,
