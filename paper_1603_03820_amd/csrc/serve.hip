@@ -500,15 +500,6 @@ __device__ __forceinline__ float score_of(uint32_t key) {
 
 __device__ __forceinline__ float unit_of(float u) { return u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f; }
 
-// floor(2^40 e), 0 <= e <= 1; NaN gives 0.
-__device__ __forceinline__ uint64_t fixed40(float e) {
-    if (!(e > 0.f)) return 0;
-    const uint32_t b = __builtin_bit_cast(uint32_t, e);
-    const uint64_t mant = (b & 0x7FFFFFu) | 0x800000u;
-    const int shift = (int)(b >> 23) - 110;
-    return shift >= 0 ? mant << shift : (shift > -32 ? mant >> -shift : 0);
-}
-
 // floor(total part / 2^24), part <= 2^24, total < 2^62.
 __device__ __forceinline__ uint64_t share_of(uint64_t total, uint32_t part) {
     return (total >> 24) * part + (((total & 0xFFFFFFu) * part) >> 24);
@@ -714,34 +705,42 @@ struct Held {
         *count = n;
     }
 
-    // A score that at least k columns reach (and few more, where scores lie in no order): the k-th largest of the
-    // threads' largest ones, as near below it as bins tell.  -inf: fewer than k threads hold a column.
-    __device__ __forceinline__ float reached_by(uint32_t k, float mine, float best) {
-        float low = wave_max(mine > -INFINITY ? -mine : -INFINITY);     // the least one's negative
+    // A value that at least k of those reach that `values(fn)` hands this thread, and few more: the k-th largest, as
+    // near below it as bins tell.  -inf: there are fewer than k.  `best` is the largest.
+    template <typename Values>
+    __device__ __forceinline__ float reached_by(uint32_t k, float best, Values values) {
+        float low = -INFINITY;      // the least one's negative
+        values([&](float v) { low = fmaxf(low, v > -INFINITY ? -v : -INFINITY); });
+        low = wave_max(low);
+        sync();
         if (lane() == 0) sh->wave_b[wave()] = low;
         for (int b = threadIdx.x; b < kBins; b += threads) sh->bin[b] = 0;
         sync();
         for (int w = 0; w < waves; ++w) low = fmaxf(low, sh->wave_b[w]);
         const Scale scale{best, best + low > 0.f ? (float)(kBins - 1) / (best + low) : 0.f};
-        const int bin = mine > -INFINITY ? bin_of(mine, scale) : kBins;
-        if (bin < kBins) atomicAdd((unsigned long long*)&sh->bin[bin], 1ull);
+        values([&](float v) {
+            if (v > -INFINITY) atomicAdd((unsigned long long*)&sh->bin[bin_of(v, scale)], 1ull);
+        });
         if (threadIdx.x == 0) sh->found_bin = kBins;
         search_bins([&](uint64_t) { return (uint64_t)k; });
         const int found = (int)sh->found_bin;
-        if (found == kBins) return -INFINITY;
-        low = wave_max(bin <= found ? -mine : -INFINITY);
+        low = -INFINITY;
+        values([&](float v) { low = fmaxf(low, v > -INFINITY && bin_of(v, scale) <= found ? -v : -INFINITY); });
+        low = wave_max(low);
         if (lane() == 0) sh->wave_b[wave()] = low;
         sync();
         for (int w = 0; w < waves; ++w) low = fmaxf(low, sh->wave_b[w]);
         sync();
-        return -low;
+        return found == kBins ? -INFINITY : -low;
     }
 
-    // The columns with a score of `least` or more on the list, by position; how many there are (if the list
-    // does not hold them, it is not written).
-    __device__ __forceinline__ uint32_t collect(float least) {
+    // put(i, score, position) for the columns that `take(score)` picks, i counting them by position, where they
+    // are no more than `most`; how many there are.
+    template <typename Take, typename Put>
+    __device__ __forceinline__ uint32_t collect(uint32_t most, Take take, Put put) {
         uint32_t mine = 0;
-        each([&](float k, uint32_t) { mine += (uint32_t)__popcll(__ballot(k >= least)); });
+        each([&](float k, uint32_t) { mine += (uint32_t)__popcll(__ballot(take(k))); });
+        sync();
         if (lane() == 0) sh->wave_c[wave()] = mine;
         sync();
         uint32_t total = 0, at = 0;
@@ -749,7 +748,8 @@ struct Held {
             if (w == wave()) at = total;
             total += sh->wave_c[w];
         }
-        if (total > (uint32_t)kList) { sync(); return total; }
+        sync();
+        if (total > most) return total;
         const uint64_t below = (1ull << lane()) - 1;
 #pragma unroll
         for (int h = 0; h < (K + 31) / 32; ++h) {
@@ -760,17 +760,14 @@ struct Held {
                 uint32_t mine = at, all = 0;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    takes[c] = __ballot(z[h][v + c] >= least);
+                    takes[c] = __ballot(take(z[h][v + c]));
                     mine += __popcll(takes[c] & below);
                     all += __popcll(takes[c]);
                 }
                 if (all) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
-                        if (takes[c] >> lane() & 1) {
-                            sh->list_z[mine] = z[h][v + c];
-                            sh->list_position[mine++] = p + c;
-                        }
+                        if (takes[c] >> lane() & 1) put(mine++, z[h][v + c], p + c);
                     at += all;
                 }
             }
@@ -821,6 +818,13 @@ struct Held {
 
     // The bin of a score: linear from the best one down, the last bin for all that is the range or more below it.
     struct Scale { float top, per; };
+    // Over all scores, but no further than 28 T below the best, where a weight is 0 (clipped).
+    static __device__ __forceinline__ Scale scale_of(float top, float least, float t, bool* clipped) {
+        const float all = top - least;
+        *clipped = all > 28.f * t;
+        const float range = *clipped ? 28.f * t : all;
+        return Scale{top, range > 0.f ? (float)(kBins - 1) / range : 0.f};
+    }
     __device__ __forceinline__ int bin_of(float k, const Scale& c) const {
         const float x = (c.top - k) * c.per;
         return k == c.top ? 0 : (x < (float)(kBins - 1) ? (int)x : kBins - 1);
@@ -904,22 +908,20 @@ struct Held {
     // The last column, in the order, with less than the target of the measure before it, among the columns
     // that `within` keeps.  by_mass: the measure is the weight and the target share_of(its sum, part), at least 1;
     // else the target is `part` columns (fewer than there are).
+    // (`given`, where it is not 0, is the target itself.)
     __device__ __forceinline__ Cut select(bool by_mass, Cut within, float least, float t, uint32_t part,
-                                          const Asked& ask) {
+                                          const Asked& ask, uint64_t given = 0) {
         sync();
         for (int b = threadIdx.x; b < kBins; b += threads) sh->bin[b] = 0;
         sync();
-        // past 28 T below the best, a weight is 0
-        const float all = ask.top - least;
-        const bool clipped = all > 28.f * t;
-        const float range = clipped ? 28.f * t : all;
-        const Scale scale{ask.top, range > 0.f ? (float)(kBins - 1) / range : 0.f};
+        bool clipped;
+        const Scale scale = scale_of(ask.top, least, t, &clipped);
         each([&](float k, uint32_t p) {
             if (within.keeps(k, p)) add_to_bin(bin_of(k, scale), by_mass, k, ask);
         });
         uint64_t goal;
         search_bins([&](uint64_t total) {
-            goal = by_mass ? share_of(total, part) : part;
+            goal = given ? given : (by_mass ? share_of(total, part) : part);
             if (goal < 1) goal = 1;
             return goal;
         });
@@ -985,7 +987,10 @@ struct Held {
 
     // The draw: the position, and the logarithm of its probability (to every thread).
     struct Drawn { uint32_t position; float log; };
-    __device__ __forceinline__ Drawn draw(float t, int top_k, float top_p, float u, const Asked& ask) {
+    template <typename Wanted>
+    __device__ __forceinline__ Drawn draw(const Wanted& want, const Asked& ask) {
+        const int top_k = want.top_k;
+        const float top_p = want.top_p;
         Cut cut;
         float least = 0.f;
         uint32_t count = 0;
@@ -993,8 +998,7 @@ struct Held {
 #pragma nounroll
         for (int by_mass = 0; by_mass < 2; ++by_mass) {     // one copy of the code for both cuts
             if (by_mass ? !(top_p < 1.f) : top_k <= 0 || (uint32_t)top_k >= count) continue;
-            const uint32_t part = by_mass ? (top_p > 0.f ? (uint32_t)(top_p * 0x1p24f) : 0) : (uint32_t)top_k;
-            cut = select(by_mass != 0, cut, least, t, part, ask);
+            cut = select(by_mass != 0, cut, least, want.t, by_mass ? want.part() : (uint32_t)top_k, ask);
         }
         const auto weight = [&](float k, uint32_t p) {
             const float e = ask.scaled(k);
@@ -1005,7 +1009,7 @@ struct Held {
         const uint64_t mine = last64(scan64(whole_of(thread)));
         uint64_t before_wave;
         const uint64_t total = sum(mine, &before_wave);
-        const uint32_t p = find(share_of(total, (uint32_t)(u * 0x1p24f)), mine, before_wave, weight);
+        const uint32_t p = find(share_of(total, (uint32_t)(want.u * 0x1p24f)), mine, before_wave, weight);
         each([&](float k, uint32_t at) { if (at == p) sh->cut_z = k; });
         sync();
         const float k = sh->cut_z;
@@ -1066,6 +1070,55 @@ __device__ __forceinline__ void load_scores(const T* row, uint32_t c, uint32_t n
     for (int i = 0; i < 4; ++i) z[i] = z[i] > -INFINITY ? z[i] : -INFINITY;    // NaN
 }
 
+// Columns base .. base + n of a row into registers, without those on the list; `bits` is LDS, one a column.
+template <typename H, typename T>
+__device__ __forceinline__ void take_columns(H& h, const T* row, uint32_t base, uint32_t n, const Rated& rated, int64_t r,
+                                             uint32_t* bits, bool* there) {
+    constexpr int K = H::kScores;
+#pragma unroll
+    for (int v = 0; v < K / 4; ++v) {
+        float four[4];
+        load_scores(row + base, h.position(v), n, four);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h.z[v / 8][v % 8 * 4 + i] = four[i];
+    }
+    const int32_t* list;
+    int64_t listed;
+    *there = rated.row(r, &list, &listed);
+    if (!*there || listed <= 0) return;
+    for (uint32_t w = threadIdx.x; w < (n + 31) / 32; w += h.threads) bits[w] = 0;
+    h.sync();
+    for (int64_t k = threadIdx.x; k < listed; k += h.threads) {
+        const uint32_t c = (uint32_t)list[k] - base;
+        if (c < n) atomicOr(&bits[c >> 5], 1u << (c & 31));
+    }
+    h.sync();
+#pragma unroll
+    for (int v = 0; v < K / 4; ++v) {
+        const uint32_t c = h.position(v);
+        const uint32_t four = c < n ? bits[c >> 5] >> (c & 31) : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            h.z[v / 8][v % 8 * 4 + i] = four >> i & 1 ? -INFINITY : h.z[v / 8][v % 8 * 4 + i];
+    }
+    h.sync();
+}
+
+// What row r asks for.
+struct Wanted {
+    float t, top_p, least, u;
+    int top_k;
+    __device__ __forceinline__ Wanted(const Limits& lim, const float* u_, int64_t r) {
+        t = limit_of(lim.temperature, lim.temperature_all, r);
+        top_p = limit_of(lim.top_p, lim.top_p_all, r);
+        const float min_p = limit_of(lim.min_p, lim.min_p_all, r);
+        least = min_p > 0.f ? fminf(min_p, 1.f) * 0x1p40f : 0.f;
+        top_k = lim.top_k ? lim.top_k[r] : lim.top_k_all;
+        u = unit_of(u_[r]);
+    }
+    __device__ __forceinline__ uint32_t part() const { return top_p > 0.f ? (uint32_t)(top_p * 0x1p24f) : 0; }
+};
+
 // A workgroup a row, the row in registers from its one read on.
 template <int K, int BINS, typename T>
 __global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 5 : 4)) void k_sample(const T* __restrict__ z, int64_t rows, uint32_t n, int64_t ldz,
@@ -1079,36 +1132,11 @@ __global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 5 : 4)) void k_sample
     h.waves = blockDim.x / kWave;
     uint32_t* bits = (uint32_t*)(shared + sizeof(typename H::Shared));   // the columns left out, one bit each
     const int64_t r = blockIdx.x;
-    const T* zr = z + r * ldz;
-#pragma unroll
-    for (int v = 0; v < K / 4; ++v) {
-        float four[4];
-        load_scores(zr, h.position(v), n, four);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h.z[v / 8][v % 8 * 4 + i] = four[i];
-    }
-    const int32_t* list;
-    int64_t listed;
-    if (!rated.row(r, &list, &listed)) {
+    bool there;
+    take_columns(h, z + r * ldz, 0, n, rated, r, bits, &there);
+    if (!there) {
         if (threadIdx.x == 0) { index[r] = -1; if (log) log[r] = NAN; }
         return;
-    }
-    if (listed > 0) {
-        for (uint32_t w = threadIdx.x; w < (n + 31) / 32; w += h.threads) bits[w] = 0;
-        h.sync();
-        for (int64_t k = threadIdx.x; k < listed; k += h.threads) {
-            const uint32_t c = (uint32_t)list[k];
-            if (c < n) atomicOr(&bits[c >> 5], 1u << (c & 31));
-        }
-        h.sync();
-#pragma unroll
-        for (int v = 0; v < K / 4; ++v) {
-            const uint32_t c = h.position(v);
-            const uint32_t four = c < n ? bits[c >> 5] >> (c & 31) : 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                h.z[v / 8][v % 8 * 4 + i] = four >> i & 1 ? -INFINITY : h.z[v / 8][v % 8 * 4 + i];
-        }
     }
     float best;
     const float mine = h.largest(&best);
@@ -1116,21 +1144,26 @@ __global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 5 : 4)) void k_sample
         if (threadIdx.x == 0) { index[r] = -1; if (log) log[r] = -INFINITY; }
         return;
     }
-    const float t = limit_of(lim.temperature, lim.temperature_all, r);
-    if (!(t > 0.f)) {
+    const Wanted want(lim, u, r);
+    const int top_k = want.top_k;
+    if (!(want.t > 0.f)) {
         const uint32_t p = h.first_of(best);
         if (threadIdx.x == 0) { index[r] = (int32_t)p; if (log) log[r] = 0.f; }
         return;
     }
-    const float min_p = limit_of(lim.min_p, lim.min_p_all, r), top_p = limit_of(lim.top_p, lim.top_p_all, r);
-    const Asked ask{best, 1.f / t, min_p > 0.f ? fminf(min_p, 1.f) * 0x1p40f : 0.f};
-    const int top_k = lim.top_k ? lim.top_k[r] : lim.top_k_all;
+    const Asked ask{best, 1.f / want.t, want.least};
     // A few best columns are looked for among the few that reach a score which enough threads' largest ones reach:
     // the passes over the row are then two comparisons a score, and all else is done on a list.
     if (K > 4 && top_k > 0 && top_k <= h.threads * 3 / 4) {
-        const float reached = h.reached_by((uint32_t)top_k, mine, best);
-        const uint32_t count = reached > -INFINITY ? h.collect(reached) : H::kList + 1;
-        if (count <= (uint32_t)H::kList && count <= 4u * h.threads) {
+        const float reached = h.reached_by((uint32_t)top_k, best, [&](auto fn) { fn(mine); });
+        const uint32_t most = 4 * h.threads < H::kList ? 4 * h.threads : H::kList;
+        const uint32_t count = !(reached > -INFINITY) ? most + 1 : h.collect(
+            most, [&](float v) { return v >= reached; },
+            [&](uint32_t i, float v, uint32_t position) {
+                h.sh->list_z[i] = v;
+                h.sh->list_position[i] = position;
+            });
+        if (count <= most) {
             Held<4, BINS> few;
             few.sh = (typename Held<4, BINS>::Shared*)shared;
             few.threads = h.threads;
@@ -1143,7 +1176,7 @@ __global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 5 : 4)) void k_sample
                 column[i] = at < count ? few.sh->list_position[at] : 0;
             }
             few.sync();
-            const auto d = few.draw(t, top_k, top_p, unit_of(u[r]), ask);
+            const auto d = few.draw(want, ask);
             if (threadIdx.x == d.position / 4) {
                 uint32_t c = column[0];
 #pragma unroll
@@ -1154,9 +1187,18 @@ __global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 5 : 4)) void k_sample
             return;
         }
     }
-    const auto d = h.draw(t, top_k, top_p, unit_of(u[r]), ask);
+    const auto d = h.draw(want, ask);
     if (threadIdx.x == 0) { index[r] = (int32_t)d.position; if (log) log[r] = d.log; }
 }
+
+enum RowKind { kRowNone, kRowBest, kRowFew, kRowShare, kRowRest, kRowSlow };
+
+// What a long row's kernels tell one another.
+struct RowPlan {
+    int kind;
+    int bin;
+    uint64_t before, goal;
+};
 
 struct SampleShared {
     uint64_t mass[kBins];
@@ -1181,7 +1223,7 @@ struct Row {
     int64_t rated_count;
     SampleShared* sh;
     uint32_t best;      // the largest key
-    float top, inv_t;
+    Asked ask;
     bool one_chunk;
 
     // Marks the left-out columns of [c0, c1).
@@ -1211,12 +1253,8 @@ struct Row {
         }
     }
 
-    __device__ float exp_of(uint32_t d) const {
-        const float v = score_of(best - d);
-        const float x = d == 0 ? 0.f : (v - top) * inv_t;
-        return expf(x);
-    }
-    __device__ uint64_t weight_of(uint32_t d) const { return fixed40(exp_of(d)); }
+    __device__ float scaled(uint32_t d) const { return ask.scaled(score_of(best - d)); }
+    __device__ uint64_t weight_of(uint32_t d) const { return whole_of(floorf(scaled(d))); }
 };
 
 // Sums over the workgroup, to every thread.
@@ -1358,15 +1396,17 @@ __device__ LongCut select_cut(Row<T>& row, LongCut within, uint32_t widest, uint
 }
 
 template <typename T>
-__global__ __launch_bounds__(kSampleThreads) void k_sample_long(const T* __restrict__ z, int64_t rows, int64_t n,
+__global__ __launch_bounds__(kSampleThreads) void k_sample_slow(const T* __restrict__ z, int64_t rows, int64_t n,
                                                            int64_t ldz, Limits lim, const float* __restrict__ u,
                                                            const int64_t* __restrict__ rated_ptr,
                                                            const int32_t* __restrict__ rated_idx,
                                                            const int32_t* __restrict__ users, int64_t of,
-                                                           int32_t* __restrict__ index, float* __restrict__ log) {
+                                                           int32_t* __restrict__ index, float* __restrict__ log,
+                                                           const RowPlan* __restrict__ plan, int64_t row0) {
     extern __shared__ unsigned char shared[];
     SampleShared* sh = (SampleShared*)shared;
-    const int64_t r = blockIdx.x;
+    if (plan[blockIdx.x].kind != kRowSlow) return;
+    const int64_t r = row0 + blockIdx.x;
     Row<T> row;
     row.z = z + r * ldz;
     row.n = n;
@@ -1407,15 +1447,11 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample_long(const T* __restr
         if (threadIdx.x == 0) { index[r] = -1; if (log) log[r] = -INFINITY; }
         return;
     }
-    const float t = lim.temperature ? lim.temperature[r] : lim.temperature_all;
-    const bool greedy = !(t > 0.f);
+    const Wanted want(lim, u, r);
+    const bool greedy = !(want.t > 0.f);
     row.best = hi;
-    row.top = score_of(hi);
-    row.inv_t = greedy ? 1.f : 1.f / t;
-    const int k = lim.top_k ? lim.top_k[r] : lim.top_k_all;
-    const float p = lim.top_p ? lim.top_p[r] : lim.top_p_all;
-    const float least = lim.min_p ? lim.min_p[r] : lim.min_p_all;
-    const float least_e = least > 0.f ? fminf(least, 1.f) : 0.f;
+    row.ask = Asked{score_of(hi), greedy ? 1.f : 1.f / want.t, want.least};
+    const int k = want.top_k;
     const uint32_t widest = hi - lo;
     LongCut cut{widest, 0xFFFFFFFFu};
     if (greedy) {
@@ -1424,37 +1460,488 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample_long(const T* __restr
         return;
     }
     if (k > 0 && (uint32_t)k < count) cut = select_cut<false>(row, cut, cut.d, (uint64_t)k);
-    if (p < 1.f) {
+    if (want.top_p < 1.f) {
         uint64_t sum = 0;
         row.each([&](int64_t c, uint32_t key) {
             if (cut.keeps(hi - key, c)) sum += row.weight_of(hi - key);
         });
         sum = block_sum(sum, sh);
-        const uint32_t part = p > 0.f ? (uint32_t)(p * 0x1p24f) : 0;
-        uint64_t target = share_of(sum, part);
+        uint64_t target = share_of(sum, want.part());
         if (target < 1) target = 1;
         cut = select_cut<true>(row, cut, cut.d, target);
     }
     auto weight = [&](int64_t c, uint32_t d) -> uint64_t {
         if (!cut.keeps(d, c)) return 0;
-        const float e = row.exp_of(d);
-        return e >= least_e ? fixed40(e) : 0;
+        const float e = row.ask.scaled(score_of(hi - d));
+        return e >= want.least ? whole_of(floorf(e)) : 0;
     };
     uint64_t sum = 0;
     row.each([&](int64_t c, uint32_t key) { sum += weight(c, hi - key); });
     sum = block_sum(sum, sh);
-    float uu = u[r];
-    uu = uu > 0.f ? fminf(uu, 1.f - 0x1p-24f) : 0.f;
-    const uint32_t c = find_column(row, share_of(sum, (uint32_t)(uu * 0x1p24f)), weight);
+    const uint32_t c = find_column(row, share_of(sum, (uint32_t)(want.u * 0x1p24f)), weight);
     if (threadIdx.x == 0) {
         index[r] = (int32_t)c;
         if (log) {
             const float v = to_float(row.z[c]);
-            const uint32_t d = hi - key_of(v);
-            const float x = d == 0 ? 0.f : (v - row.top) * row.inv_t;
+            const float x = v == row.ask.top ? 0.f : (v - row.ask.top) * row.ask.inv_t;
             log[r] = x - logf((float)sum * 0x1p-40f);
         }
     }
+}
+
+// Rows that no workgroup's registers hold, in segments of 16,384 columns, a workgroup each; what the segments find
+// out goes through the workspace from one kernel to the next, and each kernel reads the scores again
+// (from the cache that all dies share, where they fit it):
+//   k_long_stats  a segment's best and least score and number of allowed columns, and the best scores of groups of its
+//                 columns
+//   k_long_parts  top-k: the segment's columns with a score that k groups' best ones reach; top-p: a histogram of
+//                 weights over the row's scores; neither: the segment's weight
+//   k_long_rows   a workgroup a row.  top-k: the draw, among what the segments listed; top-p: the bin in which the cut
+//                 falls; neither: the draw
+//   k_long_cut    top-p: the segment's columns in that bin, and the weight of those above it
+//   k_long_draw   top-p: the cut, by ranking the listed columns, and the draw
+// Rows whose lists do not hold what they should (equal scores without end, a top_k of more than 7/8 of the groups)
+// are left to k_sample_slow.
+constexpr int kSegWaves = 8, kSegThreads = kSegWaves * kWave, kSegColumns = kSegThreads * 32;
+constexpr int kSegMax = ALS_SERVE_N_MAX / kSegColumns;
+constexpr int kSlab = 2048;              // columns a segment lists
+constexpr int kFew = 8192;               // columns a row's workgroup takes from its lists
+constexpr int kGroups = 4096;            // most groups of a row
+using Segment = Held<32, 1024>;
+using FewOfRow = Held<8, 2048>;
+using SegmentOfRow = Held<32, 2048>;
+constexpr int kRowThreads = kFew / 8;
+static_assert(kSegMax <= kSegThreads && kSegMax <= kRowThreads, "a thread a segment");
+
+struct SegStat {
+    float best, least;
+    uint32_t count, listed;
+    uint64_t mass;
+};
+// A batch's part of the workspace.  Segment s of the batch's row b is number b segments + s.
+struct LongWork {
+    RowPlan* plan;
+    SegStat* stat;
+    float* groups;              // kSegThreads / group a segment
+    uint64_t* bins;             // Segment::kBins a segment
+    float* list_z;              // kSlab a segment
+    uint32_t* list_column;
+    uint32_t segments, group;   // group: threads (of 32 columns each) that publish one best score
+    int64_t row0;               // the batch's first row
+};
+template <typename T>
+struct LongArgs {
+    const T* z;
+    int64_t n, ldz;
+    Limits lim;
+    const float* u;
+    Rated rated;
+    int32_t* index;
+    float* log;
+    LongWork work;
+    __device__ __forceinline__ uint32_t columns(uint32_t seg) const {
+        const int64_t left = n - (int64_t)seg * kSegColumns;
+        return left < kSegColumns ? (uint32_t)left : kSegColumns;
+    }
+};
+
+// Best and least score and allowed columns of a row, from its segments; by the whole workgroup.
+template <typename H>
+__device__ __forceinline__ void row_stats(H& h, const SegStat* stat, uint32_t segments, float* best, float* least,
+                                          uint32_t* count) {
+    const bool mine = threadIdx.x < segments;
+    float hi = mine ? stat[threadIdx.x].best : -INFINITY, lo = mine ? -stat[threadIdx.x].least : -INFINITY;
+    uint32_t n = mine ? stat[threadIdx.x].count : 0;
+    hi = wave_max(hi);
+    lo = wave_max(lo);
+    n = __builtin_amdgcn_readlane(scan32(n), 63);
+    if (h.lane() == 0) { h.sh->wave_a[h.wave()] = hi; h.sh->wave_b[h.wave()] = lo; h.sh->wave_c[h.wave()] = n; }
+    h.sync();
+    hi = lo = -INFINITY;
+    n = 0;
+    for (int w = 0; w < h.waves; ++w) {
+        hi = fmaxf(hi, h.sh->wave_a[w]);
+        lo = fmaxf(lo, h.sh->wave_b[w]);
+        n += h.sh->wave_c[w];
+    }
+    h.sync();
+    *best = hi;
+    *least = -lo;
+    *count = n;
+}
+
+__device__ __forceinline__ int kind_of(const Wanted& want, uint32_t count, uint32_t groups) {
+    if (count == 0) return kRowNone;
+    if (!(want.t > 0.f)) return kRowBest;
+    if (want.top_k > 0 && (uint32_t)want.top_k < count)
+        return (uint32_t)want.top_k <= groups / 8 * 7 ? kRowFew : kRowSlow;
+    return want.top_p < 1.f ? kRowShare : kRowRest;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kSegThreads) void k_long_stats(LongArgs<T> a) {
+    __shared__ Segment::Shared sh;
+    __shared__ uint32_t bits[kSegColumns / 32];
+    Segment h;
+    h.sh = &sh;
+    h.threads = kSegThreads;
+    h.waves = kSegWaves;
+    const LongWork& w = a.work;
+    const uint32_t b = blockIdx.x / w.segments, seg = blockIdx.x % w.segments;
+    const int64_t r = w.row0 + b;
+    bool there;
+    take_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
+    float best, least;
+    uint32_t count;
+    float mine = h.largest(&best);
+    h.spread(&least, &count);
+    if (threadIdx.x == 0) {
+        SegStat& s = w.stat[blockIdx.x];
+        s.best = best;
+        s.least = least;
+        s.count = there ? count : 0;
+    }
+    for (uint32_t d = 1; d < w.group; d <<= 1) mine = fmaxf(mine, __shfl_xor(mine, d));
+    if (threadIdx.x % w.group == 0)
+        w.groups[(int64_t)blockIdx.x * (kSegThreads / w.group) + threadIdx.x / w.group] = mine;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kSegThreads) void k_long_parts(LongArgs<T> a) {
+    __shared__ Segment::Shared sh;
+    __shared__ uint32_t bits[kSegColumns / 32];
+    Segment h;
+    h.sh = &sh;
+    h.threads = kSegThreads;
+    h.waves = kSegWaves;
+    const LongWork& w = a.work;
+    const uint32_t b = blockIdx.x / w.segments, seg = blockIdx.x % w.segments;
+    const int64_t r = w.row0 + b;
+    float best, least;
+    uint32_t count;
+    row_stats(h, w.stat + (int64_t)b * w.segments, w.segments, &best, &least, &count);
+    const Wanted want(a.lim, a.u, r);
+    const uint32_t per = kSegThreads / w.group, groups = w.segments * per;
+    const int kind = kind_of(want, count, groups);
+    if (kind != kRowFew && kind != kRowShare && kind != kRowRest) return;
+    const Asked ask{best, 1.f / want.t, want.least};
+    bool there;
+    take_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
+    if (kind == kRowFew) {
+        const float* all = w.groups + (int64_t)b * groups;
+        float z[kGroups / kSegThreads];
+#pragma unroll
+        for (int i = 0; i < kGroups / kSegThreads; ++i) {
+            const uint32_t at = i * kSegThreads + threadIdx.x;
+            z[i] = at < groups ? all[at] : -INFINITY;
+        }
+        const float reached = h.reached_by((uint32_t)want.top_k, best, [&](auto fn) {
+#pragma unroll
+            for (int i = 0; i < kGroups / kSegThreads; ++i) fn(z[i]);
+        });
+        // (fewer than k groups hold an allowed column: the list cannot be told to be long enough)
+        const uint32_t listed = !(reached > -INFINITY) ? kSlab + 1 : h.collect(
+            kSlab, [&](float v) { return v >= reached; },
+            [&](uint32_t i, float v, uint32_t position) {
+                w.list_z[(int64_t)blockIdx.x * kSlab + i] = v;
+                w.list_column[(int64_t)blockIdx.x * kSlab + i] = seg * kSegColumns + position;
+            });
+        if (threadIdx.x == 0) w.stat[blockIdx.x].listed = listed;
+    } else if (kind == kRowShare) {
+        for (int i = threadIdx.x; i < Segment::kBins; i += kSegThreads) sh.bin[i] = 0;
+        h.sync();
+        bool clipped;
+        const auto scale = Segment::scale_of(best, least, want.t, &clipped);
+        h.each([&](float v, uint32_t) {
+            if (v > -INFINITY) h.add_to_bin(h.bin_of(v, scale), true, v, ask);
+        });
+        h.sync();
+        for (int i = threadIdx.x; i < Segment::kBins; i += kSegThreads)
+            w.bins[(int64_t)blockIdx.x * Segment::kBins + i] = sh.bin[i];
+    } else {
+        double thread = 0.0;
+        h.each([&](float v, uint32_t) {
+            const float e = ask.scaled(v);
+            thread += v > -INFINITY && e >= ask.least ? (double)floorf(e) : 0.0;
+        });
+        uint64_t before;
+        const uint64_t mass = h.sum(last64(scan64(whole_of(thread))), &before);
+        if (threadIdx.x == 0) w.stat[blockIdx.x].mass = mass;
+    }
+}
+
+struct RowShared {
+    SegmentOfRow::Shared held;
+    uint32_t first[kSegMax + 1];         // of a segment's list, on the row's
+    uint64_t mass[kSegMax];
+    uint32_t bits[kSegColumns / 32];
+    uint32_t found;
+    uint64_t before;
+};
+static_assert(sizeof(FewOfRow::Shared) == sizeof(SegmentOfRow::Shared), "one place for both");
+
+// Where the segments' lists lie on the row's; false: some list, or all of them, are too long.
+template <typename H>
+__device__ __forceinline__ bool place_lists(H& h, const SegStat* stat, uint32_t segments, RowShared* sh) {
+    const uint32_t mine = threadIdx.x < segments ? stat[threadIdx.x].listed : 0;
+    const float longest = wave_max((float)mine);
+    const uint64_t upto = scan64(mine);
+    h.sync();
+    if (h.lane() == 63) { sh->held.wave_sum[h.wave()] = upto; sh->held.wave_a[h.wave()] = longest; }
+    h.sync();
+    uint64_t before = 0, total = 0;
+    bool fits = true;
+    for (int w = 0; w < h.waves; ++w) {
+        if (w == h.wave()) before = total;
+        total += sh->held.wave_sum[w];
+        fits = fits && sh->held.wave_a[w] <= (float)kSlab;
+    }
+    if (threadIdx.x < segments) sh->first[threadIdx.x] = (uint32_t)(before + upto - mine);
+    if (threadIdx.x == segments) sh->first[segments] = (uint32_t)total;
+    h.sync();
+    return fits && total <= (uint64_t)kFew;
+}
+
+// The row's listed columns, by column, four neighbours a thread and time; `column` are theirs.
+__device__ __forceinline__ void take_lists(FewOfRow& few, const LongWork& w, uint32_t b, const RowShared* sh,
+                                           uint32_t (&column)[8]) {
+    const uint32_t total = sh->first[w.segments];
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint32_t i = few.position(v) + c;
+            float z = -INFINITY;
+            uint32_t at = 0;
+            if (i < total) {
+                uint32_t lo = 0, hi = w.segments;      // the last segment whose list starts at or before i
+                while (hi - lo > 1) {
+                    const uint32_t mid = (lo + hi) / 2;
+                    if (sh->first[mid] <= i) lo = mid;
+                    else hi = mid;
+                }
+                const int64_t from = ((int64_t)b * w.segments + lo) * kSlab + (i - sh->first[lo]);
+                z = w.list_z[from];
+                at = w.list_column[from];
+            }
+            few.z[0][4 * v + c] = z;
+            column[4 * v + c] = at;
+        }
+}
+
+// The draw from the segments' weights (sh->mass), the columns being those that `cut` (by column) keeps.
+template <typename T>
+__device__ __forceinline__ void draw_from_segments(SegmentOfRow& h, const LongArgs<T>& a, uint32_t b, const Wanted& want,
+                                                   const Asked& ask, const Cut& cut, RowShared* sh) {
+    const LongWork& w = a.work;
+    const int64_t r = w.row0 + b;
+    h.sync();
+    const uint64_t mine = threadIdx.x < w.segments ? sh->mass[threadIdx.x] : 0;
+    const uint64_t upto = scan64(mine);
+    uint64_t before;
+    const uint64_t total = h.sum(last64(upto), &before);
+    const uint64_t t = share_of(total, (uint32_t)(want.u * 0x1p24f)), at = before + upto - mine;
+    if (t >= at && t - at < mine) { sh->found = threadIdx.x; sh->before = at; }
+    h.sync();
+    const uint32_t seg = sh->found, base = seg * kSegColumns;
+    bool there;
+    take_columns(h, a.z + r * a.ldz, base, a.columns(seg), a.rated, r, sh->bits, &there);
+    const auto weight = [&](float k, uint32_t p) {
+        const float e = ask.scaled(k);
+        return cut.keeps(k, base + p) && e >= ask.least ? floorf(e) : 0.f;
+    };
+    double thread = 0.0;
+    h.each([&](float k, uint32_t p) { thread += (double)weight(k, p); });
+    const uint64_t of_wave = last64(scan64(whole_of(thread)));
+    uint64_t before_wave;
+    h.sum(of_wave, &before_wave);
+    const uint32_t p = h.find(t - sh->before, of_wave, before_wave, weight);
+    h.each([&](float k, uint32_t i) {
+        if (i == p) {
+            a.index[r] = (int32_t)(base + p);
+            const float x = k == ask.top ? 0.f : (k - ask.top) * ask.inv_t;
+            if (a.log) a.log[r] = x - logf((float)total * 0x1p-40f);
+        }
+    });
+}
+
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void k_long_rows(LongArgs<T> a) {
+    extern __shared__ __align__(16) unsigned char shared[];
+    RowShared* sh = (RowShared*)shared;
+    SegmentOfRow h;
+    h.sh = &sh->held;
+    h.threads = kRowThreads;
+    h.waves = kRowThreads / kWave;
+    const LongWork& w = a.work;
+    const uint32_t b = blockIdx.x;
+    const int64_t r = w.row0 + b;
+    const SegStat* stat = w.stat + (int64_t)b * w.segments;
+    float best, least;
+    uint32_t count;
+    row_stats(h, stat, w.segments, &best, &least, &count);
+    const Wanted want(a.lim, a.u, r);
+    int kind = kind_of(want, count, w.segments * (kSegThreads / w.group));
+    const Asked ask{best, 1.f / want.t, want.least};
+    RowPlan plan{kind, 0, 0, 0};
+    if (kind == kRowNone) {
+        const int32_t* list;
+        int64_t listed;
+        if (threadIdx.x == 0) {
+            a.index[r] = -1;
+            if (a.log) a.log[r] = a.rated.row(r, &list, &listed) ? -INFINITY : NAN;
+        }
+    } else if (kind == kRowBest) {
+        if (threadIdx.x == 0) sh->found = w.segments;
+        h.sync();
+        if (threadIdx.x < w.segments && stat[threadIdx.x].best == best) atomicMin(&sh->found, threadIdx.x);
+        h.sync();
+        const uint32_t seg = sh->found;
+        bool there;
+        take_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), a.rated, r, sh->bits, &there);
+        const uint32_t p = h.first_of(best);
+        if (threadIdx.x == 0) { a.index[r] = (int32_t)(seg * kSegColumns + p); if (a.log) a.log[r] = 0.f; }
+    } else if (kind == kRowFew) {
+        if (place_lists(h, stat, w.segments, sh)) {
+            FewOfRow few;
+            few.sh = (FewOfRow::Shared*)&sh->held;
+            few.threads = h.threads;
+            few.waves = h.waves;
+            uint32_t column[8];
+            take_lists(few, w, b, sh, column);
+            const auto d = few.draw(want, ask);
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (few.position(v) + c == d.position) {
+                        a.index[r] = (int32_t)column[4 * v + c];
+                        if (a.log) a.log[r] = d.log;
+                    }
+        } else {
+            plan.kind = kRowSlow;
+        }
+    } else if (kind == kRowShare) {
+        for (int i = threadIdx.x; i < SegmentOfRow::kBins; i += kRowThreads) {
+            uint64_t s = 0;
+            if (i < Segment::kBins)
+                for (uint32_t seg = 0; seg < w.segments; ++seg)
+                    s += w.bins[((int64_t)b * w.segments + seg) * Segment::kBins + i];
+            sh->held.bin[i] = s;
+        }
+        h.search_bins([&](uint64_t total) {
+            const uint64_t goal = share_of(total, want.part());
+            plan.goal = goal < 1 ? 1 : goal;
+            return plan.goal;
+        });
+        plan.bin = (int)sh->held.found_bin;
+        plan.before = sh->held.found_before;
+    } else if (kind == kRowRest) {
+        if (threadIdx.x < w.segments) sh->mass[threadIdx.x] = stat[threadIdx.x].mass;
+        draw_from_segments(h, a, b, want, ask, Cut(), sh);
+    }
+    if (threadIdx.x == 0) w.plan[b] = plan;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kSegThreads) void k_long_cut(LongArgs<T> a) {
+    __shared__ Segment::Shared sh;
+    __shared__ uint32_t bits[kSegColumns / 32];
+    Segment h;
+    h.sh = &sh;
+    h.threads = kSegThreads;
+    h.waves = kSegWaves;
+    const LongWork& w = a.work;
+    const uint32_t b = blockIdx.x / w.segments, seg = blockIdx.x % w.segments;
+    const int64_t r = w.row0 + b;
+    const RowPlan plan = w.plan[b];
+    if (plan.kind != kRowShare) return;
+    float best, least;
+    uint32_t count;
+    row_stats(h, w.stat + (int64_t)b * w.segments, w.segments, &best, &least, &count);
+    const Wanted want(a.lim, a.u, r);
+    const Asked ask{best, 1.f / want.t, want.least};
+    bool there, clipped;
+    take_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
+    const auto scale = Segment::scale_of(best, least, want.t, &clipped);
+    const uint32_t listed = h.collect(
+        kSlab, [&](float v) { return v > -INFINITY && h.bin_of(v, scale) == plan.bin; },
+        [&](uint32_t i, float v, uint32_t position) {
+            w.list_z[(int64_t)blockIdx.x * kSlab + i] = v;
+            w.list_column[(int64_t)blockIdx.x * kSlab + i] = seg * kSegColumns + position;
+        });
+    double thread = 0.0;
+    h.each([&](float v, uint32_t) {
+        if (v > -INFINITY && h.bin_of(v, scale) < plan.bin) {
+            const float e = ask.scaled(v);
+            thread += e >= ask.least ? (double)floorf(e) : 0.0;
+        }
+    });
+    uint64_t before;
+    const uint64_t mass = h.sum(last64(scan64(whole_of(thread))), &before);
+    if (threadIdx.x == 0) {
+        w.stat[blockIdx.x].listed = listed;
+        w.stat[blockIdx.x].mass = mass;
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void k_long_draw(LongArgs<T> a) {
+    extern __shared__ __align__(16) unsigned char shared[];
+    RowShared* sh = (RowShared*)shared;
+    SegmentOfRow h;
+    h.sh = &sh->held;
+    h.threads = kRowThreads;
+    h.waves = kRowThreads / kWave;
+    const LongWork& w = a.work;
+    const uint32_t b = blockIdx.x;
+    const int64_t r = w.row0 + b;
+    const RowPlan plan = w.plan[b];
+    if (plan.kind != kRowShare) return;
+    const SegStat* stat = w.stat + (int64_t)b * w.segments;
+    float best, least;
+    uint32_t count;
+    row_stats(h, stat, w.segments, &best, &least, &count);
+    const Wanted want(a.lim, a.u, r);
+    const Asked ask{best, 1.f / want.t, want.least};
+    if (!place_lists(h, stat, w.segments, sh)) {
+        if (threadIdx.x == 0) w.plan[b].kind = kRowSlow;
+        return;
+    }
+    FewOfRow few;
+    few.sh = (FewOfRow::Shared*)&sh->held;
+    few.threads = h.threads;
+    few.waves = h.waves;
+    uint32_t column[8];
+    take_lists(few, w, b, sh, column);
+    float low;
+    uint32_t listed;
+    few.spread(&low, &listed);
+    Asked listed_ask = ask;
+    const Cut place = few.select(true, Cut(), low, want.t, 0, listed_ask, plan.goal - plan.before);
+    // the cut by column instead of by place on the list; what it keeps of the lists counts for its segments
+    Cut cut;
+    cut.z = place.z;
+    few.sync();
+    if (threadIdx.x < w.segments) sh->mass[threadIdx.x] = stat[threadIdx.x].mass;
+    few.sync();
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const float k = few.z[0][4 * v + c];
+            const uint32_t i = few.position(v) + c;
+            if (i == (uint32_t)place.position) sh->found = column[4 * v + c];
+            if (place.keeps(k, i)) {
+                const float e = ask.scaled(k);
+                if (e >= ask.least)
+                    atomicAdd((unsigned long long*)&sh->mass[column[4 * v + c] / kSegColumns],
+                              (unsigned long long)whole_of(floorf(e)));
+            }
+        }
+    few.sync();
+    cut.position = (int)sh->found;
+    draw_from_segments(h, a, b, want, ask, cut, sh);
 }
 
 // ---------------------------------------------------------------------------------- host --
@@ -1513,7 +2000,7 @@ int query_device(int device, int* cus) {
     return ALS_OK;
 }
 
-constexpr size_t kWorkspaceBytes = 64u << 20;
+constexpr size_t kWorkspaceBytes = 128u << 20;
 
 }  // namespace
 
@@ -1787,12 +2274,51 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
         if (n <= 4096) return held(Held<8, 1024>(), p);
         if (n <= 32768) return held(Held<32, 2048>(), p);
         if (n <= 65536) return held(Held<64, 4096>(), p);
+        // in batches of as many rows as the workspace holds
+        const int64_t segments = (n + kSegColumns - 1) / kSegColumns;
+        uint32_t group = 1;
+        while (segments * (kSegThreads / group) > kGroups) group *= 2;
+        const size_t a_segment = sizeof(SegStat) + kSegThreads / group * sizeof(float) + Segment::kBins * 8 + kSlab * 8;
+        const int64_t batch = (int64_t)(ctx->ws_bytes / (a_segment * segments + sizeof(RowPlan)));
+        const hipStream_t st = (hipStream_t)stream;
+        const size_t row_lds = sizeof(RowShared);
         const int64_t bits = rated_ptr ? (n < kChunk ? n : kChunk) : 0;
-        const size_t lds = sizeof(SampleShared) + (size_t)((bits + 31) / 32) * 4;
-        static std::atomic<uint64_t> done{0};
-        whole_lds(k_sample_long<T>, ctx->device, &done);
-        hipLaunchKernelGGL(k_sample_long<T>, dim3((unsigned)rows), dim3(kSampleThreads), lds, (hipStream_t)stream, p,
-                           rows, n, ldz, lim, u, rated_ptr, rated_idx, users, of, index, log);
+        const size_t slow_lds = sizeof(SampleShared) + (size_t)((bits + 31) / 32) * 4;
+        static std::atomic<uint64_t> of_rows{0}, of_draw{0}, of_slow{0};
+        whole_lds(k_long_rows<T>, ctx->device, &of_rows);
+        whole_lds(k_long_draw<T>, ctx->device, &of_draw);
+        whole_lds(k_sample_slow<T>, ctx->device, &of_slow);
+        const bool shares = l.top_p || l.top_p_all < 1.f;
+        for (int64_t row0 = 0; row0 < rows; row0 += batch) {
+            const int64_t some = rows - row0 < batch ? rows - row0 : batch;
+            LongArgs<T> args{p, n, ldz, lim, u, rated, index, log, {}};
+            LongWork& w = args.work;
+            unsigned char* at = ctx->ws;        // the widest types first
+            w.bins = (uint64_t*)at;
+            at += some * segments * Segment::kBins * 8;
+            w.stat = (SegStat*)at;
+            at += some * segments * sizeof(SegStat);
+            w.plan = (RowPlan*)at;
+            at += some * sizeof(RowPlan);
+            w.groups = (float*)at;
+            at += some * segments * (kSegThreads / group) * sizeof(float);
+            w.list_z = (float*)at;
+            at += some * segments * kSlab * 4;
+            w.list_column = (uint32_t*)at;
+            w.segments = (uint32_t)segments;
+            w.group = group;
+            w.row0 = row0;
+            const dim3 parts((unsigned)(some * segments)), whole((unsigned)some);
+            hipLaunchKernelGGL(k_long_stats<T>, parts, dim3(kSegThreads), 0, st, args);
+            hipLaunchKernelGGL(k_long_parts<T>, parts, dim3(kSegThreads), 0, st, args);
+            hipLaunchKernelGGL(k_long_rows<T>, whole, dim3(kRowThreads), row_lds, st, args);
+            if (shares) {
+                hipLaunchKernelGGL(k_long_cut<T>, parts, dim3(kSegThreads), 0, st, args);
+                hipLaunchKernelGGL(k_long_draw<T>, whole, dim3(kRowThreads), row_lds, st, args);
+            }
+            hipLaunchKernelGGL(k_sample_slow<T>, whole, dim3(kSampleThreads), slow_lds, st, p, rows, n, ldz, lim, u,
+                               rated_ptr, rated_idx, users, of, index, log, w.plan, row0);
+        }
     };
     if (dtype == ALS_F32) launch((const float*)z);
     else if (dtype == ALS_F16) launch((const F16*)z);
