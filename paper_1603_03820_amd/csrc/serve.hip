@@ -611,7 +611,8 @@ struct Cut {
 // in which it falls.  LDS sums are of integers, so their order does not matter.
 template <int K, int BINS>
 struct Held {
-    static constexpr int kScores = K, kBins = BINS, kList = BINS / 2, kMaxWaves = 16;
+    static constexpr int kScores = K, kBins = BINS, kList = BINS < 1024 ? BINS / 2 : 1024, kMaxWaves = 16;
+    static constexpr int kRanked = BINS / 2 < 256 ? BINS / 2 : 256;      // columns that are ranked one against another
     typedef float Scores __attribute__((ext_vector_type(K < 32 ? K : 32)));
     static_assert(K % 4 == 0 && K <= 64, "scores a thread");    // (its weights add up below 2^53)
     struct Shared {
@@ -654,6 +655,15 @@ struct Held {
         }
     }
 
+    // The same without a loop, for passes of a few instructions a score.
+    template <typename Fn>
+    __device__ __forceinline__ void each_at_once(Fn fn) const {
+#pragma unroll
+        for (int v = 0; v < K; v += 4)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) fn(z[v / 32][v % 32 + c], position(v / 4) + c);
+    }
+
     // Of the waves' sums: their sum, and the sum of those before this wave's.
     __device__ __forceinline__ uint64_t sum(uint64_t mine, uint64_t* before_wave) {
         sync();
@@ -671,7 +681,7 @@ struct Held {
     // A thread's largest score, and the workgroup's.
     __device__ __forceinline__ float largest(float* best) {
         float mine = -INFINITY;
-        each([&](float k, uint32_t) { mine = fmaxf(mine, k); });
+        each_at_once([&](float k, uint32_t) { mine = fmaxf(mine, k); });
         float hi = wave_max(mine);
         if (waves > 1) {
             if (lane() == 0) sh->wave_a[wave()] = hi;
@@ -685,7 +695,7 @@ struct Held {
     __device__ __forceinline__ void spread(float* least, uint32_t* count) {
         float lo = -INFINITY;    // the least one's negative
         uint32_t n = 0;
-        each([&](float k, uint32_t) {
+        each_at_once([&](float k, uint32_t) {
             lo = fmaxf(lo, k > -INFINITY ? -k : -INFINITY);
             n += k > -INFINITY;
         });
@@ -709,29 +719,33 @@ struct Held {
     // near below it as bins tell.  -inf: there are fewer than k.  `best` is the largest.
     template <typename Values>
     __device__ __forceinline__ float reached_by(uint32_t k, float best, Values values) {
+        constexpr int kCoarse = kBins < 256 ? kBins : 256;
         float low = -INFINITY;      // the least one's negative
         values([&](float v) { low = fmaxf(low, v > -INFINITY ? -v : -INFINITY); });
         low = wave_max(low);
         sync();
         if (lane() == 0) sh->wave_b[wave()] = low;
-        for (int b = threadIdx.x; b < kBins; b += threads) sh->bin[b] = 0;
+        for (int b = threadIdx.x; b < kCoarse; b += threads) sh->bin[b] = 0;
+        if (threadIdx.x == 0) sh->found_bin = kCoarse;
         sync();
         for (int w = 0; w < waves; ++w) low = fmaxf(low, sh->wave_b[w]);
-        const Scale scale{best, best + low > 0.f ? (float)(kBins - 1) / (best + low) : 0.f};
+        const float per = best + low > 0.f ? (float)(kCoarse - 1) / (best + low) : 0.f;
+        const auto bin_of = [&](float v) {
+            const float x = (best - v) * per;
+            return v == best ? 0 : (x < (float)(kCoarse - 1) ? (int)x : kCoarse - 1);
+        };
         values([&](float v) {
-            if (v > -INFINITY) atomicAdd((unsigned long long*)&sh->bin[bin_of(v, scale)], 1ull);
+            if (v > -INFINITY) atomicAdd((unsigned long long*)&sh->bin[bin_of(v)], 1ull);
         });
-        if (threadIdx.x == 0) sh->found_bin = kBins;
-        search_bins([&](uint64_t) { return (uint64_t)k; });
+        search_bins([&](uint64_t) { return (uint64_t)k; }, kCoarse);
         const int found = (int)sh->found_bin;
         low = -INFINITY;
-        values([&](float v) { low = fmaxf(low, v > -INFINITY && bin_of(v, scale) <= found ? -v : -INFINITY); });
+        values([&](float v) { low = fmaxf(low, v > -INFINITY && bin_of(v) <= found ? -v : -INFINITY); });
         low = wave_max(low);
-        if (lane() == 0) sh->wave_b[wave()] = low;
+        if (lane() == 0) sh->wave_a[wave()] = low;
         sync();
-        for (int w = 0; w < waves; ++w) low = fmaxf(low, sh->wave_b[w]);
-        sync();
-        return found == kBins ? -INFINITY : -low;
+        for (int w = 0; w < waves; ++w) low = fmaxf(low, sh->wave_a[w]);
+        return found == kCoarse ? -INFINITY : -low;
     }
 
     // put(i, score, position) for the columns that `take(score)` picks, i counting them by position, where they
@@ -739,7 +753,7 @@ struct Held {
     template <typename Take, typename Put>
     __device__ __forceinline__ uint32_t collect(uint32_t most, Take take, Put put) {
         uint32_t mine = 0;
-        each([&](float k, uint32_t) { mine += (uint32_t)__popcll(__ballot(take(k))); });
+        each_at_once([&](float k, uint32_t) { mine += (uint32_t)__popcll(__ballot(take(k))); });
         sync();
         if (lane() == 0) sh->wave_c[wave()] = mine;
         sync();
@@ -752,24 +766,20 @@ struct Held {
         if (total > most) return total;
         const uint64_t below = (1ull << lane()) - 1;
 #pragma unroll
-        for (int h = 0; h < (K + 31) / 32; ++h) {
-            uint32_t p = position(8 * h);
-#pragma nounroll
-            for (int v = 0; v < (K < 32 ? K : 32); v += 4, p += 4 * kWave) {
-                uint64_t takes[4];
-                uint32_t mine = at, all = 0;
+        for (int v = 0; v < K; v += 4) {
+            uint64_t takes[4];
+            uint32_t mine = at, all = 0;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    takes[c] = __ballot(take(z[h][v + c]));
-                    mine += __popcll(takes[c] & below);
-                    all += __popcll(takes[c]);
-                }
-                if (all) {
+            for (int c = 0; c < 4; ++c) {
+                takes[c] = __ballot(take(z[v / 32][v % 32 + c]));
+                mine += __popcll(takes[c] & below);
+                all += __popcll(takes[c]);
+            }
+            if (all) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        if (takes[c] >> lane() & 1) put(mine++, z[h][v + c], p + c);
-                    at += all;
-                }
+                for (int c = 0; c < 4; ++c)
+                    if (takes[c] >> lane() & 1) put(mine++, z[v / 32][v % 32 + c], position(v / 4) + c);
+                at += all;
             }
         }
         sync();
@@ -834,13 +844,24 @@ struct Held {
         if (w) atomicAdd((unsigned long long*)&sh->bin[bin], (unsigned long long)w);
     }
 
+    // The least score of bins 0 .. b (of all scores above -inf): bins fall with the score, so halving keys finds it.
+    __device__ __forceinline__ float least_of_bins(int b, const Scale& c) const {
+        uint32_t no = key_of(-INFINITY), yes = key_of(c.top);
+        while (yes - no > 1) {
+            const uint32_t mid = no + (yes - no) / 2;
+            if (bin_of(score_of(mid), c) <= b) yes = mid;
+            else no = mid;
+        }
+        return score_of(yes);
+    }
+
     // Adds up the bins in their order: the first at which the sum reaches the target (found_bin,
     // found_before).  target(total) is asked once the total is known.
     template <typename Fn>
-    __device__ __forceinline__ void search_bins(Fn target) {
+    __device__ __forceinline__ void search_bins(Fn target, int bins = kBins) {
         sync();
-        const int per = (kBins + threads - 1) / threads, first = per * threadIdx.x;
-        const int end = first + per < kBins ? first + per : kBins;
+        const int per = (bins + threads - 1) / threads, first = per * threadIdx.x;
+        const int end = first + per < bins ? first + per : bins;
         uint64_t s = 0, before;
         for (int b = first; b < end; ++b) s += sh->bin[b];
         const uint64_t upto = scan64(s);
@@ -866,23 +887,34 @@ struct Held {
         sync();
     }
 
-    // Among the listed columns, the last with less than `goal` of the measure before it.  The bins, done with,
-    // take the listed columns' measures.
-    __device__ __forceinline__ Cut rank_list(bool by_mass, uint32_t count, uint64_t before, uint64_t goal,
-                                             const Asked& ask) {
-        for (uint32_t i = threadIdx.x; i < count; i += threads)
-            sh->bin[i] = by_mass ? whole_of(ask.weight_of(sh->list_z[i])) : 1;
-        sync();
-        for (uint32_t i = threadIdx.x; i < count; i += threads) {
-            const float k = sh->list_z[i];
-            const uint32_t p = sh->list_position[i];
-            uint64_t front = before;
-            for (uint32_t j = 0; j < count; ++j) {
-                const float kj = sh->list_z[j];
-                if (kj > k || (kj == k && sh->list_position[j] < p)) front += sh->bin[j];
+    // The columns that `take` picks and their measures, in the bins' place (which are done with), as far as kRanked go;
+    // how many there are.  An entry is a number that orders the columns, and the measure.
+    template <typename Fn>
+    __device__ __forceinline__ uint32_t make_list(bool by_mass, const Asked& ask, Fn take) {
+        each([&](float k, uint32_t p) {
+            if (take(k, p)) {
+                const uint32_t at = atomicAdd(&sh->listed, 1u);
+                if (at < (uint32_t)kRanked) {
+                    sh->bin[2 * at] = (uint64_t)~key_of(k) << 32 | p;
+                    sh->bin[2 * at + 1] = by_mass ? whole_of(ask.weight_of(k)) : 1;
+                }
             }
-            const uint64_t own = sh->bin[i];
-            if (front < goal && goal <= front + own) { sh->cut_z = k; sh->cut_position = p; }
+        });
+        sync();
+        return sh->listed;
+    }
+
+    // Among the listed columns, the last with less than `goal` of the measure before it.
+    __device__ __forceinline__ Cut rank_list(uint32_t count, uint64_t before, uint64_t goal) {
+        for (uint32_t i = threadIdx.x; i < count; i += threads) {
+            const uint64_t key = sh->bin[2 * i], own = sh->bin[2 * i + 1];
+            uint64_t front = before;
+#pragma unroll 4
+            for (uint32_t j = 0; j < count; ++j) front += sh->bin[2 * j] < key ? sh->bin[2 * j + 1] : 0;
+            if (front < goal && goal <= front + own) {
+                sh->cut_z = score_of(~(uint32_t)(key >> 32));
+                sh->cut_position = (uint32_t)key;
+            }
         }
         sync();
         Cut cut;
@@ -890,19 +922,6 @@ struct Held {
         cut.position = (int)sh->cut_position;
         sync();
         return cut;
-    }
-
-    // The columns that `take` picks, on the list as far as it holds them; how many there are.
-    template <typename Fn>
-    __device__ __forceinline__ uint32_t make_list(Fn take) {
-        each([&](float k, uint32_t p) {
-            if (take(k, p)) {
-                const uint32_t at = atomicAdd(&sh->listed, 1u);
-                if (at < (uint32_t)kList) { sh->list_z[at] = k; sh->list_position[at] = p; }
-            }
-        });
-        sync();
-        return sh->listed;
     }
 
     // The last column, in the order, with less than the target of the measure before it, among the columns
@@ -928,8 +947,9 @@ struct Held {
         const int bin = sh->found_bin;
         uint64_t before = sh->found_before;
         if (!by_mass && clipped && bin == kBins - 1) return within;   // what would go has no weight
-        uint32_t listed = make_list([&](float k, uint32_t p) { return within.keeps(k, p) && bin_of(k, scale) == bin; });
-        if (listed <= (uint32_t)kList) return rank_list(by_mass, listed, before, goal, ask);
+        uint32_t listed =
+            make_list(by_mass, ask, [&](float k, uint32_t p) { return within.keeps(k, p) && bin_of(k, scale) == bin; });
+        if (listed <= (uint32_t)kRanked) return rank_list(listed, before, goal);
 
         // Many columns crowd one bin (equal scores, or some far from the others): bins of keys, narrowed until
         // the rest can be ranked or is one score.
@@ -980,8 +1000,8 @@ struct Held {
                 cut.position = (int)find(more - 1, mine, before_wave, same);
                 return cut;
             }
-            listed = make_list(in);
-            if (listed <= (uint32_t)kList) return rank_list(by_mass, listed, before, goal, ask);
+            listed = make_list(by_mass, ask, in);
+            if (listed <= (uint32_t)kRanked) return rank_list(listed, before, goal);
         }
     }
 
@@ -1005,7 +1025,8 @@ struct Held {
             return cut.keeps(k, p) && e >= ask.least ? floorf(e) : 0.f;
         };
         double thread = 0.0;
-        each([&](float k, uint32_t p) { thread += (double)weight(k, p); });
+        if (cut.position < 0 && !(ask.least > 0.f)) each([&](float k, uint32_t) { thread += (double)ask.weight_of(k); });
+        else each([&](float k, uint32_t p) { thread += (double)weight(k, p); });
         const uint64_t mine = last64(scan64(whole_of(thread)));
         uint64_t before_wave;
         const uint64_t total = sum(mine, &before_wave);
@@ -1119,9 +1140,36 @@ struct Wanted {
     __device__ __forceinline__ uint32_t part() const { return top_p > 0.f ? (uint32_t)(top_p * 0x1p24f) : 0; }
 };
 
+// The draw among the columns on a list (in LDS, by column), by the workgroup's first `waves` waves.  The list's place is
+// free once they have it.
+template <typename Few, typename Shared>
+__device__ __forceinline__ void draw_listed(Few few, Shared* sh, uint32_t count, int waves, const Wanted& want,
+                                            const Asked& ask, int64_t r, int32_t* index, float* log) {
+    constexpr int K = Few::kScores;
+    static_assert(sizeof(typename Few::Shared) <= sizeof(Shared) && K <= 32, "the list's own place");
+    few.sh = (typename Few::Shared*)sh;
+    few.threads = waves * kWave;
+    few.waves = waves;
+    uint32_t column[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        const uint32_t at = few.position(i / 4) + i % 4;
+        few.z[0][i] = at < count ? sh->list_z[at] : -INFINITY;
+        column[i] = at < count ? sh->list_position[at] : 0;
+    }
+    few.sync();
+    const auto d = few.draw(want, ask);
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+        if (few.position(i / 4) + i % 4 == d.position) {
+            index[r] = (int32_t)column[i];
+            if (log) log[r] = d.log;
+        }
+}
+
 // A workgroup a row, the row in registers from its one read on.
 template <int K, int BINS, typename T>
-__global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 5 : 4)) void k_sample(const T* __restrict__ z, int64_t rows, uint32_t n, int64_t ldz,
+__global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 6 : 4)) void k_sample(const T* __restrict__ z, int64_t rows, uint32_t n, int64_t ldz,
                                                  Limits lim, const float* __restrict__ u, Rated rated,
                                                  int32_t* __restrict__ index, float* __restrict__ log) {
     using H = Held<K, BINS>;
@@ -1154,36 +1202,20 @@ __global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 5 : 4)) void k_sample
     const Asked ask{best, 1.f / want.t, want.least};
     // A few best columns are looked for among the few that reach a score which enough threads' largest ones reach:
     // the passes over the row are then two comparisons a score, and all else is done on a list.
-    if (K > 4 && top_k > 0 && top_k <= h.threads * 3 / 4) {
+    if (h.waves > 1 && top_k > 0 && top_k <= h.threads * 3 / 4) {
         const float reached = h.reached_by((uint32_t)top_k, best, [&](auto fn) { fn(mine); });
-        const uint32_t most = 4 * h.threads < H::kList ? 4 * h.threads : H::kList;
+        const uint32_t most = H::kList;
+        static_assert(H::kList <= 16 * kWave, "one wave holds the list");
         const uint32_t count = !(reached > -INFINITY) ? most + 1 : h.collect(
             most, [&](float v) { return v >= reached; },
             [&](uint32_t i, float v, uint32_t position) {
                 h.sh->list_z[i] = v;
                 h.sh->list_position[i] = position;
             });
-        if (count <= most) {
-            Held<4, BINS> few;
-            few.sh = (typename Held<4, BINS>::Shared*)shared;
-            few.threads = h.threads;
-            few.waves = h.waves;
-            uint32_t column[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t at = 4 * threadIdx.x + i;
-                few.z[0][i] = at < count ? few.sh->list_z[at] : -INFINITY;
-                column[i] = at < count ? few.sh->list_position[at] : 0;
-            }
-            few.sync();
-            const auto d = few.draw(want, ask);
-            if (threadIdx.x == d.position / 4) {
-                uint32_t c = column[0];
-#pragma unroll
-                for (int i = 1; i < 4; ++i) c = d.position % 4 == (uint32_t)i ? column[i] : c;
-                index[r] = (int32_t)c;
-                if (log) log[r] = d.log;
-            }
+        if (count <= most) {     // one wave: no barriers
+            if (h.wave() != 0) return;
+            if (count <= 512u) draw_listed(Held<8, 256>(), h.sh, count, 1, want, ask, r, index, log);
+            else draw_listed(Held<16, 256>(), h.sh, count, 1, want, ask, r, index, log);
             return;
         }
     }
@@ -1196,7 +1228,7 @@ enum RowKind { kRowNone, kRowBest, kRowFew, kRowShare, kRowRest, kRowSlow };
 // What a long row's kernels tell one another.
 struct RowPlan {
     int kind;
-    int bin;
+    float from, to;         // the scores of the bin in which the cut falls: from <= z < to
     uint64_t before, goal;
 };
 
@@ -1783,7 +1815,7 @@ __global__ __launch_bounds__(kRowThreads) void k_long_rows(LongArgs<T> a) {
     const Wanted want(a.lim, a.u, r);
     int kind = kind_of(want, count, w.segments * (kSegThreads / w.group));
     const Asked ask{best, 1.f / want.t, want.least};
-    RowPlan plan{kind, 0, 0, 0};
+    RowPlan plan{kind, 0.f, 0.f, 0, 0};
     if (kind == kRowNone) {
         const int32_t* list;
         int64_t listed;
@@ -1834,7 +1866,12 @@ __global__ __launch_bounds__(kRowThreads) void k_long_rows(LongArgs<T> a) {
             plan.goal = goal < 1 ? 1 : goal;
             return plan.goal;
         });
-        plan.bin = (int)sh->held.found_bin;
+        bool clipped;
+        const auto scale = Segment::scale_of(best, least, want.t, &clipped);
+        Segment bins;
+        const int bin = (int)sh->held.found_bin;
+        plan.from = bins.least_of_bins(bin, scale);
+        plan.to = bin == 0 ? INFINITY : bins.least_of_bins(bin - 1, scale);
         plan.before = sh->held.found_before;
     } else if (kind == kRowRest) {
         if (threadIdx.x < w.segments) sh->mass[threadIdx.x] = stat[threadIdx.x].mass;
@@ -1861,18 +1898,19 @@ __global__ __launch_bounds__(kSegThreads) void k_long_cut(LongArgs<T> a) {
     row_stats(h, w.stat + (int64_t)b * w.segments, w.segments, &best, &least, &count);
     const Wanted want(a.lim, a.u, r);
     const Asked ask{best, 1.f / want.t, want.least};
-    bool there, clipped;
+    bool there;
     take_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
-    const auto scale = Segment::scale_of(best, least, want.t, &clipped);
+    // (a best score of +inf is below no number: its bin goes up to and with it)
+    const auto above = [&](float v) { return v >= plan.to && plan.to < INFINITY; };
     const uint32_t listed = h.collect(
-        kSlab, [&](float v) { return v > -INFINITY && h.bin_of(v, scale) == plan.bin; },
+        kSlab, [&](float v) { return v >= plan.from && !above(v); },
         [&](uint32_t i, float v, uint32_t position) {
             w.list_z[(int64_t)blockIdx.x * kSlab + i] = v;
             w.list_column[(int64_t)blockIdx.x * kSlab + i] = seg * kSegColumns + position;
         });
     double thread = 0.0;
     h.each([&](float v, uint32_t) {
-        if (v > -INFINITY && h.bin_of(v, scale) < plan.bin) {
+        if (above(v)) {
             const float e = ask.scaled(v);
             thread += e >= ask.least ? (double)floorf(e) : 0.0;
         }
@@ -1917,8 +1955,7 @@ __global__ __launch_bounds__(kRowThreads) void k_long_draw(LongArgs<T> a) {
     float low;
     uint32_t listed;
     few.spread(&low, &listed);
-    Asked listed_ask = ask;
-    const Cut place = few.select(true, Cut(), low, want.t, 0, listed_ask, plan.goal - plan.before);
+    const Cut place = few.select(true, Cut(), low, want.t, 0, ask, plan.goal - plan.before);
     // the cut by column instead of by place on the list; what it keeps of the lists counts for its segments
     Cut cut;
     cut.z = place.z;
@@ -2270,7 +2307,8 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
     };
     const auto launch = [&](auto* p) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
-        if (n <= 512) return held(Held<8, 256>(), p);
+        if (n <= 512) return held(Held<8, 256>(), p);         // (up to 1,024 a wave, without a barrier)
+        if (n <= 1024) return held(Held<16, 256>(), p);
         if (n <= 4096) return held(Held<8, 1024>(), p);
         if (n <= 32768) return held(Held<32, 2048>(), p);
         if (n <= 65536) return held(Held<64, 4096>(), p);
