@@ -1075,54 +1075,74 @@ struct Rated {
     }
 };
 
-// Four scores from column c on, -inf for columns from n on and for what may not be drawn.
+// Four neighbouring scores as they lie in memory.
 template <typename T>
-__device__ __forceinline__ void load_scores(const T* row, uint32_t c, uint32_t n, float* z) {
-    T v[4];
-    if (c + 4 <= n) {
-        __builtin_memcpy(v, row + c, sizeof v);
+struct Four { uint32_t word[sizeof(T)]; };
+__device__ __forceinline__ void less_than_all(float* v) { *v = -INFINITY; }
+__device__ __forceinline__ void less_than_all(F16* v) { *v = F16{0xFC00}; }
+__device__ __forceinline__ void less_than_all(BF16* v) { *v = BF16{0xFF80}; }
+
+// Columns base .. base + n of a row on their way into registers (-inf past them).
+template <typename H, typename T>
+__device__ __forceinline__ void fetch_columns(const H& h, const T* row, uint32_t base, uint32_t n,
+                                              Four<T> (&raw)[H::kScores / 4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = to_float(v[i]);
-    } else {
+    for (int v = 0; v < H::kScores / 4; ++v) {
+        const uint32_t c = h.position(v);
+        if (c + 4 <= n) {
+            __builtin_memcpy(&raw[v], row + base + c, sizeof raw[v]);
+        } else {
+            T t[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[i] = c + i < n ? to_float(row[c + i]) : -INFINITY;
+            for (int i = 0; i < 4; ++i) {
+                less_than_all(&t[i]);
+                if (c + i < n) t[i] = row[base + c + i];
+            }
+            __builtin_memcpy(&raw[v], t, sizeof raw[v]);
+        }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) z[i] = z[i] > -INFINITY ? z[i] : -INFINITY;    // NaN
 }
 
-// Columns base .. base + n of a row into registers, without those on the list; `bits` is LDS, one a column.
+// The fetched columns without those on the row's list and without NaN; `bits` is LDS, one a column.  `there`: the
+// row's user exists.  (Between fetch and here, a kernel finds out what to do with them.)
 template <typename H, typename T>
-__device__ __forceinline__ void take_columns(H& h, const T* row, uint32_t base, uint32_t n, const Rated& rated, int64_t r,
-                                             uint32_t* bits, bool* there) {
+__device__ __forceinline__ void take_columns(H& h, const Four<T> (&raw)[H::kScores / 4], uint32_t base, uint32_t n,
+                                             const Rated& rated, int64_t r, uint32_t* bits, bool* there) {
     constexpr int K = H::kScores;
-#pragma unroll
-    for (int v = 0; v < K / 4; ++v) {
-        float four[4];
-        load_scores(row + base, h.position(v), n, four);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) h.z[v / 8][v % 8 * 4 + i] = four[i];
-    }
     const int32_t* list;
     int64_t listed;
     *there = rated.row(r, &list, &listed);
-    if (!*there || listed <= 0) return;
-    for (uint32_t w = threadIdx.x; w < (n + 31) / 32; w += h.threads) bits[w] = 0;
-    h.sync();
-    for (int64_t k = threadIdx.x; k < listed; k += h.threads) {
-        const uint32_t c = (uint32_t)list[k] - base;
-        if (c < n) atomicOr(&bits[c >> 5], 1u << (c & 31));
+    const bool some = *there && listed > 0;
+    if (some) {
+        for (uint32_t w = threadIdx.x; w < (n + 31) / 32; w += h.threads) bits[w] = 0;
+        h.sync();
+        for (int64_t k = threadIdx.x; k < listed; k += h.threads) {
+            const uint32_t c = (uint32_t)list[k] - base;
+            if (c < n) atomicOr(&bits[c >> 5], 1u << (c & 31));
+        }
+        h.sync();
     }
-    h.sync();
 #pragma unroll
     for (int v = 0; v < K / 4; ++v) {
-        const uint32_t c = h.position(v);
-        const uint32_t four = c < n ? bits[c >> 5] >> (c & 31) : 0;
+        T t[4];
+        __builtin_memcpy(t, &raw[v], sizeof t);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            h.z[v / 8][v % 8 * 4 + i] = four >> i & 1 ? -INFINITY : h.z[v / 8][v % 8 * 4 + i];
+        for (int i = 0; i < 4; ++i) {
+            const float z = to_float(t[i]);
+            h.z[v / 8][v % 8 * 4 + i] = z > -INFINITY ? z : -INFINITY;
+        }
     }
-    h.sync();
+    if (some) {
+#pragma unroll
+        for (int v = 0; v < K / 4; ++v) {
+            const uint32_t c = h.position(v);
+            const uint32_t four = c < n ? bits[c >> 5] >> (c & 31) : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                h.z[v / 8][v % 8 * 4 + i] = four >> i & 1 ? -INFINITY : h.z[v / 8][v % 8 * 4 + i];
+        }
+        h.sync();
+    }
 }
 
 // What row r asks for.
@@ -1181,7 +1201,9 @@ __global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 6 : 4)) void k_sample
     uint32_t* bits = (uint32_t*)(shared + sizeof(typename H::Shared));   // the columns left out, one bit each
     const int64_t r = blockIdx.x;
     bool there;
-    take_columns(h, z + r * ldz, 0, n, rated, r, bits, &there);
+    Four<T> raw[K / 4];
+    fetch_columns(h, z + r * ldz, 0, n, raw);
+    take_columns<H, T>(h, raw, 0, n, rated, r, bits, &there);
     if (!there) {
         if (threadIdx.x == 0) { index[r] = -1; if (log) log[r] = NAN; }
         return;
@@ -1228,6 +1250,7 @@ enum RowKind { kRowNone, kRowBest, kRowFew, kRowShare, kRowRest, kRowSlow };
 // What a long row's kernels tell one another.
 struct RowPlan {
     int kind;
+    float best;
     float from, to;         // the scores of the bin in which the cut falls: from <= z < to
     uint64_t before, goal;
 };
@@ -1427,35 +1450,78 @@ __device__ LongCut select_cut(Row<T>& row, LongCut within, uint32_t widest, uint
     }
 }
 
+// Rows that no workgroup's registers hold, in segments of 16,384 columns, a workgroup each; what the segments find
+// out goes through the workspace from one kernel to the next, and each kernel reads the scores again
+// (from the cache that all dies share, where they fit it):
+//   k_long_stats  a segment's best and least score and number of allowed columns, and the best scores of groups of its
+//                 columns
+//   k_long_parts  top-k: the segment's columns with a score that k groups' best ones reach; top-p: a histogram of
+//                 weights over the row's scores; neither: the segment's weight
+//   k_long_rows   a workgroup a row.  top-k: the draw, among what the segments listed; top-p: the bin in which the cut
+//                 falls; neither: the draw
+//   k_long_cut    top-p: the segment's columns in that bin, and the weight of those above it
+//   k_long_draw   top-p: the cut, by ranking the listed columns, and the draw
+// Rows whose lists do not hold what they should (equal scores without end, a top_k of more than 7/8 of the groups)
+// are drawn by the last of these kernels alone, which reads the row again for every pass (sample_slowly).
+constexpr int kSegWaves = 8, kSegThreads = kSegWaves * kWave, kSegColumns = kSegThreads * 32;
+constexpr int kSegMax = ALS_SERVE_N_MAX / kSegColumns;
+constexpr int kSlab = 2048;              // columns a segment lists
+constexpr int kFew = 8192;               // columns a row's workgroup takes from its lists
+constexpr int kGroups = 4096;            // most groups of a row
+using Segment = Held<32, 1024>;
+using FewOfRow = Held<8, 2048>;
+using SegmentOfRow = Held<32, 2048>;
+constexpr int kRowThreads = kFew / 8;
+static_assert(kSegMax <= kSegThreads && kSegMax <= kRowThreads && kRowThreads == kSampleThreads, "a thread a segment");
+
+struct SegStat {
+    float best, least;
+    uint32_t count, listed;
+    uint64_t mass;
+};
+// A batch's part of the workspace.  Segment s of the batch's row b is number b segments + s.
+struct LongWork {
+    RowPlan* plan;
+    SegStat* stat;
+    float* groups;              // kSegThreads / group a segment
+    uint64_t* bins;             // Segment::kBins a segment
+    float* list_z;              // kSlab a segment
+    uint32_t* list_column;
+    uint32_t segments, group;   // group: threads (of 32 columns each) that publish one best score
+    int64_t row0;               // the batch's first row
+};
 template <typename T>
-__global__ __launch_bounds__(kSampleThreads) void k_sample_slow(const T* __restrict__ z, int64_t rows, int64_t n,
-                                                           int64_t ldz, Limits lim, const float* __restrict__ u,
-                                                           const int64_t* __restrict__ rated_ptr,
-                                                           const int32_t* __restrict__ rated_idx,
-                                                           const int32_t* __restrict__ users, int64_t of,
-                                                           int32_t* __restrict__ index, float* __restrict__ log,
-                                                           const RowPlan* __restrict__ plan, int64_t row0) {
-    extern __shared__ unsigned char shared[];
-    SampleShared* sh = (SampleShared*)shared;
-    if (plan[blockIdx.x].kind != kRowSlow) return;
-    const int64_t r = row0 + blockIdx.x;
-    Row<T> row;
-    row.z = z + r * ldz;
-    row.n = n;
-    row.sh = sh;
-    row.rated = nullptr;
-    row.rated_count = 0;
-    row.one_chunk = n <= kChunk;
-    if (rated_ptr) {
-        const int64_t src = users ? (int64_t)users[r] : r;
-        if (src < 0 || src >= of) {
-            if (threadIdx.x == 0) { index[r] = -1; if (log) log[r] = NAN; }
-            return;
-        }
-        row.rated = rated_idx + rated_ptr[src];
-        row.rated_count = rated_ptr[src + 1] - rated_ptr[src];
-        if (row.rated_count > 0 && row.one_chunk) row.mark(0, n);
+struct LongArgs {
+    const T* z;
+    int64_t n, ldz;
+    Limits lim;
+    const float* u;
+    Rated rated;
+    int32_t* index;
+    float* log;
+    LongWork work;
+    __device__ __forceinline__ uint32_t columns(uint32_t seg) const {
+        const int64_t left = n - (int64_t)seg * kSegColumns;
+        return left < kSegColumns ? (uint32_t)left : kSegColumns;
     }
+};
+
+// A whole row by one workgroup of kSampleThreads, which reads it again for every pass.
+template <typename T>
+__device__ __forceinline__ void sample_slowly(const LongArgs<T>& a, int64_t r, unsigned char* shared) {
+    SampleShared* sh = (SampleShared*)shared;
+    const Limits& lim = a.lim;
+    const float* u = a.u;
+    int32_t* index = a.index;
+    float* log = a.log;
+    Row<T> row;
+    row.z = a.z + r * a.ldz;
+    row.n = a.n;
+    row.sh = sh;
+    row.one_chunk = a.n <= kChunk;
+    if (!a.rated.row(r, &row.rated, &row.rated_count)) return;     // (has no allowed column, and is not slow)
+    __syncthreads();
+    if (row.rated_count > 0 && row.one_chunk) row.mark(0, a.n);
     // the largest and the least key, and the number of allowed columns
     uint32_t hi = 0, lo = 0xFFFFFFFFu, count = 0;
     row.each([&](int64_t, uint32_t key) { hi = max(hi, key); lo = min(lo, key); ++count; });
@@ -1521,61 +1587,6 @@ __global__ __launch_bounds__(kSampleThreads) void k_sample_slow(const T* __restr
     }
 }
 
-// Rows that no workgroup's registers hold, in segments of 16,384 columns, a workgroup each; what the segments find
-// out goes through the workspace from one kernel to the next, and each kernel reads the scores again
-// (from the cache that all dies share, where they fit it):
-//   k_long_stats  a segment's best and least score and number of allowed columns, and the best scores of groups of its
-//                 columns
-//   k_long_parts  top-k: the segment's columns with a score that k groups' best ones reach; top-p: a histogram of
-//                 weights over the row's scores; neither: the segment's weight
-//   k_long_rows   a workgroup a row.  top-k: the draw, among what the segments listed; top-p: the bin in which the cut
-//                 falls; neither: the draw
-//   k_long_cut    top-p: the segment's columns in that bin, and the weight of those above it
-//   k_long_draw   top-p: the cut, by ranking the listed columns, and the draw
-// Rows whose lists do not hold what they should (equal scores without end, a top_k of more than 7/8 of the groups)
-// are left to k_sample_slow.
-constexpr int kSegWaves = 8, kSegThreads = kSegWaves * kWave, kSegColumns = kSegThreads * 32;
-constexpr int kSegMax = ALS_SERVE_N_MAX / kSegColumns;
-constexpr int kSlab = 2048;              // columns a segment lists
-constexpr int kFew = 8192;               // columns a row's workgroup takes from its lists
-constexpr int kGroups = 4096;            // most groups of a row
-using Segment = Held<32, 1024>;
-using FewOfRow = Held<8, 2048>;
-using SegmentOfRow = Held<32, 2048>;
-constexpr int kRowThreads = kFew / 8;
-static_assert(kSegMax <= kSegThreads && kSegMax <= kRowThreads, "a thread a segment");
-
-struct SegStat {
-    float best, least;
-    uint32_t count, listed;
-    uint64_t mass;
-};
-// A batch's part of the workspace.  Segment s of the batch's row b is number b segments + s.
-struct LongWork {
-    RowPlan* plan;
-    SegStat* stat;
-    float* groups;              // kSegThreads / group a segment
-    uint64_t* bins;             // Segment::kBins a segment
-    float* list_z;              // kSlab a segment
-    uint32_t* list_column;
-    uint32_t segments, group;   // group: threads (of 32 columns each) that publish one best score
-    int64_t row0;               // the batch's first row
-};
-template <typename T>
-struct LongArgs {
-    const T* z;
-    int64_t n, ldz;
-    Limits lim;
-    const float* u;
-    Rated rated;
-    int32_t* index;
-    float* log;
-    LongWork work;
-    __device__ __forceinline__ uint32_t columns(uint32_t seg) const {
-        const int64_t left = n - (int64_t)seg * kSegColumns;
-        return left < kSegColumns ? (uint32_t)left : kSegColumns;
-    }
-};
 
 // Best and least score and allowed columns of a row, from its segments; by the whole workgroup.
 template <typename H>
@@ -1622,7 +1633,9 @@ __global__ __launch_bounds__(kSegThreads) void k_long_stats(LongArgs<T> a) {
     const uint32_t b = blockIdx.x / w.segments, seg = blockIdx.x % w.segments;
     const int64_t r = w.row0 + b;
     bool there;
-    take_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
+    Four<T> raw[Segment::kScores / 4];
+    fetch_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), raw);
+    take_columns<Segment, T>(h, raw, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
     float best, least;
     uint32_t count;
     float mine = h.largest(&best);
@@ -1649,6 +1662,8 @@ __global__ __launch_bounds__(kSegThreads) void k_long_parts(LongArgs<T> a) {
     const LongWork& w = a.work;
     const uint32_t b = blockIdx.x / w.segments, seg = blockIdx.x % w.segments;
     const int64_t r = w.row0 + b;
+    Four<T> raw[Segment::kScores / 4];
+    fetch_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), raw);
     float best, least;
     uint32_t count;
     row_stats(h, w.stat + (int64_t)b * w.segments, w.segments, &best, &least, &count);
@@ -1658,7 +1673,7 @@ __global__ __launch_bounds__(kSegThreads) void k_long_parts(LongArgs<T> a) {
     if (kind != kRowFew && kind != kRowShare && kind != kRowRest) return;
     const Asked ask{best, 1.f / want.t, want.least};
     bool there;
-    take_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
+    take_columns<Segment, T>(h, raw, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
     if (kind == kRowFew) {
         const float* all = w.groups + (int64_t)b * groups;
         float z[kGroups / kSegThreads];
@@ -1707,7 +1722,8 @@ struct RowShared {
     uint32_t first[kSegMax + 1];         // of a segment's list, on the row's
     uint64_t mass[kSegMax];
     uint32_t bits[kSegColumns / 32];
-    uint32_t found;
+    uint32_t found, cut_column;
+    float cut_z;
     uint64_t before;
 };
 static_assert(sizeof(FewOfRow::Shared) == sizeof(SegmentOfRow::Shared), "one place for both");
@@ -1735,11 +1751,12 @@ __device__ __forceinline__ bool place_lists(H& h, const SegStat* stat, uint32_t 
 }
 
 // The row's listed columns, by column, four neighbours a thread and time; `column` are theirs.
-__device__ __forceinline__ void take_lists(FewOfRow& few, const LongWork& w, uint32_t b, const RowShared* sh,
-                                           uint32_t (&column)[8]) {
+template <typename Few>
+__device__ __forceinline__ void take_lists(Few& few, const LongWork& w, uint32_t b, const RowShared* sh,
+                                           uint32_t (&column)[Few::kScores]) {
     const uint32_t total = sh->first[w.segments];
 #pragma unroll
-    for (int v = 0; v < 2; ++v)
+    for (int v = 0; v < Few::kScores / 4; ++v)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
             const uint32_t i = few.position(v) + c;
@@ -1761,6 +1778,25 @@ __device__ __forceinline__ void take_lists(FewOfRow& few, const LongWork& w, uin
         }
 }
 
+// The draw among the segments' listed columns, by the workgroup's first `waves` waves.
+template <typename Few, typename T>
+__device__ __forceinline__ void draw_lists(Few few, const LongArgs<T>& a, uint32_t b, const Wanted& want, const Asked& ask,
+                                           int waves, RowShared* sh) {
+    const int64_t r = a.work.row0 + b;
+    few.sh = (typename Few::Shared*)&sh->held;
+    few.threads = waves * kWave;
+    few.waves = waves;
+    uint32_t column[Few::kScores];
+    take_lists(few, a.work, b, sh, column);
+    const auto d = few.draw(want, ask);
+#pragma unroll
+    for (int i = 0; i < Few::kScores; ++i)
+        if (few.position(i / 4) + i % 4 == d.position) {
+            a.index[r] = (int32_t)column[i];
+            if (a.log) a.log[r] = d.log;
+        }
+}
+
 // The draw from the segments' weights (sh->mass), the columns being those that `cut` (by column) keeps.
 template <typename T>
 __device__ __forceinline__ void draw_from_segments(SegmentOfRow& h, const LongArgs<T>& a, uint32_t b, const Wanted& want,
@@ -1777,7 +1813,9 @@ __device__ __forceinline__ void draw_from_segments(SegmentOfRow& h, const LongAr
     h.sync();
     const uint32_t seg = sh->found, base = seg * kSegColumns;
     bool there;
-    take_columns(h, a.z + r * a.ldz, base, a.columns(seg), a.rated, r, sh->bits, &there);
+    Four<T> raw[SegmentOfRow::kScores / 4];
+    fetch_columns(h, a.z + r * a.ldz, base, a.columns(seg), raw);
+    take_columns<SegmentOfRow, T>(h, raw, base, a.columns(seg), a.rated, r, sh->bits, &there);
     const auto weight = [&](float k, uint32_t p) {
         const float e = ask.scaled(k);
         return cut.keeps(k, base + p) && e >= ask.least ? floorf(e) : 0.f;
@@ -1815,7 +1853,7 @@ __global__ __launch_bounds__(kRowThreads) void k_long_rows(LongArgs<T> a) {
     const Wanted want(a.lim, a.u, r);
     int kind = kind_of(want, count, w.segments * (kSegThreads / w.group));
     const Asked ask{best, 1.f / want.t, want.least};
-    RowPlan plan{kind, 0.f, 0.f, 0, 0};
+    RowPlan plan{kind, best, 0.f, 0.f, 0, 0};
     if (kind == kRowNone) {
         const int32_t* list;
         int64_t listed;
@@ -1830,35 +1868,27 @@ __global__ __launch_bounds__(kRowThreads) void k_long_rows(LongArgs<T> a) {
         h.sync();
         const uint32_t seg = sh->found;
         bool there;
-        take_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), a.rated, r, sh->bits, &there);
+        Four<T> raw[SegmentOfRow::kScores / 4];
+        fetch_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), raw);
+        take_columns<SegmentOfRow, T>(h, raw, seg * kSegColumns, a.columns(seg), a.rated, r, sh->bits, &there);
         const uint32_t p = h.first_of(best);
         if (threadIdx.x == 0) { a.index[r] = (int32_t)(seg * kSegColumns + p); if (a.log) a.log[r] = 0.f; }
     } else if (kind == kRowFew) {
-        if (place_lists(h, stat, w.segments, sh)) {
-            FewOfRow few;
-            few.sh = (FewOfRow::Shared*)&sh->held;
-            few.threads = h.threads;
-            few.waves = h.waves;
-            uint32_t column[8];
-            take_lists(few, w, b, sh, column);
-            const auto d = few.draw(want, ask);
-#pragma unroll
-            for (int v = 0; v < 2; ++v)
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (few.position(v) + c == d.position) {
-                        a.index[r] = (int32_t)column[4 * v + c];
-                        if (a.log) a.log[r] = d.log;
-                    }
+        if (!place_lists(h, stat, w.segments, sh)) {
+            kind = kRowSlow;
+        } else if (sh->first[w.segments] <= 1024u) {
+            if (h.wave() == 0) draw_lists(Held<16, 256>(), a, b, want, ask, 1, sh);
         } else {
-            plan.kind = kRowSlow;
+            draw_lists(FewOfRow(), a, b, want, ask, h.waves, sh);
         }
     } else if (kind == kRowShare) {
         for (int i = threadIdx.x; i < SegmentOfRow::kBins; i += kRowThreads) {
             uint64_t s = 0;
-            if (i < Segment::kBins)
-                for (uint32_t seg = 0; seg < w.segments; ++seg)
-                    s += w.bins[((int64_t)b * w.segments + seg) * Segment::kBins + i];
+            if (i < Segment::kBins) {
+                const uint64_t* bin = w.bins + (int64_t)b * w.segments * Segment::kBins + i;
+#pragma unroll 8
+                for (uint32_t seg = 0; seg < w.segments; ++seg) s += bin[(int64_t)seg * Segment::kBins];
+            }
             sh->held.bin[i] = s;
         }
         h.search_bins([&](uint64_t total) {
@@ -1877,6 +1907,7 @@ __global__ __launch_bounds__(kRowThreads) void k_long_rows(LongArgs<T> a) {
         if (threadIdx.x < w.segments) sh->mass[threadIdx.x] = stat[threadIdx.x].mass;
         draw_from_segments(h, a, b, want, ask, Cut(), sh);
     }
+    if (kind == kRowSlow) sample_slowly(a, r, shared);
     if (threadIdx.x == 0) w.plan[b] = plan;
 }
 
@@ -1891,15 +1922,14 @@ __global__ __launch_bounds__(kSegThreads) void k_long_cut(LongArgs<T> a) {
     const LongWork& w = a.work;
     const uint32_t b = blockIdx.x / w.segments, seg = blockIdx.x % w.segments;
     const int64_t r = w.row0 + b;
+    Four<T> raw[Segment::kScores / 4];
+    fetch_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), raw);
     const RowPlan plan = w.plan[b];
     if (plan.kind != kRowShare) return;
-    float best, least;
-    uint32_t count;
-    row_stats(h, w.stat + (int64_t)b * w.segments, w.segments, &best, &least, &count);
     const Wanted want(a.lim, a.u, r);
-    const Asked ask{best, 1.f / want.t, want.least};
+    const Asked ask{plan.best, 1.f / want.t, want.least};
     bool there;
-    take_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
+    take_columns<Segment, T>(h, raw, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
     // (a best score of +inf is below no number: its bin goes up to and with it)
     const auto above = [&](float v) { return v >= plan.to && plan.to < INFINITY; };
     const uint32_t listed = h.collect(
@@ -1923,6 +1953,32 @@ __global__ __launch_bounds__(kSegThreads) void k_long_cut(LongArgs<T> a) {
     }
 }
 
+// The cut among the segments' listed columns (of the bin in which it falls), by the workgroup's first `waves` waves.
+template <typename Few, typename T>
+__device__ __forceinline__ void cut_listed(Few few, const LongArgs<T>& a, uint32_t b, const Wanted& want, const Asked& ask,
+                                           const RowPlan& plan, int waves, RowShared* sh) {
+    few.sh = (typename Few::Shared*)&sh->held;
+    few.threads = waves * kWave;
+    few.waves = waves;
+    uint32_t column[Few::kScores];
+    take_lists(few, a.work, b, sh, column);
+    float low;
+    uint32_t listed;
+    few.spread(&low, &listed);
+    const Cut place = few.select(true, Cut(), low, want.t, 0, ask, plan.goal - plan.before);
+#pragma unroll
+    for (int i = 0; i < Few::kScores; ++i) {
+        const float k = few.z[0][i];
+        const uint32_t at = few.position(i / 4) + i % 4;
+        if (at == (uint32_t)place.position) { sh->cut_column = column[i]; sh->cut_z = place.z; }
+        if (place.keeps(k, at)) {
+            const float e = ask.scaled(k);
+            if (e >= ask.least)
+                atomicAdd((unsigned long long*)&sh->mass[column[i] / kSegColumns], (unsigned long long)whole_of(floorf(e)));
+        }
+    }
+}
+
 template <typename T>
 __global__ __launch_bounds__(kRowThreads) void k_long_draw(LongArgs<T> a) {
     extern __shared__ __align__(16) unsigned char shared[];
@@ -1937,47 +1993,24 @@ __global__ __launch_bounds__(kRowThreads) void k_long_draw(LongArgs<T> a) {
     const RowPlan plan = w.plan[b];
     if (plan.kind != kRowShare) return;
     const SegStat* stat = w.stat + (int64_t)b * w.segments;
-    float best, least;
-    uint32_t count;
-    row_stats(h, stat, w.segments, &best, &least, &count);
     const Wanted want(a.lim, a.u, r);
-    const Asked ask{best, 1.f / want.t, want.least};
+    const Asked ask{plan.best, 1.f / want.t, want.least};
     if (!place_lists(h, stat, w.segments, sh)) {
-        if (threadIdx.x == 0) w.plan[b].kind = kRowSlow;
+        sample_slowly(a, r, shared);
         return;
     }
-    FewOfRow few;
-    few.sh = (FewOfRow::Shared*)&sh->held;
-    few.threads = h.threads;
-    few.waves = h.waves;
-    uint32_t column[8];
-    take_lists(few, w, b, sh, column);
-    float low;
-    uint32_t listed;
-    few.spread(&low, &listed);
-    const Cut place = few.select(true, Cut(), low, want.t, 0, ask, plan.goal - plan.before);
-    // the cut by column instead of by place on the list; what it keeps of the lists counts for its segments
-    Cut cut;
-    cut.z = place.z;
-    few.sync();
     if (threadIdx.x < w.segments) sh->mass[threadIdx.x] = stat[threadIdx.x].mass;
-    few.sync();
-#pragma unroll
-    for (int v = 0; v < 2; ++v)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const float k = few.z[0][4 * v + c];
-            const uint32_t i = few.position(v) + c;
-            if (i == (uint32_t)place.position) sh->found = column[4 * v + c];
-            if (place.keeps(k, i)) {
-                const float e = ask.scaled(k);
-                if (e >= ask.least)
-                    atomicAdd((unsigned long long*)&sh->mass[column[4 * v + c] / kSegColumns],
-                              (unsigned long long)whole_of(floorf(e)));
-            }
-        }
-    few.sync();
-    cut.position = (int)sh->found;
+    h.sync();
+    // the cut, by column; what it keeps of the lists counts for its segments
+    if (sh->first[w.segments] <= 1024u) {
+        if (h.wave() == 0) cut_listed(Held<16, 256>(), a, b, want, ask, plan, 1, sh);
+    } else {
+        cut_listed(FewOfRow(), a, b, want, ask, plan, h.waves, sh);
+    }
+    h.sync();
+    Cut cut;
+    cut.z = sh->cut_z;
+    cut.position = (int)sh->cut_column;
     draw_from_segments(h, a, b, want, ask, cut, sh);
 }
 
@@ -2319,13 +2352,12 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
         const size_t a_segment = sizeof(SegStat) + kSegThreads / group * sizeof(float) + Segment::kBins * 8 + kSlab * 8;
         const int64_t batch = (int64_t)(ctx->ws_bytes / (a_segment * segments + sizeof(RowPlan)));
         const hipStream_t st = (hipStream_t)stream;
-        const size_t row_lds = sizeof(RowShared);
         const int64_t bits = rated_ptr ? (n < kChunk ? n : kChunk) : 0;
         const size_t slow_lds = sizeof(SampleShared) + (size_t)((bits + 31) / 32) * 4;
-        static std::atomic<uint64_t> of_rows{0}, of_draw{0}, of_slow{0};
+        const size_t row_lds = sizeof(RowShared) > slow_lds ? sizeof(RowShared) : slow_lds;
+        static std::atomic<uint64_t> of_rows{0}, of_draw{0};
         whole_lds(k_long_rows<T>, ctx->device, &of_rows);
         whole_lds(k_long_draw<T>, ctx->device, &of_draw);
-        whole_lds(k_sample_slow<T>, ctx->device, &of_slow);
         const bool shares = l.top_p || l.top_p_all < 1.f;
         for (int64_t row0 = 0; row0 < rows; row0 += batch) {
             const int64_t some = rows - row0 < batch ? rows - row0 : batch;
@@ -2354,8 +2386,6 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
                 hipLaunchKernelGGL(k_long_cut<T>, parts, dim3(kSegThreads), 0, st, args);
                 hipLaunchKernelGGL(k_long_draw<T>, whole, dim3(kRowThreads), row_lds, st, args);
             }
-            hipLaunchKernelGGL(k_sample_slow<T>, whole, dim3(kSampleThreads), slow_lds, st, p, rows, n, ldz, lim, u,
-                               rated_ptr, rated_idx, users, of, index, log, w.plan, row0);
         }
     };
     if (dtype == ALS_F32) launch((const float*)z);
