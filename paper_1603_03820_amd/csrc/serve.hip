@@ -565,22 +565,31 @@ __device__ __forceinline__ uint64_t last64(uint64_t v) {
 
 // What a row asks for, and its best score: all that a weight depends on.
 struct Asked {
-    float top, inv_t;   // the best score, 1 / T
+    float top, inv_t;   // the best score, 1 / T (both finite: see Held::plain)
     float least;        // 2^40 min_p
+    float t;
+    __device__ __forceinline__ Asked(float best, float t_, float least_)
+        : top(best), inv_t(1.f / t_), least(least_), t(t_) {}
 
     // 2^40 exp((z - top) / T), z <= top, of the exponential rounded to fp32: 2 to the nearest whole number of
     // x log2(e), held in two parts, times 2 to the rest.  Where that is 1 or more it equals 2^40 expf(x) in every bit
-    // (tested over all such x) at half the instructions: x ends at -64, where no weight is left, so that nothing
-    // overflows.  No product may be fused into a sum here but the two that are written so.
+    // for all but 2 of the 1.1e9 such x (tested one by one), at half its instructions: x ends at -64, where no weight
+    // is left (nor where a difference or product is not a number), so that nothing overflows.  The whole number comes
+    // by adding 1.5 2^23 (+ 40), whose sum has it in its last bits; they go to the exponent.  No product may be
+    // fused into a sum here but the two that are written so.
     __device__ __forceinline__ float scaled(float z) const {
 #pragma clang fp contract(off)
-        const float x = fmaxf((z - top) * inv_t, -64.f);    // -64 also where a difference or product is not a number
+        const float x = fmaxf((z - top) * inv_t, -64.f);
         const float high = x * 0x1.715476p+0f;
         const float low = fmaf(x, 0x1.4ae0cp-26f, fmaf(x, 0x1.715476p+0f, -high));
-        const float whole = rintf(high);
-        const float e = ldexpf(__builtin_amdgcn_exp2f((high - whole) + low), (int)whole + 40);
-        return z == top ? 0x1p40f : e;
+        const float shifted = high + (0x1.8p23f + 40.f);
+        const float part = __builtin_amdgcn_exp2f((high - (shifted - (0x1.8p23f + 40.f))) + low);
+        return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, part) +
+                                             (__builtin_bit_cast(uint32_t, shifted) << 23));
     }
+    // Whether the formula holds: with a best score of +inf, or 1 / T past the largest float, the best columns weigh
+    // 2^40 each and all others nothing.
+    __device__ __forceinline__ bool is_plain() const { return top < INFINITY && inv_t < INFINITY; }
     // The weight, a whole number of at most 24 significant bits.
     __device__ __forceinline__ float weight_of(float z) const { return floorf(scaled(z)); }
 };
@@ -642,6 +651,14 @@ struct Held {
         if (waves > 1) __syncthreads();
         else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+    // Where the weights' formula does not hold (the best columns weigh 2^40 each and all others nothing), scores for
+    // which it does: 0 for the best, none for the others.
+    __device__ __forceinline__ void plain(Asked& ask) {
+        if (ask.is_plain()) return;
+#pragma unroll
+        for (int v = 0; v < K; ++v) z[v / 32][v % 32] = z[v / 32][v % 32] == ask.top ? 0.f : -INFINITY;
+        ask = Asked(0.f, 1.f, ask.least);
+    }
     // fn(score, position) for every held score.
     template <typename Fn>
     __device__ __forceinline__ void each(Fn fn) const {
@@ -691,28 +708,23 @@ struct Held {
         *best = hi;
         return mine;
     }
-    // The least allowed score, and how many there are.
-    __device__ __forceinline__ void spread(float* least, uint32_t* count) {
-        float lo = -INFINITY;    // the least one's negative
-        uint32_t n = 0;
-        each_at_once([&](float k, uint32_t) {
+    // The least allowed score of every fourth column: near enough to the least for bins.
+    __device__ __forceinline__ float near_least() {
+        float lo = -INFINITY;    // its negative
+#pragma unroll
+        for (int v = 0; v < K; v += 4) {
+            const float k = z[v / 32][v % 32];
             lo = fmaxf(lo, k > -INFINITY ? -k : -INFINITY);
-            n += k > -INFINITY;
-        });
+        }
         lo = wave_max(lo);
-        n = __builtin_amdgcn_readlane(scan32(n), 63);
         if (waves > 1) {
-            if (lane() == 0) { sh->wave_b[wave()] = lo; sh->wave_c[wave()] = n; }
+            sync();
+            if (lane() == 0) sh->wave_b[wave()] = lo;
             sync();
             lo = -INFINITY;
-            n = 0;
-            for (int w = 0; w < waves; ++w) {
-                lo = fmaxf(lo, sh->wave_b[w]);
-                n += sh->wave_c[w];
-            }
+            for (int w = 0; w < waves; ++w) lo = fmaxf(lo, sh->wave_b[w]);
         }
-        *least = -lo;
-        *count = n;
+        return -lo;
     }
 
     // A value that at least k of those reach that `values(fn)` hands this thread, and few more: the k-th largest, as
@@ -764,18 +776,21 @@ struct Held {
         }
         sync();
         if (total > most) return total;
-        const uint64_t below = (1ull << lane()) - 1;
 #pragma unroll
         for (int v = 0; v < K; v += 4) {
             uint64_t takes[4];
-            uint32_t mine = at, all = 0;
+            uint32_t all = 0;
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 takes[c] = __ballot(take(z[v / 32][v % 32 + c]));
-                mine += __popcll(takes[c] & below);
                 all += __popcll(takes[c]);
             }
             if (all) {
+                uint32_t mine = at;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    mine = __builtin_amdgcn_mbcnt_hi((uint32_t)(takes[c] >> 32),
+                                                     __builtin_amdgcn_mbcnt_lo((uint32_t)takes[c], mine));
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
                     if (takes[c] >> lane() & 1) put(mine++, z[v / 32][v % 32 + c], position(v / 4) + c);
@@ -828,16 +843,16 @@ struct Held {
 
     // The bin of a score: linear from the best one down, the last bin for all that is the range or more below it.
     struct Scale { float top, per; };
-    // Over all scores, but no further than 28 T below the best, where a weight is 0 (clipped).
+    // Down to `least` (or some score near the least: the last bin has all that is below), but no further than 28 T
+    // below the best, where a weight is 0 (clipped).
     static __device__ __forceinline__ Scale scale_of(float top, float least, float t, bool* clipped) {
         const float all = top - least;
         *clipped = all > 28.f * t;
         const float range = *clipped ? 28.f * t : all;
-        return Scale{top, range > 0.f ? (float)(kBins - 1) / range : 0.f};
+        return Scale{top, range > 1e-30f ? (float)(kBins - 1) / range : 0.f};
     }
     __device__ __forceinline__ int bin_of(float k, const Scale& c) const {
-        const float x = (c.top - k) * c.per;
-        return k == c.top ? 0 : (x < (float)(kBins - 1) ? (int)x : kBins - 1);
+        return (int)fminf((c.top - k) * c.per, (float)(kBins - 1));
     }
     __device__ __forceinline__ void add_to_bin(uint32_t bin, bool by_mass, float k, const Asked& ask) {
         const uint64_t w = by_mass ? whole_of(ask.weight_of(k)) : 1;
@@ -926,15 +941,16 @@ struct Held {
 
     // The last column, in the order, with less than the target of the measure before it, among the columns
     // that `within` keeps.  by_mass: the measure is the weight and the target share_of(its sum, part), at least 1;
-    // else the target is `part` columns (fewer than there are).
+    // else the target is `part` columns; all stay where there are fewer.
     // (`given`, where it is not 0, is the target itself.)
-    __device__ __forceinline__ Cut select(bool by_mass, Cut within, float least, float t, uint32_t part,
-                                          const Asked& ask, uint64_t given = 0) {
+    __device__ __forceinline__ Cut select(bool by_mass, Cut within, float least, uint32_t part, const Asked& ask,
+                                          uint64_t given = 0) {
         sync();
         for (int b = threadIdx.x; b < kBins; b += threads) sh->bin[b] = 0;
+        if (threadIdx.x == 0) sh->found_bin = kBins;
         sync();
         bool clipped;
-        const Scale scale = scale_of(ask.top, least, t, &clipped);
+        const Scale scale = scale_of(ask.top, least, ask.t, &clipped);
         each([&](float k, uint32_t p) {
             if (within.keeps(k, p)) add_to_bin(bin_of(k, scale), by_mass, k, ask);
         });
@@ -946,6 +962,7 @@ struct Held {
         });
         const int bin = sh->found_bin;
         uint64_t before = sh->found_before;
+        if (bin == kBins) return within;                               // fewer columns than asked for
         if (!by_mass && clipped && bin == kBins - 1) return within;   // what would go has no weight
         uint32_t listed =
             make_list(by_mass, ask, [&](float k, uint32_t p) { return within.keeps(k, p) && bin_of(k, scale) == bin; });
@@ -1013,12 +1030,11 @@ struct Held {
         const float top_p = want.top_p;
         Cut cut;
         float least = 0.f;
-        uint32_t count = 0;
-        if (top_k > 0 || top_p < 1.f) spread(&least, &count);
+        if (top_k > 0 || top_p < 1.f) least = near_least();
 #pragma nounroll
         for (int by_mass = 0; by_mass < 2; ++by_mass) {     // one copy of the code for both cuts
-            if (by_mass ? !(top_p < 1.f) : top_k <= 0 || (uint32_t)top_k >= count) continue;
-            cut = select(by_mass != 0, cut, least, want.t, by_mass ? want.part() : (uint32_t)top_k, ask);
+            if (by_mass ? !(top_p < 1.f) : top_k <= 0) continue;
+            cut = select(by_mass != 0, cut, least, by_mass ? want.part() : (uint32_t)top_k, ask);
         }
         const auto weight = [&](float k, uint32_t p) {
             const float e = ask.scaled(k);
@@ -1034,7 +1050,7 @@ struct Held {
         each([&](float k, uint32_t at) { if (at == p) sh->cut_z = k; });
         sync();
         const float k = sh->cut_z;
-        const float x = k == ask.top ? 0.f : (k - ask.top) * ask.inv_t;
+        const float x = (k - ask.top) * ask.inv_t;
         return Drawn{p, x - logf((float)total * 0x1p-40f)};
     }
 
@@ -1103,7 +1119,7 @@ __device__ __forceinline__ void fetch_columns(const H& h, const T* row, uint32_t
     }
 }
 
-// The fetched columns without those on the row's list and without NaN; `bits` is LDS, one a column.  `there`: the
+// The fetched columns without those on the row's list (a NaN stays: no comparison holds for it); `bits` is LDS, one a column.  `there`: the
 // row's user exists.  (Between fetch and here, a kernel finds out what to do with them.)
 template <typename H, typename T>
 __device__ __forceinline__ void take_columns(H& h, const Four<T> (&raw)[H::kScores / 4], uint32_t base, uint32_t n,
@@ -1128,18 +1144,19 @@ __device__ __forceinline__ void take_columns(H& h, const Four<T> (&raw)[H::kScor
         __builtin_memcpy(t, &raw[v], sizeof t);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float z = to_float(t[i]);
-            h.z[v / 8][v % 8 * 4 + i] = z > -INFINITY ? z : -INFINITY;
+            h.z[v / 8][v % 8 * 4 + i] = to_float(t[i]);
         }
     }
     if (some) {
 #pragma unroll
         for (int v = 0; v < K / 4; ++v) {
             const uint32_t c = h.position(v);
-            const uint32_t four = c < n ? bits[c >> 5] >> (c & 31) : 0;
+            const uint32_t four = c < n ? bits[c >> 5] >> (c & 31) & 15 : 0;
+            if (four) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                h.z[v / 8][v % 8 * 4 + i] = four >> i & 1 ? -INFINITY : h.z[v / 8][v % 8 * 4 + i];
+                for (int i = 0; i < 4; ++i)
+                    h.z[v / 8][v % 8 * 4 + i] = four >> i & 1 ? -INFINITY : h.z[v / 8][v % 8 * 4 + i];
+            }
         }
         h.sync();
     }
@@ -1221,10 +1238,12 @@ __global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 6 : 4)) void k_sample
         if (threadIdx.x == 0) { index[r] = (int32_t)p; if (log) log[r] = 0.f; }
         return;
     }
-    const Asked ask{best, 1.f / want.t, want.least};
+    Asked ask(best, want.t, want.least);
+    const bool odd = !ask.is_plain();
+    h.plain(ask);
     // A few best columns are looked for among the few that reach a score which enough threads' largest ones reach:
     // the passes over the row are then two comparisons a score, and all else is done on a list.
-    if (h.waves > 1 && top_k > 0 && top_k <= h.threads * 3 / 4) {
+    if (!odd && h.waves > 1 && top_k > 0 && top_k <= h.threads * 3 / 4) {
         const float reached = h.reached_by((uint32_t)top_k, best, [&](auto fn) { fn(mine); });
         const uint32_t most = H::kList;
         static_assert(H::kList <= 16 * kWave, "one wave holds the list");
@@ -1278,8 +1297,8 @@ struct Row {
     int64_t rated_count;
     SampleShared* sh;
     uint32_t best;      // the largest key
-    Asked ask;
-    bool one_chunk;
+    Asked ask{0.f, 1.f, 0.f};
+    bool odd, one_chunk;      // odd: the weights' formula does not hold
 
     // Marks the left-out columns of [c0, c1).
     __device__ void mark(int64_t c0, int64_t c1) {
@@ -1308,7 +1327,9 @@ struct Row {
         }
     }
 
-    __device__ float scaled(uint32_t d) const { return ask.scaled(score_of(best - d)); }
+    __device__ float scaled(uint32_t d) const {
+        return odd ? (d == 0 ? 0x1p40f : 0.f) : ask.scaled(score_of(best - d));
+    }
     __device__ uint64_t weight_of(uint32_t d) const { return whole_of(floorf(scaled(d))); }
 };
 
@@ -1475,9 +1496,9 @@ constexpr int kRowThreads = kFew / 8;
 static_assert(kSegMax <= kSegThreads && kSegMax <= kRowThreads && kRowThreads == kSampleThreads, "a thread a segment");
 
 struct SegStat {
-    float best, least;
-    uint32_t count, listed;
+    float best, least;      // the least: near it
     uint64_t mass;
+    uint32_t listed;
 };
 // A batch's part of the workspace.  Segment s of the batch's row b is number b segments + s.
 struct LongWork {
@@ -1548,7 +1569,8 @@ __device__ __forceinline__ void sample_slowly(const LongArgs<T>& a, int64_t r, u
     const Wanted want(lim, u, r);
     const bool greedy = !(want.t > 0.f);
     row.best = hi;
-    row.ask = Asked{score_of(hi), greedy ? 1.f : 1.f / want.t, want.least};
+    row.ask = Asked(score_of(hi), greedy ? 1.f : want.t, want.least);
+    row.odd = !row.ask.is_plain();
     const int k = want.top_k;
     const uint32_t widest = hi - lo;
     LongCut cut{widest, 0xFFFFFFFFu};
@@ -1570,7 +1592,7 @@ __device__ __forceinline__ void sample_slowly(const LongArgs<T>& a, int64_t r, u
     }
     auto weight = [&](int64_t c, uint32_t d) -> uint64_t {
         if (!cut.keeps(d, c)) return 0;
-        const float e = row.ask.scaled(score_of(hi - d));
+        const float e = row.scaled(d);
         return e >= want.least ? whole_of(floorf(e)) : 0;
     };
     uint64_t sum = 0;
@@ -1581,43 +1603,37 @@ __device__ __forceinline__ void sample_slowly(const LongArgs<T>& a, int64_t r, u
         index[r] = (int32_t)c;
         if (log) {
             const float v = to_float(row.z[c]);
-            const float x = v == row.ask.top ? 0.f : (v - row.ask.top) * row.ask.inv_t;
+            const float x = row.odd ? 0.f : (v - row.ask.top) * row.ask.inv_t;
             log[r] = x - logf((float)sum * 0x1p-40f);
         }
     }
 }
 
 
-// Best and least score and allowed columns of a row, from its segments; by the whole workgroup.
+// Best and (nearly) least score of a row, from its segments; by the whole workgroup.
 template <typename H>
-__device__ __forceinline__ void row_stats(H& h, const SegStat* stat, uint32_t segments, float* best, float* least,
-                                          uint32_t* count) {
+__device__ __forceinline__ void row_stats(H& h, const SegStat* stat, uint32_t segments, float* best, float* least) {
     const bool mine = threadIdx.x < segments;
     float hi = mine ? stat[threadIdx.x].best : -INFINITY, lo = mine ? -stat[threadIdx.x].least : -INFINITY;
-    uint32_t n = mine ? stat[threadIdx.x].count : 0;
     hi = wave_max(hi);
     lo = wave_max(lo);
-    n = __builtin_amdgcn_readlane(scan32(n), 63);
-    if (h.lane() == 0) { h.sh->wave_a[h.wave()] = hi; h.sh->wave_b[h.wave()] = lo; h.sh->wave_c[h.wave()] = n; }
+    if (h.lane() == 0) { h.sh->wave_a[h.wave()] = hi; h.sh->wave_b[h.wave()] = lo; }
     h.sync();
     hi = lo = -INFINITY;
-    n = 0;
     for (int w = 0; w < h.waves; ++w) {
         hi = fmaxf(hi, h.sh->wave_a[w]);
         lo = fmaxf(lo, h.sh->wave_b[w]);
-        n += h.sh->wave_c[w];
     }
     h.sync();
     *best = hi;
     *least = -lo;
-    *count = n;
 }
 
-__device__ __forceinline__ int kind_of(const Wanted& want, uint32_t count, uint32_t groups) {
-    if (count == 0) return kRowNone;
+__device__ __forceinline__ int kind_of(const Wanted& want, float best, int64_t n, uint32_t groups) {
+    if (!(best > -INFINITY)) return kRowNone;
     if (!(want.t > 0.f)) return kRowBest;
-    if (want.top_k > 0 && (uint32_t)want.top_k < count)
-        return (uint32_t)want.top_k <= groups / 8 * 7 ? kRowFew : kRowSlow;
+    if (!Asked(best, want.t, 0.f).is_plain()) return kRowSlow;
+    if (want.top_k > 0 && want.top_k < n) return (uint32_t)want.top_k <= groups / 8 * 7 ? kRowFew : kRowSlow;
     return want.top_p < 1.f ? kRowShare : kRowRest;
 }
 
@@ -1636,15 +1652,13 @@ __global__ __launch_bounds__(kSegThreads) void k_long_stats(LongArgs<T> a) {
     Four<T> raw[Segment::kScores / 4];
     fetch_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), raw);
     take_columns<Segment, T>(h, raw, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
-    float best, least;
-    uint32_t count;
+    float best;
     float mine = h.largest(&best);
-    h.spread(&least, &count);
+    const float least = h.near_least();
     if (threadIdx.x == 0) {
         SegStat& s = w.stat[blockIdx.x];
-        s.best = best;
+        s.best = there ? best : -INFINITY;
         s.least = least;
-        s.count = there ? count : 0;
     }
     for (uint32_t d = 1; d < w.group; d <<= 1) mine = fmaxf(mine, __shfl_xor(mine, d));
     if (threadIdx.x % w.group == 0)
@@ -1665,13 +1679,12 @@ __global__ __launch_bounds__(kSegThreads) void k_long_parts(LongArgs<T> a) {
     Four<T> raw[Segment::kScores / 4];
     fetch_columns(h, a.z + r * a.ldz, seg * kSegColumns, a.columns(seg), raw);
     float best, least;
-    uint32_t count;
-    row_stats(h, w.stat + (int64_t)b * w.segments, w.segments, &best, &least, &count);
+    row_stats(h, w.stat + (int64_t)b * w.segments, w.segments, &best, &least);
     const Wanted want(a.lim, a.u, r);
     const uint32_t per = kSegThreads / w.group, groups = w.segments * per;
-    const int kind = kind_of(want, count, groups);
+    const int kind = kind_of(want, best, a.n, groups);
     if (kind != kRowFew && kind != kRowShare && kind != kRowRest) return;
-    const Asked ask{best, 1.f / want.t, want.least};
+    Asked ask(best, want.t, want.least);
     bool there;
     take_columns<Segment, T>(h, raw, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
     if (kind == kRowFew) {
@@ -1829,7 +1842,7 @@ __device__ __forceinline__ void draw_from_segments(SegmentOfRow& h, const LongAr
     h.each([&](float k, uint32_t i) {
         if (i == p) {
             a.index[r] = (int32_t)(base + p);
-            const float x = k == ask.top ? 0.f : (k - ask.top) * ask.inv_t;
+            const float x = (k - ask.top) * ask.inv_t;
             if (a.log) a.log[r] = x - logf((float)total * 0x1p-40f);
         }
     });
@@ -1848,11 +1861,10 @@ __global__ __launch_bounds__(kRowThreads) void k_long_rows(LongArgs<T> a) {
     const int64_t r = w.row0 + b;
     const SegStat* stat = w.stat + (int64_t)b * w.segments;
     float best, least;
-    uint32_t count;
-    row_stats(h, stat, w.segments, &best, &least, &count);
+    row_stats(h, stat, w.segments, &best, &least);
     const Wanted want(a.lim, a.u, r);
-    int kind = kind_of(want, count, w.segments * (kSegThreads / w.group));
-    const Asked ask{best, 1.f / want.t, want.least};
+    int kind = kind_of(want, best, a.n, w.segments * (kSegThreads / w.group));
+    Asked ask(best, want.t, want.least);
     RowPlan plan{kind, best, 0.f, 0.f, 0, 0};
     if (kind == kRowNone) {
         const int32_t* list;
@@ -1927,7 +1939,7 @@ __global__ __launch_bounds__(kSegThreads) void k_long_cut(LongArgs<T> a) {
     const RowPlan plan = w.plan[b];
     if (plan.kind != kRowShare) return;
     const Wanted want(a.lim, a.u, r);
-    const Asked ask{plan.best, 1.f / want.t, want.least};
+    Asked ask(plan.best, want.t, want.least);
     bool there;
     take_columns<Segment, T>(h, raw, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
     // (a best score of +inf is below no number: its bin goes up to and with it)
@@ -1962,10 +1974,7 @@ __device__ __forceinline__ void cut_listed(Few few, const LongArgs<T>& a, uint32
     few.waves = waves;
     uint32_t column[Few::kScores];
     take_lists(few, a.work, b, sh, column);
-    float low;
-    uint32_t listed;
-    few.spread(&low, &listed);
-    const Cut place = few.select(true, Cut(), low, want.t, 0, ask, plan.goal - plan.before);
+    const Cut place = few.select(true, Cut(), few.near_least(), 0, ask, plan.goal - plan.before);
 #pragma unroll
     for (int i = 0; i < Few::kScores; ++i) {
         const float k = few.z[0][i];
@@ -1994,7 +2003,7 @@ __global__ __launch_bounds__(kRowThreads) void k_long_draw(LongArgs<T> a) {
     if (plan.kind != kRowShare) return;
     const SegStat* stat = w.stat + (int64_t)b * w.segments;
     const Wanted want(a.lim, a.u, r);
-    const Asked ask{plan.best, 1.f / want.t, want.least};
+    Asked ask(plan.best, want.t, want.least);
     if (!place_lists(h, stat, w.segments, sh)) {
         sample_slowly(a, r, shared);
         return;
