@@ -968,15 +968,14 @@ struct Held {
             make_list(by_mass, ask, [&](float k, uint32_t p) { return within.keeps(k, p) && bin_of(k, scale) == bin; });
         if (listed <= (uint32_t)kRanked) return rank_list(listed, before, goal);
 
-        // Many columns crowd one bin (equal scores, or some far from the others): bins of keys, narrowed until
+        // Many columns crowd the bin (equal scores, or some far from the others): bins of its keys, narrowed until
         // the rest can be ranked or is one score.
-        before = 0;
         const uint32_t best = key_of(ask.top);
-        uint32_t lo = 0, hi = 0xFFFFFFFFu;     // distances of keys from the best
-        for (;;) {
+        uint32_t lo = 0, hi = 0;     // distances of keys from the best
+        for (bool keys = false;; keys = true) {
             const auto in = [&](float k, uint32_t p) {
                 const uint32_t d = best - key_of(k);
-                return d >= lo && d <= hi && within.keeps(k, p);
+                return within.keeps(k, p) && (keys ? d >= lo && d <= hi : bin_of(k, scale) == bin);
             };
             uint32_t far = 0, near = 0;        // the largest distance, the least one's complement
             each([&](float k, uint32_t p) {
@@ -993,16 +992,19 @@ struct Held {
             sync();
             lo = ~sh->low;
             hi = sh->high;
-            int shift = 0;
-            while (((hi - lo) >> shift) >= (uint32_t)kBins) ++shift;
-            each([&](float k, uint32_t p) {
-                if (in(k, p)) add_to_bin((best - key_of(k) - lo) >> shift, by_mass, k, ask);
-            });
-            search_bins([&](uint64_t) { return goal - before; });
-            before += sh->found_before;
-            lo += sh->found_bin << shift;
-            const uint32_t end = lo + ((1u << shift) - 1);
-            hi = end < hi ? end : hi;
+            if (lo != hi) {
+                int shift = 0;
+                while (((hi - lo) >> shift) >= (uint32_t)kBins) ++shift;
+                each([&](float k, uint32_t p) {
+                    const uint32_t d = best - key_of(k) - lo;
+                    if (d <= hi - lo && within.keeps(k, p)) add_to_bin(d >> shift, by_mass, k, ask);
+                });
+                search_bins([&](uint64_t) { return goal - before; });
+                before += sh->found_before;
+                lo += sh->found_bin << shift;
+                const uint32_t end = lo + ((1u << shift) - 1);
+                hi = end < hi ? end : hi;
+            }
             if (lo == hi) {     // equal scores: as many of them, by position, as reach the goal
                 Cut cut;
                 cut.z = score_of(best - lo);
@@ -1017,7 +1019,9 @@ struct Held {
                 cut.position = (int)find(more - 1, mine, before_wave, same);
                 return cut;
             }
-            listed = make_list(by_mass, ask, in);
+            listed = make_list(by_mass, ask, [&](float k, uint32_t p) {
+                return best - key_of(k) - lo <= hi - lo && within.keeps(k, p);
+            });
             if (listed <= (uint32_t)kRanked) return rank_list(listed, before, goal);
         }
     }
@@ -1177,6 +1181,19 @@ struct Wanted {
     __device__ __forceinline__ uint32_t part() const { return top_p > 0.f ? (uint32_t)(top_p * 0x1p24f) : 0; }
 };
 
+// The draw among held columns that are some columns of a row, `column` being theirs.
+template <typename Few>
+__device__ __forceinline__ void draw_held(Few& few, const uint32_t (&column)[Few::kScores], const Wanted& want,
+                                          const Asked& ask, int64_t r, int32_t* index, float* log) {
+    const auto d = few.draw(want, ask);
+#pragma unroll
+    for (int i = 0; i < Few::kScores; ++i)
+        if (few.position(i / 4) + i % 4 == d.position) {
+            index[r] = (int32_t)column[i];
+            if (log) log[r] = d.log;
+        }
+}
+
 // The draw among the columns on a list (in LDS, by column), by the workgroup's first `waves` waves.  The list's place is
 // free once they have it.
 template <typename Few, typename Shared>
@@ -1195,13 +1212,7 @@ __device__ __forceinline__ void draw_listed(Few few, Shared* sh, uint32_t count,
         column[i] = at < count ? sh->list_position[at] : 0;
     }
     few.sync();
-    const auto d = few.draw(want, ask);
-#pragma unroll
-    for (int i = 0; i < K; ++i)
-        if (few.position(i / 4) + i % 4 == d.position) {
-            index[r] = (int32_t)column[i];
-            if (log) log[r] = d.log;
-        }
+    draw_held(few, column, want, ask, r, index, log);
 }
 
 // A workgroup a row, the row in registers from its one read on.
@@ -1270,7 +1281,8 @@ enum RowKind { kRowNone, kRowBest, kRowFew, kRowShare, kRowRest, kRowSlow };
 struct RowPlan {
     int kind;
     float best;
-    float from, to;         // the scores of the bin in which the cut falls: from <= z < to
+    int bin;                // the bin in which the cut falls,
+    float from, to;         // and its scores: from <= z < to
     uint64_t before, goal;
 };
 
@@ -1638,7 +1650,7 @@ __device__ __forceinline__ int kind_of(const Wanted& want, float best, int64_t n
 }
 
 template <typename T>
-__global__ __launch_bounds__(kSegThreads) void k_long_stats(LongArgs<T> a) {
+__global__ __launch_bounds__(kSegThreads, 8) void k_long_stats(LongArgs<T> a) {
     __shared__ Segment::Shared sh;
     __shared__ uint32_t bits[kSegColumns / 32];
     Segment h;
@@ -1791,23 +1803,17 @@ __device__ __forceinline__ void take_lists(Few& few, const LongWork& w, uint32_t
         }
 }
 
-// The draw among the segments' listed columns, by the workgroup's first `waves` waves.
-template <typename Few, typename T>
-__device__ __forceinline__ void draw_lists(Few few, const LongArgs<T>& a, uint32_t b, const Wanted& want, const Asked& ask,
-                                           int waves, RowShared* sh) {
-    const int64_t r = a.work.row0 + b;
-    few.sh = (typename Few::Shared*)&sh->held;
-    few.threads = waves * kWave;
-    few.waves = waves;
-    uint32_t column[Few::kScores];
-    take_lists(few, a.work, b, sh, column);
-    const auto d = few.draw(want, ask);
-#pragma unroll
-    for (int i = 0; i < Few::kScores; ++i)
-        if (few.position(i / 4) + i % 4 == d.position) {
-            a.index[r] = (int32_t)column[i];
-            if (a.log) a.log[r] = d.log;
+// The row's listed columns into LDS, by column (there are at most kList).
+__device__ __forceinline__ void gather_lists(const LongWork& w, uint32_t b, RowShared* sh) {
+    for (uint32_t seg = threadIdx.x / kWave; seg < w.segments; seg += kRowThreads / kWave) {
+        const uint32_t first = sh->first[seg], count = sh->first[seg + 1] - first;
+        const int64_t from = ((int64_t)b * w.segments + seg) * kSlab;
+        for (uint32_t i = threadIdx.x % kWave; i < count; i += kWave) {
+            sh->held.list_z[first + i] = w.list_z[from + i];
+            sh->held.list_position[first + i] = w.list_column[from + i];
         }
+    }
+    __syncthreads();
 }
 
 // The draw from the segments' weights (sh->mass), the columns being those that `cut` (by column) keeps.
@@ -1865,7 +1871,7 @@ __global__ __launch_bounds__(kRowThreads) void k_long_rows(LongArgs<T> a) {
     const Wanted want(a.lim, a.u, r);
     int kind = kind_of(want, best, a.n, w.segments * (kSegThreads / w.group));
     Asked ask(best, want.t, want.least);
-    RowPlan plan{kind, best, 0.f, 0.f, 0, 0};
+    RowPlan plan{kind, best, 0, 0.f, 0.f, 0, 0};
     if (kind == kRowNone) {
         const int32_t* list;
         int64_t listed;
@@ -1888,17 +1894,25 @@ __global__ __launch_bounds__(kRowThreads) void k_long_rows(LongArgs<T> a) {
     } else if (kind == kRowFew) {
         if (!place_lists(h, stat, w.segments, sh)) {
             kind = kRowSlow;
-        } else if (sh->first[w.segments] <= 1024u) {
-            if (h.wave() == 0) draw_lists(Held<16, 256>(), a, b, want, ask, 1, sh);
+        } else if (sh->first[w.segments] <= (uint32_t)SegmentOfRow::kList) {
+            gather_lists(w, b, sh);
+            if (h.wave() == 0)
+                draw_listed(Held<16, 256>(), &sh->held, sh->first[w.segments], 1, want, ask, r, a.index, a.log);
         } else {
-            draw_lists(FewOfRow(), a, b, want, ask, h.waves, sh);
+            FewOfRow few;
+            few.sh = (FewOfRow::Shared*)&sh->held;
+            few.threads = h.threads;
+            few.waves = h.waves;
+            uint32_t column[FewOfRow::kScores];
+            take_lists(few, w, b, sh, column);
+            draw_held(few, column, want, ask, r, a.index, a.log);
         }
     } else if (kind == kRowShare) {
         for (int i = threadIdx.x; i < SegmentOfRow::kBins; i += kRowThreads) {
             uint64_t s = 0;
             if (i < Segment::kBins) {
                 const uint64_t* bin = w.bins + (int64_t)b * w.segments * Segment::kBins + i;
-#pragma unroll 8
+#pragma unroll 16
                 for (uint32_t seg = 0; seg < w.segments; ++seg) s += bin[(int64_t)seg * Segment::kBins];
             }
             sh->held.bin[i] = s;
@@ -1912,6 +1926,7 @@ __global__ __launch_bounds__(kRowThreads) void k_long_rows(LongArgs<T> a) {
         const auto scale = Segment::scale_of(best, least, want.t, &clipped);
         Segment bins;
         const int bin = (int)sh->held.found_bin;
+        plan.bin = bin;
         plan.from = bins.least_of_bins(bin, scale);
         plan.to = bin == 0 ? INFINITY : bins.least_of_bins(bin - 1, scale);
         plan.before = sh->held.found_before;
@@ -1942,23 +1957,30 @@ __global__ __launch_bounds__(kSegThreads) void k_long_cut(LongArgs<T> a) {
     Asked ask(plan.best, want.t, want.least);
     bool there;
     take_columns<Segment, T>(h, raw, seg * kSegColumns, a.columns(seg), a.rated, r, bits, &there);
-    // (a best score of +inf is below no number: its bin goes up to and with it)
-    const auto above = [&](float v) { return v >= plan.to && plan.to < INFINITY; };
+    const auto above = [&](float v) { return v >= plan.to; };
     const uint32_t listed = h.collect(
         kSlab, [&](float v) { return v >= plan.from && !above(v); },
         [&](uint32_t i, float v, uint32_t position) {
             w.list_z[(int64_t)blockIdx.x * kSlab + i] = v;
             w.list_column[(int64_t)blockIdx.x * kSlab + i] = seg * kSegColumns + position;
         });
-    double thread = 0.0;
-    h.each([&](float v, uint32_t) {
-        if (above(v)) {
-            const float e = ask.scaled(v);
-            thread += e >= ask.least ? (double)floorf(e) : 0.0;
-        }
-    });
+    // the weight above the bin is in the histogram, unless min_p takes some of it
+    uint64_t thread = 0;
+    if (plan.bin == 0 || ask.scaled(plan.to) >= ask.least) {
+        for (int i = threadIdx.x; i < plan.bin; i += kSegThreads)
+            thread += w.bins[(int64_t)blockIdx.x * Segment::kBins + i];
+    } else {
+        double sum = 0.0;
+        h.each([&](float v, uint32_t) {
+            if (above(v)) {
+                const float e = ask.scaled(v);
+                sum += e >= ask.least ? (double)floorf(e) : 0.0;
+            }
+        });
+        thread = whole_of(sum);
+    }
     uint64_t before;
-    const uint64_t mass = h.sum(last64(scan64(whole_of(thread))), &before);
+    const uint64_t mass = h.sum(last64(scan64(thread)), &before);
     if (threadIdx.x == 0) {
         w.stat[blockIdx.x].listed = listed;
         w.stat[blockIdx.x].mass = mass;
@@ -1973,7 +1995,18 @@ __device__ __forceinline__ void cut_listed(Few few, const LongArgs<T>& a, uint32
     few.threads = waves * kWave;
     few.waves = waves;
     uint32_t column[Few::kScores];
-    take_lists(few, a.work, b, sh, column);
+    if (waves == 1) {
+        const uint32_t count = sh->first[a.work.segments];
+#pragma unroll
+        for (int i = 0; i < Few::kScores; ++i) {
+            const uint32_t at = few.position(i / 4) + i % 4;
+            few.z[0][i] = at < count ? sh->held.list_z[at] : -INFINITY;
+            column[i] = at < count ? sh->held.list_position[at] : 0;
+        }
+        few.sync();
+    } else {
+        take_lists(few, a.work, b, sh, column);
+    }
     const Cut place = few.select(true, Cut(), few.near_least(), 0, ask, plan.goal - plan.before);
 #pragma unroll
     for (int i = 0; i < Few::kScores; ++i) {
@@ -2011,7 +2044,8 @@ __global__ __launch_bounds__(kRowThreads) void k_long_draw(LongArgs<T> a) {
     if (threadIdx.x < w.segments) sh->mass[threadIdx.x] = stat[threadIdx.x].mass;
     h.sync();
     // the cut, by column; what it keeps of the lists counts for its segments
-    if (sh->first[w.segments] <= 1024u) {
+    if (sh->first[w.segments] <= (uint32_t)SegmentOfRow::kList) {
+        gather_lists(w, b, sh);
         if (h.wave() == 0) cut_listed(Held<16, 256>(), a, b, want, ask, plan, 1, sh);
     } else {
         cut_listed(FewOfRow(), a, b, want, ask, plan, h.waves, sh);
