@@ -2383,9 +2383,14 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
     };
     const auto launch = [&](auto* p) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
-        if (n <= 512) return held(Held<8, 256>(), p);         // (up to 1,024 a wave, without a barrier)
+        // As few waves as hold the row, up to 1,024 columns one (which needs no barrier); then 8 or 16 scores a thread,
+        // so that a row's passes are short, and 32 where there are rows enough for every CU.  Top-k 200, top-p 0.9
+        // and left-out columns, us: 2,000 x 8,000 8 a thread 83, 16 48, 32 89; 1 x 16,000 16 20.5, 32 20.6, by top-p
+        // alone 21 and 28; 2,000 x 16,000 16 108, 32 68.
+        if (n <= 512) return held(Held<8, 256>(), p);
         if (n <= 1024) return held(Held<16, 256>(), p);
         if (n <= 4096) return held(Held<8, 1024>(), p);
+        if (n <= 8192 || (n <= 16384 && rows <= ctx->cus)) return held(Held<16, 1024>(), p);
         if (n <= 32768) return held(Held<32, 2048>(), p);
         if (n <= 65536) return held(Held<64, 4096>(), p);
         // in batches of as many rows as the workspace holds
