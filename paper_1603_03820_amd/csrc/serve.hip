@@ -2310,8 +2310,12 @@ int als_score(als_serve_ctx* ctx, const int8_t* xq, int64_t ldx, const float* xs
     // rows that a tile's loads cannot take are first laid out anew, where the workspace holds them
     const int64_t whole = ((int64_t)f + 15) / 16 * 16;
     const auto direct = [](const int8_t* q, int64_t ld) { return aligned(q, 16) && ld % 16 == 0 && ld < kTileStride; };
-    const int64_t x_need = direct(xq, ldx) ? 0 : m * whole, t_need = direct(tq, ldt) ? 0 : n * whole;
-    if (m <= (int64_t)ctx->ws_bytes && n <= (int64_t)ctx->ws_bytes && x_need + t_need <= (int64_t)ctx->ws_bytes) {
+    const int64_t room = (int64_t)ctx->ws_bytes;
+    const auto need = [&](const int8_t* q, int64_t ld, int64_t rows) {
+        return direct(q, ld) ? 0 : (rows > room / whole ? room + 1 : rows * whole);
+    };
+    const int64_t x_need = need(xq, ldx, m), t_need = need(tq, ldt, n);
+    if (x_need + t_need <= room) {
         const auto pack = [&](const int8_t*& q, int64_t& ld, int64_t rows, unsigned char* to) {
             const int64_t groups = whole / 16, blocks = (rows * groups + 255) / 256;
             hipLaunchKernelGGL(k_pack, dim3((unsigned)blocks), dim3(256), 0, st, q, ld, rows, f, (int8_t*)to, groups);

@@ -225,7 +225,7 @@ def als_sample(ctx: Context, scores, u, temperature=1.0, top_k=0, top_p=1.0, min
     if isinstance(top_k, torch.Tensor):
         lim.top_k = _vector(ctx, top_k, "top_k", _I32, rows, other)
     else:
-        lim.top_k_all = top_k
+        lim.top_k_all = min(max(int(top_k), 0), 2 ** 31 - 1)
     if isinstance(top_p, torch.Tensor):
         lim.top_p = _vector(ctx, top_p, "top_p", _F32, rows, other)
     else:

@@ -256,6 +256,51 @@ def test_sample_long_rows(ctx, n):
             draw_rows(ctx, zz, [0.2, 0.5, 0.99], rated=(ptr, idx), **limits)
 
 
+@pytest.mark.parametrize("n", [16_000, 60_000, 131_073, 4_194_304])
+def test_sample_longest_and_between(ctx, n):
+    """The longest row there may be, and lengths at which rows are held in other ways."""
+    rng = np.random.default_rng(n)
+    rows = 2
+    z = dev((3.5 + 0.7 * rng.standard_normal((rows, n))).astype(np.float32))
+    idx = rng.integers(0, n, 300)
+    for zz in (z, z.to(torch.bfloat16)):
+        for limits in (dict(temperature=0.3), dict(temperature=0.2, top_p=0.9), dict(top_k=200, top_p=0.8),
+                       dict(top_k=3000), dict(temperature=0.3, top_p=0.95, min_p=0.05), dict(temperature=0.0)):
+            log(f"sample n {n} {zz.dtype} {limits}")
+            draw_rows(ctx, zz, [0.3, 0.97], rated=(np.array([0, 300, 300]), idx), **limits)
+
+
+@pytest.mark.parametrize("rows,n", [(300, 9_000), (300, 16_000), (900, 100_003)])
+def test_sample_rows_alone_and_together(ctx, rows, n):
+    """A row's draw does not depend on the rows beside it (how many there are chooses how they are held, and
+    many long rows go through the workspace in batches)."""
+    from paper_1603_03820_amd import serve
+    g = torch.Generator("cuda:0").manual_seed(n)
+    z = (3.5 + 0.7 * torch.randn(rows, n, device="cuda:0", generator=g)).to(torch.float16)
+    u = torch.rand(rows, device="cuda:0", generator=g)
+    k = torch.randint(0, 400, (rows,), device="cuda:0", generator=g, dtype=torch.int32)
+    p = 0.8 + 0.3 * torch.rand(rows, device="cuda:0", generator=g)
+    t = torch.rand(rows, device="cuda:0", generator=g) * 0.5
+    log(f"sample {rows} x {n} together")
+    index, lg = serve.als_sample(ctx, z, u, temperature=t, top_k=k, top_p=p)
+    for r in range(0, rows, 97):
+        log(f"row {r} alone")
+        i, l1 = serve.als_sample(ctx, z[r:r + 1], u[r:r + 1], temperature=t[r:r + 1], top_k=k[r:r + 1], top_p=p[r:r + 1])
+        assert i.item() == index[r].item() and l1.item() == lg[r].item()
+    draw_rows(ctx, z[-3:], u[-3:].cpu().numpy(), temperature=t[-3:].cpu().numpy(), top_k=k[-3:].cpu().numpy(),
+              top_p=p[-3:].cpu().numpy())
+
+
+def test_sample_sorted_scores(ctx):
+    """Best columns next to one another: they crowd one wave, one segment."""
+    for n in (5_000, 17_770, 200_000):
+        z = torch.linspace(5, 0, n, device="cuda:0").expand(3, n).contiguous()
+        z[1] = z[1].flip(0)
+        for limits in (dict(top_k=300), dict(temperature=0.2, top_p=0.9), dict(top_k=2000, top_p=0.5), dict(top_p=0.99)):
+            log(f"sample of sorted scores n {n} {limits}")
+            draw_rows(ctx, z, [0.1, 0.6, 0.95], **limits)
+
+
 def test_sample_limits_by_row(ctx):
     rng = np.random.default_rng(8)
     rows, n = 64, 3000
