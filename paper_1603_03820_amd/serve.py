@@ -92,7 +92,9 @@ class Context:
 
 
 # A call's checks take as long as its launch where the work is small, so they read each property of a tensor
-# once and pass plain numbers on (an empty tensor's pointer is 0, which is NULL).
+# once and pass plain numbers on (an empty tensor's pointer is 0, which is NULL).  A tensor that is used on another
+# stream than the current one is recorded there, so that its memory is not handed out again while the call may
+# still run.
 
 
 def _stream(ctx: Context, stream):
@@ -106,17 +108,14 @@ def _stream(ctx: Context, stream):
     return handle, stream if handle != current else None
 
 
-def _use(ctx: Context, t, name, dtypes, other):
-    """Checks a tensor's place and type.  One that is used on another stream than the current one is recorded
-    there, so that its memory is not handed out again while the call may still run."""
+def _use(ctx: Context, t, name, dtypes):
+    """Says what is wrong with a tensor's place or type."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
     if t.get_device() != ctx.index:
         raise ValueError(f"{name} is on {t.device}, the context on {ctx.device}")
     if t.dtype not in dtypes:
         raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, got {t.dtype}")
-    if other is not None:
-        t.record_stream(other)
 
 
 def _empty(ctx: Context, shape, dtype, other):
@@ -129,29 +128,42 @@ def _empty(ctx: Context, shape, dtype, other):
 
 def _vector(ctx: Context, t, name, dtypes, length, other):
     """Pointer of a contiguous vector of that length."""
-    _use(ctx, t, name, dtypes, other)
+    try:
+        if (t.dtype in dtypes and t.get_device() == ctx.index and t.dim() == 1 and t.numel() == length
+                and t.is_contiguous()):
+            if other is not None:
+                t.record_stream(other)
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _use(ctx, t, name, dtypes)
     if t.dim() != 1 or t.numel() != length:
         raise ValueError(f"{name} must have {length} elements, has shape {tuple(t.shape)}")
-    if length > 1 and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _matrix(ctx: Context, t, name, dtypes, rows, cols, other):
     """(pointer, row stride, rows, columns) of a matrix whose rows are contiguous, at any distance."""
-    _use(ctx, t, name, dtypes, other)
+    try:
+        fits = t.dtype in dtypes and t.get_device() == ctx.index and t.dim() == 2
+    except AttributeError:
+        fits = False
+    if not fits:
+        _use(ctx, t, name, dtypes)
     shape = t.shape
-    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+    if not fits or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
         want = ("any" if rows is None else rows, "any" if cols is None else cols)
         raise ValueError(f"{name} must be a matrix of {want[0]} x {want[1]}, has shape {tuple(shape)}")
     rows, cols = shape
     ld, one = t.stride()
-    if cols > 1 and one != 1:
+    if one != 1 and cols > 1:
         raise ValueError(f"the rows of {name} must be contiguous")
     if ld < cols:
         if rows > 1:
             raise ValueError(f"the rows of {name} overlap")
         ld = cols
+    if other is not None:
+        t.record_stream(other)
     return t.data_ptr(), ld, rows, cols
 
 
