@@ -859,13 +859,18 @@ struct Held {
         if (w) atomicAdd((unsigned long long*)&sh->bin[bin], (unsigned long long)w);
     }
 
-    // The least score of bins 0 .. b (of all scores above -inf): bins fall with the score, so halving keys finds it.
+    // The least score of bins 0 .. b (of all scores above -inf): bins fall with the score, so the wave cuts the range
+    // of keys into 64 until it is one key.
     __device__ __forceinline__ float least_of_bins(int b, const Scale& c) const {
-        uint32_t no = key_of(-INFINITY), yes = key_of(c.top);
+        uint32_t no = key_of(-INFINITY), yes = key_of(c.top);      // the last key above the bins, the first within
         while (yes - no > 1) {
-            const uint32_t mid = no + (yes - no) / 2;
-            if (bin_of(score_of(mid), c) <= b) yes = mid;
-            else no = mid;
+            const uint32_t step = (yes - no - 1) / kWave + 1;
+            const uint64_t at = (uint64_t)no + (uint64_t)step * (lane() + 1);
+            const uint64_t in = __ballot(at >= yes || bin_of(score_of((uint32_t)at), c) <= b);
+            const int first = in ? __ffsll((unsigned long long)in) - 1 : kWave;
+            const uint64_t next = (uint64_t)no + (uint64_t)step * (first + 1);
+            no += step * first;
+            yes = next < yes ? (uint32_t)next : yes;
         }
         return score_of(yes);
     }
@@ -1503,8 +1508,9 @@ constexpr int kFew = 8192;               // columns a row's workgroup takes from
 constexpr int kGroups = 4096;            // most groups of a row
 using Segment = Held<32, 1024>;
 using FewOfRow = Held<8, 2048>;
-using SegmentOfRow = Held<32, 2048>;
+using SegmentOfRow = Held<16, 2048>;      // (more waves than the segment's own workgroup)
 constexpr int kRowThreads = kFew / 8;
+static_assert(kSegColumns <= 16 * kRowThreads, "a segment in a row's workgroup");
 static_assert(kSegMax <= kSegThreads && kSegMax <= kRowThreads && kRowThreads == kSampleThreads, "a thread a segment");
 
 struct SegStat {
@@ -1908,15 +1914,22 @@ __global__ __launch_bounds__(kRowThreads) void k_long_rows(LongArgs<T> a) {
             draw_held(few, column, want, ask, r, a.index, a.log);
         }
     } else if (kind == kRowShare) {
-        for (int i = threadIdx.x; i < SegmentOfRow::kBins; i += kRowThreads) {
-            uint64_t s = 0;
-            if (i < Segment::kBins) {
-                const uint64_t* bin = w.bins + (int64_t)b * w.segments * Segment::kBins + i;
-#pragma unroll 16
-                for (uint32_t seg = 0; seg < w.segments; ++seg) s += bin[(int64_t)seg * Segment::kBins];
-            }
-            sh->held.bin[i] = s;
+        // the segments' histograms: two bins a thread, every second segment
+        for (int i = threadIdx.x; i < SegmentOfRow::kBins; i += kRowThreads) sh->held.bin[i] = 0;
+        h.sync();
+        constexpr uint32_t kHalf = Segment::kBins / 2;
+        static_assert(kRowThreads == 2 * kHalf, "two bins a thread");
+        const uint32_t i = threadIdx.x % kHalf;
+        const ulonglong2* two = (const ulonglong2*)(w.bins + (int64_t)b * w.segments * Segment::kBins) + i;
+        uint64_t s0 = 0, s1 = 0;
+#pragma unroll 10
+        for (uint32_t seg = threadIdx.x / kHalf; seg < w.segments; seg += 2) {
+            const ulonglong2 v = two[(int64_t)seg * kHalf];
+            s0 += v.x;
+            s1 += v.y;
         }
+        if (s0) atomicAdd((unsigned long long*)&sh->held.bin[2 * i], (unsigned long long)s0);
+        if (s1) atomicAdd((unsigned long long*)&sh->held.bin[2 * i + 1], (unsigned long long)s1);
         h.search_bins([&](uint64_t total) {
             const uint64_t goal = share_of(total, want.part());
             plan.goal = goal < 1 ? 1 : goal;
