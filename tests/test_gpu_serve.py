@@ -612,3 +612,22 @@ def test_refusals(ctx):
     c.close()
     with pytest.raises(ValueError):
         serve.als_quantize(c, x)
+
+
+def test_recommend_command():
+    """The command's run on the tiny workload: every user gets an item it has not rated, within the best 50 of the
+    8-bit scores, the same on every run."""
+    import synth
+    from paper_1603_03820_amd import recommend
+    p = synth.config("tiny")
+    log("train and recommend, tiny workload")
+    rmse, items, lg, _ = recommend.run("tiny", iters=3, batch=300)
+    assert len(rmse) == 3 and rmse[2] < rmse[0]
+    items = items.cpu().numpy()
+    assert items.shape == (p.m,) and items.min() >= 0 and items.max() < p.n
+    assert bool((lg <= 0).all()) and bool((lg >= -np.log(50) - 20).all())
+    for u in range(p.m):
+        assert items[u] not in p.colidx[p.rowptr[u]:p.rowptr[u + 1]]
+    log("and with other batches")
+    _, again, lg2, _ = recommend.run("tiny", iters=3, batch=1000)
+    assert np.array_equal(items, again.cpu().numpy()) and torch.equal(lg, lg2)
