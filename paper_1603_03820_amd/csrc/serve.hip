@@ -814,19 +814,17 @@ struct Held {
                 uint32_t p = position(8 * h);
 #pragma nounroll
                 for (int v = 0; open && v < (K < 32 ? K : 32); v += 4, p += 4 * kWave) {
-                    uint64_t w[4], s = 0;
+                    uint64_t s = 0;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        w[c] = whole_of(measure(z[h][v + c], p + c));
-                        s += w[c];
-                    }
+                    for (int c = 0; c < 4; ++c) s += whole_of(measure(z[h][v + c], p + c));
                     const uint64_t upto = scan64(s), all = last64(upto);
                     if (left < all) {
                         uint64_t at = upto - s;
-#pragma unroll
+#pragma nounroll
                         for (int c = 0; c < 4; ++c) {
-                            if (left >= at && left < at + w[c]) sh->cut_position = p + c;
-                            at += w[c];
+                            const uint64_t w = whole_of(measure(z[h][v + c], p + c));
+                            if (left >= at && left < at + w) sh->cut_position = p + c;
+                            at += w;
                         }
                         open = false;
                     } else {
