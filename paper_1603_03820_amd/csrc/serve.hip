@@ -1,8 +1,17 @@
 // Answering with a trained factor model on gfx950 (MI355X): the C ABI of include/als_serve.h plus its kernels.
 //
-//   k_quantize   rows to 8-bit integers with one scale a row
-//   k_score      scores of users against items from 8-bit rows (integer matrix instructions)
-//   k_sample     one column a row from its scores: temperature, top-k, top-p, min-p, columns left out
+//   k_quantize    rows to 8-bit integers with one scale a row (k_quantize_long: rows of over 8,192 fp32 values)
+//   k_score_tiles scores of users against items from 8-bit rows, by integer matrix instructions on tiles in LDS
+//                 (k_pack lays rows of other strides out for it; k_score takes what the workspace does not hold)
+//   k_sample      one column a row from its scores: temperature, top-k, top-p, min-p, columns left out; a workgroup a
+//                 row, which stays in registers
+//   k_long_*      the same for rows past 65,536 columns, in segments
+//
+// The draw's arithmetic: a weight is a whole number, 2^40 times the exponential rounded down, and sums of
+// weights are 64-bit integers.  So every sum is exact and may be taken in any order, by any number of threads and by
+// atomics, and the set that top-p keeps and the column that a uniform number meets do not depend on how a row is
+// held.  The rounding down costs a column at most 2^-40 of the best one's weight.
+
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
@@ -113,7 +122,9 @@ __device__ __forceinline__ void store_row(int8_t* row, int k, int end, const Row
 }
 
 // G lanes a row (or, G = 256, a workgroup), 16 bytes a lane and load, E loads, all of which stay in registers between
-// the largest magnitude and the quotients: each row is read once.
+// the largest magnitude and the quotients: each row is read once.  Bound by memory: 625,000 x 100 fp32 in 61 us
+// (5.1 TB/s), 8,192 x 8,192 bf16 in 46 us (4.3 TB/s); in 16 bits, short rows by their conversions and quotients
+// (625,000 x 100 bf16 in 66 us, 2.9 TB/s).
 template <typename T, int G, int E>
 __global__ __launch_bounds__(kQuantThreads) void k_quantize(const T* __restrict__ x, int64_t of, int64_t ldx,
                                                             const int32_t* __restrict__ users, int64_t rows,
@@ -239,6 +250,13 @@ __global__ __launch_bounds__(kScoreThreads) void k_score(const int8_t* __restric
 // one operand read spread over all banks: s is r / 2 % 8 where an operand's rows are neighbours.  For
 // outputs of 16 bits an item operand takes rows 0..3 of every 8 of 32, or 4..7 (so that a lane's four items of two
 // fragments are neighbours and go out as 16 bytes), and s is r / 2 % 2 + 2 (r / 8 % 4).
+// v_mfma_i32_16x16x64_i8 with the items as the first operand: a lane holds four neighbouring items of one user.  Items
+// and users past the end, and values past f, are multiplied too: their results are not written, or one side is 0.
+// 8,192^3 in 437 us, 2.5 Pop/s (a 256 x 256 tile reads 64 KB of LDS and 16 KB of memory for 16.8 Mop; matrix
+// instructions at the clock that they leave bound it).  At f <= 128 the scores' way out bounds it: 1,024 x 17,770 to fp32
+// in 16.5 us (4.4 TB/s), 4,096 x 40,000 in 150 us (4.4 TB/s; a kernel that only writes so takes 125), to bf16 in
+// 90 to 111 us (3.0 to 3.6 TB/s).  Few users and wide rows are bound by the items' bytes: 5 x 8,192 x 8,192 in 14.8 us
+// (4.5 TB/s).
 constexpr int kStep = 128;
 constexpr int64_t kTileStride = 1 << 22;        // row strides below it keep a tile's offsets below 2^30 ...
 constexpr uint32_t kPastEnd = 0x7FFFFFF0u;      // ... and this past every tile's end
@@ -274,8 +292,11 @@ __device__ __forceinline__ void load_to_lds(i4 buffer, uint32_t voffset, uint32_
     asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
                  :
                  : "v"(voffset), "s"(buffer), "s"(soffset), "s"(lds)
-                 : "memory");
+                 : "memory", "m0");
 }
+// A load reads a scalar register that a vector instruction wrote (readfirstlane) no sooner than five wait states
+// later; the compiler keeps them for the loads it knows.
+__device__ __forceinline__ void buffer_settle(i4 a, i4 b) { asm volatile("s_nop 4" : : "s"(a), "s"(b)); }
 // All of this wave's loads but the last LEFT have arrived, and its LDS reads are done.
 template <int LEFT>
 __device__ __forceinline__ void settle() {
@@ -322,6 +343,7 @@ __global__ __launch_bounds__(64 * WU * WI) void k_score_tiles(
     const int whole = (f + 15) / 16 * 16;
     const i4 from_u = buffer_of(xq + u0 * ldx, (uint32_t)((users - 1) * ldx + whole));
     const i4 from_i = buffer_of(tq + i0 * ldt, (uint32_t)((items - 1) * ldt + whole));
+    buffer_settle(from_u, from_i);
     const int first_u = wave * C::kUserLoads * 8, first_i = wave * C::kItemLoads * 8;   // this wave's rows
     const auto spread_u = [](int r) { return r >> 1 & 7; };
     const auto spread_i = [](int r) { return kPairs ? (r >> 1 & 1) | (r >> 3 & 3) << 1 : r >> 1 & 7; };
@@ -524,15 +546,6 @@ __device__ __forceinline__ uint64_t scan64(uint64_t v) {
     v += dpp64<0x118, 0xF>(v);
     v += dpp64<0x142, 0xA>(v);   // row_bcast:15 into rows 1 and 3
     v += dpp64<0x143, 0xC>(v);   // row_bcast:31 into rows 2 and 3
-    return v;
-}
-__device__ __forceinline__ uint32_t scan32(uint32_t v) {
-    v += dpp32<0x111, 0xF>(v);
-    v += dpp32<0x112, 0xF>(v);
-    v += dpp32<0x114, 0xF>(v);
-    v += dpp32<0x118, 0xF>(v);
-    v += dpp32<0x142, 0xA>(v);
-    v += dpp32<0x143, 0xC>(v);
     return v;
 }
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
@@ -1126,8 +1139,8 @@ __device__ __forceinline__ void fetch_columns(const H& h, const T* row, uint32_t
     }
 }
 
-// The fetched columns without those on the row's list (a NaN stays: no comparison holds for it); `bits` is LDS, one a column.  `there`: the
-// row's user exists.  (Between fetch and here, a kernel finds out what to do with them.)
+// The fetched columns without those on the row's list (a NaN stays: no comparison holds for it); `bits` is LDS, one
+// a column.  `there`: the row's user exists.  (Between fetch and here, a kernel finds out what to do with them.)
 template <typename H, typename T>
 __device__ __forceinline__ void take_columns(H& h, const Four<T> (&raw)[H::kScores / 4], uint32_t base, uint32_t n,
                                              const Rated& rated, int64_t r, uint32_t* bits, bool* there) {
@@ -1218,11 +1231,14 @@ __device__ __forceinline__ void draw_listed(Few few, Shared* sh, uint32_t count,
     draw_held(few, column, want, ask, r, index, log);
 }
 
-// A workgroup a row, the row in registers from its one read on.
+// A workgroup a row, the row in registers from its one read on.  1,024 x 17,770 fp32 scores (13.9 us of reading), us:
+// the best column 21, temperature 44, top-k 200 48, with top-p 0.9 51, with 208 columns left out 58; top-p alone 97.
+// Bound by vector instructions and by waits between a row's short passes: 15 instructions an exponential, about 30 a
+// score and pass that weighs all of them; four to five waves a SIMD.
 template <int K, int BINS, typename T>
-__global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 6 : 4)) void k_sample(const T* __restrict__ z, int64_t rows, uint32_t n, int64_t ldz,
-                                                 Limits lim, const float* __restrict__ u, Rated rated,
-                                                 int32_t* __restrict__ index, float* __restrict__ log) {
+__global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 6 : 4)) void k_sample(
+    const T* __restrict__ z, int64_t rows, uint32_t n, int64_t ldz, Limits lim, const float* __restrict__ u, Rated rated,
+    int32_t* __restrict__ index, float* __restrict__ log) {
     using H = Held<K, BINS>;
     extern __shared__ __align__(16) unsigned char shared[];
     H h;
@@ -1489,8 +1505,7 @@ __device__ LongCut select_cut(Row<T>& row, LongCut within, uint32_t widest, uint
 // Rows that no workgroup's registers hold, in segments of 16,384 columns, a workgroup each; what the segments find
 // out goes through the workspace from one kernel to the next, and each kernel reads the scores again
 // (from the cache that all dies share, where they fit it):
-//   k_long_stats  a segment's best and least score and number of allowed columns, and the best scores of groups of its
-//                 columns
+//   k_long_stats  a segment's best and (nearly) least score, and the best scores of groups of its columns
 //   k_long_parts  top-k: the segment's columns with a score that k groups' best ones reach; top-p: a histogram of
 //                 weights over the row's scores; neither: the segment's weight
 //   k_long_rows   a workgroup a row.  top-k: the draw, among what the segments listed; top-p: the bin in which the cut
@@ -1499,6 +1514,8 @@ __device__ LongCut select_cut(Row<T>& row, LongCut within, uint32_t widest, uint
 //   k_long_draw   top-p: the cut, by ranking the listed columns, and the draw
 // Rows whose lists do not hold what they should (equal scores without end, a top_k of more than 7/8 of the groups)
 // are drawn by the last of these kernels alone, which reads the row again for every pass (sample_slowly).
+// 64 x 625,000 bf16 scores (15.3 us of reading), us: the best column 33, temperature 61, top-k 200 64, top-p 0.9 131, by
+// kernel 19 (memory), 44 (vector instructions: a weight a score), 13 (a workgroup a row: waits), 36 and 35 (waits).
 constexpr int kSegWaves = 8, kSegThreads = kSegWaves * kWave, kSegColumns = kSegThreads * 32;
 constexpr int kSegMax = ALS_SERVE_N_MAX / kSegColumns;
 constexpr int kSlab = 2048;              // columns a segment lists
@@ -2186,7 +2203,7 @@ bool launch_tiles(const ScoreArgs& a) {
 //   512 x 512 x 4,096          64 x 128: 14.9    64 x 64: 10.8     16 x 64: 8.9
 //   5 x 8,192 x 8,192          64 x 128: 35      64 x 64: 18       16 x 64: 15
 // Up to f = 128 there is one step and the scores' way out counts: 4,096 x 40,000 x 128 to fp32 in 150 us by 128 x 128
-// tiles and 170 by 64 x 128; to 16 bits in 86 by 32 x 256 (half a line of memory a user and wave), 100 and 110.
+// tiles and 170 by 64 x 128; to 16 bits in 90 to 111 by 32 x 256, 100 and 110 by those.
 template <typename T>
 bool score_tiles(const ScoreArgs& a, int cus) {
     const auto tiles = [&](int64_t users, int64_t items) {

@@ -48,6 +48,71 @@ def test_device_code_shape():
     assert re.search(r"v_mfma_i32_\w+_i8", text)
 
 
+def _sgprs(token):
+    m = re.match(r"s\[(\d+):(\d+)\]$", token) or re.match(r"s(\d+)()$", token)
+    return set(range(int(m.group(1)), int(m.group(2) or m.group(1)) + 1)) if m else set()
+
+
+def lds_load_violations(text):
+    """Loads to LDS (which are inline assembly, so the compiler keeps no wait states for them) that read a scalar
+    register less than five wait states after a vector instruction wrote it, or M0 less than one after its write."""
+    bad, hist = [], []
+    for line in text.splitlines():
+        t = line.split("//")[0].strip()
+        if t.endswith(">:"):
+            hist = []
+            continue
+        if not t or t.endswith(":"):
+            continue
+        op = t.split()[0]
+        args = [a.strip().split()[0] for a in t[len(op):].split(",") if a.strip()]
+        if op == "s_nop":
+            hist.append((op, set(), int(args[0], 0) + 1))
+            continue
+        if op.startswith("buffer_load") and t.split()[-1] == "lds":
+            reads = set().union(*(_sgprs(a) for a in args))
+            states = 0
+            for prior, written, n in reversed(hist):
+                if (states < 5 and prior.startswith("v_") and written & reads) or (states < 1 and "m0" in written):
+                    bad.append(t)
+                    break
+                states += n
+        written = set()
+        if args and op.startswith(("v_", "s_")):
+            written = {"m0"} if args[0] == "m0" else _sgprs(args[0])
+            if op.startswith("v_cmp") or op.startswith("v_add_co") or len(args) > 1 and op.startswith("v_div_scale"):
+                written |= _sgprs(args[min(1, len(args) - 1)])
+        hist = (hist + [(op, written, 1)])[-8:]
+    return bad
+
+
+def test_loads_to_lds_settled():
+    """The wait states of the loads to LDS, and that the check catches planted violations."""
+    if not os.path.exists("/opt/rocm/llvm/bin/clang-offload-bundler"):
+        pytest.skip("ROCm LLVM tools not installed")
+    from paper_1603_03820_amd import build
+    planted = ("<k>:\n\tv_readfirstlane_b32 s9, v1\n\ts_mov_b32 m0, s4\n\ts_nop {}\n"
+               "\tbuffer_load_dwordx4 v0, s[8:11], s3 offen lds\n")
+    assert len(lds_load_violations(planted.format(2))) == 1
+    assert lds_load_violations(planted.format(3)) == []
+    assert len(lds_load_violations(planted.replace("s9", "s3").format(0))) == 1
+    assert len(lds_load_violations("<k>:\n\ts_mov_b32 m0, s4\n\tbuffer_load_dwordx4 v0, s[8:11], s3 offen lds\n")) == 1
+    text = _device_disassembly(build.SERVE_LIB)
+    assert len(re.findall(r"buffer_load_dwordx4 .* lds", text)) > 50
+    assert lds_load_violations(text) == []
+
+
+def test_inline_assembly_has_no_result_in_flight():
+    """The library's inline assembly writes no register (loads go to LDS), so nothing can be overwritten by a
+    load on its way."""
+    source = open(os.path.join(ROOT, "paper_1603_03820_amd", "csrc", "serve.hip")).read()
+    blocks = re.findall(r"\basm volatile\((.*?)\);", source, flags=re.S)
+    assert blocks
+    for b in blocks:
+        outputs = b.split(":")[1] if ":" in b else ""
+        assert "=" not in outputs and "+v" not in outputs, b
+
+
 def test_refusals_without_a_device():
     """Null contexts and a device that does not exist."""
     from paper_1603_03820_amd import serve
