@@ -51,8 +51,9 @@ int als_serve_last_hip_error(const als_serve_ctx* ctx);
  * Rows of x as 8-bit integers with one scale each:
  *   a = max_k |x_uk|,   q_uk = rint(127 x_uk / a),   scale_u = a (1 / 127)     (so x_uk ~ scale_u q_uk)
  * 127 x and its quotient by a are each rounded to fp32, the quotient then to the nearest integer, ties to
- * even; 1 / 127 and its product with a are rounded to fp32.  The result is the same on every run.  A row of zeros gets scale 0 and zeros.  A row with an
- * infinity or a NaN gets scale NaN and zeros, so that its scores are NaN.
+ * even; 1 / 127 and its product with a are rounded to fp32.  The result is the same on every run.  A row of
+ * zeros gets scale 0 and zeros.  A row with an infinity or a NaN gets scale NaN and zeros, so that its scores are
+ * NaN.
  *   x      : `of` rows of f values of type dtype, row stride ldx >= f
  *   users  : int32[rows], the rows of x to take (repeats allowed), or NULL: rows 0 .. rows - 1 (rows <= of).
  *            An entry outside [0, of) gives a row of scale NaN and zeros.
