@@ -2,7 +2,7 @@
 //
 //   k_quantize    rows to 8-bit integers with one scale a row (k_quantize_long: rows of over 8,192 fp32 values)
 //   k_score_tiles scores of users against items from 8-bit rows, by integer matrix instructions on tiles in LDS
-//                 (k_pack lays rows of other strides out for it; k_score takes what the workspace does not hold)
+//                 (k_pack lays rows of other strides and alignments out for it, in the workspace)
 //   k_sample      one column a row from its scores: temperature, top-k, top-p, min-p, columns left out; a workgroup a
 //                 row, which stays in registers
 //   k_long_*      the same for rows past 65,536 columns, in segments
@@ -202,45 +202,6 @@ __device__ __forceinline__ i4 load16(const int8_t* row, int k, int f) {
         v = i4{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
     }
     return v;
-}
-
-constexpr int kScoreThreads = 256;
-constexpr int kScoreTiles = 4;                                   // 16-item tiles of a wave
-constexpr int kScoreItems = 16 * kScoreTiles * (kScoreThreads / kWave);
-
-// A wave: 16 users x 64 items by v_mfma_i32_16x16x64_i8, the items as the first operand, so that a lane
-// holds four neighbouring items of one user (C layout: column l & 15, rows 4 (l >> 4) + r).
-template <typename T>
-__global__ __launch_bounds__(kScoreThreads) void k_score(const int8_t* __restrict__ xq, int64_t ldx,
-                                                         const float* __restrict__ xs, int64_t m,
-                                                         const int8_t* __restrict__ tq, int64_t ldt,
-                                                         const float* __restrict__ ts, int64_t n, int f,
-                                                         T* __restrict__ out, int64_t ldo, int64_t item_blocks) {
-    const int lane = threadIdx.x & (kWave - 1);
-    const int64_t i0 = (int64_t)blockIdx.x / item_blocks * 16;
-    const int64_t j0 = (int64_t)blockIdx.x % item_blocks * kScoreItems + (threadIdx.x >> 6) * (16 * kScoreTiles);
-    const int64_t i = i0 + (lane & 15);
-    i4 acc[kScoreTiles];
-#pragma unroll
-    for (int t = 0; t < kScoreTiles; ++t) acc[t] = i4{0, 0, 0, 0};
-    for (int k = 16 * (lane >> 4); k < (f + 63) / 64 * 64; k += 64) {
-        const i4 b = i < m ? load16(xq + i * ldx, k, f) : i4{0, 0, 0, 0};
-#pragma unroll
-        for (int t = 0; t < kScoreTiles; ++t) {
-            const int64_t j = j0 + 16 * t + (lane & 15);
-            const i4 a = j < n ? load16(tq + j * ldt, k, f) : i4{0, 0, 0, 0};
-            acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, acc[t], 0, 0, 0);
-        }
-    }
-    if (i >= m) return;
-    const float s = xs[i];
-#pragma unroll
-    for (int t = 0; t < kScoreTiles; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int64_t j = j0 + 16 * t + 4 * (lane >> 4) + r;
-            if (j < n) from_float((float)acc[t][r] * s * ts[j], out + i * ldo + j);
-        }
 }
 
 // The product in tiles: a workgroup of WU x WI waves holds a tile of users x items, each wave FU x FI
@@ -2335,40 +2296,34 @@ int als_score(als_serve_ctx* ctx, const int8_t* xq, int64_t ldx, const float* xs
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return ALS_ERR_DEVICE;
     const hipStream_t st = (hipStream_t)stream;
-    // rows that a tile's loads cannot take are first laid out anew, where the workspace holds them
-    const int64_t whole = ((int64_t)f + 15) / 16 * 16;
+    // rows that a tile's loads cannot take are first laid out anew in the workspace, half of it for either side, as many
+    // at a time as it holds (512 at least)
+    const int64_t whole = ((int64_t)f + 15) / 16 * 16, half = (int64_t)(ctx->ws_bytes / 2), fit = half / whole;
     const auto direct = [](const int8_t* q, int64_t ld) { return aligned(q, 16) && ld % 16 == 0 && ld < kTileStride; };
-    const int64_t room = (int64_t)ctx->ws_bytes;
-    const auto need = [&](const int8_t* q, int64_t ld, int64_t rows) {
-        return direct(q, ld) ? 0 : (rows > room / whole ? room + 1 : rows * whole);
+    const bool x_direct = direct(xq, ldx), t_direct = direct(tq, ldt);
+    const int64_t users = x_direct || m < fit ? m : fit, items = t_direct || n < fit ? n : fit;
+    const auto pack = [&](const int8_t* q, int64_t ld, int64_t rows, unsigned char* to) {
+        const int64_t groups = whole / 16, blocks = (rows * groups + 255) / 256;
+        hipLaunchKernelGGL(k_pack, dim3((unsigned)blocks), dim3(256), 0, st, q, ld, rows, f, (int8_t*)to, groups);
+        return (const int8_t*)to;
     };
-    const int64_t x_need = need(xq, ldx, m), t_need = need(tq, ldt, n);
-    if (x_need + t_need <= room) {
-        const auto pack = [&](const int8_t*& q, int64_t& ld, int64_t rows, unsigned char* to) {
-            const int64_t groups = whole / 16, blocks = (rows * groups + 255) / 256;
-            hipLaunchKernelGGL(k_pack, dim3((unsigned)blocks), dim3(256), 0, st, q, ld, rows, f, (int8_t*)to, groups);
-            q = (const int8_t*)to;
-            ld = whole;
-        };
-        if (x_need) pack(xq, ldx, m, ctx->ws);
-        if (t_need) pack(tq, ldt, n, ctx->ws + x_need);
-        const ScoreArgs args{xq, ldx, xs, m, tq, ldt, ts, n, f, out, ldo, st, ctx->device};
-        bool ok = false;
-        if (dtype == ALS_F32) ok = score_tiles<float>(args, ctx->cus);
-        else if (dtype == ALS_F16) ok = score_tiles<F16>(args, ctx->cus);
-        else ok = score_tiles<BF16>(args, ctx->cus);
-        return ok ? finish(ctx) : ALS_ERR_INVALID_ARG;
+    for (int64_t i = 0; i < m; i += users) {
+        const int64_t mi = m - i < users ? m - i : users;
+        const int8_t* x = x_direct ? xq + i * ldx : pack(xq + i * ldx, ldx, mi, ctx->ws);
+        for (int64_t j = 0; j < n; j += items) {
+            const int64_t nj = n - j < items ? n - j : items;
+            const int8_t* t = (const int8_t*)(ctx->ws + half);
+            if (t_direct) t = tq + j * ldt;
+            else if (i == 0 || items < n) pack(tq + j * ldt, ldt, nj, ctx->ws + half);      // else all items are there
+            const ScoreArgs args{x, x_direct ? ldx : whole, xs + i, mi, t, t_direct ? ldt : whole, ts + j, nj, f,
+                                 (char*)out + (i * ldo + j) * type_bytes(dtype), ldo, st, ctx->device};
+            bool ok = false;
+            if (dtype == ALS_F32) ok = score_tiles<float>(args, ctx->cus);
+            else if (dtype == ALS_F16) ok = score_tiles<F16>(args, ctx->cus);
+            else ok = score_tiles<BF16>(args, ctx->cus);
+            if (!ok) return ALS_ERR_INVALID_ARG;
+        }
     }
-    const int64_t item_blocks = (n + kScoreItems - 1) / kScoreItems, user_blocks = (m + 15) / 16;
-    if (item_blocks > INT32_MAX / user_blocks) return ALS_ERR_INVALID_ARG;
-    const auto launch = [&](auto* p) {
-        using T = std::remove_pointer_t<decltype(p)>;
-        hipLaunchKernelGGL(k_score<T>, dim3((unsigned)(item_blocks * user_blocks)), dim3(kScoreThreads), 0,
-                           (hipStream_t)stream, xq, ldx, xs, m, tq, ldt, ts, n, f, p, ldo, item_blocks);
-    };
-    if (dtype == ALS_F32) launch((float*)out);
-    else if (dtype == ALS_F16) launch((F16*)out);
-    else launch((BF16*)out);
     return finish(ctx);
 }
 

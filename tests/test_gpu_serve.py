@@ -145,6 +145,34 @@ def test_score(ctx, dtype, m, n, f):
         assert bool((out[:, n:] == 9.0).all())
 
 
+@pytest.mark.parametrize("m,n,f", [(9, 260_000, 300), (260_000, 9, 300), (900, 1100, 100_003)])
+def test_score_of_odd_strides_past_the_workspace(ctx, m, n, f):
+    """Rows that are laid out anew, more of them than the workspace holds at a time."""
+    from paper_1603_03820_amd import serve
+    assert max(m, n) * f > ctx.workspace.numel() // 2
+    g = torch.Generator("cuda:0").manual_seed(m)
+    xq = torch.randint(-128, 128, (m, f + 1), dtype=torch.int8, device="cuda:0", generator=g)[:, 1:]
+    tq = torch.randint(-128, 128, (n, f + 3), dtype=torch.int8, device="cuda:0", generator=g)[:, :f]
+    xs, ts = torch.rand(m, device="cuda:0", generator=g), torch.rand(n, device="cuda:0", generator=g)
+    log(f"score of odd strides, m {m} n {n} f {f}")
+    out = serve.als_score(ctx, xq, xs, tq, ts)
+    # a sample of users and items, the ends of the parts among them
+    part = ctx.workspace.numel() // 2 // ((f + 15) // 16 * 16)
+    pick = lambda k: sorted({0, k - 1, k // 2} | {c for c in (part - 1, part, 2 * part) if 0 <= c < k})  # noqa: E731
+    us, it = pick(m), pick(n)
+    exact = serve_oracle.score(xq[us].cpu().numpy(), xs[us].cpu().numpy(), tq[it].cpu().numpy(), ts[it].cpu().numpy())
+    assert np.all(np.abs(f64(out[us][:, it]) - exact) <= serve_oracle.score_bound(exact, "f32"))
+    a = serve.als_score(ctx, *serve_aligned(xq, xs), *serve_aligned(tq, ts))
+    assert torch.equal(a, out)
+
+
+def serve_aligned(q, s):
+    rows, f = q.shape
+    wide = torch.zeros(rows, (f + 15) // 16 * 16, dtype=torch.int8, device=q.device)
+    wide[:, :f] = q
+    return wide[:, :f], s
+
+
 def test_score_sums_at_their_limit(ctx):
     """128^2 times the longest row stays exact."""
     from paper_1603_03820_amd import serve
