@@ -248,12 +248,13 @@ __device__ __forceinline__ i4 buffer_of(const void* base, uint32_t bytes) {
 
 // 16 bytes a lane from buffer + voffset + soffset to LDS at `lds` + 16 lane.  Inline assembly: the compiler would
 // wait for every load to LDS before any LDS read.  It has no result register; the caller waits
-// (settle) before the data are read.  M0 needs one wait state.
+// (settle) before the data are read.  M0 needs one wait state.  (M0 is reserved and cannot be named as clobbered: a
+// kernel with these loads must have nothing else that reads or keeps it, such as registers picked by an index.)
 __device__ __forceinline__ void load_to_lds(i4 buffer, uint32_t voffset, uint32_t soffset, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
                  :
                  : "v"(voffset), "s"(buffer), "s"(soffset), "s"(lds)
-                 : "memory", "m0");
+                 : "memory");
 }
 // A load reads a scalar register that a vector instruction wrote (readfirstlane) no sooner than five wait states
 // later; the compiler keeps them for the loads it knows.

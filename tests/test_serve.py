@@ -102,6 +102,20 @@ def test_loads_to_lds_settled():
     assert lds_load_violations(text) == []
 
 
+def test_loads_to_lds_have_m0_to_themselves():
+    """Kernels with loads to LDS use M0 for nothing else (the compiler does not know that they write it)."""
+    if not os.path.exists("/opt/rocm/llvm/bin/clang-offload-bundler"):
+        pytest.skip("ROCm LLVM tools not installed")
+    from paper_1603_03820_amd import build
+    kernels = re.split(r"\n(?=[0-9a-f]+ <)", _device_disassembly(build.SERVE_LIB))
+    loading = [k for k in kernels if re.search(r"buffer_load_dwordx4 .* lds", k)]
+    assert len(loading) == 18       # six shapes of tiles, three types
+    for k in loading:
+        assert not re.search(r"gpr_idx|v_movrel|s_movrel|s_sendmsg\b", k)
+        uses = [line.split("//")[0].strip() for line in k.splitlines() if re.search(r"\bm0\b", line.split("//")[0])]
+        assert uses and all(u.startswith("s_mov_b32 m0,") for u in uses), set(uses)
+
+
 def test_inline_assembly_has_no_result_in_flight():
     """The library's inline assembly writes no register (loads go to LDS), so nothing can be overwritten by a
     load on its way."""
