@@ -2371,14 +2371,20 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
     };
     const auto launch = [&](auto* p) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
-        // As few waves as hold the row, up to 1,024 columns one (which needs no barrier); then 8 or 16 scores a thread,
-        // so that a row's passes are short, and 32 where there are rows enough for every CU.  Top-k 200, top-p 0.9
-        // and left-out columns, us: 2,000 x 8,000 8 a thread 83, 16 48, 32 89; 1 x 16,000 16 20.5, 32 20.6, by top-p
-        // alone 21 and 28; 2,000 x 16,000 16 108, 32 68.
-        if (n <= 512) return held(Held<8, 256>(), p);
-        if (n <= 1024) return held(Held<16, 256>(), p);
-        if (n <= 4096) return held(Held<8, 1024>(), p);
-        if (n <= 8192 || (n <= 16384 && rows <= ctx->cus)) return held(Held<16, 1024>(), p);
+        // Few rows: few scores a thread, as a row's passes are what is waited for.  More rows than CUs: more scores a
+        // thread and fewer waves, up to one, which needs no barrier.  Top-k 200, top-p 0.9 and left-out columns, us,
+        // by scores a thread: 1 x 500 4 12.6, 8 15.6; 1 x 1,000 4 13, 16 19; 2,048 x 1,000 4 29, 16 25; 2,048 x 2,000 8
+        // 41, 16 31; 2,048 x 4,000 8 38, 16 49; 2,000 x 8,000 8 83, 16 48, 32 89; 1 x 16,000 by top-p alone 16 21, 32 28; 2,000 x 16,000 16 108, 32 68.
+        if (rows <= ctx->cus) {
+            if (n <= 1024) return held(Held<4, 256>(), p);
+            if (n <= 4096) return held(Held<8, 1024>(), p);
+            if (n <= 16384) return held(Held<16, 1024>(), p);
+        } else {
+            if (n <= 512) return held(Held<8, 256>(), p);
+            if (n <= 2048) return held(Held<16, 512>(), p);
+            if (n <= 4096) return held(Held<8, 1024>(), p);     // (enough threads for a top-k of some hundreds)
+            if (n <= 8192) return held(Held<16, 1024>(), p);
+        }
         if (n <= 32768) return held(Held<32, 2048>(), p);
         if (n <= 65536) return held(Held<64, 4096>(), p);
         // in batches of as many rows as the workspace holds

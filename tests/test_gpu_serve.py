@@ -298,7 +298,7 @@ def test_sample_longest_and_between(ctx, n):
             draw_rows(ctx, zz, [0.3, 0.97], rated=(np.array([0, 300, 300]), idx), **limits)
 
 
-@pytest.mark.parametrize("rows,n", [(300, 9_000), (300, 16_000), (900, 100_003)])
+@pytest.mark.parametrize("rows,n", [(300, 400), (300, 1_000), (300, 3_000), (300, 9_000), (300, 16_000), (900, 100_003)])
 def test_sample_rows_alone_and_together(ctx, rows, n):
     """A row's draw does not depend on the rows beside it (how many there are chooses how they are held, and
     many long rows go through the workspace in batches)."""
