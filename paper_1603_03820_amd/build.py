@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -44,9 +45,10 @@ PEAKS_LIB = os.path.join(PKG, "libpeaks.so")
 def build(verbose: bool = False) -> str:
     """Compile libals.so, libals_serve.so and the bench's peak microbenchmarks (libpeaks.so) unconditionally
     (the build check compiles every time); return the libals.so path."""
-    _compile(PEAKS_SRC, PEAKS_LIB, verbose)
-    _compile(SERVE_SRC, SERVE_LIB, verbose)
-    return _compile(SRC, LIB, verbose)
+    with ThreadPoolExecutor(3) as pool:      # each waits for a compiler of its own
+        jobs = [pool.submit(_compile, src, lib, verbose)
+                for src, lib in ((PEAKS_SRC, PEAKS_LIB), (SERVE_SRC, SERVE_LIB), (SRC, LIB))]
+        return [j.result() for j in jobs][-1]
 
 
 def _compile(src: str, lib: str, verbose: bool) -> str:

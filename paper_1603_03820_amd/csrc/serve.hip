@@ -1481,12 +1481,12 @@ __device__ LongCut select_cut(Row<T>& row, LongCut within, uint32_t widest, uint
 constexpr int kSegWaves = 8, kSegThreads = kSegWaves * kWave, kSegColumns = kSegThreads * 32;
 constexpr int kSegMax = ALS_SERVE_N_MAX / kSegColumns;
 constexpr int kSlab = 2048;              // columns a segment lists
-constexpr int kFew = 8192;               // columns a row's workgroup takes from its lists
+constexpr int kFew = 16384;              // columns a row's workgroup takes from its lists
 constexpr int kGroups = 4096;            // most groups of a row
 using Segment = Held<32, 1024>;
-using FewOfRow = Held<8, 2048>;
+using FewOfRow = Held<16, 2048>;
 using SegmentOfRow = Held<16, 2048>;      // (more waves than the segment's own workgroup)
-constexpr int kRowThreads = kFew / 8;
+constexpr int kRowThreads = kFew / 16;
 static_assert(kSegColumns <= 16 * kRowThreads, "a segment in a row's workgroup");
 static_assert(kSegMax <= kSegThreads && kSegMax <= kRowThreads && kRowThreads == kSampleThreads, "a thread a segment");
 
@@ -1979,7 +1979,7 @@ __global__ __launch_bounds__(kSegThreads) void k_long_cut(LongArgs<T> a) {
 
 // The cut among the segments' listed columns (of the bin in which it falls), by the workgroup's first `waves` waves.
 template <typename Few, typename T>
-__device__ __forceinline__ void cut_listed(Few few, const LongArgs<T>& a, uint32_t b, const Wanted& want, const Asked& ask,
+__device__ __forceinline__ void cut_listed(Few few, const LongArgs<T>& a, uint32_t b, const Asked& ask,
                                            const RowPlan& plan, int waves, RowShared* sh) {
     few.sh = (typename Few::Shared*)&sh->held;
     few.threads = waves * kWave;
@@ -2006,7 +2006,8 @@ __device__ __forceinline__ void cut_listed(Few few, const LongArgs<T>& a, uint32
         if (place.keeps(k, at)) {
             const float e = ask.scaled(k);
             if (e >= ask.least)
-                atomicAdd((unsigned long long*)&sh->mass[column[i] / kSegColumns], (unsigned long long)whole_of(floorf(e)));
+                atomicAdd((unsigned long long*)&sh->mass[column[i] / kSegColumns],
+                          (unsigned long long)whole_of(floorf(e)));
         }
     }
 }
@@ -2036,9 +2037,9 @@ __global__ __launch_bounds__(kRowThreads) void k_long_draw(LongArgs<T> a) {
     // the cut, by column; what it keeps of the lists counts for its segments
     if (sh->first[w.segments] <= (uint32_t)SegmentOfRow::kList) {
         gather_lists(w, b, sh);
-        if (h.wave() == 0) cut_listed(Held<16, 256>(), a, b, want, ask, plan, 1, sh);
+        if (h.wave() == 0) cut_listed(Held<16, 256>(), a, b, ask, plan, 1, sh);
     } else {
-        cut_listed(FewOfRow(), a, b, want, ask, plan, h.waves, sh);
+        cut_listed(FewOfRow(), a, b, ask, plan, h.waves, sh);
     }
     h.sync();
     Cut cut;
@@ -2374,7 +2375,8 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
         // Few rows: few scores a thread, as a row's passes are what is waited for.  More rows than CUs: more scores a
         // thread and fewer waves, up to one, which needs no barrier.  Top-k 200, top-p 0.9 and left-out columns, us,
         // by scores a thread: 1 x 500 4 12.6, 8 15.6; 1 x 1,000 4 13, 16 19; 2,048 x 1,000 4 29, 16 25; 2,048 x 2,000 8
-        // 41, 16 31; 2,048 x 4,000 8 38, 16 49; 2,000 x 8,000 8 83, 16 48, 32 89; 1 x 16,000 by top-p alone 16 21, 32 28; 2,000 x 16,000 16 108, 32 68.
+        // 41, 16 31; 2,048 x 4,000 8 38, 16 49; 2,000 x 8,000 8 83, 16 48, 32 89; 1 x 16,000 by top-p alone 16 21, 32 28;
+        // 2,000 x 16,000 16 108, 32 68.
         if (rows <= ctx->cus) {
             if (n <= 1024) return held(Held<4, 256>(), p);
             if (n <= 4096) return held(Held<8, 1024>(), p);
