@@ -1199,7 +1199,7 @@ __device__ __forceinline__ void draw_listed(Few few, Shared* sh, uint32_t count,
 // score and pass that weighs all of them; four to five waves a SIMD.
 template <int K, int BINS, typename T>
 __global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 6 : 4)) void k_sample(
-    const T* __restrict__ z, int64_t rows, uint32_t n, int64_t ldz, Limits lim, const float* __restrict__ u, Rated rated,
+    const T* __restrict__ z, int64_t row0, uint32_t n, int64_t ldz, Limits lim, const float* __restrict__ u, Rated rated,
     int32_t* __restrict__ index, float* __restrict__ log) {
     using H = Held<K, BINS>;
     extern __shared__ __align__(16) unsigned char shared[];
@@ -1208,7 +1208,7 @@ __global__ __launch_bounds__(1024, K <= 8 ? 8 : (K <= 32 ? 6 : 4)) void k_sample
     h.threads = blockDim.x;
     h.waves = blockDim.x / kWave;
     uint32_t* bits = (uint32_t*)(shared + sizeof(typename H::Shared));   // the columns left out, one bit each
-    const int64_t r = blockIdx.x;
+    const int64_t r = row0 + blockIdx.x;
     bool there;
     Four<T> raw[K / 4];
     fetch_columns(h, z + r * ldz, 0, n, raw);
@@ -2104,7 +2104,7 @@ int query_device(int device, int* cus) {
     return ALS_OK;
 }
 
-constexpr size_t kWorkspaceBytes = 128u << 20;
+constexpr size_t kWorkspaceBytes = 128u << 20, kWorkspaceMost = (size_t)1 << 34;   // (what a launch can walk)
 
 }  // namespace
 
@@ -2126,6 +2126,14 @@ void whole_lds(Kernel kernel, int device, std::atomic<uint64_t>* done) {
         done->fetch_or(1ull << device, std::memory_order_release);
 }
 
+// A launch counts its threads in 32 bits: one of 2^32 or more fails or, worse, runs only what is left of the count and
+// reports nothing.  fn(first, count) for parts of `total` rows, `most` at a time.
+constexpr int64_t kMaxThreads = UINT32_MAX;
+template <typename Fn>
+void in_parts(int64_t total, int64_t most, Fn fn) {
+    for (int64_t first = 0; first < total; first += most) fn(first, total - first < most ? total - first : most);
+}
+
 struct ScoreArgs {
     const int8_t* xq;
     int64_t ldx;
@@ -2143,18 +2151,16 @@ struct ScoreArgs {
 };
 
 template <typename T, int WU, int WI, int FU, int FI, int STAGES>
-bool launch_tiles(const ScoreArgs& a) {
+void launch_tiles(const ScoreArgs& a) {
     using C = Tiles<WU, WI, FU, FI, STAGES>;
     static std::atomic<uint64_t> done{0};
     auto* kernel = k_score_tiles<T, WU, WI, FU, FI, STAGES>;
     const int64_t tu = (a.m + C::kUsers - 1) / C::kUsers, ti = (a.n + C::kItems - 1) / C::kItems;
-    if (tu > INT32_MAX / ti) return false;
     const int steps = (a.f + kStep - 1) / kStep;
     whole_lds(kernel, a.device, &done);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(tu * ti)), dim3(64 * C::kWaves),
                        (steps < STAGES ? steps : STAGES) * C::kStage, a.stream, a.xq, a.ldx, a.xs, a.m, a.tq, a.ldt,
                        a.ts, a.n, a.f, (T*)a.out, a.ldo, (uint32_t)tu, (uint32_t)ti);
-    return true;
 }
 
 // The tile: the largest that still gives every CU enough of them.  A large tile reads the rows fewer times, which
@@ -2168,7 +2174,7 @@ bool launch_tiles(const ScoreArgs& a) {
 // Up to f = 128 there is one step and the scores' way out counts: 4,096 x 40,000 x 128 to fp32 in 150 us by 128 x 128
 // tiles and 170 by 64 x 128; to 16 bits in 90 to 111 by 32 x 256, 100 and 110 by those.
 template <typename T>
-bool score_tiles(const ScoreArgs& a, int cus) {
+void score_tiles(const ScoreArgs& a, int cus) {
     const auto tiles = [&](int64_t users, int64_t items) {
         return ((a.m + users - 1) / users) * ((a.n + items - 1) / items);
     };
@@ -2215,7 +2221,7 @@ int als_serve_init(als_serve_ctx** out, int device, void* workspace, size_t work
     ctx->device = device;
     ctx->cus = cus;
     ctx->ws = (unsigned char*)workspace;
-    ctx->ws_bytes = workspace_bytes;
+    ctx->ws_bytes = workspace_bytes < kWorkspaceMost ? workspace_bytes : kWorkspaceMost;
     ctx->last_hip = 0;
     *out = ctx;
     return ALS_OK;
@@ -2244,42 +2250,42 @@ int als_quantize(als_serve_ctx* ctx, const void* x, int32_t dtype, int64_t of, i
         return ALS_ERR_ALIAS;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return ALS_ERR_DEVICE;
+    // kernel(x, of, users, rows, q, scale) for parts of the rows, a workgroup taking `per` of them
+    const auto rows_by = [&](auto* p, int64_t per, auto kernel) {
+        in_parts(rows, kMaxThreads / kQuantThreads * per, [&](int64_t r, int64_t some) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((some + per - 1) / per)), dim3(kQuantThreads), 0,
+                               (hipStream_t)stream, users ? p : p + r * ldx, users ? of : of - r, ldx,
+                               users ? users + r : users, some, f, q + r * ldq, ldq, scale + r);
+        });
+    };
     const auto go = [&](auto* p, auto lanes, auto loads) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
         constexpr int G = decltype(lanes)::value, E = decltype(loads)::value;
-        const int64_t per = kQuantThreads / G, blocks = (rows + per - 1) / per;
-        if (blocks > INT32_MAX) return false;
-        hipLaunchKernelGGL((k_quantize<T, G, E>), dim3((unsigned)blocks), dim3(kQuantThreads), 0,
-                           (hipStream_t)stream, p, of, ldx, users, rows, f, q, ldq, scale);
-        return true;
+        rows_by(p, kQuantThreads / G, k_quantize<T, G, E>);
     };
     // Two loads a lane and the fewest lanes that hold the row so, up to a wave; then more loads, then a workgroup.
     // 625,000 x 100 fp32: 16 lanes of 2 loads 61 us, 8 of 4 65, 32 of 1 100, 32 of 2 94 (half the lanes idle);
     // 200,000 x 256: 32 of 2 44, 16 of 4 49, 64 of 1 56; 1,000,000 x 16: 4 of 2 17, 8 of 1 30, 16 of 1 58.
-    bool ok = true;
     const auto launch = [&](auto* p) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
         using std::integral_constant;
         using Two = integral_constant<int, 2>;
         const int groups = (int)((pad + 16 / sizeof(T) - 1) / (16 / sizeof(T)));      // loads of a row
-        if (groups <= 8) ok = go(p, integral_constant<int, 4>(), Two());
-        else if (groups <= 16) ok = go(p, integral_constant<int, 8>(), Two());
-        else if (groups <= 32) ok = go(p, integral_constant<int, 16>(), Two());
-        else if (groups <= 64) ok = go(p, integral_constant<int, 32>(), Two());
-        else if (groups <= 128) ok = go(p, integral_constant<int, 64>(), Two());
-        else if (groups <= 256) ok = go(p, integral_constant<int, 64>(), integral_constant<int, 4>());
-        else if (groups <= 512) ok = go(p, integral_constant<int, 256>(), Two());
-        else if (groups <= 1024) ok = go(p, integral_constant<int, 256>(), integral_constant<int, 4>());
-        else if (groups <= 2048) ok = go(p, integral_constant<int, 256>(), integral_constant<int, 8>());
-        else if (rows > INT32_MAX) ok = false;
-        else
-            hipLaunchKernelGGL(k_quantize_long<T>, dim3((unsigned)rows), dim3(kQuantThreads), 0, (hipStream_t)stream,
-                               p, of, ldx, users, rows, f, q, ldq, scale);
+        if (groups <= 8) go(p, integral_constant<int, 4>(), Two());
+        else if (groups <= 16) go(p, integral_constant<int, 8>(), Two());
+        else if (groups <= 32) go(p, integral_constant<int, 16>(), Two());
+        else if (groups <= 64) go(p, integral_constant<int, 32>(), Two());
+        else if (groups <= 128) go(p, integral_constant<int, 64>(), Two());
+        else if (groups <= 256) go(p, integral_constant<int, 64>(), integral_constant<int, 4>());
+        else if (groups <= 512) go(p, integral_constant<int, 256>(), Two());
+        else if (groups <= 1024) go(p, integral_constant<int, 256>(), integral_constant<int, 4>());
+        else if (groups <= 2048) go(p, integral_constant<int, 256>(), integral_constant<int, 8>());
+        else rows_by(p, 1, k_quantize_long<T>);
     };
     if (dtype == ALS_F32) launch((const float*)x);
     else if (dtype == ALS_F16) launch((const F16*)x);
     else launch((const BF16*)x);
-    return ok ? finish(ctx) : ALS_ERR_INVALID_ARG;
+    return finish(ctx);
 }
 
 int als_score(als_serve_ctx* ctx, const int8_t* xq, int64_t ldx, const float* xs, int64_t m, const int8_t* tq,
@@ -2303,7 +2309,15 @@ int als_score(als_serve_ctx* ctx, const int8_t* xq, int64_t ldx, const float* xs
     const int64_t whole = ((int64_t)f + 15) / 16 * 16, half = (int64_t)(ctx->ws_bytes / 2), fit = half / whole;
     const auto direct = [](const int8_t* q, int64_t ld) { return aligned(q, 16) && ld % 16 == 0 && ld < kTileStride; };
     const bool x_direct = direct(xq, ldx), t_direct = direct(tq, ldt);
-    const int64_t users = x_direct || m < fit ? m : fit, items = t_direct || n < fit ? n : fit;
+    int64_t users = x_direct || m < fit ? m : fit, items = t_direct || n < fit ? n : fit;
+    // no launch of more than 2^31 threads: the most a tile takes is 128 of them for 16 users and 64 items (half the
+    // limit: the larger tiles' last rows); the narrower side stays whole, and parts are whole tiles
+    const int64_t most = kMaxThreads / 128 / 2, tu = (users + 15) / 16, ti = (items + 63) / 64;
+    if (tu > most / ti) {
+        if (tu > 4096 && ti > 4096) items = 4096 * 64;
+        if (tu <= 4096) items = most / tu / 4 * 4 * 64;
+        else users = most / ((items + 63) / 64) / 16 * 16 * 16;
+    }
     const auto pack = [&](const int8_t* q, int64_t ld, int64_t rows, unsigned char* to) {
         const int64_t groups = whole / 16, blocks = (rows * groups + 255) / 256;
         hipLaunchKernelGGL(k_pack, dim3((unsigned)blocks), dim3(256), 0, st, q, ld, rows, f, (int8_t*)to, groups);
@@ -2319,11 +2333,9 @@ int als_score(als_serve_ctx* ctx, const int8_t* xq, int64_t ldx, const float* xs
             else if (i == 0 || items < n) pack(tq + j * ldt, ldt, nj, ctx->ws + half);      // else all items are there
             const ScoreArgs args{x, x_direct ? ldx : whole, xs + i, mi, t, t_direct ? ldt : whole, ts + j, nj, f,
                                  (char*)out + (i * ldo + j) * type_bytes(dtype), ldo, st, ctx->device};
-            bool ok = false;
-            if (dtype == ALS_F32) ok = score_tiles<float>(args, ctx->cus);
-            else if (dtype == ALS_F16) ok = score_tiles<F16>(args, ctx->cus);
-            else ok = score_tiles<BF16>(args, ctx->cus);
-            if (!ok) return ALS_ERR_INVALID_ARG;
+            if (dtype == ALS_F32) score_tiles<float>(args, ctx->cus);
+            else if (dtype == ALS_F16) score_tiles<F16>(args, ctx->cus);
+            else score_tiles<BF16>(args, ctx->cus);
         }
     }
     return finish(ctx);
@@ -2367,8 +2379,10 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
         static std::atomic<uint64_t> done{0};
         whole_lds(kernel, ctx->device, &done);
         const int64_t a_wave = kWave * H::kScores, waves = n < a_wave ? 1 : (n + a_wave - 1) / a_wave;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3((unsigned)(kWave * waves)), lds, (hipStream_t)stream, p,
-                           rows, (uint32_t)n, ldz, lim, u, rated, index, log);
+        in_parts(rows, kMaxThreads / (kWave * waves), [&](int64_t row0, int64_t some) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)some), dim3((unsigned)(kWave * waves)), lds, (hipStream_t)stream, p,
+                               row0, (uint32_t)n, ldz, lim, u, rated, index, log);
+        });
     };
     const auto launch = [&](auto* p) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(p)>>;
