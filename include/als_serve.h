@@ -58,13 +58,22 @@ int als_serve_last_hip_error(const als_serve_ctx* ctx);
  *   users  : int32[rows], the rows of x to take (repeats allowed), or NULL: rows 0 .. rows - 1 (rows <= of).
  *            An entry outside [0, of) gives a row of scale NaN and zeros.
  *   q      : rows x f, row stride ldq >= f; columns f .. ldq - 1 are written as zeros up to the next
- *            multiple of 16 (or ldq, if that is less).  A stride that is a multiple of 16 is the fastest for als_score.
+ *            multiple of 16 (or ldq, if that is less), in the last row too.  A stride that is a multiple of 16 is the fastest for als_score.
  *   scale  : fp32[rows]
  * q and scale must not overlap x, users or each other (ALS_ERR_ALIAS).  f in [1, ALS_SERVE_F_MAX].
  */
 int als_quantize(als_serve_ctx* ctx, const void* x, int32_t dtype, int64_t of, int64_t ldx,
                  const int32_t* users, int64_t rows, int32_t f, int8_t* q, int64_t ldq, float* scale,
                  void* stream);
+
+/*
+ * als_quantize into rows of which only the first `width` columns are the caller's to write, f <= width <= ldq and
+ * width no more than f's next multiple of 16: columns f .. width - 1 are written as zeros, what lies past them (columns
+ * of other matrices, the end of the memory) is left alone.
+ */
+int als_quantize_into(als_serve_ctx* ctx, const void* x, int32_t dtype, int64_t of, int64_t ldx,
+                      const int32_t* users, int64_t rows, int32_t f, int8_t* q, int64_t ldq, int32_t width,
+                      float* scale, void* stream);
 
 /*
  * Scores of m users against n items (or any product of 8-bit rows with a scale for each row of either):

@@ -106,7 +106,7 @@ __device__ __forceinline__ uint32_t load_row(const T* row, int k, int f, float (
     return most;
 }
 
-// The values' whole numbers at k, as far as `end` (f and its padding).
+// The values' whole numbers at k, as far as `end` (f, or with its padding).
 template <int V>
 __device__ __forceinline__ void store_row(int8_t* row, int k, int end, const RowScale& s, const float (&x)[V]) {
     if (k >= end) return;
@@ -128,7 +128,7 @@ __device__ __forceinline__ void store_row(int8_t* row, int k, int end, const Row
 template <typename T, int G, int E>
 __global__ __launch_bounds__(kQuantThreads) void k_quantize(const T* __restrict__ x, int64_t of, int64_t ldx,
                                                             const int32_t* __restrict__ users, int64_t rows,
-                                                            int f, int8_t* __restrict__ q, int64_t ldq,
+                                                            int f, int8_t* __restrict__ q, int64_t ldq, int end,
                                                             float* __restrict__ scale) {
     constexpr int V = 16 / sizeof(T);
     __shared__ uint32_t of_waves[kQuantThreads / kWave];
@@ -151,8 +151,6 @@ __global__ __launch_bounds__(kQuantThreads) void k_quantize(const T* __restrict_
     }
     if (row >= rows) return;
     const RowScale s(most);
-    const int64_t pad = ((int64_t)f + 15) / 16 * 16;
-    const int end = (int)(pad < ldq ? pad : ldq);
 #pragma unroll
     for (int e = 0; e < E; ++e) store_row<V>(q + row * ldq, (e * G + lane) * V, end, s, v[e]);
     if (lane == 0) scale[row] = s.scale();
@@ -162,7 +160,7 @@ __global__ __launch_bounds__(kQuantThreads) void k_quantize(const T* __restrict_
 template <typename T>
 __global__ __launch_bounds__(kQuantThreads) void k_quantize_long(const T* __restrict__ x, int64_t of, int64_t ldx,
                                                                  const int32_t* __restrict__ users, int64_t rows,
-                                                                 int f, int8_t* __restrict__ q, int64_t ldq,
+                                                                 int f, int8_t* __restrict__ q, int64_t ldq, int end,
                                                                  float* __restrict__ scale) {
     constexpr int V = 16 / sizeof(T);
     __shared__ uint32_t of_waves[kQuantThreads / kWave];
@@ -170,8 +168,6 @@ __global__ __launch_bounds__(kQuantThreads) void k_quantize_long(const T* __rest
     const int64_t src = users ? (int64_t)users[row] : row;
     const bool there = src >= 0 && src < of;
     const T* xr = x + (there ? src * ldx : 0);
-    const int64_t pad = ((int64_t)f + 15) / 16 * 16;
-    const int end = (int)(pad < ldq ? pad : ldq);
     uint32_t m = there ? 0 : 0x7FC00000u;
     float v[V];
     for (int k = threadIdx.x * V; k < f; k += kQuantThreads * V) m = max(m, load_row<T, V>(xr, k, there ? f : 0, v));
@@ -2236,15 +2232,22 @@ int als_serve_last_hip_error(const als_serve_ctx* ctx) { return ctx ? ctx->last_
 
 int als_quantize(als_serve_ctx* ctx, const void* x, int32_t dtype, int64_t of, int64_t ldx, const int32_t* users,
                  int64_t rows, int32_t f, int8_t* q, int64_t ldq, float* scale, void* stream) {
+    const int64_t pad = ((int64_t)f + 15) / 16 * 16;
+    return als_quantize_into(ctx, x, dtype, of, ldx, users, rows, f, q, ldq, (int32_t)(pad < ldq ? pad : ldq), scale,
+                             stream);
+}
+
+int als_quantize_into(als_serve_ctx* ctx, const void* x, int32_t dtype, int64_t of, int64_t ldx, const int32_t* users,
+                      int64_t rows, int32_t f, int8_t* q, int64_t ldq, int32_t width, float* scale, void* stream) {
     if (!ctx || of < 0 || rows < 0 || dtype < ALS_F32 || dtype > ALS_BF16) return ALS_ERR_INVALID_ARG;
     if (f < 1 || f > ALS_SERVE_F_MAX) return ALS_ERR_UNSUPPORTED_F;
-    if (ldx < f || ldq < f || (!users && rows > of)) return ALS_ERR_INVALID_ARG;
+    const int64_t pad = ((int64_t)f + 15) / 16 * 16;
+    if (ldx < f || ldq < f || width < f || width > ldq || width > pad || (!users && rows > of)) return ALS_ERR_INVALID_ARG;
     if (rows == 0) return ALS_OK;
     if (!q || !scale || (of > 0 && !x)) return ALS_ERR_INVALID_ARG;
     if (!aligned(x, type_bytes(dtype)) || !aligned(users, 4) || !aligned(scale, 4)) return ALS_ERR_ALIGN;
-    const int64_t pad = ((int64_t)f + 15) / 16 * 16;
     const uint64_t xn = span_of(of, f, ldx, type_bytes(dtype));
-    const uint64_t qn = span_of(rows, pad < ldq ? pad : ldq, ldq, 1), sn = (uint64_t)rows * 4;
+    const uint64_t qn = span_of(rows, width, ldq, 1), sn = (uint64_t)rows * 4;
     if (overlap(q, qn, x, xn) || overlap(scale, sn, x, xn) || overlap(q, qn, scale, sn) ||
         overlap(q, qn, users, sn) || overlap(scale, sn, users, sn))
         return ALS_ERR_ALIAS;
@@ -2255,7 +2258,7 @@ int als_quantize(als_serve_ctx* ctx, const void* x, int32_t dtype, int64_t of, i
         in_parts(rows, kMaxThreads / kQuantThreads * per, [&](int64_t r, int64_t some) {
             hipLaunchKernelGGL(kernel, dim3((unsigned)((some + per - 1) / per)), dim3(kQuantThreads), 0,
                                (hipStream_t)stream, users ? p : p + r * ldx, users ? of : of - r, ldx,
-                               users ? users + r : users, some, f, q + r * ldq, ldq, scale + r);
+                               users ? users + r : users, some, f, q + r * ldq, ldq, width, scale + r);
         });
     };
     const auto go = [&](auto* p, auto lanes, auto loads) {

@@ -21,7 +21,7 @@ LIB_PATH = os.path.join(_PKG, "libals_serve.so")
 ALS_SERVE_F_MAX = 131_071
 ALS_SERVE_N_MAX = 4_194_304
 EXPORTED = ("als_serve_workspace_bytes", "als_serve_init", "als_serve_destroy",
-            "als_serve_last_hip_error", "als_quantize", "als_score", "als_sample")
+            "als_serve_last_hip_error", "als_quantize", "als_quantize_into", "als_score", "als_sample")
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
@@ -43,6 +43,7 @@ def _load():
     lib.als_serve_destroy.argtypes = [P]
     lib.als_serve_last_hip_error.argtypes = [P]
     lib.als_quantize.argtypes = [P, P, i32, i64, i64, P, i64, i32, P, i64, P, P]
+    lib.als_quantize_into.argtypes = [P, P, i32, i64, i64, P, i64, i32, P, i64, i32, P, P]
     lib.als_score.argtypes = [P, P, i64, P, i64, P, i64, P, i64, i32, P, i32, i64, P]
     lib.als_sample.argtypes = [P, P, i32, i64, i64, i64, ctypes.POINTER(_Limits), P, P, P, P, i64, P, P, P]
     for fn in EXPORTED[1:]:
@@ -170,10 +171,21 @@ def _matrix(ctx: Context, t, name, dtypes, rows, cols, other):
 _I8, _I32, _I64, _F32, _FLOATS = (torch.int8,), (torch.int32,), (torch.int64,), (torch.float32,), tuple(_DTYPES)
 
 
+def _own_columns(q, rows, f, ldq):
+    """How many columns of each row of a given q may be written: those of the view, and its padding only where
+    the rows start their memory's and leave no room for another such matrix.  (No operator needs the zeros.)"""
+    start, width = q.storage_offset(), min(ldq, (f + 15) // 16 * 16)
+    if ldq < 2 * f and start % ldq == 0 and start + (rows - 1) * ldq + width <= q.untyped_storage().nbytes():
+        return width
+    return f
+
+
 def als_quantize(ctx: Context, x, users=None, q=None, scale=None, stream=None):
     """(q, scale): the rows of x (f32, f16 or bf16), or the rows `users` (int32) of it, as 8-bit integers
     with one scale each, x ~ scale q.  Without `q` the result is a view of rows whose stride is the next
-    multiple of 16."""
+    multiple of 16, with zeros up to it.  A given `q` may have any row stride; nothing but its elements is written,
+    with one exception: where its rows start those of the memory that it is a view of, and are too short a distance
+    apart for a second matrix like it (less than 2 f), zeros go up to the next multiple of 16 as far as the stride."""
     handle, other = _stream(ctx, stream)
     px, ldx, of, f = _matrix(ctx, x, "x", _FLOATS, None, None, other)
     rows, pu = of, None
@@ -183,17 +195,18 @@ def als_quantize(ctx: Context, x, users=None, q=None, scale=None, stream=None):
     if q is None:
         ldq = (f + 15) // 16 * 16
         q = _empty(ctx, (rows, ldq), torch.int8, other)
-        pq = q.data_ptr()
+        pq, width = q.data_ptr(), ldq
         if ldq != f:
             q = q[:, :f]
     else:
         pq, ldq, _, _ = _matrix(ctx, q, "q", _I8, rows, f, other)
+        width = f if ldq == f else _own_columns(q, rows, f, ldq)
     if scale is None:
         scale = _empty(ctx, (rows,), torch.float32, other)
         ps = scale.data_ptr()
     else:
         ps = _vector(ctx, scale, "scale", _F32, rows, other)
-    rc = _lib.als_quantize(ctx.handle, px, _DTYPES[x.dtype], of, ldx, pu, rows, f, pq, ldq, ps, handle)
+    rc = _lib.als_quantize_into(ctx.handle, px, _DTYPES[x.dtype], of, ldx, pu, rows, f, pq, ldq, width, ps, handle)
     if rc:
         _check("als_quantize", rc, ctx.handle)
     return q, scale

@@ -1,0 +1,63 @@
+"""What the serving operators write and hold: nothing beside a given view is touched."""
+import numpy as np
+import pytest
+import torch
+
+from tests import serve_oracle
+from tests.gpu_util import log
+
+pytestmark = pytest.mark.gpu
+D = "cuda:0"
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_1603_03820_amd import serve
+    c = serve.Context(0)
+    yield c
+    c.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("f", [1, 21, 100, 128, 300, 1100, 3001, 9001, 20_003])
+def test_quantize_into_columns_of_a_buffer(ctx, dtype, f):
+    """X and Theta side by side in one buffer, in either order, and a slice from its middle: each holds its own rows,
+    and the columns beside them and the memory behind the last row keep their values."""
+    from paper_1603_03820_amd import serve
+    rows, guard = 7, 64
+    rng = np.random.default_rng(f)
+    xs = [torch.from_numpy(rng.standard_normal((rows, f)).astype(np.float32)).to(D).to(TYPES[dtype]) for _ in range(2)]
+    want = [serve_oracle.quantize(x.float().cpu().numpy()) for x in xs]
+    for order in ((0, 1), (1, 0)):
+        memory = torch.full((rows * 2 * f + guard,), 99, dtype=torch.int8, device=D)
+        both = memory[:rows * 2 * f].view(rows, 2 * f)
+        log(f"quantize {dtype} side by side, f {f}, order {order}")
+        for k in order:
+            _, scale = serve.als_quantize(ctx, xs[k], q=both[:, k * f:(k + 1) * f])
+            assert np.array_equal(scale.cpu().numpy(), want[k][1])
+        got = both.cpu().numpy()
+        assert np.array_equal(got[:, :f], want[0][0]) and np.array_equal(got[:, f:], want[1][0])
+        assert bool((memory[rows * 2 * f:] == 99).all())
+    for before, after in ((1, 0), (16, 0), (11, 3), (5, 40)):
+        width = before + f + after
+        memory = torch.full((rows * width + guard,), 99, dtype=torch.int8, device=D)
+        part = memory[:rows * width].view(rows, width)
+        log(f"quantize {dtype} into columns {before} to {before + f} of {width}")
+        serve.als_quantize(ctx, xs[0], q=part[:, before:before + f])
+        assert np.array_equal(part[:, before:before + f].cpu().numpy(), want[0][0])
+        assert bool((part[:, :before] == 99).all()) and bool((part[:, before + f:] == 99).all())
+        assert bool((memory[rows * width:] == 99).all())
+
+
+def test_quantize_into_refusals(ctx):
+    from paper_1603_03820_amd import serve
+    x, q, s = torch.zeros(4, 32, device=D), torch.zeros(4096, dtype=torch.int8, device=D), torch.zeros(4, device=D)
+
+    def into(f, ldq, width):
+        return serve._lib.als_quantize_into(ctx.handle, x.data_ptr(), 0, 4, 32, None, 4, f, q.data_ptr(), ldq, width,
+                                            s.data_ptr(), None)
+    log("als_quantize_into: widths")
+    assert into(21, 40, 21) == 0 and into(21, 40, 32) == 0 and into(21, 25, 25) == 0 and into(32, 32, 32) == 0
+    assert into(21, 40, 20) == -1 and into(21, 40, 33) == -1 and into(21, 25, 26) == -1 and into(21, 40, -1) == -1
+    torch.cuda.synchronize()
