@@ -31,6 +31,10 @@ enum { ALS_F32 = 0, ALS_F16 = 1, ALS_BF16 = 2 };
 /* Most columns of als_sample: sums of 2^40 n stay below 2^62. */
 #define ALS_SERVE_N_MAX 4194304
 
+/* Columns of the longest row that als_sample draws from without the workspace.  (als_score does without it where both
+   sides' rows lie at addresses and strides that are multiples of 16, strides below 2^22; als_quantize always.) */
+#define ALS_SERVE_HELD_MAX 65536
+
 typedef struct als_serve_ctx als_serve_ctx;
 
 /* Bytes of device workspace a context on `device` needs; 0 if the device cannot be queried or is not a

@@ -2405,7 +2405,7 @@ int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, i
             if (n <= 8192) return held(Held<16, 1024>(), p);
         }
         if (n <= 32768) return held(Held<32, 2048>(), p);
-        if (n <= 65536) return held(Held<64, 4096>(), p);
+        if (n <= ALS_SERVE_HELD_MAX) return held(Held<64, 4096>(), p);
         // in batches of as many rows as the workspace holds
         const int64_t segments = (n + kSegColumns - 1) / kSegColumns;
         uint32_t group = 1;

@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_PKG, "libals_serve.so")
 
 ALS_SERVE_F_MAX = 131_071
 ALS_SERVE_N_MAX = 4_194_304
+ALS_SERVE_HELD_MAX = 65_536
 EXPORTED = ("als_serve_workspace_bytes", "als_serve_init", "als_serve_destroy",
             "als_serve_last_hip_error", "als_quantize", "als_quantize_into", "als_score", "als_sample")
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
@@ -77,8 +78,19 @@ class Context:
         _check("als_serve_init", _lib.als_serve_init(ctypes.byref(h), device,
                                                      ctypes.c_void_p(self.workspace.data_ptr()), nbytes))
         self.handle = h
+        self._start(torch.cuda.current_stream(self.device))
+
+    def _start(self, stream):
         self._limits = _Limits()
         self._limits_ref = ctypes.byref(self._limits)
+        self._streams = {stream.cuda_stream}       # those that keep the workspace's memory
+
+    def _use_workspace(self, handle, other):
+        """For a call on stream `handle` (`other`, or the current one where that is None) that works in the workspace:
+        its memory is not handed out again before the call has run, whenever the context goes."""
+        if handle not in self._streams:
+            self.workspace.record_stream(other or torch.cuda.current_stream(self.device))
+            self._streams.add(handle)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -95,7 +107,7 @@ class Context:
 # A call's checks take as long as its launch where the work is small, so they read each property of a tensor
 # once and pass plain numbers on (an empty tensor's pointer is 0, which is NULL).  A tensor that is used on another
 # stream than the current one is recorded there, so that its memory is not handed out again while the call may
-# still run.
+# still run; the workspace on every stream but the one that it was allocated on.
 
 
 def _stream(ctx: Context, stream):
@@ -212,6 +224,11 @@ def als_quantize(ctx: Context, x, users=None, q=None, scale=None, stream=None):
     return q, scale
 
 
+def _in_place(p, ld):
+    """Whether als_score reads rows where they lie (else it lays them out anew in the workspace)."""
+    return (p | ld) % 16 == 0 and ld < 1 << 22
+
+
 def als_score(ctx: Context, xq, xs, tq, ts, out=None, dtype=torch.float32, stream=None):
     """out[i, j] = xs_i ts_j sum_k xq_ik tq_jk for 8-bit rows with a scale each; out (f32, f16 or bf16, `dtype`
     where it is not given) may have any row stride."""
@@ -226,6 +243,8 @@ def als_score(ctx: Context, xq, xs, tq, ts, out=None, dtype=torch.float32, strea
     else:
         dtype = out.dtype
         po, ldo, _, _ = _matrix(ctx, out, "out", _FLOATS, m, n, other)
+    if not (_in_place(px, ldx) and _in_place(pt, ldt)):
+        ctx._use_workspace(handle, other)
     rc = _lib.als_score(ctx.handle, px, ldx, _vector(ctx, xs, "xs", _F32, m, other), m, pt, ldt,
                         _vector(ctx, ts, "ts", _F32, n, other), n, f, po, _DTYPES[dtype], ldo, handle)
     if rc:
@@ -283,6 +302,8 @@ def als_sample(ctx: Context, scores, u, temperature=1.0, top_k=0, top_p=1.0, min
         p_log = log.data_ptr()
     else:
         p_log = _vector(ctx, log, "log", _F32, rows, other)
+    if n > ALS_SERVE_HELD_MAX:
+        ctx._use_workspace(handle, other)
     rc = _lib.als_sample(ctx.handle, pz, _DTYPES[scores.dtype], rows, n, ldz, ctx._limits_ref,
                          _vector(ctx, u, "u", _F32, rows, other), pp, pi, pu, of, p_index, p_log, handle)
     if rc:

@@ -61,3 +61,48 @@ def test_quantize_into_refusals(ctx):
     assert into(21, 40, 21) == 0 and into(21, 40, 32) == 0 and into(21, 25, 25) == 0 and into(32, 32, 32) == 0
     assert into(21, 40, 20) == -1 and into(21, 40, 33) == -1 and into(21, 25, 26) == -1 and into(21, 40, -1) == -1
     torch.cuda.synchronize()
+
+
+def _long_rows(seed, rows=3, n=200_000):
+    g = torch.Generator(D).manual_seed(seed)
+    z = 3.5 + 0.7 * torch.randn(rows, n, device=D, generator=g)
+    return z, torch.rand(rows, device=D, generator=g)
+
+
+@pytest.mark.parametrize("how", ["argument", "current"])
+@pytest.mark.parametrize("call", ["sample", "score"])
+def test_workspace_outlives_its_context(how, call):
+    """A context that goes while a call on another stream has yet to run: the workspace's memory is not handed out
+    before it has."""
+    from paper_1603_03820_amd import serve
+
+    def run(c, stream=None):
+        if call == "sample":
+            return serve.als_sample(c, z, u, temperature=0.3, top_p=0.9, stream=stream)
+        return (serve.als_score(c, xq, xs, tq, ts, stream=stream),)
+    z, u = _long_rows(1)
+    g = torch.Generator(D).manual_seed(2)
+    xq, tq = (torch.randint(-127, 128, (k, 101), device=D, generator=g, dtype=torch.int8) for k in (40, 9000))
+    xs, ts = (torch.rand(k, device=D, generator=g) for k in (40, 9000))
+    want = run(serve.Context(0))
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    c = serve.Context(0)
+    nbytes, at = c.workspace.numel(), c.workspace.data_ptr()
+    s.wait_stream(torch.cuda.current_stream())
+    log(f"{call} on a busy stream ({how}), then the context goes")
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(50_000_000)
+    if how == "argument":
+        got = run(c, s)
+    else:
+        with torch.cuda.stream(s):
+            got = run(c)
+    del c
+    busy = not s.query()
+    other = torch.empty(nbytes, dtype=torch.uint8, device=D)
+    overlap = abs(other.data_ptr() - at) < nbytes
+    torch.cuda.current_stream().wait_stream(s)
+    assert busy and not overlap
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)

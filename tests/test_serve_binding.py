@@ -1,7 +1,5 @@
 """The serving binding without a GPU: what it hands to the library for tensors of every layout.  The library is a
 stand-in that keeps the arguments; tensors are the host's."""
-import types
-
 import pytest
 import torch
 
@@ -25,14 +23,41 @@ class Library:
 def lib(monkeypatch):
     stand_in = Library()
     monkeypatch.setattr(serve, "_lib", stand_in)
-    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0)
+    stand_in.current = Stream(0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: stand_in.current.cuda_stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: stand_in.current)
     return stand_in
 
 
+class Stream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+class Workspace:
+    """Keeps the streams that it is recorded on."""
+
+    def __init__(self):
+        self.recorded = []
+
+    def record_stream(self, stream):
+        self.recorded.append(stream.cuda_stream)
+
+
+class HostContext(serve.Context):
+    """A context whose device is the host (whose tensors are on device -1), created on stream 0."""
+
+    def __init__(self):
+        self.handle, self.index, self.device = 1, -1, torch.device("cpu")
+        self.workspace = Workspace()
+        self._start(Stream(0))
+
+    def close(self):
+        pass
+
+
 def context():
-    """A context whose device is the host (whose tensors are on device -1)."""
-    return types.SimpleNamespace(handle=1, index=-1, device=torch.device("cpu"), _limits=serve._Limits(),
-                                 _limits_ref=None)
+    return HostContext()
 
 
 def quantize_writes(call):
@@ -77,3 +102,47 @@ def test_quantize_pads_its_own_rows(lib):
     q, _ = serve.als_quantize(context(), torch.zeros(4, 21))
     assert q.stride() == (32, 1)
     assert quantize_writes(lib.calls[-1]) == [(q.data_ptr() + 32 * r, 32) for r in range(4)]
+
+
+def sample(ctx, n):
+    return serve.als_sample(ctx, torch.zeros(2, n), torch.zeros(2))
+
+
+def score(ctx, extra=0):
+    q = torch.zeros(2, 32 + extra, dtype=torch.int8)[:, :32]
+    return serve.als_score(ctx, q, torch.zeros(2), q, torch.zeros(2))
+
+
+def test_the_bounds_are_the_librarys():
+    """Up to which calls do without the workspace."""
+    import os
+    import re
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    header = open(os.path.join(root, "include", "als_serve.h")).read()
+    assert int(re.search(r"#define ALS_SERVE_HELD_MAX (\d+)", header).group(1)) == serve.ALS_SERVE_HELD_MAX
+    source = open(os.path.join(root, "paper_1603_03820_amd", "csrc", "serve.hip")).read()
+    assert "constexpr int64_t kTileStride = 1 << 22;" in source
+    assert "return aligned(q, 16) && ld % 16 == 0 && ld < kTileStride;" in source
+    for p, ld, there in ((0, 16, True), (1, 16, False), (16, 17, False), (32, (1 << 22) - 16, True), (0, 1 << 22, False)):
+        assert serve._in_place(p, ld) == there
+
+
+def test_the_workspace_is_recorded_where_it_is_used(lib):
+    """Its memory must not be handed out again while a call on another stream than its own still works in it."""
+    ctx = context()
+    sample(ctx, 70_000)
+    score(ctx, 1)
+    assert ctx.workspace.recorded == []
+    lib.current = Stream(5)
+    sample(ctx, 65_536)          # these do without it
+    score(ctx)
+    assert ctx.workspace.recorded == []
+    sample(ctx, 65_537)
+    assert ctx.workspace.recorded == [5]
+    lib.current = Stream(6)
+    score(ctx, 1)
+    assert ctx.workspace.recorded == [5, 6]
+    sample(ctx, 70_000)
+    lib.current = Stream(0)
+    score(ctx, 1)
+    assert ctx.workspace.recorded == [5, 6]      # once is enough
