@@ -64,8 +64,17 @@ def als_serve_workspace_bytes(device: int = 0) -> int:
     return int(_lib.als_serve_workspace_bytes(device))
 
 
+def _capturing(stream):
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class Context:
-    """An als_serve_ctx plus the workspace tensor it runs in (one per device)."""
+    """An als_serve_ctx plus the workspace tensor it runs in (one per device).  Calls that work in the workspace (draws
+    from rows of more than ALS_SERVE_HELD_MAX columns, scores of rows that are not read in place) follow one
+    another also where they are on different streams: each waits for the last one's stream.  Not so calls that are
+    captured into a graph: whoever launches it keeps its launches, and the eager calls beside them, apart, and keeps
+    the context as long as the graph."""
 
     def __init__(self, device: int = 0):
         self.device = torch.device("cuda", device)
@@ -84,13 +93,21 @@ class Context:
         self._limits = _Limits()
         self._limits_ref = ctypes.byref(self._limits)
         self._streams = {stream.cuda_stream}       # those that keep the workspace's memory
+        self._last = stream                        # the one that used it last
 
     def _use_workspace(self, handle, other):
         """For a call on stream `handle` (`other`, or the current one where that is None) that works in the workspace:
-        its memory is not handed out again before the call has run, whenever the context goes."""
+        it follows the last such call, and the workspace's memory is not handed out again before it has run."""
+        last = self._last
+        if handle == last.cuda_stream:
+            return
+        stream = other or torch.cuda.current_stream(self.device)
         if handle not in self._streams:
-            self.workspace.record_stream(other or torch.cuda.current_stream(self.device))
+            self.workspace.record_stream(stream)
             self._streams.add(handle)
+        if not (_capturing(stream) or _capturing(last)):
+            stream.wait_stream(last)
+            self._last = stream
 
     def close(self):
         if getattr(self, "handle", None):

@@ -106,3 +106,31 @@ def test_workspace_outlives_its_context(how, call):
     assert busy and not overlap
     for a, b in zip(want, got):
         assert torch.equal(a, b)
+
+
+def test_two_streams_of_one_context(ctx):
+    """Draws from long rows and scores of rows laid out anew, in turn on two streams with nothing between them: each
+    equals the call alone, and waits for the one before."""
+    from paper_1603_03820_amd import serve
+    rows = [_long_rows(10 + k, rows=40) for k in range(2)]
+    g = torch.Generator(D).manual_seed(3)
+    q = [torch.randint(-127, 128, (5000, 101), device=D, generator=g, dtype=torch.int8) for _ in range(2)]
+    s = torch.ones(5000, device=D)
+    want = [serve.als_sample(ctx, *rows[k], temperature=0.3, top_p=0.9) + (serve.als_score(ctx, q[k][:300], s[:300], q[k], s),)
+            for k in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    log("two streams in turn")
+    with torch.cuda.stream(streams[0]):
+        torch.cuda._sleep(50_000_000)
+    for turn in range(6):
+        with torch.cuda.stream(streams[turn % 2]):
+            got.append(serve.als_sample(ctx, *rows[turn % 2], temperature=0.3, top_p=0.9)
+                       + (serve.als_score(ctx, q[turn % 2][:300], s[:300], q[turn % 2], s),))
+    waits = not streams[1].query()       # for the first one, which sleeps
+    torch.cuda.synchronize()
+    assert waits
+    for turn, results in enumerate(got):
+        for a, b in zip(want[turn % 2], results):
+            assert torch.equal(a, b), turn

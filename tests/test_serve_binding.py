@@ -26,12 +26,18 @@ def lib(monkeypatch):
     stand_in.current = Stream(0)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: stand_in.current.cuda_stream)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: stand_in.current)
+    monkeypatch.setattr(serve, "_capturing", lambda stream: stream.capturing, raising=False)
     return stand_in
 
 
 class Stream:
-    def __init__(self, handle):
-        self.cuda_stream = handle
+    """Keeps the streams that it was told to wait for."""
+
+    def __init__(self, handle, capturing=False):
+        self.cuda_stream, self.capturing, self.waits = handle, capturing, []
+
+    def wait_stream(self, stream):
+        self.waits.append(stream.cuda_stream)
 
 
 class Workspace:
@@ -146,3 +152,29 @@ def test_the_workspace_is_recorded_where_it_is_used(lib):
     lib.current = Stream(0)
     score(ctx, 1)
     assert ctx.workspace.recorded == [5, 6]      # once is enough
+
+
+def test_calls_in_the_workspace_follow_one_another(lib):
+    """On whatever streams they are; a captured call waits for nobody, and nobody for it."""
+    ctx = context()
+    a, b, captured = Stream(5), Stream(6), Stream(7, capturing=True)
+    lib.current = a
+    score(ctx, 1)
+    assert a.waits == [0]          # the memory's own stream, which may have used it before
+    sample(ctx, 70_000)
+    assert a.waits == [0]
+    lib.current = b
+    sample(ctx, 100)
+    score(ctx)
+    assert b.waits == []           # without the workspace
+    sample(ctx, 70_000)
+    assert b.waits == [5]
+    lib.current = captured
+    sample(ctx, 70_000)
+    assert captured.waits == [] and ctx.workspace.recorded == [5, 6, 7]
+    lib.current = b
+    sample(ctx, 70_000)
+    assert b.waits == [5]
+    lib.current = a
+    sample(ctx, 70_000)
+    assert a.waits == [0, 6]
