@@ -23,6 +23,7 @@ ALS_SERVE_N_MAX = 4_194_304
 ALS_SERVE_HELD_MAX = 65_536
 EXPORTED = ("als_serve_workspace_bytes", "als_serve_init", "als_serve_destroy",
             "als_serve_last_hip_error", "als_quantize", "als_quantize_into", "als_score", "als_sample")
+_INT32_MAX = 2 ** 31 - 1       # (numbers that the library takes in 32 bits and that pass it are refused there)
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
@@ -235,7 +236,8 @@ def als_quantize(ctx: Context, x, users=None, q=None, scale=None, stream=None):
         ps = scale.data_ptr()
     else:
         ps = _vector(ctx, scale, "scale", _F32, rows, other)
-    rc = _lib.als_quantize_into(ctx.handle, px, _DTYPES[x.dtype], of, ldx, pu, rows, f, pq, ldq, width, ps, handle)
+    rc = _lib.als_quantize_into(ctx.handle, px, _DTYPES[x.dtype], of, ldx, pu, rows, min(f, _INT32_MAX), pq, ldq,
+                                min(width, _INT32_MAX), ps, handle)
     if rc:
         _check("als_quantize", rc, ctx.handle)
     return q, scale
@@ -263,7 +265,7 @@ def als_score(ctx: Context, xq, xs, tq, ts, out=None, dtype=torch.float32, strea
     if not (_in_place(px, ldx) and _in_place(pt, ldt)):
         ctx._use_workspace(handle, other)
     rc = _lib.als_score(ctx.handle, px, ldx, _vector(ctx, xs, "xs", _F32, m, other), m, pt, ldt,
-                        _vector(ctx, ts, "ts", _F32, n, other), n, f, po, _DTYPES[dtype], ldo, handle)
+                        _vector(ctx, ts, "ts", _F32, n, other), n, min(f, _INT32_MAX), po, _DTYPES[dtype], ldo, handle)
     if rc:
         _check("als_score", rc, ctx.handle)
     return out
@@ -286,7 +288,7 @@ def als_sample(ctx: Context, scores, u, temperature=1.0, top_k=0, top_p=1.0, min
     if isinstance(top_k, torch.Tensor):
         lim.top_k = _vector(ctx, top_k, "top_k", _I32, rows, other)
     else:
-        lim.top_k_all = min(max(int(top_k), 0), 2 ** 31 - 1)
+        lim.top_k_all = min(max(int(top_k), 0), _INT32_MAX)
     if isinstance(top_p, torch.Tensor):
         lim.top_p = _vector(ctx, top_p, "top_p", _F32, rows, other)
     else:

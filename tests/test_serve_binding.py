@@ -1,5 +1,7 @@
 """The serving binding without a GPU: what it hands to the library for tensors of every layout.  The library is a
 stand-in that keeps the arguments; tensors are the host's."""
+import ctypes
+
 import pytest
 import torch
 
@@ -178,3 +180,20 @@ def test_calls_in_the_workspace_follow_one_another(lib):
     lib.current = a
     sample(ctx, 70_000)
     assert a.waits == [0, 6]
+
+
+@pytest.mark.parametrize("f", [2 ** 31, 2 ** 32 + 5])
+def test_rows_past_32_bits_are_not_cut(lib, f):
+    """A row length goes to the library as a 32-bit number; one that does not fit must not arrive as another that
+    does (the library refuses all past ALS_SERVE_F_MAX)."""
+    ctx = context()
+    rows = torch.empty(1, f, dtype=torch.int8)       # (never touched)
+
+    def length(call):
+        name, args = call
+        return ctypes.c_int32(args[{"als_quantize_into": 7, "als_score": 9}[name]]).value
+    serve.als_score(ctx, rows, torch.zeros(1), rows, torch.zeros(1))
+    assert length(lib.calls[-1]) > serve.ALS_SERVE_F_MAX
+    x = torch.empty(1, f, dtype=torch.float16)
+    serve.als_quantize(ctx, x, q=rows)
+    assert length(lib.calls[-1]) > serve.ALS_SERVE_F_MAX
