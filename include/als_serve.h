@@ -126,7 +126,8 @@ typedef struct {
  * rated_ptr, rated_idx : a CSR with `of` rows (int64[of + 1], int32) of columns to leave out, in any order (one
  *         outside [0, n) is skipped), or both NULL.  Row r leaves out CSR row users[r] (int32[rows]), or r if
  *         users is NULL (then of >= rows).  An entry of users outside [0, of) gives index -1 and log NaN.
- * index and log must not overlap an input or each other (ALS_ERR_ALIAS).
+ * index and log must not overlap an input or each other (ALS_ERR_ALIAS; rated_idx is the caller's to look at, as its
+ * length is on the device).
  */
 int als_sample(als_serve_ctx* ctx, const void* z, int32_t dtype, int64_t rows, int64_t n, int64_t ldz,
                const als_sample_limits* limits, const float* u, const int64_t* rated_ptr,

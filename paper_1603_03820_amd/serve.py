@@ -18,6 +18,7 @@ from .als import ALS_OK, ALSError
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libals_serve.so")
 
+ALS_ERR_ALIAS = -6
 ALS_SERVE_F_MAX = 131_071
 ALS_SERVE_N_MAX = 4_194_304
 ALS_SERVE_HELD_MAX = 65_536
@@ -271,6 +272,12 @@ def als_score(ctx: Context, xq, xs, tq, ts, out=None, dtype=torch.float32, strea
     return out
 
 
+def _apart(p, rows, rated):
+    """Refuses results on the left-out columns, of which the library does not know how many there are."""
+    if rated is not None and p < rated[1].data_ptr() + 4 * rated[1].numel() and rated[1].data_ptr() < p + 4 * rows:
+        raise ALSError("als_sample", ALS_ERR_ALIAS)
+
+
 def als_sample(ctx: Context, scores, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, rated=None, users=None,
                index=None, log=None, stream=None):
     """(index, log): one column a row of `scores`, drawn by the uniform numbers `u` (float32, one a row), and the
@@ -316,11 +323,13 @@ def als_sample(ctx: Context, scores, u, temperature=1.0, top_k=0, top_p=1.0, min
         p_index = index.data_ptr()
     else:
         p_index = _vector(ctx, index, "index", _I32, rows, other)
+        _apart(p_index, rows, rated)
     if log is None:
         log = _empty(ctx, (rows,), torch.float32, other)
         p_log = log.data_ptr()
     else:
         p_log = _vector(ctx, log, "log", _F32, rows, other)
+        _apart(p_log, rows, rated)
     if n > ALS_SERVE_HELD_MAX:
         ctx._use_workspace(handle, other)
     rc = _lib.als_sample(ctx.handle, pz, _DTYPES[scores.dtype], rows, n, ldz, ctx._limits_ref,

@@ -197,3 +197,20 @@ def test_rows_past_32_bits_are_not_cut(lib, f):
     x = torch.empty(1, f, dtype=torch.float16)
     serve.als_quantize(ctx, x, q=rows)
     assert length(lib.calls[-1]) > serve.ALS_SERVE_F_MAX
+
+
+@pytest.mark.parametrize("first,fits", [(8, True), (9, False), (20, False), (29, False), (30, True)])
+def test_results_on_the_rated_columns_are_refused(lib, first, fits):
+    """`index` or `log` on the CSR's columns, whose number the library does not know."""
+    from paper_1603_03820_amd.als import ALSError
+    memory = torch.zeros(64, dtype=torch.int32)
+    rated = (torch.zeros(3, dtype=torch.int64), memory[10:30])
+    for kind in ("index", "log"):
+        result = memory[first:first + 2]
+        given = {kind: result if kind == "index" else result.view(torch.float32)}
+        if fits:
+            serve.als_sample(context(), torch.zeros(2, 9), torch.zeros(2), rated=rated, **given)
+        else:
+            with pytest.raises(ALSError) as e:
+                serve.als_sample(context(), torch.zeros(2, 9), torch.zeros(2), rated=rated, **given)
+            assert e.value.code == -6
