@@ -55,14 +55,15 @@ int als_serve_last_hip_error(const als_serve_ctx* ctx);
  * Rows of x as 8-bit integers with one scale each:
  *   a = max_k |x_uk|,   q_uk = rint(127 x_uk / a),   scale_u = a (1 / 127)     (so x_uk ~ scale_u q_uk)
  * 127 x and its quotient by a are each rounded to fp32, the quotient then to the nearest integer, ties to
- * even; 1 / 127 and its product with a are rounded to fp32.  The result is the same on every run.  A row of
- * zeros gets scale 0 and zeros.  A row with an infinity or a NaN gets scale NaN and zeros, so that its scores are
- * NaN.
+ * even (127 x as if fp32 had no largest value); 1 / 127 and its product with a are rounded to fp32.  The result
+ * is the same on every run.  A row of zeros gets scale 0 and zeros.  A row with an infinity or a NaN gets scale
+ * NaN and zeros, so that its scores are NaN.
  *   x      : `of` rows of f values of type dtype, row stride ldx >= f
  *   users  : int32[rows], the rows of x to take (repeats allowed), or NULL: rows 0 .. rows - 1 (rows <= of).
  *            An entry outside [0, of) gives a row of scale NaN and zeros.
  *   q      : rows x f, row stride ldq >= f; columns f .. ldq - 1 are written as zeros up to the next
- *            multiple of 16 (or ldq, if that is less), in the last row too.  A stride that is a multiple of 16 is the fastest for als_score.
+ *            multiple of 16 (or ldq, if that is less), in the last row too.  A stride that is a multiple of 16 is
+ *            the fastest for als_score.
  *   scale  : fp32[rows]
  * q and scale must not overlap x, users or each other (ALS_ERR_ALIAS).  f in [1, ALS_SERVE_F_MAX].
  */
@@ -112,8 +113,9 @@ typedef struct {
  *      gets index -1 and log -inf.
  *   2. Order: z descending, among equals the lower column first (-0 equals 0).  The first top_k stay.
  *   3. Weights: whole numbers w = floor(2^40 exp((z - max z) / T)), in fp32 up to the rounding down: the
- *      difference, its product with 1 / T (rounded once) and the exponential.  A score of +inf weighs
- *      2^40, and then finite ones nothing.  Sums of weights are exact, so no result depends on an order of summation.
+ *      difference, its product with 1 / T (rounded once) and the exponential.  A difference past fp32's
+ *      range weighs nothing, whatever T.  A score of +inf weighs 2^40, and then finite ones nothing.
+ *      Sums of weights are exact, so no result depends on an order of summation.
  *   4. top_p: with W the sum of the weights so far, a column stays while the weight before it in the
  *      order is below floor(W floor(2^24 top_p) / 2^24), at least one column.
  *   5. min_p: columns whose exponential is below min_p go.

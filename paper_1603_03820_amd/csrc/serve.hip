@@ -209,11 +209,12 @@ __device__ __forceinline__ i4 load16(const int8_t* row, int k, int f) {
 // fragments are neighbours and go out as 16 bytes), and s is r / 2 % 2 + 2 (r / 8 % 4).
 // v_mfma_i32_16x16x64_i8 with the items as the first operand: a lane holds four neighbouring items of one user.  Items
 // and users past the end, and values past f, are multiplied too: their results are not written, or one side is 0.
-// 8,192^3 in 437 us, 2.5 Pop/s (a 256 x 256 tile reads 64 KB of LDS and 16 KB of memory for 16.8 Mop; matrix
-// instructions at the clock that they leave bound it).  At f <= 128 the scores' way out bounds it: 1,024 x 17,770 to fp32
-// in 16.5 us (4.4 TB/s), 4,096 x 40,000 in 150 us (4.4 TB/s; a kernel that only writes so takes 125), to bf16 in
-// 90 to 111 us (3.0 to 3.6 TB/s).  Few users and wide rows are bound by the items' bytes: 5 x 8,192 x 8,192 in 14.8 us
-// (4.5 TB/s).
+// 8,192^3 in 435 us, 2.5 Pop/s.  A step of a 256 x 256 tile brings 64 KB from memory and its eight waves read 192 KB of
+// LDS for 16.8 Mop; counters: the matrix units are busy in 58% of the cycles, at about 2.0 GHz under this load (2.4 is
+// the most), LDS without bank conflicts, waits for LDS in 2% of the waves' time.  At f <= 128 the scores' way out bounds
+// it: 1,024 x 17,770 to fp32 in 16.3 us (4.6 TB/s), 4,096 x 40,000 in 150 us (4.4 TB/s; a kernel that only writes so takes
+// 125), to bf16 in 91 us into two buffers in turn and 112 into fresh ones (3.6 and 3.0 TB/s).  Few users and wide rows are
+// bound by the items' bytes: 5 x 8,192 x 8,192 in 14.7 us (4.6 TB/s).
 constexpr int kStep = 128;
 constexpr int64_t kTileStride = 1 << 22;        // row strides below it keep a tile's offsets below 2^30 ...
 constexpr uint32_t kPastEnd = 0x7FFFFFF0u;      // ... and this past every tile's end
@@ -439,7 +440,9 @@ __global__ __launch_bounds__(64 * WU * WI) void k_score_tiles(
     }
 }
 
-// Rows of any stride and alignment to rows of a stride that is a multiple of 16, zeros past f.
+// Rows of any stride and alignment to rows of a stride that is a multiple of 16, zeros past f: anew in every call, so rows
+// that are scored again and again are better held so.  With it and without, us: 1,024 x 17,770 x 100 23 and 16,
+// 1 x 625,000 x 100 45 and 14, 8,192^3 461 and 418.
 __global__ __launch_bounds__(256) void k_pack(const int8_t* __restrict__ from, int64_t ld, int64_t rows, int f,
                                               int8_t* __restrict__ to, int64_t groups) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -545,7 +548,8 @@ struct Asked {
     // 2^40 exp((z - top) / T), z <= top, of the exponential rounded to fp32: 2 to the nearest whole number of
     // x log2(e), held in two parts, times 2 to the rest.  Where that is 1 or more it equals 2^40 expf(x) in every bit
     // for all but 2 of the 1.1e9 such x (tested one by one), at half its instructions: x ends at -64, where no weight
-    // is left (nor where a difference or product is not a number), so that nothing overflows.  The whole number comes
+    // is left (nor where a difference or product is not a number), so that nothing overflows.  (The reduction by log2(e)
+    // in two parts is Cody and Waite's; the result falls with x over all those floats, tested too.)  The whole number comes
     // by adding 1.5 2^23 (+ 40), whose sum has it in its last bits; they go to the exponent.  No product may be
     // fused into a sum here but the two that are written so.
     __device__ __forceinline__ float scaled(float z) const {
@@ -1470,10 +1474,15 @@ __device__ LongCut select_cut(Row<T>& row, LongCut within, uint32_t widest, uint
 //                 falls; neither: the draw
 //   k_long_cut    top-p: the segment's columns in that bin, and the weight of those above it
 //   k_long_draw   top-p: the cut, by ranking the listed columns, and the draw
-// Rows whose lists do not hold what they should (equal scores without end, a top_k of more than 7/8 of the groups)
-// are drawn by the last of these kernels alone, which reads the row again for every pass (sample_slowly).
-// 64 x 625,000 bf16 scores (15.3 us of reading), us: the best column 33, temperature 61, top-k 200 64, top-p 0.9 131, by
-// kernel 19 (memory), 44 (vector instructions: a weight a score), 13 (a workgroup a row: waits), 36 and 35 (waits).
+// Rows whose lists do not hold what they should are drawn by the last of these kernels alone, one workgroup that reads
+// the row again for every pass (sample_slowly): with a top_k above 7/8 of the groups (2,184 of 2,496 groups at 625,000
+// columns, 2,240 at 70,000, 3,584 at most); a top_k whose best columns stand side by side (sorted rows: over 2,048
+// listed in one segment); over 2,048 columns of a segment, or 16,384 of the row, in the bin of a top-p cut (bf16 scores
+// close to one another); a best score of +inf.
+// 64 x 625,000 bf16 scores (15.3 us of reading), us: the best column 33, temperature 61, top-k 200 66, top-p 0.9 149
+// (two sets of inputs in turn; 132 over one), by kernel 19 (memory), 45 (vector instructions: a weight a score), 13 (a
+// workgroup a row: waits), 37 and 39 (waits).  By sample_slowly, 1 and 64 such rows: top-k 5,000 930 and 1,980; sorted
+// fp32 rows with top-k 200 1,030 and 1,560; scores of 4 +- 0.2 with top-p 0.9 2,120 and 2,930; +inf in fp32 300 and 560.
 constexpr int kSegWaves = 8, kSegThreads = kSegWaves * kWave, kSegColumns = kSegThreads * 32;
 constexpr int kSegMax = ALS_SERVE_N_MAX / kSegColumns;
 constexpr int kSlab = 2048;              // columns a segment lists
@@ -2162,13 +2171,21 @@ void launch_tiles(const ScoreArgs& a) {
 // The tile: the largest that still gives every CU enough of them.  A large tile reads the rows fewer times, which
 // counts where f is large; with few tiles, CUs stand idle (256 x 8,192 x 8,192, us: 256 x 256 tiles 90, 128 x 128
 // 42, 64 x 128 37, 64 x 64 in four stages 27).  Measured (us, users x items x f):
-//   8,192 x 8,192 x 8,192      256 x 256: 437    128 x 128: 492    64 x 128: 586
-//   1,024 x 8,192 x 8,192      256 x 256: 95     128 x 128: 63     64 x 128: 85
-//   2,048 x 2,048 x 1,024      128 x 128: 10.0   64 x 128: 8.9     64 x 64: 11.4
-//   512 x 512 x 4,096          64 x 128: 14.9    64 x 64: 10.8     16 x 64: 8.9
-//   5 x 8,192 x 8,192          64 x 128: 35      64 x 64: 18       16 x 64: 15
-// Up to f = 128 there is one step and the scores' way out counts: 4,096 x 40,000 x 128 to fp32 in 150 us by 128 x 128
-// tiles and 170 by 64 x 128; to 16 bits in 90 to 111 by 32 x 256, 100 and 110 by those.
+//   8,192 x 8,192 x 8,192      256 x 256: 445    128 x 128: 489    64 x 128: 589
+//   1,024 x 8,192 x 8,192      256 x 256: 99     128 x 128: 64     64 x 128: 87
+//   2,048 x 2,048 x 1,024      128 x 128: 9.6    64 x 128: 8.4     64 x 64: 11.0
+//   512 x 512 x 4,096          64 x 128: 14.7    64 x 64: 10.2     16 x 64: 8.6
+//   5 x 8,192 x 8,192          64 x 128: 34      64 x 64: 18       16 x 64: 15
+// Up to f = 128 there is one step and the scores' way out counts (into two buffers in turn):
+//   fp32   4,096 x 40,000 x 128    128 x 128: 150    64 x 128: 170    32 x 256: 186
+//          6,000 x 6,000 x 100     128 x 128: 26.7   64 x 128: 26.0   32 x 256: 27.3
+//   bf16   4,096 x 40,000 x 128    128 x 128: 102    64 x 128: 111    32 x 256: 91      (f16 101, 108, 90)
+//          4,096 x 40,000 x 100    128 x 128: 99     64 x 128: 108    32 x 256: 88
+//          1,024 x 17,770 x 100    128 x 128: 12.7   64 x 128: 12.3   32 x 256: 13.2
+//          2,100 x 8,200 x 100     128 x 128: 12.7   64 x 128: 11.8   32 x 256: 12.8
+//          8,192 x 12,000 x 64     128 x 128: 44.5   64 x 128: 45.8   32 x 256: 49.8
+//          6,000 x 6,000 x 16      128 x 128: 17.8   64 x 128: 19.1   32 x 256: 19.7
+// So 32 x 256 gains a tenth on outputs larger than the card's cache and loses as much on those that fit it.
 template <typename T>
 void score_tiles(const ScoreArgs& a, int cus) {
     const auto tiles = [&](int64_t users, int64_t items) {
