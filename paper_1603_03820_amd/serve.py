@@ -24,7 +24,9 @@ ALS_SERVE_N_MAX = 4_194_304
 ALS_SERVE_HELD_MAX = 65_536
 EXPORTED = ("als_serve_workspace_bytes", "als_serve_init", "als_serve_destroy",
             "als_serve_last_hip_error", "als_quantize", "als_quantize_into", "als_score", "als_sample")
-_INT32_MAX = 2 ** 31 - 1       # (numbers that the library takes in 32 bits and that pass it are refused there)
+_INT32_MAX = 2 ** 31 - 1
+_FAR = 1 << 22               # row stride from which als_score does not read rows in place
+_REFUSED = ALS_SERVE_F_MAX + 1       # what the library, which takes row lengths in 32 bits, is told of all longer ones
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
@@ -237,16 +239,12 @@ def als_quantize(ctx: Context, x, users=None, q=None, scale=None, stream=None):
         ps = scale.data_ptr()
     else:
         ps = _vector(ctx, scale, "scale", _F32, rows, other)
-    rc = _lib.als_quantize_into(ctx.handle, px, _DTYPES[x.dtype], of, ldx, pu, rows, min(f, _INT32_MAX), pq, ldq,
-                                min(width, _INT32_MAX), ps, handle)
+    if f > ALS_SERVE_F_MAX:
+        f = width = _REFUSED
+    rc = _lib.als_quantize_into(ctx.handle, px, _DTYPES[x.dtype], of, ldx, pu, rows, f, pq, ldq, width, ps, handle)
     if rc:
         _check("als_quantize", rc, ctx.handle)
     return q, scale
-
-
-def _in_place(p, ld):
-    """Whether als_score reads rows where they lie (else it lays them out anew in the workspace)."""
-    return (p | ld) % 16 == 0 and ld < 1 << 22
 
 
 def als_score(ctx: Context, xq, xs, tq, ts, out=None, dtype=torch.float32, stream=None):
@@ -263,10 +261,10 @@ def als_score(ctx: Context, xq, xs, tq, ts, out=None, dtype=torch.float32, strea
     else:
         dtype = out.dtype
         po, ldo, _, _ = _matrix(ctx, out, "out", _FLOATS, m, n, other)
-    if not (_in_place(px, ldx) and _in_place(pt, ldt)):
+    if (px | ldx | pt | ldt) & 15 or ldx >= _FAR or ldt >= _FAR:      # these rows are laid out anew
         ctx._use_workspace(handle, other)
     rc = _lib.als_score(ctx.handle, px, ldx, _vector(ctx, xs, "xs", _F32, m, other), m, pt, ldt,
-                        _vector(ctx, ts, "ts", _F32, n, other), n, min(f, _INT32_MAX), po, _DTYPES[dtype], ldo, handle)
+                        _vector(ctx, ts, "ts", _F32, n, other), n, f if f <= ALS_SERVE_F_MAX else _REFUSED, po, _DTYPES[dtype], ldo, handle)
     if rc:
         _check("als_score", rc, ctx.handle)
     return out

@@ -121,7 +121,7 @@ def score(ctx, extra=0):
     return serve.als_score(ctx, q, torch.zeros(2), q, torch.zeros(2))
 
 
-def test_the_bounds_are_the_librarys():
+def test_the_bounds_are_the_librarys(lib):
     """Up to which calls do without the workspace."""
     import os
     import re
@@ -131,8 +131,16 @@ def test_the_bounds_are_the_librarys():
     source = open(os.path.join(root, "paper_1603_03820_amd", "csrc", "serve.hip")).read()
     assert "constexpr int64_t kTileStride = 1 << 22;" in source
     assert "return aligned(q, 16) && ld % 16 == 0 && ld < kTileStride;" in source
-    for p, ld, there in ((0, 16, True), (1, 16, False), (16, 17, False), (32, (1 << 22) - 16, True), (0, 1 << 22, False)):
-        assert serve._in_place(p, ld) == there
+    memory = torch.empty((1 << 23) + 64, dtype=torch.int8)
+    near = torch.zeros(2, 32, dtype=torch.int8)
+    assert memory.data_ptr() % 16 == 0 and near.data_ptr() % 16 == 0
+    for start, ld, there in ((0, 32, True), (1, 32, False), (0, 33, False), (16, (1 << 22) - 16, True), (0, 1 << 22, False)):
+        rows = torch.as_strided(memory, (2, 32), (ld, 1), start)
+        for xq, tq in ((rows, near), (near, rows)):
+            ctx = context()
+            lib.current = Stream(5)
+            serve.als_score(ctx, xq, torch.zeros(2), tq, torch.zeros(2))
+            assert (ctx.workspace.recorded == []) == there
 
 
 def test_the_workspace_is_recorded_where_it_is_used(lib):
