@@ -264,7 +264,8 @@ def als_score(ctx: Context, xq, xs, tq, ts, out=None, dtype=torch.float32, strea
     if (px | ldx | pt | ldt) & 15 or ldx >= _FAR or ldt >= _FAR:      # these rows are laid out anew
         ctx._use_workspace(handle, other)
     rc = _lib.als_score(ctx.handle, px, ldx, _vector(ctx, xs, "xs", _F32, m, other), m, pt, ldt,
-                        _vector(ctx, ts, "ts", _F32, n, other), n, f if f <= ALS_SERVE_F_MAX else _REFUSED, po, _DTYPES[dtype], ldo, handle)
+                        _vector(ctx, ts, "ts", _F32, n, other), n, f if f <= ALS_SERVE_F_MAX else _REFUSED, po,
+                        _DTYPES[dtype], ldo, handle)
     if rc:
         _check("als_score", rc, ctx.handle)
     return out
