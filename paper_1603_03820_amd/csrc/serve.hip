@@ -12,44 +12,14 @@
 // atomics, and the set that top-p keeps and the column that a uniform number meets do not depend on how a row is
 // held.  The rounding down costs a column at most 2^-40 of the best one's weight.
 
-#include <hip/hip_bf16.h>
-#include <hip/hip_fp16.h>
-#include <hip/hip_runtime.h>
-
-#include <atomic>
-#include <cmath>
-#include <cstdint>
-#include <cstring>
-#include <mutex>
 #include <new>
-#include <type_traits>
 
 #include "als_serve.h"
+#include "common.h"
 
 namespace {
 
 typedef int i4 __attribute__((ext_vector_type(4)));
-
-constexpr int kWave = 64;
-
-struct F16 { uint16_t bits; };
-struct BF16 { uint16_t bits; };
-
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(F16 v) {
-    return (float)__builtin_bit_cast(_Float16, v.bits);
-}
-__device__ __forceinline__ float to_float(BF16 v) {
-    return __builtin_bit_cast(float, (uint32_t)v.bits << 16);
-}
-// The nearest value of the type, ties to even.
-__device__ __forceinline__ void from_float(float v, float* out) { *out = v; }
-__device__ __forceinline__ void from_float(float v, F16* out) {
-    *out = F16{__builtin_bit_cast(uint16_t, (_Float16)v)};
-}
-__device__ __forceinline__ void from_float(float v, BF16* out) {
-    *out = BF16{__builtin_bit_cast(uint16_t, (__bf16)v)};
-}
 
 // ------------------------------------------------------------------------------ quantize --
 
@@ -471,16 +441,6 @@ struct Limits {
     float min_p_all;
 };
 
-// Larger scores have larger keys; -0 has +0's.
-__device__ __forceinline__ uint32_t key_of(float z) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, z + 0.f);
-    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float score_of(uint32_t key) {
-    const uint32_t b = key & 0x80000000u ? key ^ 0x80000000u : ~key;
-    return __builtin_bit_cast(float, b);
-}
-
 __device__ __forceinline__ float unit_of(float u) { return u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f; }
 
 // floor(total part / 2^24), part <= 2^24, total < 2^62.
@@ -495,10 +455,6 @@ __device__ __forceinline__ uint64_t dpp64(uint64_t v) {
     const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
     return (uint64_t)hi << 32 | lo;
 }
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t dpp32(uint32_t v) {
-    return __builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
-}
 // Inclusive sums over the wave: within rows of 16 lanes, then across rows.
 __device__ __forceinline__ uint64_t scan64(uint64_t v) {
     v += dpp64<0x111, 0xF>(v);   // row_shr:1, 2, 4, 8
@@ -508,29 +464,6 @@ __device__ __forceinline__ uint64_t scan64(uint64_t v) {
     v += dpp64<0x142, 0xA>(v);   // row_bcast:15 into rows 1 and 3
     v += dpp64<0x143, 0xC>(v);   // row_bcast:31 into rows 2 and 3
     return v;
-}
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-    v = max(v, dpp32<0x111, 0xF>(v));
-    v = max(v, dpp32<0x112, 0xF>(v));
-    v = max(v, dpp32<0x114, 0xF>(v));
-    v = max(v, dpp32<0x118, 0xF>(v));
-    v = max(v, dpp32<0x142, 0xA>(v));
-    v = max(v, dpp32<0x143, 0xC>(v));
-    return __builtin_amdgcn_readlane(v, 63);
-}
-__device__ __forceinline__ float wave_max(float v) {      // NaN-free
-    const uint32_t least = __builtin_bit_cast(uint32_t, -INFINITY);
-#define ALS_STEP(CTRL, ROWS)                                                                                        \
-    v = fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(                                             \
-                     (int)least, (int)__builtin_bit_cast(uint32_t, v), CTRL, ROWS, 0xF, false)))
-    ALS_STEP(0x111, 0xF);
-    ALS_STEP(0x112, 0xF);
-    ALS_STEP(0x114, 0xF);
-    ALS_STEP(0x118, 0xF);
-    ALS_STEP(0x142, 0xA);
-    ALS_STEP(0x143, 0xC);
-#undef ALS_STEP
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 __device__ __forceinline__ uint64_t last64(uint64_t v) {
     return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), 63) << 32 |
@@ -1048,28 +981,6 @@ struct Held {
             for (int w = 0; w < waves; ++w) p = max(p, sh->wave_c[w]);
         }
         return ~p;
-    }
-};
-
-__device__ __forceinline__ float limit_of(const float* each, float all, int64_t r) { return each ? each[r] : all; }
-
-// A row's CSR row of columns to leave out.
-struct Rated {
-    const int64_t* ptr;
-    const int32_t* idx;
-    const int32_t* users;
-    int64_t of;
-    // false: the row's user does not exist
-    __device__ __forceinline__ bool row(int64_t r, const int32_t** list, int64_t* count) const {
-        *list = nullptr;
-        *count = 0;
-        if (!ptr) return true;
-        const int64_t u = users ? (int64_t)users[r] : r;
-        if (u < 0 || u >= of) return false;
-        const int64_t first = ptr[u];
-        *list = idx + first;
-        *count = ptr[u + 1] - first;
-        return true;
     }
 };
 
@@ -2055,60 +1966,6 @@ __global__ __launch_bounds__(kRowThreads) void k_long_draw(LongArgs<T> a) {
 
 // ---------------------------------------------------------------------------------- host --
 
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-
-size_t type_bytes(int dtype) { return dtype == ALS_F32 ? 4 : 2; }
-
-// Bytes from the first element of a strided matrix to past its last.
-uint64_t span_of(int64_t rows, int64_t cols, int64_t ld, size_t bytes) {
-    return rows <= 0 || cols <= 0 ? 0 : ((uint64_t)(rows - 1) * (uint64_t)ld + (uint64_t)cols) * bytes;
-}
-
-bool overlap(const void* a, uint64_t an, const void* b, uint64_t bn) {
-    if (!a || !b || an == 0 || bn == 0) return false;
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return x < y + bn && y < x + an;
-}
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev) {
-        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-        ok = (prev == dev) || hipSetDevice(dev) == hipSuccess;
-    }
-    ~DeviceGuard() {
-        int cur = -1;
-        if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
-    }
-};
-
-// What a device is: asked for once per device and process.
-constexpr int kMaxDevices = 64;
-struct DeviceInfo {
-    std::mutex mu;
-    bool known = false;
-    int cus = 0;
-};
-DeviceInfo g_device[kMaxDevices];
-
-int query_device(int device, int* cus) {
-    int count = 0;
-    if (hipGetDeviceCount(&count) != hipSuccess || device < 0 || device >= count || device >= kMaxDevices)
-        return ALS_ERR_DEVICE;
-    DeviceInfo& d = g_device[device];
-    std::lock_guard<std::mutex> lock(d.mu);
-    if (!d.known) {
-        hipDeviceProp_t prop;
-        if (hipGetDeviceProperties(&prop, device) != hipSuccess) return ALS_ERR_DEVICE;
-        if (strncmp(prop.gcnArchName, "gfx950", 6) != 0) return ALS_ERR_DEVICE;
-        d.cus = prop.multiProcessorCount;
-        d.known = true;
-    }
-    *cus = d.cus;
-    return ALS_OK;
-}
-
 constexpr size_t kWorkspaceBytes = 128u << 20, kWorkspaceMost = (size_t)1 << 34;   // (what a launch can walk)
 
 }  // namespace
@@ -2122,22 +1979,6 @@ struct als_serve_ctx {
 };
 
 namespace {
-
-// Lets a kernel use all of a CU's LDS; once per kernel and device.
-template <typename Kernel>
-void whole_lds(Kernel kernel, int device, std::atomic<uint64_t>* done) {
-    if (done->load(std::memory_order_acquire) >> device & 1) return;
-    if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess)
-        done->fetch_or(1ull << device, std::memory_order_release);
-}
-
-// A launch counts its threads in 32 bits: one of 2^32 or more fails or, worse, runs only what is left of the count and
-// reports nothing.  fn(first, count) for parts of `total` rows, `most` at a time.
-constexpr int64_t kMaxThreads = UINT32_MAX;
-template <typename Fn>
-void in_parts(int64_t total, int64_t most, Fn fn) {
-    for (int64_t first = 0; first < total; first += most) fn(first, total - first < most ? total - first : most);
-}
 
 struct ScoreArgs {
     const int8_t* xq;
