@@ -38,16 +38,19 @@ def hipcc() -> str:
 # the operators that answer with a trained model (include/als_serve.h): a library of its own
 SERVE_SRC = os.path.join(PKG, "csrc", "serve.hip")
 SERVE_LIB = os.path.join(PKG, "libals_serve.so")
+# the operators that say how probable items are (include/als_predict.h): a third one
+PREDICT_SRC = os.path.join(PKG, "csrc", "predict.hip")
+PREDICT_LIB = os.path.join(PKG, "libals_predict.so")
 PEAKS_SRC = os.path.join(PKG, "csrc", "peaks.hip")
 PEAKS_LIB = os.path.join(PKG, "libpeaks.so")
 
 
 def build(verbose: bool = False) -> str:
-    """Compile libals.so, libals_serve.so and the bench's peak microbenchmarks (libpeaks.so) unconditionally
-    (the build check compiles every time); return the libals.so path."""
-    with ThreadPoolExecutor(3) as pool:      # each waits for a compiler of its own
+    """Compile libals.so, libals_serve.so, libals_predict.so and the bench's peak microbenchmarks (libpeaks.so)
+    unconditionally (the build check compiles every time); return the libals.so path."""
+    with ThreadPoolExecutor(4) as pool:      # each waits for a compiler of its own
         jobs = [pool.submit(_compile, src, lib, verbose)
-                for src, lib in ((PEAKS_SRC, PEAKS_LIB), (SERVE_SRC, SERVE_LIB), (SRC, LIB))]
+                for src, lib in ((PEAKS_SRC, PEAKS_LIB), (PREDICT_SRC, PREDICT_LIB), (SERVE_SRC, SERVE_LIB), (SRC, LIB))]
         return [j.result() for j in jobs][-1]
 
 

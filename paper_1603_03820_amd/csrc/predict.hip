@@ -1,0 +1,1207 @@
+// How probable items are under a trained factor model, on gfx950 (MI355X): the C ABI of include/als_predict.h plus its
+// kernels.
+//
+//   k_product     predictions from rows of any alignment, which pass through registers into LDS; fp32 rows as three bf16
+//                 parts (k_join: the products' parts along f into one, where few tiles are cut along it)
+//   k_row         a row of scores, or a segment of one, as a distribution: statistics, given columns, best columns
+//                 (k_row_join: a row's segments into one)
+//   k_gradient    the gradient with respect to scores and offsets (k_columns: the offsets' from its parts)
+
+#include <new>
+
+#include "als_predict.h"
+#include "common.h"
+
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+// ------------------------------------------------------------------------------- product --
+
+// What follows a product: its offsets, activation and residual, and where it goes.
+struct Epilogue {
+    const float* user_offset;
+    const float* item_offset;
+    const void* residual;
+    int64_t ldr;
+    void* out;
+    int64_t ldo;
+    float low, high;
+    int activation;
+    int type;      // of residual and out
+};
+
+struct Product {
+    const void* x;
+    int64_t of, ldx;
+    const int32_t* users;
+    int64_t m;
+    const void* theta;
+    int64_t n, ldt;
+    int f;
+    uint32_t tu, ti;         // tiles of users and of items
+    int steps;               // along f in one part of it
+    Epilogue end;
+    float* parts;            // where f is cut: parts x m x n sums; else NULL
+
+    // The row of X that row i of the result is for; -1: there is none.
+    __device__ __forceinline__ int64_t user_of(int64_t i) const {
+        const int64_t u = users ? (int64_t)users[i] : i;
+        return u >= 0 && u < of ? u : -1;
+    }
+};
+
+// GELU by erfc, which keeps its relative precision for negative y, where 1 + erf(y) does not.  The bounds below
+// are past where either function is -0 in fp32, and keep -inf from meeting its 0.
+__device__ __forceinline__ float activated(float y, const Epilogue& e) {
+    switch (e.activation) {
+        case ALS_ACT_CLIP: y = y < e.low ? e.low : y; return y > e.high ? e.high : y;
+        case ALS_ACT_RELU: return y < 0.f ? 0.f : y;
+        case ALS_ACT_GELU: y = y < -30.f ? -30.f : y; return 0.5f * y * erfcf(y * -0.70710678f);
+        case ALS_ACT_SILU: y = y < -200.f ? -200.f : y; return y / (1.f + expf(-y));
+        case ALS_ACT_SIGMOID: return 1.f / (1.f + expf(-y));
+        case ALS_ACT_TANH: return tanhf(y);
+        default: return y;
+    }
+}
+
+// Four neighbouring values of a row, as far as `left` of them are there.
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, int64_t left, float (&v)[4]) {
+    T t[4];
+    if (left >= 4) {
+        __builtin_memcpy(t, p, sizeof t);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = to_float(t[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < left ? to_float(p[i]) : 0.f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, int64_t left, const float (&v)[4]) {
+    T t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) from_float(v[i], &t[i]);
+    if (left >= 4) {
+        __builtin_memcpy(p, t, sizeof t);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) p[i] = t[i];
+    }
+}
+
+// Four neighbouring results of user i from their sums (a user that there is not: NaN), `left` of them to write.
+__device__ __forceinline__ void finish4(const Product& a, int64_t i, int64_t item, float (&v)[4], const float (&offset)[4]) {
+    const Epilogue& e = a.end;
+    const int64_t u = a.user_of(i), left = a.n - item;
+    const float own = u < 0 ? NAN : (e.user_offset ? e.user_offset[u] : 0.f);
+    float r[4] = {0.f, 0.f, 0.f, 0.f};
+    if (e.residual) {
+        const int64_t at = i * e.ldr + item;
+        if (e.type == ALS_F32) load4((const float*)e.residual + at, left, r);
+        else if (e.type == ALS_F16) load4((const F16*)e.residual + at, left, r);
+        else load4((const BF16*)e.residual + at, left, r);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = activated(v[k] + own + offset[k], e) + r[k];
+    const int64_t at = i * e.ldo + item;
+    if (e.type == ALS_F32) store4((float*)e.out + at, left, v);
+    else if (e.type == ALS_F16) store4((F16*)e.out + at, left, v);
+    else store4((BF16*)e.out + at, left, v);
+}
+
+// Tile t of a grid of tu x ti: the eight dies take workgroups in turn, so each gets a run of tiles of its own, and
+// runs go down eight tiles of users before the next of items (their rows stay in the die's L2).
+__device__ __forceinline__ void tile_of(uint32_t t, uint32_t tu, uint32_t ti, uint32_t* u, uint32_t* i) {
+    const uint32_t total = tu * ti, per = total / 8;
+    if (t < per * 8) t = (t % 8) * per + t / 8;
+    const uint32_t band = 8 * ti, b = t / band, left = t % band;
+    const uint32_t high = tu - 8 * b < 8 ? tu - 8 * b : 8;
+    *u = 8 * b + left % high;
+    *i = left / high;
+}
+
+// Matrix instructions of eight values a lane, by the type of the parts that are multiplied.
+__device__ __forceinline__ f4 multiply8(u4 a, u4 b, f4 c, BF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f4 multiply8(u4 a, u4 b, f4 c, F16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+
+// A type's rows as they are multiplied: `kParts` parts of 16 bits a value.
+template <typename T>
+struct Parts {
+    static constexpr int kParts = 1;
+    static constexpr int kValues = 64;       // of a row in a step
+    using Part = T;
+    // eight values, zeros past `left`
+    static __device__ __forceinline__ void load(const T* p, int left, u4 (&v)[1]) {
+        if (left >= 8) {
+            __builtin_memcpy(&v[0], p, 16);
+        } else {
+            uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) w[i / 2] |= (uint32_t)p[i].bits << (i % 2 * 16);
+            v[0] = u4{w[0], w[1], w[2], w[3]};
+        }
+    }
+    static __device__ __forceinline__ void split(const u4 (&raw)[1], u4 (&part)[1]) { part[0] = raw[0]; }
+    static constexpr int kRaw = 1;
+};
+
+__device__ __forceinline__ uint32_t two_bf16(float a, float b) {
+    BF16 t[2];
+    from_float(a, &t[0]);
+    from_float(b, &t[1]);
+    return (uint32_t)t[0].bits | (uint32_t)t[1].bits << 16;
+}
+
+template <>
+struct Parts<float> {
+    static constexpr int kParts = 3;
+    static constexpr int kValues = 32;
+    using Part = BF16;
+    static constexpr int kRaw = 2;
+    static __device__ __forceinline__ void load(const float* p, int left, u4 (&v)[2]) {
+        if (left >= 8) {
+            __builtin_memcpy(v, p, 32);
+        } else {
+            float w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = i < left ? p[i] : 0.f;
+            __builtin_memcpy(v, w, 32);
+        }
+    }
+    // x = high + mid + low: the upper 16 bits of x (cut off, so that the largest floats stay finite), then what is left
+    // rounded to bf16 twice; |mid| < 2^-7 |x|, |low| <= 2^-16 |x|, and what is left after it is 0.
+    static __device__ __forceinline__ void split(const u4 (&raw)[2], u4 (&part)[3]) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const uint32_t b0 = raw[w / 2][w % 2 * 2], b1 = raw[w / 2][w % 2 * 2 + 1];
+            part[0][w] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+            const float r0 = __builtin_bit_cast(float, b0) - __builtin_bit_cast(float, b0 & 0xFFFF0000u);
+            const float r1 = __builtin_bit_cast(float, b1) - __builtin_bit_cast(float, b1 & 0xFFFF0000u);
+            const uint32_t mid = two_bf16(r0, r1);
+            part[1][w] = mid;
+            part[2][w] = two_bf16(r0 - __builtin_bit_cast(float, mid << 16),
+                                  r1 - __builtin_bit_cast(float, mid & 0xFFFF0000u));
+        }
+    }
+};
+
+template <typename T, int WU, int WI, int FU, int FI>
+struct Staged {
+    using P = Parts<T>;
+    static constexpr int kThreads = 64 * WU * WI;
+    static constexpr int kUsers = WU * FU * 16, kItems = WI * FI * 16, kRows = kUsers + kItems;
+    static constexpr int kRowBytes = 2 * P::kValues, kGroups = P::kValues / 8;      // of a part of a row
+    static constexpr int kPart = kRows * kRowBytes, kStage = P::kParts * kPart;
+    static constexpr int kUnits = kRows * kGroups, kLoads = (kUnits + kThreads - 1) / kThreads;
+    // the way out: so many fragments of users at a time, rows of items four values apart from one bank
+    static constexpr int kOut = FU < 2 ? 1 : 2, kOutRows = WU * kOut * 16, kOutStride = kItems + 4;
+    static constexpr int kLds = kStage > kOutRows * kOutStride * 4 ? kStage : kOutRows * kOutStride * 4;
+    static_assert(FU % kOut == 0, "whole passes");
+};
+
+// The products of a tile on their way out, through LDS, so that a wave writes whole lines and what follows a product
+// is there once in the code.  A lane holds four neighbouring items (of group lane / 16) of one user (lane % 16).
+template <typename C, int WU, int WI, int FU, int FI>
+__device__ __forceinline__ void write_tile(const Product& a, const f4 (&acc)[FU][FI], float* lds, int64_t u0, int64_t i0,
+                                           int wu, int wi, int part) {
+    const int lane = threadIdx.x & 63;
+    constexpr int kFours = C::kItems / 4, kAtOnce = C::kThreads / kFours;
+    const int four = threadIdx.x % kFours, first = threadIdx.x / kFours;
+    const int64_t item = i0 + 4 * four;
+    float offset[4] = {0.f, 0.f, 0.f, 0.f};
+    if (a.end.item_offset && !a.parts) load4(a.end.item_offset + item, a.n - item, offset);
+#pragma unroll
+    for (int pass = 0; pass < FU / C::kOut; ++pass) {
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < C::kOut; ++u)
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+                *(f4*)(lds + ((wu * C::kOut + u) * 16 + (lane & 15)) * C::kOutStride + (wi * FI + i) * 16 + 4 * (lane >> 4)) =
+                    acc[pass * C::kOut + u][i];
+        __syncthreads();
+        for (int r = first; r < C::kOutRows; r += kAtOnce) {
+            const int64_t user = u0 + (r / (16 * C::kOut) * FU + pass * C::kOut) * 16 + r % (16 * C::kOut);
+            if (user >= a.m || item >= a.n) continue;
+            const f4 s = *(const f4*)(lds + r * C::kOutStride + 4 * four);
+            float v[4] = {s[0], s[1], s[2], s[3]};
+            if (a.parts) store4(a.parts + ((int64_t)part * a.m + user) * a.n + item, a.n - item, v);
+            else finish4(a, user, item, v, offset);
+        }
+    }
+}
+
+// The product in tiles, rows through registers: a workgroup of WU x WI waves holds a tile of users x items, each wave
+// FU x FI fragments of 16 x 16, and walks f in steps of 32 fp32 or 64 16-bit values.  While a step is multiplied
+// from LDS the next one's rows arrive in registers; fp32 values are split there, once for all that they meet.
+// The 16-byte group c of a part of row r lies in slot c ^ s(r), so that the 16 rows of an operand read spread
+// over all banks: s is r / 4 % 4 for rows of 64 bytes, r / 2 % 8 for 128.
+template <typename T, int WU, int WI, int FU, int FI>
+__global__ __launch_bounds__(64 * WU * WI) void k_product(Product a) {
+    using C = Staged<T, WU, WI, FU, FI>;
+    using P = Parts<T>;
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t tile_u, tile_i;
+    tile_of(blockIdx.x, a.tu, a.ti, &tile_u, &tile_i);
+    const int64_t u0 = (int64_t)tile_u * C::kUsers, i0 = (int64_t)tile_i * C::kItems;
+    const auto slot = [](int r, int g) { return C::kRowBytes == 64 ? g ^ (r >> 2 & 3) : g ^ (r >> 1 & 7); };
+
+    // this thread's groups of eight values: a row each, at the same place in every step
+    const T* from[C::kLoads];
+    int to[C::kLoads];
+    int at[C::kLoads];
+#pragma unroll
+    for (int l = 0; l < C::kLoads; ++l) {
+        const int unit = threadIdx.x + l * C::kThreads, r = unit / C::kGroups, g = unit % C::kGroups;
+        from[l] = nullptr;
+        at[l] = 8 * g;
+        to[l] = unit < C::kUnits ? r * C::kRowBytes + 16 * slot(r, g) : -1;
+        if (r < C::kUsers) {
+            const int64_t u = u0 + r < a.m ? a.user_of(u0 + r) : -1;
+            if (u >= 0) from[l] = (const T*)a.x + u * a.ldx;
+        } else if (unit < C::kUnits && i0 + r - C::kUsers < a.n) {
+            from[l] = (const T*)a.theta + (i0 + r - C::kUsers) * a.ldt;
+        }
+    }
+    u4 raw[C::kLoads][P::kRaw];
+    const auto fetch = [&](int step) {
+#pragma unroll
+        for (int l = 0; l < C::kLoads; ++l) {
+            const int k = step * P::kValues + at[l];
+            P::load(from[l] + k, from[l] ? a.f - k : 0, raw[l]);
+        }
+    };
+    const auto stage = [&]() {
+#pragma unroll
+        for (int l = 0; l < C::kLoads; ++l) {
+            u4 part[P::kParts];
+            P::split(raw[l], part);
+            if (to[l] < 0) continue;
+#pragma unroll
+            for (int p = 0; p < P::kParts; ++p) *(u4*)(lds + p * C::kPart + to[l]) = part[p];
+        }
+    };
+
+    const int wu = wave / WI, wi = wave % WI, row = lane & 15, group = lane >> 4;
+    f4 acc[FU][FI];
+#pragma unroll
+    for (int u = 0; u < FU; ++u)
+#pragma unroll
+        for (int i = 0; i < FI; ++i) acc[u][i] = f4{0.f, 0.f, 0.f, 0.f};
+    const auto read = [&](int r, int h, u4 (&v)[P::kParts]) {
+#pragma unroll
+        for (int p = 0; p < P::kParts; ++p)
+            v[p] = *(const u4*)(lds + p * C::kPart + r * C::kRowBytes + 16 * slot(r, 4 * h + group));
+    };
+    const auto multiply = [&]() {
+#pragma unroll
+        for (int h = 0; h < P::kValues / 32; ++h) {
+            u4 t[FI][P::kParts];
+#pragma unroll
+            for (int i = 0; i < FI; ++i) read(C::kUsers + (wi * FI + i) * 16 + row, h, t[i]);
+#pragma unroll
+            for (int u = 0; u < FU; ++u) {
+                u4 x[P::kParts];
+                read((wu * FU + u) * 16 + row, h, x);
+                // the smallest products first; of nine, those of mid x low and below are left out
+                const auto add = [&](int p, int q) {
+#pragma unroll
+                    for (int i = 0; i < FI; ++i) acc[u][i] = multiply8(t[i][p], x[q], acc[u][i], typename P::Part());
+                };
+                if constexpr (P::kParts == 3) {
+                    add(2, 0);
+                    add(0, 2);
+                    add(1, 1);
+                    add(1, 0);
+                    add(0, 1);
+                }
+                add(0, 0);
+            }
+        }
+    };
+
+    const int steps = (a.f + P::kValues - 1) / P::kValues, begin = blockIdx.y * a.steps;
+    const int end = begin + a.steps < steps ? begin + a.steps : steps;
+    fetch(begin);
+    for (int step = begin; step < end; ++step) {
+        stage();
+        __syncthreads();
+        if (step + 1 < end) fetch(step + 1);
+        multiply();
+        if (step + 1 < end) __syncthreads();
+    }
+    write_tile<C, WU, WI, FU, FI>(a, acc, (float*)lds, u0, i0, wu, wi, blockIdx.y);
+}
+
+// The sums of the parts of f into one, in their order, and what follows a product.
+__global__ __launch_bounds__(256) void k_join(Product a, int count, int64_t row0) {
+    const int64_t fours = (a.n + 3) / 4, at = row0 * fours + (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t i = at / fours, item = at % fours * 4;
+    if (i >= a.m) return;
+    float v[4], offset[4] = {0.f, 0.f, 0.f, 0.f};
+    load4(a.parts + i * a.n + item, a.n - item, v);
+    for (int p = 1; p < count; ++p) {
+        float w[4];
+        load4(a.parts + (p * a.m + i) * a.n + item, a.n - item, w);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] += w[k];
+    }
+    if (a.end.item_offset) load4(a.end.item_offset + item, a.n - item, offset);
+    finish4(a, i, item, v, offset);
+}
+
+// --------------------------------------------------------------------------- distribution --
+
+__device__ __forceinline__ float wave_sum(float v) {
+#define ALS_STEP(CTRL, ROWS) v += __builtin_bit_cast(float, dpp32<CTRL, ROWS>(__builtin_bit_cast(uint32_t, v)))
+    ALS_STEP(0x111, 0xF);
+    ALS_STEP(0x112, 0xF);
+    ALS_STEP(0x114, 0xF);
+    ALS_STEP(0x118, 0xF);
+    ALS_STEP(0x142, 0xA);
+    ALS_STEP(0x143, 0xC);
+#undef ALS_STEP
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
+constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147181f;
+constexpr float kNothing = -200.f;       // 2 to it is 0 in fp32
+
+// Some scores' best one, their weights' sum and the sum of weight times exponent; weights are 2^((z - best) c),
+// c = log2(e) / T.
+struct Mass {
+    float best, sum, spread;
+};
+
+// (z - best) c, from -200 up; what is not a number (NaN scores, +inf less +inf) weighs nothing
+__device__ __forceinline__ float exponent(float z, float best, float c) { return fmaxf((z - best) * c, kNothing); }
+
+// The masses that the wave's lanes hold as one (best -inf, sums 0: nothing).
+__device__ __forceinline__ Mass joined(Mass a, float c) {
+    Mass all;
+    all.best = wave_max(a.best);
+    const float x = a.best == all.best ? 0.f : exponent(a.best, all.best, c);
+    const float w = exp2f(x) * a.sum;
+    all.sum = wave_sum(w);
+    all.spread = wave_sum(exp2f(x) * a.spread + w * x);
+    return all;
+}
+
+// log2(e) / T, finite.
+__device__ __forceinline__ float rate_of(float t) { return fminf((float)(1.4426950408889634 / (double)t), 3.402823466e38f); }
+
+// A row's distribution as its results need it.
+struct Law {
+    float best, t, size;     // size: log of the weights' sum
+    uint32_t first;          // the first best column, where T is not above 0 (else unused)
+    bool there;              // the row's user exists
+    __device__ __forceinline__ bool greedy() const { return !(t > 0.f); }
+    __device__ __forceinline__ bool none() const { return best == -INFINITY; }
+    // log p of an allowed column
+    __device__ __forceinline__ float log_of(float z, uint32_t column) const {
+        if (!there) return NAN;
+        if (!(z > -INFINITY)) return -INFINITY;
+        if (greedy()) return column == first ? 0.f : -INFINITY;
+        const float d = z - best;
+        return z == best ? -size : (d > -INFINITY ? d / t - size : -INFINITY);
+    }
+};
+
+template <typename T>
+struct RowArgs {
+    const T* z;
+    int64_t row0, rows, n, ldz;
+    const float* temperature;
+    float temperature_all;
+    Rated rated;
+    als_given given;
+    float* log;
+    float* stats;
+    float* entropy;
+    int top;
+    int32_t* top_index;
+    float* top_log;
+    // rows in segments
+    uint32_t segments, columns;     // of a row; of a segment
+    struct SegMass* mass;           // rows x segments
+    uint64_t* keys;                 // rows x segments x top
+
+    __device__ __forceinline__ void entries(int64_t r, int64_t* begin, int64_t* end) const {
+        if (given.ptr) {
+            const int64_t b = given.ptr[r], e = given.ptr[r + 1];
+            *begin = b < 0 ? 0 : b;
+            *end = e > given.entries ? given.entries : e;
+        } else {
+            *begin = r * given.each;
+            *end = *begin + given.each;
+        }
+    }
+};
+
+struct SegMass {
+    Mass mass;
+    uint32_t first;
+};
+
+// Order of columns: higher scores first, then lower columns; 0 is no column.
+__device__ __forceinline__ uint64_t place_of(float z, uint32_t column) {
+    return z > -INFINITY ? (uint64_t)key_of(z) << 32 | (0xFFFFFFFFu - column) : 0;
+}
+__device__ __forceinline__ float score_at(uint64_t place) { return score_of((uint32_t)(place >> 32)); }
+__device__ __forceinline__ uint32_t column_at(uint64_t place) { return 0xFFFFFFFFu - (uint32_t)place; }
+
+__device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        const uint64_t o = (uint64_t)__shfl_xor((unsigned long long)v, d);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+
+constexpr int kMaxWaves = 16;
+constexpr int kList = 1024;
+
+struct RowShared {
+    Mass mass[kMaxWaves];
+    uint64_t place[kMaxWaves];
+    uint32_t first;
+};
+
+// The first `top` places in their order: emit(rank, place) for each, by some thread; how many there are is the result.
+// `below(limit)` is the best of this thread's places below a limit.
+template <typename Below, typename Emit>
+__device__ __forceinline__ int best_places(int top, RowShared* sh, Below below, Emit emit) {
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    uint64_t limit = ~0ull;
+    int found = 0;
+    for (; found < top; ++found) {
+        uint64_t p = wave_max64(below(limit));
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) sh->place[wave] = p;
+        __syncthreads();
+        for (int w = 0; w < waves; ++w) p = sh->place[w] > p ? sh->place[w] : p;
+        if (p == 0) break;
+        if (threadIdx.x == 0) emit(found, p);
+        limit = p;
+    }
+    return found;
+}
+
+// What a row's distribution gives, but its log p of given columns; called by all of the workgroup's threads.
+template <typename T>
+__device__ __forceinline__ void write_law(const RowArgs<T>& a, int64_t r, const Law& law, const Mass& mass) {
+    if (threadIdx.x != 0) return;
+    if (a.stats) {
+        const bool as_is = law.there && !law.none();
+        a.stats[2 * r] = law.there ? law.best : NAN;
+        a.stats[2 * r + 1] = as_is ? (law.greedy() ? 0.f : law.size) : (law.there ? -INFINITY : NAN);
+    }
+    if (a.entropy) {
+        float h = law.size - kLn2 * (mass.spread / mass.sum);
+        if (law.none() || law.greedy()) h = 0.f;
+        a.entropy[r] = law.there ? h : NAN;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void write_top(const RowArgs<T>& a, int64_t r, const Law& law, int rank, uint64_t place) {
+    if (a.top_index) a.top_index[r * a.top + rank] = law.there ? (int32_t)column_at(place) : -1;
+    if (a.top_log) a.top_log[r * a.top + rank] = law.log_of(score_at(place), column_at(place));
+}
+template <typename T>
+__device__ __forceinline__ void write_no_top(const RowArgs<T>& a, int64_t r, const Law& law, int from) {
+    for (int k = from + threadIdx.x; k < a.top; k += blockDim.x) {
+        if (a.top_index) a.top_index[r * a.top + k] = -1;
+        if (a.top_log) a.top_log[r * a.top + k] = law.there ? -INFINITY : NAN;
+    }
+}
+
+// A row, or a segment of one, of up to E scores a thread, which stay in registers from their one read on.
+template <typename T, int E>
+__global__ __launch_bounds__(1024) void k_row(RowArgs<T> a) {
+    constexpr int V = E * sizeof(T) < 16 ? E : 16 / sizeof(T);
+    __shared__ RowShared sh;
+    extern __shared__ uint32_t bits[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const uint32_t segment = blockIdx.x % a.segments;
+    const int64_t local = blockIdx.x / a.segments, r = a.row0 + local;
+    const uint32_t base = segment * a.columns;
+    const uint32_t n = (uint32_t)a.n - base < a.columns ? (uint32_t)a.n - base : a.columns;
+    const T* row = a.z + r * a.ldz + base;
+    const auto position = [&](int v) { return (uint32_t)(v * blockDim.x + threadIdx.x) * V; };
+
+    float z[E];
+#pragma unroll
+    for (int v = 0; v < E / V; ++v) {
+        const uint32_t c = position(v);
+        T t[V];
+        if (c + V <= n) {
+            __builtin_memcpy(t, row + c, sizeof t);
+#pragma unroll
+            for (int i = 0; i < V; ++i) z[v * V + i] = to_float(t[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) z[v * V + i] = c + i < n ? to_float(row[c + i]) : -INFINITY;
+        }
+    }
+    const int32_t* list;
+    int64_t listed;
+    Law law;
+    law.there = a.rated.row(r, &list, &listed);
+    law.t = limit_of(a.temperature, a.temperature_all, r);
+    const bool some = law.there && listed > 0;
+    if (threadIdx.x == 0) sh.first = ~0u;
+    if (some) {
+        for (uint32_t w = threadIdx.x; w < (n + 31) / 32; w += blockDim.x) bits[w] = 0;
+        __syncthreads();
+        for (int64_t k = threadIdx.x; k < listed; k += blockDim.x) {
+            const uint32_t c = (uint32_t)list[k] - base;
+            if (c < n) atomicOr(&bits[c >> 5], 1u << (c & 31));
+        }
+    }
+    __syncthreads();
+    const auto left_out = [&](uint32_t c) { return some && (bits[c >> 5] >> (c & 31) & 1); };
+    if (some) {
+#pragma unroll
+        for (int v = 0; v < E / V; ++v) {
+            const uint32_t c = position(v);
+            if (c >= n) continue;
+            const uint32_t w = bits[c >> 5] >> (c & 31);      // V divides 32
+#pragma unroll
+            for (int i = 0; i < V; ++i) z[v * V + i] = w >> i & 1 ? -INFINITY : z[v * V + i];
+        }
+    }
+
+    const float c = law.greedy() ? 1.f : rate_of(law.t);
+    Mass mass{-INFINITY, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < E; ++e) mass.best = fmaxf(mass.best, z[e]);
+    mass.best = wave_max(mass.best);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const float x = exponent(z[e], mass.best, c), w = exp2f(x);
+        mass.sum += w;
+        mass.spread = fmaf(w, x, mass.spread);
+    }
+    if (mass.best == INFINITY) {
+        mass.sum = mass.spread = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) mass.sum += z[e] == INFINITY ? 1.f : 0.f;
+    }
+    mass.sum = wave_sum(mass.sum);
+    mass.spread = wave_sum(mass.spread);
+    if (lane == 0) sh.mass[wave] = mass;
+    __syncthreads();
+    mass = joined(lane < waves ? sh.mass[lane] : Mass{-INFINITY, 0.f, 0.f}, c);
+    law.best = mass.best;
+    law.size = logf(mass.sum);
+    if (law.greedy()) {
+        uint32_t first = ~0u;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (z[e] == mass.best && z[e] > -INFINITY) {
+                const uint32_t at = position(e / V) + e % V;
+                first = at < first ? at : first;
+            }
+        if (first != ~0u) atomicMin(&sh.first, base + first);
+        __syncthreads();
+    }
+    law.first = sh.first;
+
+    const bool whole = a.segments == 1;
+    int64_t begin, end;
+    a.entries(r, &begin, &end);
+    for (int64_t e = begin + threadIdx.x; e < end; e += blockDim.x) {
+        const uint32_t column = (uint32_t)a.given.idx[e], at = column - base;
+        if (at < n) {
+            const float s = to_float(row[at]), v = left_out(at) ? -INFINITY : s;
+            a.log[e] = whole ? law.log_of(v, column) : v;
+        } else if (column >= (uint32_t)a.n && segment == 0) {
+            a.log[e] = law.there ? -INFINITY : NAN;
+        }
+    }
+    const auto below = [&](uint64_t limit) {
+        uint64_t best = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint64_t p = place_of(z[e], base + position(e / V) + e % V);
+            best = p < limit && p > best ? p : best;
+        }
+        return best;
+    };
+    if (whole) {
+        write_law(a, r, law, mass);
+        if (a.top == 0) return;
+        const int found = best_places(a.top, &sh, below, [&](int k, uint64_t p) { write_top(a, r, law, k, p); });
+        write_no_top(a, r, law, found);
+    } else {
+        const int64_t part = local * a.segments + segment;
+        if (threadIdx.x == 0) a.mass[part] = SegMass{mass, law.first};
+        if (a.top == 0) return;
+        uint64_t* keys = a.keys + part * a.top;
+        const int found = best_places(a.top, &sh, below, [&](int k, uint64_t p) { keys[k] = p; });
+        for (int k = found + threadIdx.x; k < a.top; k += blockDim.x) keys[k] = 0;
+    }
+}
+
+// A row's segments into one.
+constexpr int kJoinThreads = 256;
+template <typename T>
+__global__ __launch_bounds__(kJoinThreads) void k_row_join(RowArgs<T> a) {
+    __shared__ RowShared sh;
+    const int64_t local = blockIdx.x, r = a.row0 + local;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int32_t* list;
+    int64_t listed;
+    Law law;
+    law.there = a.rated.row(r, &list, &listed);
+    law.t = limit_of(a.temperature, a.temperature_all, r);
+    const float c = law.greedy() ? 1.f : rate_of(law.t);
+    if (threadIdx.x == 0) sh.first = ~0u;
+    Mass mass{-INFINITY, 0.f, 0.f};
+    uint32_t first = ~0u;
+    if (threadIdx.x < a.segments) {
+        const SegMass s = a.mass[local * a.segments + threadIdx.x];
+        mass = s.mass;
+        first = s.first;
+    }
+    const float own = mass.best;
+    mass = joined(mass, c);
+    if (lane == 0) sh.mass[wave] = mass;
+    __syncthreads();
+    mass = joined(lane < kJoinThreads / 64 ? sh.mass[lane] : Mass{-INFINITY, 0.f, 0.f}, c);
+    law.best = mass.best;
+    law.size = logf(mass.sum);
+    if (law.greedy()) {
+        if (own == mass.best && first != ~0u) atomicMin(&sh.first, first);
+        __syncthreads();
+    }
+    law.first = sh.first;
+    int64_t begin, end;
+    a.entries(r, &begin, &end);
+    for (int64_t e = begin + threadIdx.x; e < end; e += blockDim.x) {
+        const uint32_t column = (uint32_t)a.given.idx[e];
+        if (column < (uint32_t)a.n) a.log[e] = law.log_of(a.log[e], column);
+    }
+    write_law(a, r, law, mass);
+    if (a.top == 0) return;
+    const uint64_t* keys = a.keys + local * a.segments * a.top;
+    const uint32_t count = a.segments * a.top;
+    const auto below = [&](uint64_t limit) {
+        uint64_t best = 0;
+        for (uint32_t k = threadIdx.x; k < count; k += blockDim.x) {
+            const uint64_t p = keys[k];
+            best = p < limit && p > best ? p : best;
+        }
+        return best;
+    };
+    const int found = best_places(a.top, &sh, below, [&](int k, uint64_t p) { write_top(a, r, law, k, p); });
+    write_no_top(a, r, law, found);
+}
+
+// ------------------------------------------------------------------------------- gradient --
+
+template <typename T>
+struct GradArgs {
+    RowArgs<T> of;               // (log, stats and entropy are inputs here)
+    const float* grad_log;
+    const float* grad_entropy;
+    T* grad;
+    int64_t ldg;
+    float* parts;                // groups x n sums of rows, or NULL
+    uint32_t chunks, groups;     // of a row's columns; of rows
+};
+
+constexpr int kGradThreads = 256, kGradEach = 8, kGradWave = kWave * kGradEach;
+constexpr int kGradChunk = kGradThreads * kGradEach;
+
+// A wave's 512 columns of a row, and of the rows that follow it `groups` apart.  Each wave looks through the row's lists
+// for itself: what lies in its columns goes to the lane that has it, in the lists' order, so that sums of repeated columns
+// are the same on every run, and no wave waits for another.
+template <typename T>
+__global__ __launch_bounds__(kGradThreads) void k_gradient(GradArgs<T> g) {
+    constexpr int E = kGradEach, V = 16 / sizeof(T);
+    const RowArgs<T>& a = g.of;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t chunk = blockIdx.x % g.chunks, group = blockIdx.x / g.chunks;
+    const uint32_t base = chunk * kGradChunk + wave * kGradWave, n = (uint32_t)a.n;
+    if (base >= n) return;
+    const auto position = [&](int v) { return base + (uint32_t)(v * kWave + lane) * V; };
+    float total[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) total[e] = 0.f;
+    for (int64_t r = group; r < a.rows; r += g.groups) {
+        const T* row = a.z + r * a.ldz;
+        float z[E];
+#pragma unroll
+        for (int v = 0; v < E / V; ++v) {
+            const uint32_t c = position(v);
+            T t[V];
+            if (c + V <= n) {
+                __builtin_memcpy(t, row + c, sizeof t);
+#pragma unroll
+                for (int i = 0; i < V; ++i) z[v * V + i] = to_float(t[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) z[v * V + i] = c + i < n ? to_float(row[c + i]) : -INFINITY;
+            }
+        }
+        const int32_t* list;
+        int64_t listed;
+        const bool there = a.rated.row(r, &list, &listed);
+        const float t = limit_of(a.temperature, a.temperature_all, r);
+        const float best = a.stats[2 * r], size = a.stats[2 * r + 1];
+        float d[E];
+        if (there && t > 0.f && best > -INFINITY) {
+            // the owner of a column, and its place there
+            const auto owner_of = [&](uint32_t at, int* owner, int* e) {
+                *owner = at / V % kWave;
+                *e = at / (V * kWave) * V + at % V;
+            };
+            uint32_t out = 0;
+            for (int64_t k0 = 0; k0 < listed; k0 += kWave) {
+                const uint32_t at = k0 + lane < listed ? (uint32_t)list[k0 + lane] - base : ~0u;
+                uint64_t in = __ballot(at < kGradWave);
+                while (in) {
+                    const int l = __builtin_ctzll(in);
+                    in &= in - 1;
+                    int owner, e;
+                    owner_of(__builtin_amdgcn_readlane(at, l), &owner, &e);
+                    if (lane == owner) out |= 1u << e;
+                }
+            }
+            int64_t begin, end;
+            a.entries(r, &begin, &end);
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] = 0.f;
+            for (int64_t k0 = begin; k0 < end; k0 += kWave) {
+                uint32_t at = ~0u;
+                float w = 0.f;
+                if (k0 + lane < end && a.log[k0 + lane] > -INFINITY) {
+                    at = (uint32_t)a.given.idx[k0 + lane] - base;
+                    w = g.grad_log[k0 + lane];
+                }
+                sum += w;
+                uint64_t in = __ballot(at < kGradWave);
+                while (in) {
+                    const int l = __builtin_ctzll(in);
+                    in &= in - 1;
+                    int owner, place;
+                    owner_of(__builtin_amdgcn_readlane(at, l), &owner, &place);
+                    const float more = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), l));
+                    if (lane == owner) {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) d[e] += e == place ? more : 0.f;
+                    }
+                }
+            }
+            sum = wave_sum(sum);
+            // (1 / T of the smallest T overflows: the rest of it then comes as a power of two)
+            const float boost = t < 0x1p-100f ? 0x1p64f : 1.f;
+            const float c = rate_of(t), inverse = 1.f / (t * boost), shift = size * kLog2E;
+            const float h = g.grad_entropy ? g.grad_entropy[r] : 0.f;
+            const float constant = g.grad_entropy ? fmaf(h, a.entropy[r], sum) : sum, slope = h * kLn2;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float s = out >> e & 1 ? -INFINITY : z[e];
+                const float x = fmaxf((s == best ? 0.f : (s - best) * c) - shift, kNothing);
+                d[e] = (d[e] - exp2f(x) * fmaf(slope, x, constant)) * inverse * boost;
+            }
+        } else {
+            const float all = there && !(best != best) ? 0.f : NAN;
+#pragma unroll
+            for (int e = 0; e < E; ++e) d[e] = all;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) total[e] += d[e];
+        if (g.grad) {
+            T* to = g.grad + r * g.ldg;
+#pragma unroll
+            for (int v = 0; v < E / V; ++v) {
+                const uint32_t c = position(v);
+                T w[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) from_float(d[v * V + i], &w[i]);
+                if (c + V <= n) {
+                    __builtin_memcpy(to + c, w, sizeof w);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        if (c + i < n) to[c + i] = w[i];
+                }
+            }
+        }
+    }
+    if (g.parts) {
+        float* to = g.parts + (int64_t)group * n;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const uint32_t c = position(e / V) + e % V;
+            if (c < n) to[c] = total[e];
+        }
+    }
+}
+
+// The groups' sums into one, in four runs of groups, then across them.
+__global__ __launch_bounds__(256) void k_columns(const float* __restrict__ parts, uint32_t groups, int64_t n,
+                                                 float* __restrict__ columns) {
+    __shared__ float runs[4][kWave];
+    const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * kWave + lane;
+    float sum = 0.f;
+    if (c < n) {
+        const uint32_t per = (groups + 3) / 4, end = (run + 1) * per < groups ? (run + 1) * per : groups;
+        for (uint32_t g = run * per; g < end; ++g) sum += parts[g * n + c];
+    }
+    runs[run][lane] = sum;
+    __syncthreads();
+    if (run == 0 && c < n) columns[c] = runs[0][lane] + runs[1][lane] + (runs[2][lane] + runs[3][lane]);
+}
+
+constexpr size_t kWorkspaceBytes = 128u << 20, kWorkspaceMost = (size_t)1 << 34;
+
+}  // namespace
+
+struct als_predict_ctx {
+    int device;
+    int cus;
+    unsigned char* ws;
+    size_t ws_bytes;
+    int last_hip;
+};
+
+namespace {
+
+int finish(als_predict_ctx* ctx) {
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return ALS_OK;
+    ctx->last_hip = (int)e;
+    return ALS_ERR_HIP;
+}
+
+// fn(a null pointer to the type)
+template <typename Fn>
+void by_type(int dtype, Fn fn) {
+    if (dtype == ALS_F32) fn((const float*)nullptr);
+    else if (dtype == ALS_F16) fn((const F16*)nullptr);
+    else fn((const BF16*)nullptr);
+}
+template <typename P>
+using Type = std::remove_cv_t<std::remove_pointer_t<P>>;
+
+// `rows` rows of the product that are one launch's.
+template <typename T, int WU, int WI, int FU, int FI>
+void launch_product(const als_predict_ctx* ctx, Product a, hipStream_t st) {
+    using C = Staged<T, WU, WI, FU, FI>;
+    static std::atomic<uint64_t> done{0};
+    auto* kernel = k_product<T, WU, WI, FU, FI>;
+    whole_lds(kernel, ctx->device, &done);
+    a.tu = (uint32_t)((a.m + C::kUsers - 1) / C::kUsers);
+    a.ti = (uint32_t)((a.n + C::kItems - 1) / C::kItems);
+    const int64_t steps = (a.f + Parts<T>::kValues - 1) / Parts<T>::kValues, tiles = (int64_t)a.tu * a.ti;
+    // few tiles: f in parts of 4 steps at least, as many as give every CU two workgroups and the workspace holds
+    int64_t parts = 2 * ctx->cus / tiles;
+    if (parts > steps / 4) parts = steps / 4;
+    const int64_t fit = (int64_t)(ctx->ws_bytes / 4) / (a.m * a.n);
+    if (parts > fit) parts = fit;
+    if (parts < 1) parts = 1;
+    a.steps = (int)((steps + parts - 1) / parts);
+    parts = (steps + a.steps - 1) / a.steps;
+    a.parts = parts > 1 ? (float*)ctx->ws : nullptr;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)parts), dim3(C::kThreads), C::kLds, st, a);
+    if (parts > 1) {
+        const int64_t fours = a.m * ((a.n + 3) / 4);
+        hipLaunchKernelGGL(k_join, dim3((unsigned)((fours + 255) / 256)), dim3(256), 0, st, a, (int)parts, (int64_t)0);
+    }
+}
+
+template <typename T>
+void product(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
+    const auto tiles = [&](int64_t users, int64_t items) {
+        return ((a.m + users - 1) / users) * ((a.n + items - 1) / items);
+    };
+    if (a.m > 16) {
+        if (tiles(128, 128) >= 2 * ctx->cus) return launch_product<T, 2, 2, 4, 4>(ctx, a, st);
+        if (tiles(64, 128) >= 2 * ctx->cus) return launch_product<T, 2, 2, 2, 4>(ctx, a, st);
+        return launch_product<T, 2, 2, 2, 2>(ctx, a, st);
+    }
+    return launch_product<T, 1, 4, 1, 1>(ctx, a, st);
+}
+
+// A row's registers: as many scores a thread as E; longer rows in segments.
+constexpr int64_t kHeld = 32 * 1024;
+constexpr int64_t kSegment = 16384;
+static_assert(ALS_PREDICT_N_MAX <= kSegment * kJoinThreads, "a thread a segment");
+
+int check_scores(const als_scores* s, const als_given* g) {
+    if (!s || !g || s->rows < 0 || s->n < 0 || s->n > ALS_PREDICT_N_MAX || s->dtype < ALS_F32 || s->dtype > ALS_BF16 ||
+        s->ldz < s->n || s->of < 0 || s->rows > INT32_MAX || g->entries < 0 || g->each < 0)
+        return ALS_ERR_INVALID_ARG;
+    if (!s->rated_ptr != !s->rated_idx || (s->users && !s->rated_ptr) || (s->rated_ptr && !s->users && s->of < s->rows))
+        return ALS_ERR_INVALID_ARG;
+    // (without entries each is 0; a quotient, as the product may not fit)
+    if (!g->ptr && (s->rows == 0 || g->each == 0 ? g->entries != 0
+                                                 : g->entries % s->rows != 0 || g->entries / s->rows != g->each))
+        return ALS_ERR_INVALID_ARG;
+    if ((s->rows > 0 && s->n > 0 && !s->z) || (g->entries > 0 && !g->idx)) return ALS_ERR_INVALID_ARG;
+    if (!aligned(s->z, type_bytes(s->dtype)) || !aligned(s->temperature, 4) || !aligned(s->rated_ptr, 8) ||
+        !aligned(s->rated_idx, 4) || !aligned(s->users, 4) || !aligned(g->ptr, 8) || !aligned(g->idx, 4))
+        return ALS_ERR_ALIGN;
+    return ALS_OK;
+}
+
+// Whether an output lies on one of the inputs (but on the scores, where `beside_scores` says so).
+bool on_inputs(const void* o, uint64_t bytes, const als_scores* s, const als_given* g, bool beside_scores = false) {
+    const uint64_t rn = (uint64_t)s->rows * 4;
+    return (!beside_scores && overlap(o, bytes, s->z, span_of(s->rows, s->n, s->ldz, type_bytes(s->dtype)))) ||
+           overlap(o, bytes, s->temperature, rn) || overlap(o, bytes, s->rated_ptr, ((uint64_t)s->of + 1) * 8) ||
+           overlap(o, bytes, s->users, rn) || overlap(o, bytes, g->ptr, ((uint64_t)s->rows + 1) * 8) ||
+           overlap(o, bytes, g->idx, (uint64_t)g->entries * 4);
+}
+
+template <typename T>
+RowArgs<T> row_args(const als_scores* s, const als_given* g) {
+    RowArgs<T> a{};
+    a.z = (const T*)s->z;
+    a.rows = s->rows;
+    a.n = s->n;
+    a.ldz = s->ldz;
+    a.temperature = s->temperature;
+    a.temperature_all = s->temperature_all;
+    a.rated = Rated{s->rated_ptr, s->rated_idx, s->users, s->of};
+    a.given = *g;
+    a.segments = 1;
+    a.columns = (uint32_t)(s->n > 0 ? s->n : 1);
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t als_predict_workspace_bytes(int device) {
+    int cus = 0;
+    return query_device(device, &cus) == ALS_OK ? kWorkspaceBytes : 0;
+}
+
+int als_predict_init(als_predict_ctx** out, int device, void* workspace, size_t workspace_bytes) {
+    if (!out) return ALS_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!workspace) return ALS_ERR_WORKSPACE;
+    if (!aligned(workspace, 256)) return ALS_ERR_ALIGN;
+    int cus = 0;
+    if (const int rc = query_device(device, &cus); rc != ALS_OK) return rc;
+    if (workspace_bytes < kWorkspaceBytes) return ALS_ERR_WORKSPACE;
+    als_predict_ctx* ctx = new (std::nothrow) als_predict_ctx();
+    if (!ctx) return ALS_ERR_INVALID_ARG;
+    ctx->device = device;
+    ctx->cus = cus;
+    ctx->ws = (unsigned char*)workspace;
+    ctx->ws_bytes = workspace_bytes < kWorkspaceMost ? workspace_bytes : kWorkspaceMost;
+    ctx->last_hip = 0;
+    *out = ctx;
+    return ALS_OK;
+}
+
+int als_predict_destroy(als_predict_ctx* ctx) {
+    delete ctx;
+    return ALS_OK;
+}
+
+int als_predict_last_hip_error(const als_predict_ctx* ctx) { return ctx ? ctx->last_hip : 0; }
+
+int als_predict(als_predict_ctx* ctx, const void* x, int64_t of, int64_t ldx, const int32_t* users, int64_t m,
+                const void* theta, int64_t n, int64_t ldt, int32_t dtype, int32_t f, const float* user_offset,
+                const float* item_offset, int32_t activation, float low, float high, const void* residual,
+                int64_t ldr, void* out, int64_t ldo, int32_t out_dtype, void* stream) {
+    if (!ctx || of < 0 || m < 0 || n < 0 || dtype < ALS_F32 || dtype > ALS_BF16 || out_dtype < ALS_F32 ||
+        out_dtype > ALS_BF16 || activation < ALS_ACT_NONE || activation > ALS_ACT_TANH)
+        return ALS_ERR_INVALID_ARG;
+    if (f < 1 || f > ALS_PREDICT_F_MAX) return ALS_ERR_UNSUPPORTED_F;
+    if (ldx < f || ldt < f || ldo < n || (residual && ldr < n) || (!users && m > of) ||
+        (activation == ALS_ACT_CLIP && !(low <= high)))
+        return ALS_ERR_INVALID_ARG;
+    if (m == 0 || n == 0) return ALS_OK;
+    if (!theta || !out || (of > 0 && !x)) return ALS_ERR_INVALID_ARG;
+    const size_t in = type_bytes(dtype), each = type_bytes(out_dtype);
+    if (!aligned(x, in) || !aligned(theta, in) || !aligned(users, 4) || !aligned(user_offset, 4) ||
+        !aligned(item_offset, 4) || !aligned(residual, each) || !aligned(out, each))
+        return ALS_ERR_ALIGN;
+    const uint64_t on = span_of(m, n, ldo, each);
+    if (overlap(out, on, x, span_of(of, f, ldx, in)) || overlap(out, on, theta, span_of(n, f, ldt, in)) ||
+        overlap(out, on, users, (uint64_t)m * 4) || overlap(out, on, user_offset, (uint64_t)of * 4) ||
+        overlap(out, on, item_offset, (uint64_t)n * 4) ||
+        (!(residual == out && ldr == ldo) && overlap(out, on, residual, span_of(m, n, ldr, each))))
+        return ALS_ERR_ALIAS;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return ALS_ERR_DEVICE;
+    const hipStream_t st = (hipStream_t)stream;
+    // Launches of at most 2^31 threads (a tile takes 256 for 16 users and 64 items at least): the users in parts of
+    // whole tiles, and the items where one row of tiles is too long already.
+    const int64_t most = (kMaxThreads / 2) / 256;
+    const int64_t items = (n + 63) / 64 < most ? n : most * 64;
+    const int64_t fit = most / ((items + 63) / 64) * 16, users_at_once = m < fit ? m : (fit >= 128 ? fit / 128 * 128 : fit);
+    by_type(dtype, [&](auto* p) {
+        using T = Type<decltype(p)>;
+        for (int64_t i = 0; i < m; i += users_at_once)
+            for (int64_t j = 0; j < n; j += items) {
+                Product a{};
+                a.x = users ? x : (const T*)x + i * ldx;
+                a.of = users ? of : of - i;
+                a.ldx = ldx;
+                a.users = users ? users + i : nullptr;
+                a.m = m - i < users_at_once ? m - i : users_at_once;
+                a.theta = (const T*)theta + j * ldt;
+                a.n = n - j < items ? n - j : items;
+                a.ldt = ldt;
+                a.f = f;
+                a.end = Epilogue{user_offset ? user_offset + (users ? 0 : i) : nullptr,
+                                 item_offset ? item_offset + j : nullptr,
+                                 residual ? (const char*)residual + (i * ldr + j) * each : nullptr, ldr,
+                                 (char*)out + (i * ldo + j) * each, ldo, low, high, activation, out_dtype};
+                product<T>(ctx, a, st);
+            }
+    });
+    return finish(ctx);
+}
+
+int als_log_prob(als_predict_ctx* ctx, const als_scores* scores, const als_given* given, float* log, float* stats,
+                 float* entropy, int32_t top, int32_t* top_index, float* top_log, void* stream) {
+    if (!ctx) return ALS_ERR_INVALID_ARG;
+    if (const int rc = check_scores(scores, given); rc != ALS_OK) return rc;
+    const als_scores& s = *scores;
+    if (top < 0 || top > ALS_PREDICT_TOP_MAX || (given->entries > 0 && !log)) return ALS_ERR_INVALID_ARG;
+    if (!aligned(log, 4) || !aligned(stats, 4) || !aligned(entropy, 4) || !aligned(top_index, 4) || !aligned(top_log, 4))
+        return ALS_ERR_ALIGN;
+    const uint64_t rn = (uint64_t)s.rows * 4;
+    const void* outs[5] = {log, stats, entropy, top_index, top_log};
+    const uint64_t bytes[5] = {(uint64_t)given->entries * 4, 2 * rn, rn, rn * top, rn * top};
+    for (int i = 0; i < 5; ++i) {
+        if (on_inputs(outs[i], bytes[i], scores, given)) return ALS_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (overlap(outs[i], bytes[i], outs[j], bytes[j])) return ALS_ERR_ALIAS;
+    }
+    if (s.rows == 0) return ALS_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return ALS_ERR_DEVICE;
+    by_type(s.dtype, [&](auto* p) {
+        using T = Type<decltype(p)>;
+        RowArgs<T> a = row_args<T>(scores, given);
+        a.log = log;
+        a.stats = stats;
+        a.entropy = entropy;
+        a.top = top_index || top_log ? top : 0;
+        a.top_index = top_index;
+        a.top_log = top_log;
+        const auto go = [&](auto each, int64_t rows) {
+            constexpr int E = decltype(each)::value;
+            const int64_t threads = ((int64_t)a.columns + E - 1) / E, waves = (threads + kWave - 1) / kWave;
+            const size_t lds = s.rated_ptr ? (size_t)(a.columns + 31) / 32 * 4 : 0;
+            const int64_t row0 = a.row0;
+            in_parts(rows, kMaxThreads / (kWave * waves * a.segments), [&](int64_t first, int64_t some) {
+                a.row0 = row0 + first;
+                hipLaunchKernelGGL((k_row<T, E>), dim3((unsigned)(some * a.segments)), dim3((unsigned)(kWave * waves)),
+                                   lds, (hipStream_t)stream, a);
+            });
+            a.row0 = row0;
+        };
+        using std::integral_constant;
+        if (s.n <= kHeld) {
+            if (s.n <= 1024) return go(integral_constant<int, 8>(), s.rows);
+            if (s.n <= 16384) return go(integral_constant<int, 16>(), s.rows);
+            return go(integral_constant<int, 32>(), s.rows);
+        }
+        a.segments = (uint32_t)((s.n + kSegment - 1) / kSegment);
+        a.columns = kSegment;
+        const size_t a_row = a.segments * (sizeof(SegMass) + a.top * sizeof(uint64_t));
+        int64_t batch = (int64_t)(ctx->ws_bytes / a_row);
+        const int64_t most = kMaxThreads / (1024 * a.segments);
+        if (batch > most) batch = most;
+        a.keys = (uint64_t*)ctx->ws;
+        for (int64_t row0 = 0; row0 < s.rows; row0 += batch) {
+            const int64_t some = s.rows - row0 < batch ? s.rows - row0 : batch;
+            a.mass = (SegMass*)(ctx->ws + some * a.segments * a.top * sizeof(uint64_t));
+            a.row0 = row0;
+            go(integral_constant<int, 32>(), some);
+            hipLaunchKernelGGL(k_row_join<T>, dim3((unsigned)some), dim3(kJoinThreads), 0, (hipStream_t)stream, a);
+        }
+    });
+    return finish(ctx);
+}
+
+int als_log_prob_grad(als_predict_ctx* ctx, const als_scores* scores, const als_given* given, const float* log,
+                      const float* stats, const float* entropy, const float* grad_log, const float* grad_entropy,
+                      void* grad, int64_t ldg, float* columns, void* stream) {
+    if (!ctx) return ALS_ERR_INVALID_ARG;
+    if (const int rc = check_scores(scores, given); rc != ALS_OK) return rc;
+    const als_scores& s = *scores;
+    if ((given->entries > 0 && (!log || !grad_log)) || (s.rows > 0 && !stats) ||
+        (s.rows > 0 && grad_entropy && !entropy) || (grad && ldg < s.n))
+        return ALS_ERR_INVALID_ARG;
+    const size_t each = type_bytes(s.dtype);
+    if (!aligned(log, 4) || !aligned(stats, 4) || !aligned(entropy, 4) || !aligned(grad_log, 4) ||
+        !aligned(grad_entropy, 4) || !aligned(grad, each) || !aligned(columns, 4))
+        return ALS_ERR_ALIGN;
+    const uint64_t rn = (uint64_t)s.rows * 4, en = (uint64_t)given->entries * 4, cn = (uint64_t)s.n * 4;
+    const uint64_t gn = grad ? span_of(s.rows, s.n, ldg, each) : 0;
+    const bool in_place = grad == s.z && ldg == s.ldz;
+    const auto on_more = [&](const void* o, uint64_t bytes) {
+        return overlap(o, bytes, log, en) || overlap(o, bytes, stats, 2 * rn) || overlap(o, bytes, entropy, rn) ||
+               overlap(o, bytes, grad_log, en) || overlap(o, bytes, grad_entropy, rn);
+    };
+    if (on_inputs(grad, gn, scores, given, in_place) || on_inputs(columns, cn, scores, given) || on_more(grad, gn) ||
+        on_more(columns, cn) || overlap(grad, gn, columns, cn))
+        return ALS_ERR_ALIAS;
+    if (s.n == 0 || (!grad && !columns) || (s.rows == 0 && !columns)) return ALS_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return ALS_ERR_DEVICE;
+    const hipStream_t st = (hipStream_t)stream;
+    const int64_t chunks = (s.n + kGradChunk - 1) / kGradChunk;
+    // a workgroup takes one row's chunk, or with the columns' sums as many rows as leave every CU eight workgroups
+    int64_t groups = s.rows;
+    if (columns) {
+        groups = (8 * ctx->cus + chunks - 1) / chunks;
+        const int64_t fit = (int64_t)(ctx->ws_bytes / 4) / s.n;
+        groups = groups < fit ? groups : fit;
+    }
+    const int64_t most = kMaxThreads / kGradThreads / chunks;
+    groups = groups < most ? groups : most;
+    groups = groups < s.rows ? groups : s.rows;
+    if (s.rows > 0)
+        by_type(s.dtype, [&](auto* p) {
+            using T = Type<decltype(p)>;
+            GradArgs<T> g{};
+            g.of = row_args<T>(scores, given);
+            g.of.log = const_cast<float*>(log);
+            g.of.stats = const_cast<float*>(stats);
+            g.of.entropy = const_cast<float*>(entropy);
+            g.grad_log = grad_log;
+            g.grad_entropy = grad_entropy;
+            g.grad = (T*)grad;
+            g.ldg = ldg;
+            g.parts = columns ? (float*)ctx->ws : nullptr;
+            g.chunks = (uint32_t)chunks;
+            g.groups = (uint32_t)groups;
+            hipLaunchKernelGGL(k_gradient<T>, dim3((unsigned)(chunks * groups)), dim3(kGradThreads), 0, st, g);
+        });
+    if (columns)
+        hipLaunchKernelGGL(k_columns, dim3((unsigned)((s.n + kWave - 1) / kWave)), dim3(256), 0, st,
+                           (const float*)ctx->ws, (uint32_t)groups, s.n, columns);
+    return finish(ctx);
+}
+
+}  // extern "C"
