@@ -393,9 +393,9 @@ __device__ __forceinline__ Mass joined(Mass a, float c) {
     Mass all;
     all.best = wave_max(a.best);
     const float x = a.best == all.best ? 0.f : exponent(a.best, all.best, c);
-    const float w = exp2f(x) * a.sum;
+    const float w = __builtin_amdgcn_exp2f(x) * a.sum;
     all.sum = wave_sum(w);
-    all.spread = wave_sum(exp2f(x) * a.spread + w * x);
+    all.spread = wave_sum(__builtin_amdgcn_exp2f(x) * a.spread + w * x);
     return all;
 }
 
@@ -472,33 +472,98 @@ __device__ __forceinline__ uint64_t wave_max64(uint64_t v) {
 }
 
 constexpr int kMaxWaves = 16;
+constexpr int kGroups = 256;
 constexpr int kList = 1024;
 
 struct RowShared {
     Mass mass[kMaxWaves];
     uint64_t place[kMaxWaves];
     uint32_t first;
+    uint32_t cut, count;
+    uint32_t group[kGroups];
+    uint64_t list[kList];
 };
 
-// The first `top` places in their order: emit(rank, place) for each, by some thread; how many there are is the result.
-// `below(limit)` is the best of this thread's places below a limit.
-template <typename Below, typename Emit>
-__device__ __forceinline__ int best_places(int top, RowShared* sh, Below below, Emit emit) {
-    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    uint64_t limit = ~0ull;
-    int found = 0;
-    for (; found < top; ++found) {
-        uint64_t p = wave_max64(below(limit));
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) sh->place[wave] = p;
-        __syncthreads();
-        for (int w = 0; w < waves; ++w) p = sh->place[w] > p ? sh->place[w] : p;
-        if (p == 0) break;
-        if (threadIdx.x == 0) emit(found, p);
-        limit = p;
+// The first `top` places in their order, for few that are given: emit(rank, place) for each, by some thread; how many
+// there are is the result.  A score that `top` groups of threads have reached at their best is below none of the first
+// `top`; the columns from it on are listed (random rows: hardly more than `top`, as the groups' best are mostly of
+// different groups) and each one's rank is counted among them.  Where the list does not hold them (the best columns stand
+// in few groups, or many are equal) they are taken one at a time.
+//   offer     before the barrier that the caller has anyway: each thread's best key (0: none)
+//   finish    after it; each(fn) calls fn(place) for all of a thread's places whose key is at least its argument
+struct Top {
+    RowShared* sh;
+    int top;
+
+    __device__ __forceinline__ void offer(uint32_t key) const {
+        int d = 0;
+        if (blockDim.x > kGroups) {
+            key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0xB1, 0xF, 0xF, true));     // lanes 1, 0, 3, 2
+            d = 1;
+        }
+        if (blockDim.x > 2 * kGroups) {
+            key = max(key, (uint32_t)__builtin_amdgcn_mov_dpp((int)key, 0x4E, 0xF, 0xF, true));     // lanes 2, 3, 0, 1
+            d = 2;
+        }
+        if ((threadIdx.x & ((1 << d) - 1)) == 0) sh->group[threadIdx.x >> d] = key;
+        if (threadIdx.x == 0) sh->count = 0;
     }
-    return found;
-}
+
+    template <typename Each, typename Below, typename Emit>
+    __device__ __forceinline__ int finish(uint32_t own, Each each, Below below, Emit emit) const {
+        if (threadIdx.x < kWave) {
+            const int d = blockDim.x > 2 * kGroups ? 2 : (blockDim.x > kGroups ? 1 : 0), groups = blockDim.x >> d;
+            uint32_t key[kGroups / kWave];
+#pragma unroll
+            for (int k = 0; k < kGroups / kWave; ++k) {
+                const int at = k * kWave + threadIdx.x;
+                key[k] = at < groups ? sh->group[at] : 0;
+            }
+            uint32_t cut = 0;
+            for (uint32_t bit = 1u << 31; bit != 0; bit >>= 1) {
+                int reached = 0;
+#pragma unroll
+                for (int k = 0; k < kGroups / kWave; ++k) reached += __popcll(__ballot(key[k] >= (cut | bit)));
+                if (reached >= top) cut |= bit;
+                if (reached == top) break;
+            }
+            if (threadIdx.x == 0) sh->cut = cut < 1 ? 1 : cut;
+        }
+        __syncthreads();
+        const uint32_t cut = sh->cut;
+        if (own >= cut)
+            each(cut, [&](uint64_t place) {
+                const uint32_t at = atomicAdd(&sh->count, 1u);
+                if (at < kList) sh->list[at] = place;
+            });
+        __syncthreads();
+        const int count = sh->count;
+        if (count <= kList) {
+            for (int i = threadIdx.x; i < count; i += blockDim.x) {
+                const uint64_t mine = sh->list[i];
+                int rank = 0;
+#pragma unroll 4
+                for (int j = 0; j < count; ++j) rank += sh->list[j] > mine;
+                if (rank < top) emit(rank, mine);
+            }
+            return count < top ? count : top;
+        }
+        const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+        uint64_t limit = ~0ull;
+        int found = 0;
+        for (; found < top; ++found) {
+            uint64_t p = wave_max64(below(limit));
+            __syncthreads();
+            if ((threadIdx.x & 63) == 0) sh->place[wave] = p;
+            __syncthreads();
+            for (int w = 0; w < waves; ++w) p = sh->place[w] > p ? sh->place[w] : p;
+            if (p == 0) break;
+            if (threadIdx.x == 0) emit(found, p);
+            limit = p;
+        }
+        return found;
+    }
+};
 
 // What a row's distribution gives, but its log p of given columns; called by all of the workgroup's threads.
 template <typename T>
@@ -589,10 +654,13 @@ __global__ __launch_bounds__(1024) void k_row(RowArgs<T> a) {
     Mass mass{-INFINITY, 0.f, 0.f};
 #pragma unroll
     for (int e = 0; e < E; ++e) mass.best = fmaxf(mass.best, z[e]);
+    const uint32_t own = mass.best > -INFINITY ? key_of(mass.best) : 0;
+    const Top top{&sh, a.top};
+    if (a.top) top.offer(own);
     mass.best = wave_max(mass.best);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const float x = exponent(z[e], mass.best, c), w = exp2f(x);
+        const float x = exponent(z[e], mass.best, c), w = __builtin_amdgcn_exp2f(x);
         mass.sum += w;
         mass.spread = fmaf(w, x, mass.spread);
     }
@@ -642,17 +710,23 @@ __global__ __launch_bounds__(1024) void k_row(RowArgs<T> a) {
         }
         return best;
     };
+    const auto each = [&](uint32_t cut, auto fn) {
+        const float least = fmaxf(score_of(cut < 0x00800000u ? 0x00800000u : cut), -3.402823466e38f);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (z[e] >= least) fn(place_of(z[e], base + position(e / V) + e % V));
+    };
     if (whole) {
         write_law(a, r, law, mass);
         if (a.top == 0) return;
-        const int found = best_places(a.top, &sh, below, [&](int k, uint64_t p) { write_top(a, r, law, k, p); });
+        const int found = top.finish(own, each, below, [&](int k, uint64_t p) { write_top(a, r, law, k, p); });
         write_no_top(a, r, law, found);
     } else {
         const int64_t part = local * a.segments + segment;
         if (threadIdx.x == 0) a.mass[part] = SegMass{mass, law.first};
         if (a.top == 0) return;
         uint64_t* keys = a.keys + part * a.top;
-        const int found = best_places(a.top, &sh, below, [&](int k, uint64_t p) { keys[k] = p; });
+        const int found = top.finish(own, each, below, [&](int k, uint64_t p) { keys[k] = p; });
         for (int k = found + threadIdx.x; k < a.top; k += blockDim.x) keys[k] = 0;
     }
 }
@@ -681,6 +755,14 @@ __global__ __launch_bounds__(kJoinThreads) void k_row_join(RowArgs<T> a) {
     const float own = mass.best;
     mass = joined(mass, c);
     if (lane == 0) sh.mass[wave] = mass;
+    const uint64_t* keys = a.keys + local * a.segments * a.top;
+    const uint32_t count = a.segments * a.top;
+    const Top top{&sh, a.top};
+    uint32_t most = 0;
+    if (a.top) {
+        for (uint32_t k = threadIdx.x; k < count; k += kJoinThreads) most = max(most, (uint32_t)(keys[k] >> 32));
+        top.offer(most);
+    }
     __syncthreads();
     mass = joined(lane < kJoinThreads / 64 ? sh.mass[lane] : Mass{-INFINITY, 0.f, 0.f}, c);
     law.best = mass.best;
@@ -698,17 +780,19 @@ __global__ __launch_bounds__(kJoinThreads) void k_row_join(RowArgs<T> a) {
     }
     write_law(a, r, law, mass);
     if (a.top == 0) return;
-    const uint64_t* keys = a.keys + local * a.segments * a.top;
-    const uint32_t count = a.segments * a.top;
+    const auto each = [&](uint32_t cut, auto fn) {
+        for (uint32_t k = threadIdx.x; k < count; k += kJoinThreads)
+            if ((uint32_t)(keys[k] >> 32) >= cut) fn(keys[k]);
+    };
     const auto below = [&](uint64_t limit) {
         uint64_t best = 0;
-        for (uint32_t k = threadIdx.x; k < count; k += blockDim.x) {
+        for (uint32_t k = threadIdx.x; k < count; k += kJoinThreads) {
             const uint64_t p = keys[k];
             best = p < limit && p > best ? p : best;
         }
         return best;
     };
-    const int found = best_places(a.top, &sh, below, [&](int k, uint64_t p) { write_top(a, r, law, k, p); });
+    const int found = top.finish(most, each, below, [&](int k, uint64_t p) { write_top(a, r, law, k, p); });
     write_no_top(a, r, law, found);
 }
 
@@ -819,7 +903,7 @@ __global__ __launch_bounds__(kGradThreads) void k_gradient(GradArgs<T> g) {
             for (int e = 0; e < E; ++e) {
                 const float s = out >> e & 1 ? -INFINITY : z[e];
                 const float x = fmaxf((s == best ? 0.f : (s - best) * c) - shift, kNothing);
-                d[e] = (d[e] - exp2f(x) * fmaf(slope, x, constant)) * inverse * boost;
+                d[e] = (d[e] - __builtin_amdgcn_exp2f(x) * fmaf(slope, x, constant)) * inverse * boost;
             }
         } else {
             const float all = there && !(best != best) ? 0.f : NAN;
