@@ -596,7 +596,7 @@ __device__ __forceinline__ void write_no_top(const RowArgs<T>& a, int64_t r, con
 
 // A row, or a segment of one, of up to E scores a thread, which stay in registers from their one read on.
 template <typename T, int E>
-__global__ __launch_bounds__(1024) void k_row(RowArgs<T> a) {
+__global__ __launch_bounds__(1024, E <= 16 ? 8 : (E <= 32 ? 7 : 5)) void k_row(RowArgs<T> a) {
     constexpr int V = E * sizeof(T) < 16 ? E : 16 / sizeof(T);
     __shared__ RowShared sh;
     extern __shared__ uint32_t bits[];
@@ -701,11 +701,10 @@ __global__ __launch_bounds__(1024) void k_row(RowArgs<T> a) {
             a.log[e] = law.there ? -INFINITY : NAN;
         }
     }
-    const auto below = [&](uint64_t limit) {
+    const auto below = [&](uint64_t limit) {      // (from memory, so that no key is kept in a register)
         uint64_t best = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const uint64_t p = place_of(z[e], base + position(e / V) + e % V);
+        for (uint32_t at = threadIdx.x; at < n; at += blockDim.x) {
+            const uint64_t p = left_out(at) ? 0 : place_of(to_float(row[at]), base + at);
             best = p < limit && p > best ? p : best;
         }
         return best;
@@ -800,127 +799,220 @@ __global__ __launch_bounds__(kJoinThreads) void k_row_join(RowArgs<T> a) {
 
 template <typename T>
 struct GradArgs {
-    RowArgs<T> of;               // (log, stats and entropy are inputs here)
-    const float* grad_log;
-    const float* grad_entropy;
+    const T* z;
+    int64_t rows, n, ldz;
+    float temperature_all;
+    int64_t of;                  // rows of the left-out columns
+    int64_t entries, each;
     T* grad;
     int64_t ldg;
-    float* parts;                // groups x n sums of rows, or NULL
+    float* parts;                // groups x n sums of rows
     uint32_t chunks, groups;     // of a row's columns; of rows
 };
 
-constexpr int kGradThreads = 256, kGradEach = 8, kGradWave = kWave * kGradEach;
-constexpr int kGradChunk = kGradThreads * kGradEach;
+constexpr int kGradThreads = 256;
+template <bool COLUMNS>
+struct Grad {
+    static constexpr int kEach = COLUMNS ? 8 : 16;       // columns a lane
+    static constexpr int kRun = kWave * kEach, kChunk = kGradThreads * kEach;      // of a wave, of a workgroup
+};
 
-// A wave's 512 columns of a row, and of the rows that follow it `groups` apart.  Each wave looks through the row's lists
-// for itself: what lies in its columns goes to the lane that has it, in the lists' order, so that sums of repeated columns
-// are the same on every run, and no wave waits for another.
-template <typename T>
-__global__ __launch_bounds__(kGradThreads) void k_gradient(GradArgs<T> g) {
-    constexpr int E = kGradEach, V = 16 / sizeof(T);
-    const RowArgs<T>& a = g.of;
+// A chunk of a row's columns, and of the rows that follow it `groups` apart, each wave having a run of them.  The
+// left-out columns are marked in LDS by all of the workgroup (three rows' marks in turn: one is cleared while one is read,
+// so a row takes one barrier).  The given columns each wave looks through for itself: what lies in its run goes to the
+// lane that has it, in the list's order, so that sums of repeated columns are the same on every run.
+template <typename T, bool COLUMNS>
+__global__ __launch_bounds__(kGradThreads, COLUMNS ? 6 : 5) void k_gradient(
+    GradArgs<T> a, const float* __restrict__ temperature, const int64_t* __restrict__ rated_ptr,
+    const int32_t* __restrict__ rated_idx, const int32_t* __restrict__ users, const int64_t* __restrict__ given_ptr,
+    const int32_t* __restrict__ given_idx, const float* __restrict__ log, const float* __restrict__ stats,
+    const float* __restrict__ entropy, const float* __restrict__ grad_log, const float* __restrict__ grad_entropy) {
+    constexpr int E = Grad<COLUMNS>::kEach, V = 16 / sizeof(T), kMarks = Grad<COLUMNS>::kChunk / 32;
+    constexpr uint32_t kRun = Grad<COLUMNS>::kRun, kChunk = Grad<COLUMNS>::kChunk;
+    __shared__ uint32_t marks[3][kMarks];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t chunk = blockIdx.x % g.chunks, group = blockIdx.x / g.chunks;
-    const uint32_t base = chunk * kGradChunk + wave * kGradWave, n = (uint32_t)a.n;
-    if (base >= n) return;
+    const uint32_t chunk = blockIdx.x % a.chunks, group = blockIdx.x / a.chunks;
+    const uint32_t start = chunk * kChunk, base = start + wave * kRun, n = (uint32_t)a.n;
     const auto position = [&](int v) { return base + (uint32_t)(v * kWave + lane) * V; };
-    float total[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) total[e] = 0.f;
-    for (int64_t r = group; r < a.rows; r += g.groups) {
+    const bool inside = base + kRun <= n;
+
+    // What a row needs, in the order in which it can be asked for: where its lists lie, then their first entries
+    // and the scores.
+    struct Place {
+        int64_t rated, rated_end, begin, end;
+        bool there;
+    };
+    struct Fetched {
+        T z[E];
+        uint32_t rated, given;
+        float g, log;
+        float t, best, size, h, spread;
+    };
+    const auto place_of_row = [&](int64_t r) {
+        Place p{0, 0, r * a.each, (r + 1) * a.each, true};
+        if (rated_ptr) {
+            const int64_t u = users ? (int64_t)users[r] : r;
+            p.there = u >= 0 && u < a.of;
+            if (p.there) {
+                p.rated = rated_ptr[u];
+                p.rated_end = rated_ptr[u + 1];
+            }
+        }
+        if (given_ptr) {
+            p.begin = given_ptr[r];
+            p.end = given_ptr[r + 1];
+            p.begin = p.begin < 0 ? 0 : p.begin;
+            p.end = p.end > a.entries ? a.entries : p.end;
+        }
+        return p;
+    };
+    const auto fetch = [&](int64_t r, const Place& p) {
+        Fetched f;
         const T* row = a.z + r * a.ldz;
-        float z[E];
 #pragma unroll
         for (int v = 0; v < E / V; ++v) {
             const uint32_t c = position(v);
-            T t[V];
-            if (c + V <= n) {
-                __builtin_memcpy(t, row + c, sizeof t);
-#pragma unroll
-                for (int i = 0; i < V; ++i) z[v * V + i] = to_float(t[i]);
+            if (inside) {
+                __builtin_memcpy(&f.z[v * V], row + c, V * sizeof(T));
             } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) z[v * V + i] = c + i < n ? to_float(row[c + i]) : -INFINITY;
-            }
-        }
-        const int32_t* list;
-        int64_t listed;
-        const bool there = a.rated.row(r, &list, &listed);
-        const float t = limit_of(a.temperature, a.temperature_all, r);
-        const float best = a.stats[2 * r], size = a.stats[2 * r + 1];
-        float d[E];
-        if (there && t > 0.f && best > -INFINITY) {
-            // the owner of a column, and its place there
-            const auto owner_of = [&](uint32_t at, int* owner, int* e) {
-                *owner = at / V % kWave;
-                *e = at / (V * kWave) * V + at % V;
-            };
-            uint32_t out = 0;
-            for (int64_t k0 = 0; k0 < listed; k0 += kWave) {
-                const uint32_t at = k0 + lane < listed ? (uint32_t)list[k0 + lane] - base : ~0u;
-                uint64_t in = __ballot(at < kGradWave);
-                while (in) {
-                    const int l = __builtin_ctzll(in);
-                    in &= in - 1;
-                    int owner, e;
-                    owner_of(__builtin_amdgcn_readlane(at, l), &owner, &e);
-                    if (lane == owner) out |= 1u << e;
+                for (int i = 0; i < V; ++i) {
+                    from_float(-INFINITY, &f.z[v * V + i]);
+                    if (c + i < n) f.z[v * V + i] = row[c + i];
                 }
             }
-            int64_t begin, end;
-            a.entries(r, &begin, &end);
+        }
+        f.rated = p.rated + threadIdx.x < p.rated_end ? (uint32_t)rated_idx[p.rated + threadIdx.x] : ~0u;
+        const bool in = p.begin + lane < p.end;
+        f.given = in ? (uint32_t)given_idx[p.begin + lane] : ~0u;
+        f.g = in ? grad_log[p.begin + lane] : 0.f;
+        f.log = in ? log[p.begin + lane] : -INFINITY;
+        f.t = limit_of(temperature, a.temperature_all, r);
+        f.best = stats[2 * r];
+        f.size = stats[2 * r + 1];
+        f.h = grad_entropy ? grad_entropy[r] : 0.f;
+        f.spread = grad_entropy ? entropy[r] : 0.f;
+        return f;
+    };
+    float total[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) total[e] = 0.f;
+    int turn = 0;
+    if (rated_ptr) {
+        for (int w = threadIdx.x; w < 3 * kMarks; w += kGradThreads) marks[0][w] = 0;
+        __syncthreads();
+    }
+    // with the columns' sums a workgroup has several rows: the next one's values and the places after it are on their
+    // way while a row is worked on
+    const auto after = [&](int64_t r) { return r + a.groups < a.rows ? r + a.groups : r; };
+    Place place = place_of_row(group), place_after = COLUMNS ? place_of_row(after(group)) : Place{};
+    Fetched now = fetch(group, place);
+    for (int64_t r = group; r < a.rows; r += a.groups) {
+        const Place p = place;
+        const Fetched f = now;
+        if (COLUMNS) {
+            now = fetch(after(r), place_after);
+            place = place_after;
+            place_after = place_of_row(after(after(r)));
+        }
+        const bool there = p.there;
+        const int64_t begin = p.begin, end = p.end;
+        const float t = f.t, best = f.best, size = f.size, h = f.h, spread = f.spread;
+        const bool some = there && t > 0.f && best > -INFINITY;
+        if (rated_ptr) {
+            if (some) {
+                const auto mark = [&](uint32_t column) {
+                    const uint32_t at = column - start;
+                    if (at < kChunk) atomicOr(&marks[turn][at >> 5], 1u << (at & 31));
+                };
+                mark(f.rated);
+                for (int64_t k = p.rated + threadIdx.x + kGradThreads; k < p.rated_end; k += kGradThreads)
+                    mark((uint32_t)rated_idx[k]);
+            }
+            __syncthreads();
+        }
+        const uint32_t* marked = marks[turn];
+        if (rated_ptr) {
+            turn = turn == 2 ? 0 : turn + 1;
+            const int clear = turn == 2 ? 0 : turn + 1;
+            for (int w = threadIdx.x; w < kMarks; w += kGradThreads) marks[clear][w] = 0;
+        }
+        float d[E];
+        if (some) {
+            // (1 / T of the smallest T overflows: the rest of it then comes as a power of two)
+            const float boost = t < 0x1p-100f ? 0x1p64f : 1.f, inverse = 1.f / (t * boost);
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < E; ++e) d[e] = 0.f;
             for (int64_t k0 = begin; k0 < end; k0 += kWave) {
-                uint32_t at = ~0u;
-                float w = 0.f;
-                if (k0 + lane < end && a.log[k0 + lane] > -INFINITY) {
-                    at = (uint32_t)a.given.idx[k0 + lane] - base;
-                    w = g.grad_log[k0 + lane];
+                uint32_t column = f.given;
+                float g = f.g, entry = f.log;
+                if (k0 != begin) {
+                    const bool in = k0 + lane < end;
+                    column = in ? (uint32_t)given_idx[k0 + lane] : ~0u;
+                    g = in ? grad_log[k0 + lane] : 0.f;
+                    entry = in ? log[k0 + lane] : -INFINITY;
                 }
+                const bool counts = entry > -INFINITY;
+                const uint32_t at = counts ? column - base : ~0u;
+                const float w = counts ? g : 0.f;
                 sum += w;
-                uint64_t in = __ballot(at < kGradWave);
+                uint64_t in = __ballot(at < kRun);
                 while (in) {
                     const int l = __builtin_ctzll(in);
                     in &= in - 1;
-                    int owner, place;
-                    owner_of(__builtin_amdgcn_readlane(at, l), &owner, &place);
+                    const uint32_t to = __builtin_amdgcn_readlane(at, l), place = to / (V * kWave) * V + to % V;
                     const float more = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), l));
-                    if (lane == owner) {
+                    if (lane == to / V % kWave) {
 #pragma unroll
                         for (int e = 0; e < E; ++e) d[e] += e == place ? more : 0.f;
                     }
                 }
             }
             sum = wave_sum(sum);
-            // (1 / T of the smallest T overflows: the rest of it then comes as a power of two)
-            const float boost = t < 0x1p-100f ? 0x1p64f : 1.f;
-            const float c = rate_of(t), inverse = 1.f / (t * boost), shift = size * kLog2E;
-            const float h = g.grad_entropy ? g.grad_entropy[r] : 0.f;
-            const float constant = g.grad_entropy ? fmaf(h, a.entropy[r], sum) : sum, slope = h * kLn2;
+            const float c = fminf(kLog2E / t, 3.402823466e38f), shift = size * kLog2E;
+            const float constant = fmaf(h, spread, sum) * inverse, slope = h * kLn2 * inverse;
+            const auto each = [&](auto endless) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float s = out >> e & 1 ? -INFINITY : z[e];
-                const float x = fmaxf((s == best ? 0.f : (s - best) * c) - shift, kNothing);
-                d[e] = (d[e] - __builtin_amdgcn_exp2f(x) * fmaf(slope, x, constant)) * inverse * boost;
+                for (int v = 0; v < E / V; ++v) {
+                    const uint32_t at = position(v) - start;
+                    const uint32_t out = rated_ptr ? marked[at >> 5] >> (at & 31) : 0;      // V divides 32
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const int e = v * V + i;
+                        // a left-out score becomes NaN, which weighs nothing
+                        const float s = __builtin_bit_cast(
+                            float, __builtin_bit_cast(uint32_t, to_float(f.z[e])) | (uint32_t)((int32_t)(out << (31 - i)) >> 31));
+                        // (of equal best scores +inf: their difference is 0, of a finite one and +inf -inf)
+                        const float x = fmaxf(fmaf(endless.value ? (s == best ? 0.f : -INFINITY) : s - best, c, -shift), kNothing);
+                        d[e] = fmaf(d[e], inverse, -(__builtin_amdgcn_exp2f(x) * fmaf(slope, x, constant)));
+                    }
+                }
+            };
+            if (best == INFINITY) each(std::true_type());
+            else each(std::false_type());
+            if (boost != 1.f) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[e] *= boost;
             }
         } else {
             const float all = there && !(best != best) ? 0.f : NAN;
 #pragma unroll
             for (int e = 0; e < E; ++e) d[e] = all;
         }
+        if (COLUMNS) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) total[e] += d[e];
-        if (g.grad) {
-            T* to = g.grad + r * g.ldg;
+            for (int e = 0; e < E; ++e) total[e] += d[e];
+        }
+        if (a.grad) {
+            T* to = a.grad + r * a.ldg;
 #pragma unroll
             for (int v = 0; v < E / V; ++v) {
                 const uint32_t c = position(v);
                 T w[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) from_float(d[v * V + i], &w[i]);
-                if (c + V <= n) {
+                if (inside) {
                     __builtin_memcpy(to + c, w, sizeof w);
                 } else {
 #pragma unroll
@@ -929,9 +1021,13 @@ __global__ __launch_bounds__(kGradThreads) void k_gradient(GradArgs<T> g) {
                 }
             }
         }
+        if (!COLUMNS && r + a.groups < a.rows) {
+            place = place_of_row(r + a.groups);
+            now = fetch(r + a.groups, place);
+        }
     }
-    if (g.parts) {
-        float* to = g.parts + (int64_t)group * n;
+    if (COLUMNS) {
+        float* to = a.parts + (int64_t)group * n;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const uint32_t c = position(e / V) + e % V;
@@ -940,20 +1036,30 @@ __global__ __launch_bounds__(kGradThreads) void k_gradient(GradArgs<T> g) {
     }
 }
 
-// The groups' sums into one, in four runs of groups, then across them.
-__global__ __launch_bounds__(256) void k_columns(const float* __restrict__ parts, uint32_t groups, int64_t n,
-                                                 float* __restrict__ columns) {
-    __shared__ float runs[4][kWave];
+// The groups' sums into one: runs of groups, eight at a time, then across the runs.
+constexpr int kRuns = 16;
+__global__ __launch_bounds__(kRuns * kWave) void k_columns(const float* __restrict__ parts, uint32_t groups, int64_t n,
+                                                           float* __restrict__ columns) {
+    __shared__ float runs[kRuns][kWave];
     const int lane = threadIdx.x & 63, run = threadIdx.x >> 6;
     const int64_t c = (int64_t)blockIdx.x * kWave + lane;
     float sum = 0.f;
     if (c < n) {
-        const uint32_t per = (groups + 3) / 4, end = (run + 1) * per < groups ? (run + 1) * per : groups;
-        for (uint32_t g = run * per; g < end; ++g) sum += parts[g * n + c];
+        for (uint32_t g = run; g < groups; g += 8 * kRuns) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = g + k * kRuns < groups ? parts[(g + k * kRuns) * n + c] : 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += v[k];
+        }
     }
     runs[run][lane] = sum;
     __syncthreads();
-    if (run == 0 && c < n) columns[c] = runs[0][lane] + runs[1][lane] + (runs[2][lane] + runs[3][lane]);
+    if (run == 0 && c < n) {
+#pragma unroll
+        for (int k = 1; k < kRuns; ++k) sum += runs[k][lane];
+        columns[c] = sum;
+    }
 }
 
 constexpr size_t kWorkspaceBytes = 128u << 20, kWorkspaceMost = (size_t)1 << 34;
@@ -1207,7 +1313,7 @@ int als_log_prob(als_predict_ctx* ctx, const als_scores* scores, const als_given
         if (s.n <= kHeld) {
             if (s.n <= 1024) return go(integral_constant<int, 8>(), s.rows);
             if (s.n <= 16384) return go(integral_constant<int, 16>(), s.rows);
-            return go(integral_constant<int, 32>(), s.rows);
+            return go(integral_constant<int, 40>(), s.rows);
         }
         a.segments = (uint32_t)((s.n + kSegment - 1) / kSegment);
         a.columns = kSegment;
@@ -1254,36 +1360,32 @@ int als_log_prob_grad(als_predict_ctx* ctx, const als_scores* scores, const als_
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return ALS_ERR_DEVICE;
     const hipStream_t st = (hipStream_t)stream;
-    const int64_t chunks = (s.n + kGradChunk - 1) / kGradChunk;
     // a workgroup takes one row's chunk, or with the columns' sums as many rows as leave every CU eight workgroups
-    int64_t groups = s.rows;
-    if (columns) {
-        groups = (8 * ctx->cus + chunks - 1) / chunks;
-        const int64_t fit = (int64_t)(ctx->ws_bytes / 4) / s.n;
-        groups = groups < fit ? groups : fit;
-    }
-    const int64_t most = kMaxThreads / kGradThreads / chunks;
-    groups = groups < most ? groups : most;
-    groups = groups < s.rows ? groups : s.rows;
-    if (s.rows > 0)
-        by_type(s.dtype, [&](auto* p) {
-            using T = Type<decltype(p)>;
-            GradArgs<T> g{};
-            g.of = row_args<T>(scores, given);
-            g.of.log = const_cast<float*>(log);
-            g.of.stats = const_cast<float*>(stats);
-            g.of.entropy = const_cast<float*>(entropy);
-            g.grad_log = grad_log;
-            g.grad_entropy = grad_entropy;
-            g.grad = (T*)grad;
-            g.ldg = ldg;
-            g.parts = columns ? (float*)ctx->ws : nullptr;
-            g.chunks = (uint32_t)chunks;
-            g.groups = (uint32_t)groups;
-            hipLaunchKernelGGL(k_gradient<T>, dim3((unsigned)(chunks * groups)), dim3(kGradThreads), 0, st, g);
-        });
+    int64_t groups = 0;
+    by_type(s.dtype, [&](auto* p) {
+        using T = Type<decltype(p)>;
+        const int64_t chunk = columns ? Grad<true>::kChunk : Grad<false>::kChunk, chunks = (s.n + chunk - 1) / chunk;
+        groups = s.rows;
+        if (columns) {
+            const int64_t wanted = (8 * ctx->cus + chunks - 1) / chunks, fit = (int64_t)(ctx->ws_bytes / 4) / s.n;
+            groups = groups < wanted ? groups : wanted;
+            groups = groups < fit ? groups : fit;
+        }
+        const int64_t most = kMaxThreads / kGradThreads / chunks;
+        groups = groups < most ? groups : most;
+        if (groups == 0) return;
+        const GradArgs<T> g{(const T*)s.z, s.rows, s.n, s.ldz, s.temperature_all, s.of, given->entries, given->each,
+                            (T*)grad, ldg, (float*)ctx->ws, (uint32_t)chunks, (uint32_t)groups};
+        const auto go = [&](auto* kernel) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)(chunks * groups)), dim3(kGradThreads), 0, st, g, s.temperature,
+                               s.rated_ptr, s.rated_idx, s.users, given->ptr, given->idx, log, stats, entropy, grad_log,
+                               grad_entropy);
+        };
+        if (columns) go(k_gradient<T, true>);
+        else go(k_gradient<T, false>);
+    });
     if (columns)
-        hipLaunchKernelGGL(k_columns, dim3((unsigned)((s.n + kWave - 1) / kWave)), dim3(256), 0, st,
+        hipLaunchKernelGGL(k_columns, dim3((unsigned)((s.n + kWave - 1) / kWave)), dim3(kRuns * kWave), 0, st,
                            (const float*)ctx->ws, (uint32_t)groups, s.n, columns);
     return finish(ctx);
 }
