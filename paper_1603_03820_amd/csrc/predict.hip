@@ -1,7 +1,8 @@
 // How probable items are under a trained factor model, on gfx950 (MI355X): the C ABI of include/als_predict.h plus its
 // kernels.
 //
-//   k_product     predictions from rows of any alignment, which pass through registers into LDS; fp32 rows as three bf16
+//   k_product_lds predictions from 16-bit rows at multiples of 16 bytes, which arrive in LDS straight from memory
+//   k_product     predictions from any other rows, which pass through registers into LDS; fp32 rows as three bf16
 //                 parts (k_join: the products' parts along f into one, where few tiles are cut along it)
 //   k_row         a row of scores, or a segment of one, as a distribution: statistics, given columns, best columns
 //                 (k_row_join: a row's segments into one)
@@ -18,6 +19,7 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef int i4 __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------------------- product --
 
@@ -54,18 +56,75 @@ struct Product {
     }
 };
 
-// GELU by erfc, which keeps its relative precision for negative y, where 1 + erf(y) does not.  The bounds below
-// are past where either function is -0 in fp32, and keep -inf from meeting its 0.
+// exp(x + low), x in [-300, 0] and low of its last bits: a product with log2(e) in two parts, as the whole exponent's
+// rounding would cost |x| units.
+__device__ __forceinline__ float exp_of(float x, float low) {
+    const float high = x * 0x1.715476p+0f;
+    const float rest = fmaf(x, 0x1.715476p+0f, -high) + fmaf(x, 0x1.4ae0cp-26f, low * 0x1.715476p+0f);
+    const float e = __builtin_amdgcn_exp2f(high);
+    return fmaf(e, rest * 0x1.62e43p-1f, e);
+}
+// 1 / d, d in [1, 2^30], to half a unit and a little.
+__device__ __forceinline__ float inverse_of(float d) {
+    const float r = __builtin_amdgcn_rcpf(d);
+    return fmaf(fmaf(-d, r, 1.f), r, r);
+}
+// 1 / (1 + exp(-y)) by exp(-|y|), which neither overflows nor loses the small values.
+__device__ __forceinline__ float sigmoid(float y) {
+    const float e = exp_of(-fminf(fabsf(y), 126.f), 0.f), r = inverse_of(1.f + e);
+    return y != y ? y : (y < 0.f ? e * r : r);
+}
+// y erfc(-y / sqrt 2) / 2.  With a = |y| / sqrt 2 and t = 1 / (1 + 0.3 a), erfc(a) exp(a^2) / t is a polynomial in t to
+// 2.1e-8 of its value for a up to 12 (fitted by least squares, weighted towards the largest error, to scipy's
+// erfcx); in fp32 GELU is off by at most 5e-7 of its value, also where it is small: 1 + erf(y / sqrt 2) would lose it.
+__device__ __forceinline__ float gelu(float y) {
+    const float a = fminf(fabsf(y), 18.f), t = inverse_of(fmaf(a, 0.212132034f, 1.f));
+    float q = -0.12925273f;
+    q = fmaf(q, t, 0.48429954f);
+    q = fmaf(q, t, -0.5097682f);
+    q = fmaf(q, t, 0.5449625f);
+    q = fmaf(q, t, -0.092823245f);
+    q = fmaf(q, t, 0.21418034f);
+    q = fmaf(q, t, 0.14852151f);
+    q = fmaf(q, t, 0.1706909f);
+    q = fmaf(q, t, 0.16918935f);
+    const float square = a * a, half = 0.5f * fminf(fmaxf(y, -30.f), 30.f);
+    const float tail = t * q * exp_of(-0.5f * square, -0.5f * fmaf(a, a, -square));
+    return y < 0.f ? half * tail : fmaf(-half, tail, y);
+}
+
+template <int ACT>
 __device__ __forceinline__ float activated(float y, const Epilogue& e) {
-    switch (e.activation) {
-        case ALS_ACT_CLIP: y = y < e.low ? e.low : y; return y > e.high ? e.high : y;
-        case ALS_ACT_RELU: return y < 0.f ? 0.f : y;
-        case ALS_ACT_GELU: y = y < -30.f ? -30.f : y; return 0.5f * y * erfcf(y * -0.70710678f);
-        case ALS_ACT_SILU: y = y < -200.f ? -200.f : y; return y / (1.f + expf(-y));
-        case ALS_ACT_SIGMOID: return 1.f / (1.f + expf(-y));
-        case ALS_ACT_TANH: return tanhf(y);
-        default: return y;
+    if constexpr (ACT == ALS_ACT_CLIP) {
+        y = y < e.low ? e.low : y;
+        return y > e.high ? e.high : y;
     }
+    if constexpr (ACT == ALS_ACT_RELU) return y < 0.f ? 0.f : y;
+    if constexpr (ACT == ALS_ACT_GELU) return gelu(y);
+    if constexpr (ACT == ALS_ACT_SILU) return fmaxf(y, -126.f) * sigmoid(y);
+    if constexpr (ACT == ALS_ACT_SIGMOID) return sigmoid(y);
+    if constexpr (ACT == ALS_ACT_TANH) return tanhf(y);
+    return y;
+}
+// fn(the activation as a constant): once for many values, as a choice for each takes longer than most of them do
+template <typename Fn>
+__device__ __forceinline__ void by_activation(int activation, Fn fn) {
+    using std::integral_constant;
+    switch (activation) {
+        case ALS_ACT_CLIP: return fn(integral_constant<int, ALS_ACT_CLIP>());
+        case ALS_ACT_RELU: return fn(integral_constant<int, ALS_ACT_RELU>());
+        case ALS_ACT_GELU: return fn(integral_constant<int, ALS_ACT_GELU>());
+        case ALS_ACT_SILU: return fn(integral_constant<int, ALS_ACT_SILU>());
+        case ALS_ACT_SIGMOID: return fn(integral_constant<int, ALS_ACT_SIGMOID>());
+        case ALS_ACT_TANH: return fn(integral_constant<int, ALS_ACT_TANH>());
+        default: return fn(integral_constant<int, ALS_ACT_NONE>());
+    }
+}
+template <typename Fn>
+__device__ __forceinline__ void by_out_type(int type, Fn fn) {
+    if (type == ALS_F32) fn((float*)nullptr);
+    else if (type == ALS_F16) fn((F16*)nullptr);
+    else fn((BF16*)nullptr);
 }
 
 // Four neighbouring values of a row, as far as `left` of them are there.
@@ -95,24 +154,38 @@ __device__ __forceinline__ void store4(T* p, int64_t left, const float (&v)[4]) 
     }
 }
 
-// Four neighbouring results of user i from their sums (a user that there is not: NaN), `left` of them to write.
-__device__ __forceinline__ void finish4(const Product& a, int64_t i, int64_t item, float (&v)[4], const float (&offset)[4]) {
+// What user i's results have added: its offset; NaN for a user that there is not.
+__device__ __forceinline__ float own_offset(const Product& a, int64_t i) {
+    const int64_t u = i < a.m ? a.user_of(i) : -1;
+    return u < 0 ? NAN : (a.end.user_offset ? a.end.user_offset[u] : 0.f);
+}
+
+// Of N rows of results, from the sums of four neighbouring items each: the residuals first, all of them on their way
+// together; then what follows a product.  Row k is user[k], `left` of its items are there (none: left <= 0).
+template <int N, int ACT>
+__device__ __forceinline__ void finish(const Product& a, const int64_t (&user)[N], const int64_t (&left)[N], int64_t item,
+                                       float (&v)[N][4], const float (&own)[N], const float (&offset)[4]) {
     const Epilogue& e = a.end;
-    const int64_t u = a.user_of(i), left = a.n - item;
-    const float own = u < 0 ? NAN : (e.user_offset ? e.user_offset[u] : 0.f);
-    float r[4] = {0.f, 0.f, 0.f, 0.f};
-    if (e.residual) {
-        const int64_t at = i * e.ldr + item;
-        if (e.type == ALS_F32) load4((const float*)e.residual + at, left, r);
-        else if (e.type == ALS_F16) load4((const F16*)e.residual + at, left, r);
-        else load4((const BF16*)e.residual + at, left, r);
-    }
+    float r[N][4];
+    if (e.residual)
+        by_out_type(e.type, [&](auto* p) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = activated(v[k] + own + offset[k], e) + r[k];
-    const int64_t at = i * e.ldo + item;
-    if (e.type == ALS_F32) store4((float*)e.out + at, left, v);
-    else if (e.type == ALS_F16) store4((F16*)e.out + at, left, v);
-    else store4((BF16*)e.out + at, left, v);
+            for (int k = 0; k < N; ++k) load4((decltype(p))e.residual + user[k] * e.ldr + item, left[k], r[k]);
+        });
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[k][i] = activated<ACT>(v[k][i] + own[k] + offset[i], e);
+    if (e.residual) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[k][i] += r[k][i];
+    }
+    by_out_type(e.type, [&](auto* p) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) store4((decltype(p))e.out + user[k] * e.ldo + item, left[k], v[k]);
+    });
 }
 
 // Tile t of a grid of tu x ti: the eight dies take workgroups in turn, so each gets a run of tiles of its own, and
@@ -196,6 +269,8 @@ struct Parts<float> {
     }
 };
 
+constexpr int kHead = 1024;      // of LDS: a tile's users' offsets
+
 template <typename T, int WU, int WI, int FU, int FI>
 struct Staged {
     using P = Parts<T>;
@@ -208,38 +283,68 @@ struct Staged {
     static constexpr int kOut = FU < 2 ? 1 : 2, kOutRows = WU * kOut * 16, kOutStride = kItems + 4;
     static constexpr int kLds = kStage > kOutRows * kOutStride * 4 ? kStage : kOutRows * kOutStride * 4;
     static_assert(FU % kOut == 0, "whole passes");
+    static_assert(kUsers * 4 <= kHead && kHead + kLds <= 160 * 1024, "LDS");
 };
+
+// The users' offsets of a tile, in LDS from the start on.
+template <typename C>
+__device__ __forceinline__ void fetch_offsets(const Product& a, float* own, int64_t u0) {
+    if (a.parts) return;
+    for (int r = threadIdx.x; r < C::kUsers; r += C::kThreads) own[r] = own_offset(a, u0 + r);
+}
 
 // The products of a tile on their way out, through LDS, so that a wave writes whole lines and what follows a product
 // is there once in the code.  A lane holds four neighbouring items (of group lane / 16) of one user (lane % 16).
 template <typename C, int WU, int WI, int FU, int FI>
-__device__ __forceinline__ void write_tile(const Product& a, const f4 (&acc)[FU][FI], float* lds, int64_t u0, int64_t i0,
-                                           int wu, int wi, int part) {
+__device__ __forceinline__ void write_tile(const Product& a, const f4 (&acc)[FU][FI], float* lds, const float* own,
+                                           int64_t u0, int64_t i0, int wu, int wi, int part) {
     const int lane = threadIdx.x & 63;
-    constexpr int kFours = C::kItems / 4, kAtOnce = C::kThreads / kFours;
+    constexpr int kFours = C::kItems / 4, kAtOnce = C::kThreads / kFours, kRuns = C::kOutRows / kAtOnce;
+    constexpr int N = kRuns < 4 ? kRuns : 4;
+    static_assert(C::kOutRows % kAtOnce == 0 && kRuns % N == 0, "whole runs of rows");
     const int four = threadIdx.x % kFours, first = threadIdx.x / kFours;
     const int64_t item = i0 + 4 * four;
     float offset[4] = {0.f, 0.f, 0.f, 0.f};
     if (a.end.item_offset && !a.parts) load4(a.end.item_offset + item, a.n - item, offset);
+    const auto all = [&](auto go) {
 #pragma unroll
-    for (int pass = 0; pass < FU / C::kOut; ++pass) {
-        __syncthreads();
+        for (int pass = 0; pass < FU / C::kOut; ++pass) {
+            __syncthreads();
 #pragma unroll
-        for (int u = 0; u < C::kOut; ++u)
+            for (int u = 0; u < C::kOut; ++u)
 #pragma unroll
-            for (int i = 0; i < FI; ++i)
-                *(f4*)(lds + ((wu * C::kOut + u) * 16 + (lane & 15)) * C::kOutStride + (wi * FI + i) * 16 + 4 * (lane >> 4)) =
-                    acc[pass * C::kOut + u][i];
-        __syncthreads();
-        for (int r = first; r < C::kOutRows; r += kAtOnce) {
-            const int64_t user = u0 + (r / (16 * C::kOut) * FU + pass * C::kOut) * 16 + r % (16 * C::kOut);
-            if (user >= a.m || item >= a.n) continue;
-            const f4 s = *(const f4*)(lds + r * C::kOutStride + 4 * four);
-            float v[4] = {s[0], s[1], s[2], s[3]};
-            if (a.parts) store4(a.parts + ((int64_t)part * a.m + user) * a.n + item, a.n - item, v);
-            else finish4(a, user, item, v, offset);
+                for (int i = 0; i < FI; ++i)
+                    *(f4*)(lds + ((wu * C::kOut + u) * 16 + (lane & 15)) * C::kOutStride + (wi * FI + i) * 16 + 4 * (lane >> 4)) =
+                        acc[pass * C::kOut + u][i];
+            __syncthreads();
+#pragma unroll 1
+            for (int run = 0; run < kRuns; run += N) {
+                float v[N][4], mine[N];
+                int64_t user[N], left[N];
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const int r = first + (run + k) * kAtOnce;
+                    const int local = (r / (16 * C::kOut) * FU + pass * C::kOut) * 16 + r % (16 * C::kOut);
+                    user[k] = u0 + local;
+                    left[k] = user[k] < a.m ? a.n - item : 0;
+                    mine[k] = own[local];
+                    const f4 s = *(const f4*)(lds + r * C::kOutStride + 4 * four);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[k][i] = s[i];
+                }
+                go(user, left, v, mine);
+            }
         }
-    }
+    };
+    if (a.parts)
+        all([&](auto& user, auto& left, auto& v, auto&) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) store4(a.parts + ((int64_t)part * a.m + user[k]) * a.n + item, left[k], v[k]);
+        });
+    else
+        by_activation(a.end.activation, [&](auto act) {
+            all([&](auto& user, auto& left, auto& v, auto& mine) { finish<N, act.value>(a, user, left, item, v, mine, offset); });
+        });
 }
 
 // The product in tiles, rows through registers: a workgroup of WU x WI waves holds a tile of users x items, each wave
@@ -251,11 +356,14 @@ template <typename T, int WU, int WI, int FU, int FI>
 __global__ __launch_bounds__(64 * WU * WI) void k_product(Product a) {
     using C = Staged<T, WU, WI, FU, FI>;
     using P = Parts<T>;
-    extern __shared__ __align__(1024) unsigned char lds[];
+    extern __shared__ __align__(1024) unsigned char shared[];
+    float* own = (float*)shared;
+    unsigned char* lds = shared + kHead;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t tile_u, tile_i;
     tile_of(blockIdx.x, a.tu, a.ti, &tile_u, &tile_i);
     const int64_t u0 = (int64_t)tile_u * C::kUsers, i0 = (int64_t)tile_i * C::kItems;
+    fetch_offsets<C>(a, own, u0);
     const auto slot = [](int r, int g) { return C::kRowBytes == 64 ? g ^ (r >> 2 & 3) : g ^ (r >> 1 & 7); };
 
     // this thread's groups of eight values: a row each, at the same place in every step
@@ -342,24 +450,190 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product(Product a) {
         multiply();
         if (step + 1 < end) __syncthreads();
     }
-    write_tile<C, WU, WI, FU, FI>(a, acc, (float*)lds, u0, i0, wu, wi, blockIdx.y);
+    write_tile<C, WU, WI, FU, FI>(a, acc, (float*)lds, own, u0, i0, wu, wi, blockIdx.y);
+}
+
+// A buffer of `bytes` bytes from `base` on (both the same in every lane).
+__device__ __forceinline__ i4 buffer_of(const void* base, uint32_t bytes) {
+    const uint64_t b = (uint64_t)base;
+    i4 r;
+    r[0] = __builtin_amdgcn_readfirstlane((uint32_t)b);
+    r[1] = __builtin_amdgcn_readfirstlane((uint32_t)(b >> 32) & 0xFFFFu);
+    r[2] = __builtin_amdgcn_readfirstlane(bytes);
+    r[3] = 0x00020000;
+    return r;
+}
+
+// 16 bytes a lane from buffer + voffset + soffset to LDS at `lds` + 16 lane.  Inline assembly: the compiler would
+// wait for every load to LDS before any LDS read.  It has no result register; the caller waits (settle) before the data
+// are read.  M0 needs one wait state, and is these loads' alone in their kernels (it cannot be named as clobbered).
+__device__ __forceinline__ void load_to_lds(i4 buffer, uint32_t voffset, uint32_t soffset, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds"
+                 :
+                 : "v"(voffset), "s"(buffer), "s"(soffset), "s"(lds)
+                 : "memory");
+}
+// A load reads a scalar register that a vector instruction wrote (readfirstlane) no sooner than five wait states
+// later; the compiler keeps them for the loads it knows.
+__device__ __forceinline__ void buffer_settle(i4 a, i4 b) { asm volatile("s_nop 4" : : "s"(a), "s"(b)); }
+// All of this wave's loads but the last LEFT have arrived, and its LDS reads are done.
+template <int LEFT>
+__device__ __forceinline__ void settle() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(LEFT) : "memory");
+}
+
+// The values of a group of eight 16-bit ones of which `left` are there, zeros in the others' place.
+__device__ __forceinline__ u4 keep_values(u4 v, int left) {
+#pragma unroll
+    for (int d = 0; d < 4; ++d) v[d] &= left >= 2 * d + 2 ? 0xFFFFFFFFu : (left == 2 * d + 1 ? 0xFFFFu : 0u);
+    return v;
+}
+
+constexpr int kStep = 64, kStepBytes = 128;
+constexpr int64_t kNear = 1 << 21;              // row strides below it (4 MiB) keep a tile's offsets below 2^30 ...
+constexpr uint32_t kPastEnd = 0x7FFFFFF0u;      // ... and this past every buffer's end
+
+template <int WU, int WI, int FU, int FI, int STAGES>
+struct Direct {
+    static constexpr int kWaves = WU * WI, kThreads = 64 * kWaves;
+    static constexpr int kUsers = WU * FU * 16, kItems = WI * FI * 16, kRows = kUsers + kItems;
+    static constexpr int kUserLoads = kUsers / 8 / kWaves, kItemLoads = kItems / 8 / kWaves;   // 1 KB, a wave and step
+    static constexpr int kStage = kRows * kStepBytes;
+    static constexpr int kOut = FU < 2 ? 1 : 2, kOutRows = WU * kOut * 16, kOutStride = kItems + 4;
+    static constexpr int kOutBytes = kOutRows * kOutStride * 4;
+    static_assert(kUsers % (8 * kWaves) == 0 && kItems % (8 * kWaves) == 0, "whole loads");
+    static_assert((STAGES - 2) * (kUserLoads + kItemLoads) < 64, "loads that can be counted");
+    static_assert(kUsers * 4 <= kHead && kHead + STAGES * kStage <= 160 * 1024 && kHead + kOutBytes <= 160 * 1024, "LDS");
+};
+
+// The product in tiles as k_product has them, of 16-bit rows at multiples of 16 bytes: a step's rows of both sides lie
+// in LDS, 128 bytes a row, while the next steps' (STAGES - 1 of them) arrive straight from memory beside them
+// (buffer_load ... lds: no registers, no instructions but the load).  Items and users past the end read as zeros; in the
+// last step values past f are masked on both sides, as what lies in their place may be no number.
+template <typename T, int WU, int WI, int FU, int FI, int STAGES>
+__global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
+    using C = Direct<WU, WI, FU, FI, STAGES>;
+    extern __shared__ __align__(1024) unsigned char shared[];
+    float* own = (float*)shared;
+    unsigned char* lds = shared + kHead;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t tile_u, tile_i;
+    tile_of(blockIdx.x, a.tu, a.ti, &tile_u, &tile_i);
+    const int64_t u0 = (int64_t)tile_u * C::kUsers, i0 = (int64_t)tile_i * C::kItems;
+    fetch_offsets<C>(a, own, u0);
+
+    // what the buffers hold: the tile's rows (all of X where users are taken by index), the last up to the end of its
+    // last group
+    const int64_t users = a.m - u0 < C::kUsers ? a.m - u0 : C::kUsers, items = a.n - i0 < C::kItems ? a.n - i0 : C::kItems;
+    const int64_t from = a.users ? 0 : u0, rows = a.users ? a.of : users;
+    const int whole = (a.f + 7) / 8 * 16;
+    const i4 from_u = buffer_of((const T*)a.x + from * a.ldx, rows > 0 ? (uint32_t)((rows - 1) * a.ldx * 2 + whole) : 0);
+    const i4 from_i = buffer_of((const T*)a.theta + i0 * a.ldt, (uint32_t)((items - 1) * a.ldt * 2 + whole));
+    buffer_settle(from_u, from_i);
+    const int first_u = wave * C::kUserLoads * 8, first_i = wave * C::kItemLoads * 8;   // this wave's rows
+    const auto group_of = [&](int r) { return 16 * ((lane & 7) ^ (r >> 1 & 7)); };
+    uint32_t of_u[C::kUserLoads], of_i[C::kItemLoads];
+#pragma unroll
+    for (int l = 0; l < C::kUserLoads; ++l) {
+        const int r = first_u + 8 * l + (lane >> 3);
+        const int64_t u = u0 + r < a.m ? a.user_of(u0 + r) : -1;
+        of_u[l] = u < 0 ? kPastEnd : (uint32_t)((u - from) * a.ldx * 2) + group_of(r);
+    }
+#pragma unroll
+    for (int l = 0; l < C::kItemLoads; ++l) {
+        const int r = first_i + 8 * l + (lane >> 3);
+        of_i[l] = (uint32_t)(r * a.ldt * 2) + group_of(r);
+    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
+    const int steps = (a.f + kStep - 1) / kStep, begin = blockIdx.y * a.steps;
+    const int end = begin + a.steps < steps ? begin + a.steps : steps;
+    // groups past f are not read: their offset is past the buffer's end
+    const auto fetch = [&](int step, int stage) {
+        const uint32_t to = lds0 + stage * C::kStage;
+        const int left = 2 * a.f - step * kStepBytes;
+#pragma unroll
+        for (int l = 0; l < C::kUserLoads; ++l) {
+            const int r = first_u + 8 * l;
+            load_to_lds(from_u, group_of(r + (lane >> 3)) < left ? of_u[l] : kPastEnd, step * kStepBytes,
+                        __builtin_amdgcn_readfirstlane(to + r * kStepBytes));
+        }
+#pragma unroll
+        for (int l = 0; l < C::kItemLoads; ++l) {
+            const int r = first_i + 8 * l;
+            load_to_lds(from_i, group_of(r + (lane >> 3)) < left ? of_i[l] : kPastEnd, step * kStepBytes,
+                        __builtin_amdgcn_readfirstlane(to + (C::kUsers + r) * kStepBytes));
+        }
+    };
+
+    const int wu = wave / WI, wi = wave % WI;
+    const int row = lane & 15, group = lane >> 4;
+    f4 acc[FU][FI];
+#pragma unroll
+    for (int u = 0; u < FU; ++u)
+#pragma unroll
+        for (int i = 0; i < FI; ++i) acc[u][i] = f4{0.f, 0.f, 0.f, 0.f};
+    const auto multiply = [&](int step, int stage, auto tail) {
+        const unsigned char* at = lds + stage * C::kStage;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            u4 t[FI], x[FU];
+            const int left = a.f - step * kStep - 32 * h - 8 * group;
+            const auto read = [&](int r) {
+                const u4 v = *(const u4*)(at + r * kStepBytes + 16 * ((4 * h + group) ^ (r >> 1 & 7)));
+                return tail.value ? keep_values(v, left) : v;
+            };
+#pragma unroll
+            for (int i = 0; i < FI; ++i) t[i] = read(C::kUsers + (wi * FI + i) * 16 + row);
+#pragma unroll
+            for (int u = 0; u < FU; ++u) x[u] = read((wu * FU + u) * 16 + row);
+#pragma unroll
+            for (int u = 0; u < FU; ++u)
+#pragma unroll
+                for (int i = 0; i < FI; ++i) acc[u][i] = multiply8(t[i], x[u], acc[u][i], T());
+        }
+    };
+
+#pragma unroll
+    for (int p = 0; p < STAGES - 1; ++p)
+        if (begin + p < end) fetch(begin + p, p);
+    // a step: its rows are there and the last step's are done with (one barrier for both), whose place the rows
+    // STAGES - 1 steps on take
+    int stage = 0;
+    const auto after = [](int x) { return x + 1 == STAGES ? 0 : x + 1; };
+    int step = begin;
+    for (; step + STAGES - 1 < end; ++step) {
+        settle<(STAGES - 2) * (C::kUserLoads + C::kItemLoads)>();
+        __builtin_amdgcn_s_barrier();
+        fetch(step + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
+        multiply(step, stage, std::false_type());
+        stage = after(stage);
+    }
+    settle<0>();
+    __builtin_amdgcn_s_barrier();
+    for (; step + 1 < end; ++step) {
+        multiply(step, stage, std::false_type());
+        stage = after(stage);
+    }
+    multiply(step, stage, std::true_type());
+    write_tile<C, WU, WI, FU, FI>(a, acc, (float*)lds, own, u0, i0, wu, wi, blockIdx.y);
 }
 
 // The sums of the parts of f into one, in their order, and what follows a product.
-__global__ __launch_bounds__(256) void k_join(Product a, int count, int64_t row0) {
-    const int64_t fours = (a.n + 3) / 4, at = row0 * fours + (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(256) void k_join(Product a, int count) {
+    const int64_t fours = (a.n + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t i = at / fours, item = at % fours * 4;
     if (i >= a.m) return;
-    float v[4], offset[4] = {0.f, 0.f, 0.f, 0.f};
-    load4(a.parts + i * a.n + item, a.n - item, v);
+    float v[1][4], offset[4] = {0.f, 0.f, 0.f, 0.f};
+    load4(a.parts + i * a.n + item, a.n - item, v[0]);
     for (int p = 1; p < count; ++p) {
         float w[4];
         load4(a.parts + (p * a.m + i) * a.n + item, a.n - item, w);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] += w[k];
+        for (int k = 0; k < 4; ++k) v[0][k] += w[k];
     }
     if (a.end.item_offset) load4(a.end.item_offset + item, a.n - item, offset);
-    finish4(a, i, item, v, offset);
+    const float own = own_offset(a, i);
+    by_activation(a.end.activation, [&](auto act) { finish<1, act.value>(a, {i}, {a.n - item}, item, v, {own}, offset); });
 }
 
 // --------------------------------------------------------------------------- distribution --
@@ -1093,17 +1367,14 @@ void by_type(int dtype, Fn fn) {
 template <typename P>
 using Type = std::remove_cv_t<std::remove_pointer_t<P>>;
 
-// `rows` rows of the product that are one launch's.
-template <typename T, int WU, int WI, int FU, int FI>
-void launch_product(const als_predict_ctx* ctx, Product a, hipStream_t st) {
-    using C = Staged<T, WU, WI, FU, FI>;
-    static std::atomic<uint64_t> done{0};
-    auto* kernel = k_product<T, WU, WI, FU, FI>;
-    whole_lds(kernel, ctx->device, &done);
-    a.tu = (uint32_t)((a.m + C::kUsers - 1) / C::kUsers);
-    a.ti = (uint32_t)((a.n + C::kItems - 1) / C::kItems);
-    const int64_t steps = (a.f + Parts<T>::kValues - 1) / Parts<T>::kValues, tiles = (int64_t)a.tu * a.ti;
-    // few tiles: f in parts of 4 steps at least, as many as give every CU two workgroups and the workspace holds
+// The product's tiles in one launch, and where there are few of them f in parts of 4 steps at least, as many as give every CU
+// two workgroups and the workspace holds.
+template <typename Kernel>
+void launch_product(const als_predict_ctx* ctx, Kernel kernel, Product a, int users, int items, int values, int threads,
+                    int lds, hipStream_t st) {
+    a.tu = (uint32_t)((a.m + users - 1) / users);
+    a.ti = (uint32_t)((a.n + items - 1) / items);
+    const int64_t steps = (a.f + values - 1) / values, tiles = (int64_t)a.tu * a.ti;
     int64_t parts = 2 * ctx->cus / tiles;
     if (parts > steps / 4) parts = steps / 4;
     const int64_t fit = (int64_t)(ctx->ws_bytes / 4) / (a.m * a.n);
@@ -1112,11 +1383,30 @@ void launch_product(const als_predict_ctx* ctx, Product a, hipStream_t st) {
     a.steps = (int)((steps + parts - 1) / parts);
     parts = (steps + a.steps - 1) / a.steps;
     a.parts = parts > 1 ? (float*)ctx->ws : nullptr;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)parts), dim3(C::kThreads), C::kLds, st, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles, (unsigned)parts), dim3(threads), kHead + lds, st, a);
     if (parts > 1) {
         const int64_t fours = a.m * ((a.n + 3) / 4);
-        hipLaunchKernelGGL(k_join, dim3((unsigned)((fours + 255) / 256)), dim3(256), 0, st, a, (int)parts, (int64_t)0);
+        hipLaunchKernelGGL(k_join, dim3((unsigned)((fours + 255) / 256)), dim3(256), 0, st, a, (int)parts);
     }
+}
+
+template <typename T, int WU, int WI, int FU, int FI>
+void staged(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
+    using C = Staged<T, WU, WI, FU, FI>;
+    static std::atomic<uint64_t> done{0};
+    auto* kernel = k_product<T, WU, WI, FU, FI>;
+    whole_lds(kernel, ctx->device, &done);
+    launch_product(ctx, kernel, a, C::kUsers, C::kItems, C::P::kValues, C::kThreads, C::kLds, st);
+}
+
+template <typename T, int WU, int WI, int FU, int FI, int STAGES>
+void direct(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
+    using C = Direct<WU, WI, FU, FI, STAGES>;
+    static std::atomic<uint64_t> done{0};
+    auto* kernel = k_product_lds<T, WU, WI, FU, FI, STAGES>;
+    whole_lds(kernel, ctx->device, &done);
+    const int steps = (a.f + kStep - 1) / kStep, rows = (steps < STAGES ? steps : STAGES) * C::kStage;
+    launch_product(ctx, kernel, a, C::kUsers, C::kItems, kStep, C::kThreads, rows > C::kOutBytes ? rows : C::kOutBytes, st);
 }
 
 template <typename T>
@@ -1124,12 +1414,24 @@ void product(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
     const auto tiles = [&](int64_t users, int64_t items) {
         return ((a.m + users - 1) / users) * ((a.n + items - 1) / items);
     };
-    if (a.m > 16) {
-        if (tiles(128, 128) >= 2 * ctx->cus) return launch_product<T, 2, 2, 4, 4>(ctx, a, st);
-        if (tiles(64, 128) >= 2 * ctx->cus) return launch_product<T, 2, 2, 2, 4>(ctx, a, st);
-        return launch_product<T, 2, 2, 2, 2>(ctx, a, st);
+    if constexpr (sizeof(T) == 2) {
+        const auto near = [](const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0 && ld < kNear; };
+        if (near(a.x, a.ldx) && near(a.theta, a.ldt) && (!a.users || a.of < (int64_t)(kPastEnd / 2) / a.ldx)) {
+            if (a.m > 16) {
+                if (a.f >= 512 && tiles(256, 256) >= ctx->cus) return direct<T, 2, 4, 8, 4, 2>(ctx, a, st);
+                if (tiles(128, 128) >= 2 * ctx->cus) return direct<T, 2, 2, 4, 4, 2>(ctx, a, st);
+                if (tiles(64, 128) >= 2 * ctx->cus) return direct<T, 2, 2, 2, 4, 2>(ctx, a, st);
+                return direct<T, 2, 2, 2, 2, 4>(ctx, a, st);
+            }
+            return direct<T, 1, 2, 1, 2, 4>(ctx, a, st);
+        }
     }
-    return launch_product<T, 1, 4, 1, 1>(ctx, a, st);
+    if (a.m > 16) {
+        if (tiles(128, 128) >= 2 * ctx->cus) return staged<T, 2, 2, 4, 4>(ctx, a, st);
+        if (tiles(64, 128) >= 2 * ctx->cus) return staged<T, 2, 2, 2, 4>(ctx, a, st);
+        return staged<T, 2, 2, 2, 2>(ctx, a, st);
+    }
+    return staged<T, 1, 4, 1, 1>(ctx, a, st);
 }
 
 // A row's registers: as many scores a thread as E; longer rows in segments.

@@ -67,6 +67,22 @@ def test_predict_whole_numbers(ctx, dtype, m, n, f):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("m,n,f", [(4101, 4105, 520), (4101, 4105, 515), (2300, 2100, 64), (2300, 2100, 200), (1100, 2100, 1000),
+                                   (1500, 1400, 72), (600, 900, 4100), (20, 300, 9000), (16, 8192, 2048), (4096, 4097, 512)])
+def test_predict_large(ctx, dtype, m, n, f):
+    """Enough tiles for every shape of them, and few that are cut along f: whole numbers against 64-bit products, rows taken
+    by index and in order."""
+    from paper_1603_03820_amd import predict
+    gen = torch.Generator(device=D).manual_seed(m + n + f)
+    x, t = (torch.randint(-3, 4, (r, f), device=D, generator=gen).to(TYPES[dtype]) for r in (m + 3, n))
+    users = torch.randint(0, m + 3, (m,), device=D, generator=gen, dtype=torch.int32)
+    log(f"predict {dtype} {m}x{n}x{f}")
+    want = x.double() @ t.double().t()
+    assert torch.equal(predict.als_predict(ctx, x, t).double(), want)
+    assert torch.equal(predict.als_predict(ctx, x, t, users=users).double(), want[users.long()])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("extra,offset", [(0, 1), (1, 0), (3, 5), (4, 8), (8, 0), (7, 2)])
 @pytest.mark.parametrize("f", [5, 64, 100, 130])
 def test_predict_strides(ctx, dtype, f, extra, offset):
