@@ -21,6 +21,29 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef int i4 __attribute__((ext_vector_type(4)));
 
+// Two values to 16 bits each by one instruction, where the type has one.
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t two_bf16(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), bf2));
+}
+template <int N, typename T>
+__device__ __forceinline__ void from_floats(const float* v, T (&out)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) from_float(v[i], &out[i]);
+}
+template <int N>
+__device__ __forceinline__ void from_floats(const float* v, BF16 (&out)[N]) {
+    uint32_t w[N / 2];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) w[i] = two_bf16(v[2 * i], v[2 * i + 1]);
+    __builtin_memcpy(out, w, sizeof out);
+}
+
+// A barrier for what the workgroup's waves write to LDS and read there: __syncthreads() would also wait for the loads and
+// stores that are on their way to or from memory.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // ------------------------------------------------------------------------------- product --
 
 // What follows a product: its offsets, activation and residual, and where it goes.
@@ -93,6 +116,26 @@ __device__ __forceinline__ float gelu(float y) {
     return y < 0.f ? half * tail : fmaf(-half, tail, y);
 }
 
+// For results of 16 bits, whose half a unit is 2^-11 or more of them: exponentials of arguments rounded to fp32 (a few
+// units of 2^-24, times the exponent's size), and for GELU a polynomial (in t = 1 / (1 + 0.44 a)) to 5e-06.
+__device__ __forceinline__ float sigmoid16(float y) {
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y * -0x1.715476p+0f));
+}
+__device__ __forceinline__ float gelu16(float y) {
+    const float a = fminf(fabsf(y), 18.f), t = __builtin_amdgcn_rcpf(fmaf(a, 0.31112698f, 1.f));
+    float q = -0.14610672f;
+    q = fmaf(q, t, 0.35065565f);
+    q = fmaf(q, t, 0.040727474f);
+    q = fmaf(q, t, 0.26358837f);
+    q = fmaf(q, t, 0.242569f);
+    q = fmaf(q, t, 0.24856107f);
+    const float half = 0.5f * fminf(fmaxf(y, -30.f), 30.f);
+    const float tail = t * q * __builtin_amdgcn_exp2f(a * a * -0.72134752f);
+    return y < 0.f ? half * tail : fmaf(-half, tail, y);
+}
+
+// The activations, and those of results of 16 bits.
+enum { kSigmoid16 = 16, kSilu16, kGelu16 };
 template <int ACT>
 __device__ __forceinline__ float activated(float y, const Epilogue& e) {
     if constexpr (ACT == ALS_ACT_CLIP) {
@@ -104,18 +147,23 @@ __device__ __forceinline__ float activated(float y, const Epilogue& e) {
     if constexpr (ACT == ALS_ACT_SILU) return fmaxf(y, -126.f) * sigmoid(y);
     if constexpr (ACT == ALS_ACT_SIGMOID) return sigmoid(y);
     if constexpr (ACT == ALS_ACT_TANH) return tanhf(y);
+    if constexpr (ACT == kGelu16) return gelu16(y);
+    if constexpr (ACT == kSilu16) return fmaxf(y, -126.f) * sigmoid16(y);
+    if constexpr (ACT == kSigmoid16) return sigmoid16(y);
     return y;
 }
 // fn(the activation as a constant): once for many values, as a choice for each takes longer than most of them do
 template <typename Fn>
-__device__ __forceinline__ void by_activation(int activation, Fn fn) {
+__device__ __forceinline__ void by_activation(const Epilogue& e, Fn fn) {
     using std::integral_constant;
-    switch (activation) {
+    const bool fine = e.type == ALS_F32;
+    switch (e.activation) {
         case ALS_ACT_CLIP: return fn(integral_constant<int, ALS_ACT_CLIP>());
         case ALS_ACT_RELU: return fn(integral_constant<int, ALS_ACT_RELU>());
-        case ALS_ACT_GELU: return fn(integral_constant<int, ALS_ACT_GELU>());
-        case ALS_ACT_SILU: return fn(integral_constant<int, ALS_ACT_SILU>());
-        case ALS_ACT_SIGMOID: return fn(integral_constant<int, ALS_ACT_SIGMOID>());
+        case ALS_ACT_GELU: return fine ? fn(integral_constant<int, ALS_ACT_GELU>()) : fn(integral_constant<int, kGelu16>());
+        case ALS_ACT_SILU: return fine ? fn(integral_constant<int, ALS_ACT_SILU>()) : fn(integral_constant<int, kSilu16>());
+        case ALS_ACT_SIGMOID:
+            return fine ? fn(integral_constant<int, ALS_ACT_SIGMOID>()) : fn(integral_constant<int, kSigmoid16>());
         case ALS_ACT_TANH: return fn(integral_constant<int, ALS_ACT_TANH>());
         default: return fn(integral_constant<int, ALS_ACT_NONE>());
     }
@@ -127,12 +175,24 @@ __device__ __forceinline__ void by_out_type(int type, Fn fn) {
     else fn((BF16*)nullptr);
 }
 
-// Four neighbouring values of a row, as far as `left` of them are there.
+// Four neighbouring values of a row, as far as `left` of them are there.  (As a vector of the elements' alignment: of four
+// values the compiler takes apart what both branches do, and the whole four are no longer one access.)
 template <typename T>
-__device__ __forceinline__ void load4(const T* p, int64_t left, float (&v)[4]) {
+struct Vector4;
+template <>
+struct Vector4<float> { typedef uint32_t Type __attribute__((ext_vector_type(4), aligned(4))); };
+template <>
+struct Vector4<F16> { typedef uint16_t Type __attribute__((ext_vector_type(4), aligned(2))); };
+template <>
+struct Vector4<BF16> { typedef uint16_t Type __attribute__((ext_vector_type(4), aligned(2))); };
+
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, int left, float (&v)[4]) {
+    using Vector = typename Vector4<T>::Type;
     T t[4];
     if (left >= 4) {
-        __builtin_memcpy(t, p, sizeof t);
+        const Vector w = *(const Vector*)p;
+        __builtin_memcpy(t, &w, sizeof t);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = to_float(t[i]);
     } else {
@@ -141,12 +201,14 @@ __device__ __forceinline__ void load4(const T* p, int64_t left, float (&v)[4]) {
     }
 }
 template <typename T>
-__device__ __forceinline__ void store4(T* p, int64_t left, const float (&v)[4]) {
+__device__ __forceinline__ void store4(T* p, int left, const float (&v)[4]) {
+    using Vector = typename Vector4<T>::Type;
     T t[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) from_float(v[i], &t[i]);
+    from_floats<4>(v, t);
     if (left >= 4) {
-        __builtin_memcpy(p, t, sizeof t);
+        Vector w;
+        __builtin_memcpy(&w, t, sizeof t);
+        *(Vector*)p = w;
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -160,17 +222,25 @@ __device__ __forceinline__ float own_offset(const Product& a, int64_t i) {
     return u < 0 ? NAN : (a.end.user_offset ? a.end.user_offset[u] : 0.f);
 }
 
+// How many of the four items from `item` on there are.
+__device__ __forceinline__ int items_left(const Product& a, int64_t item) {
+    const int64_t left = a.n - item;
+    return left >= 4 ? 4 : (left > 0 ? (int)left : 0);
+}
+
 // Of N rows of results, from the sums of four neighbouring items each: the residuals first, all of them on their way
-// together; then what follows a product.  Row k is user[k], `left` of its items are there (none: left <= 0).
+// together; then what follows a product.  The rows lie `row[k]` (the same in every lane, so that no lane multiplies by a
+// row stride) past the user whose results are at out_at and residuals at residual_at; `left[k]` of the four are there.
 template <int N, int ACT>
-__device__ __forceinline__ void finish(const Product& a, const int64_t (&user)[N], const int64_t (&left)[N], int64_t item,
-                                       float (&v)[N][4], const float (&own)[N], const float (&offset)[4]) {
+__device__ __forceinline__ void finish(const Product& a, int64_t out_at, int64_t residual_at, const int (&row)[N],
+                                       const int (&left)[N], float (&v)[N][4], const float (&own)[N],
+                                       const float (&offset)[4]) {
     const Epilogue& e = a.end;
     float r[N][4];
     if (e.residual)
         by_out_type(e.type, [&](auto* p) {
 #pragma unroll
-            for (int k = 0; k < N; ++k) load4((decltype(p))e.residual + user[k] * e.ldr + item, left[k], r[k]);
+            for (int k = 0; k < N; ++k) load4((decltype(p))e.residual + row[k] * e.ldr + residual_at, left[k], r[k]);
         });
 #pragma unroll
     for (int k = 0; k < N; ++k)
@@ -184,7 +254,7 @@ __device__ __forceinline__ void finish(const Product& a, const int64_t (&user)[N
     }
     by_out_type(e.type, [&](auto* p) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) store4((decltype(p))e.out + user[k] * e.ldo + item, left[k], v[k]);
+        for (int k = 0; k < N; ++k) store4((decltype(p))e.out + row[k] * e.ldo + out_at, left[k], v[k]);
     });
 }
 
@@ -228,13 +298,6 @@ struct Parts {
     static __device__ __forceinline__ void split(const u4 (&raw)[1], u4 (&part)[1]) { part[0] = raw[0]; }
     static constexpr int kRaw = 1;
 };
-
-__device__ __forceinline__ uint32_t two_bf16(float a, float b) {
-    BF16 t[2];
-    from_float(a, &t[0]);
-    from_float(b, &t[1]);
-    return (uint32_t)t[0].bits | (uint32_t)t[1].bits << 16;
-}
 
 template <>
 struct Parts<float> {
@@ -286,10 +349,15 @@ struct Staged {
     static_assert(kUsers * 4 <= kHead && kHead + kLds <= 160 * 1024, "LDS");
 };
 
-// The users' offsets of a tile, in LDS from the start on.
+// What a tile's results have added: the users' offsets in LDS, and those of this thread's four items.  Asked for once the
+// first rows are on their way, so that neither they nor the results wait for it.
 template <typename C>
-__device__ __forceinline__ void fetch_offsets(const Product& a, float* own, int64_t u0) {
+__device__ __forceinline__ void fetch_offsets(const Product& a, float* own, float (&offset)[4], int64_t u0, int64_t i0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) offset[i] = 0.f;
     if (a.parts) return;
+    const int64_t item = i0 + 4 * (threadIdx.x % (C::kItems / 4));
+    if (a.end.item_offset) load4(a.end.item_offset + item, items_left(a, item), offset);
     for (int r = threadIdx.x; r < C::kUsers; r += C::kThreads) own[r] = own_offset(a, u0 + r);
 }
 
@@ -297,54 +365,57 @@ __device__ __forceinline__ void fetch_offsets(const Product& a, float* own, int6
 // is there once in the code.  A lane holds four neighbouring items (of group lane / 16) of one user (lane % 16).
 template <typename C, int WU, int WI, int FU, int FI>
 __device__ __forceinline__ void write_tile(const Product& a, const f4 (&acc)[FU][FI], float* lds, const float* own,
-                                           int64_t u0, int64_t i0, int wu, int wi, int part) {
+                                           const float (&offset)[4], int64_t u0, int64_t i0, int wu, int wi, int part) {
     const int lane = threadIdx.x & 63;
     constexpr int kFours = C::kItems / 4, kAtOnce = C::kThreads / kFours, kRuns = C::kOutRows / kAtOnce;
     constexpr int N = kRuns < 4 ? kRuns : 4;
-    static_assert(C::kOutRows % kAtOnce == 0 && kRuns % N == 0, "whole runs of rows");
+    static_assert(16 * C::kOut % kAtOnce == 0 && kRuns % N == 0, "whole runs of rows, each of one wave's users");
     const int four = threadIdx.x % kFours, first = threadIdx.x / kFours;
-    const int64_t item = i0 + 4 * four;
-    float offset[4] = {0.f, 0.f, 0.f, 0.f};
-    if (a.end.item_offset && !a.parts) load4(a.end.item_offset + item, a.n - item, offset);
-    const auto all = [&](auto go) {
-#pragma unroll
-        for (int pass = 0; pass < FU / C::kOut; ++pass) {
-            __syncthreads();
-#pragma unroll
-            for (int u = 0; u < C::kOut; ++u)
-#pragma unroll
-                for (int i = 0; i < FI; ++i)
-                    *(f4*)(lds + ((wu * C::kOut + u) * 16 + (lane & 15)) * C::kOutStride + (wi * FI + i) * 16 + 4 * (lane >> 4)) =
-                        acc[pass * C::kOut + u][i];
-            __syncthreads();
+    const int64_t item = i0 + 4 * four, user0 = u0 + first;
+    const int items = items_left(a, item), users = a.m - u0 < C::kUsers ? (int)(a.m - u0) : C::kUsers;
+    const int64_t out_at = user0 * a.end.ldo + item, residual_at = user0 * a.end.ldr + item, parts_at = (part * a.m + user0) * a.n + item;
+    const auto rows = [&](int pass, auto go) {
 #pragma unroll 1
-            for (int run = 0; run < kRuns; run += N) {
-                float v[N][4], mine[N];
-                int64_t user[N], left[N];
+        for (int run = 0; run < kRuns; run += N) {
+            float v[N][4], mine[N];
+            int row[N], left[N];
 #pragma unroll
-                for (int k = 0; k < N; ++k) {
-                    const int r = first + (run + k) * kAtOnce;
-                    const int local = (r / (16 * C::kOut) * FU + pass * C::kOut) * 16 + r % (16 * C::kOut);
-                    user[k] = u0 + local;
-                    left[k] = user[k] < a.m ? a.n - item : 0;
-                    mine[k] = own[local];
-                    const f4 s = *(const f4*)(lds + r * C::kOutStride + 4 * four);
+            for (int k = 0; k < N; ++k) {
+                const int r = (run + k) * kAtOnce;
+                row[k] = (r / (16 * C::kOut) * FU + pass * C::kOut) * 16 + r % (16 * C::kOut);
+                left[k] = first + row[k] < users ? items : 0;
+                mine[k] = own[first + row[k]];
+                const f4 s = *(const f4*)(lds + (first + r) * C::kOutStride + 4 * four);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v[k][i] = s[i];
-                }
-                go(user, left, v, mine);
+                for (int i = 0; i < 4; ++i) v[k][i] = s[i];
             }
+            go(row, left, v, mine);
         }
     };
-    if (a.parts)
-        all([&](auto& user, auto& left, auto& v, auto&) {
+#pragma unroll 1
+    for (int pass = 0; pass < FU / C::kOut; ++pass) {
+        lds_barrier();
 #pragma unroll
-            for (int k = 0; k < N; ++k) store4(a.parts + ((int64_t)part * a.m + user[k]) * a.n + item, left[k], v[k]);
-        });
-    else
-        by_activation(a.end.activation, [&](auto act) {
-            all([&](auto& user, auto& left, auto& v, auto& mine) { finish<N, act.value>(a, user, left, item, v, mine, offset); });
-        });
+        for (int u = 0; u < FU; ++u) {
+            if (u / C::kOut != pass) continue;
+#pragma unroll
+            for (int i = 0; i < FI; ++i)
+                *(f4*)(lds + ((wu * C::kOut + u % C::kOut) * 16 + (lane & 15)) * C::kOutStride + (wi * FI + i) * 16 +
+                       4 * (lane >> 4)) = acc[u][i];
+        }
+        lds_barrier();
+        if (a.parts)
+            rows(pass, [&](auto& row, auto& left, auto& v, auto&) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) store4(a.parts + row[k] * a.n + parts_at, left[k], v[k]);
+            });
+        else
+            by_activation(a.end, [&](auto act) {
+                rows(pass, [&](auto& row, auto& left, auto& v, auto& mine) {
+                    finish<N, act.value>(a, out_at, residual_at, row, left, v, mine, offset);
+                });
+            });
+    }
 }
 
 // The product in tiles, rows through registers: a workgroup of WU x WI waves holds a tile of users x items, each wave
@@ -363,7 +434,6 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product(Product a) {
     uint32_t tile_u, tile_i;
     tile_of(blockIdx.x, a.tu, a.ti, &tile_u, &tile_i);
     const int64_t u0 = (int64_t)tile_u * C::kUsers, i0 = (int64_t)tile_i * C::kItems;
-    fetch_offsets<C>(a, own, u0);
     const auto slot = [](int r, int g) { return C::kRowBytes == 64 ? g ^ (r >> 2 & 3) : g ^ (r >> 1 & 7); };
 
     // this thread's groups of eight values: a row each, at the same place in every step
@@ -443,14 +513,16 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product(Product a) {
     const int steps = (a.f + P::kValues - 1) / P::kValues, begin = blockIdx.y * a.steps;
     const int end = begin + a.steps < steps ? begin + a.steps : steps;
     fetch(begin);
+    float offset[4];
+    fetch_offsets<C>(a, own, offset, u0, i0);
     for (int step = begin; step < end; ++step) {
         stage();
-        __syncthreads();
+        lds_barrier();
         if (step + 1 < end) fetch(step + 1);
         multiply();
-        if (step + 1 < end) __syncthreads();
+        if (step + 1 < end) lds_barrier();
     }
-    write_tile<C, WU, WI, FU, FI>(a, acc, (float*)lds, own, u0, i0, wu, wi, blockIdx.y);
+    write_tile<C, WU, WI, FU, FI>(a, acc, (float*)lds, own, offset, u0, i0, wu, wi, blockIdx.y);
 }
 
 // A buffer of `bytes` bytes from `base` on (both the same in every lane).
@@ -520,7 +592,6 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
     uint32_t tile_u, tile_i;
     tile_of(blockIdx.x, a.tu, a.ti, &tile_u, &tile_i);
     const int64_t u0 = (int64_t)tile_u * C::kUsers, i0 = (int64_t)tile_i * C::kItems;
-    fetch_offsets<C>(a, own, u0);
 
     // what the buffers hold: the tile's rows (all of X where users are taken by index), the last up to the end of its
     // last group
@@ -596,6 +667,8 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
 #pragma unroll
     for (int p = 0; p < STAGES - 1; ++p)
         if (begin + p < end) fetch(begin + p, p);
+    float offset[4];
+    fetch_offsets<C>(a, own, offset, u0, i0);
     // a step: its rows are there and the last step's are done with (one barrier for both), whose place the rows
     // STAGES - 1 steps on take
     int stage = 0;
@@ -615,7 +688,7 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
         stage = after(stage);
     }
     multiply(step, stage, std::true_type());
-    write_tile<C, WU, WI, FU, FI>(a, acc, (float*)lds, own, u0, i0, wu, wi, blockIdx.y);
+    write_tile<C, WU, WI, FU, FI>(a, acc, (float*)lds, own, offset, u0, i0, wu, wi, blockIdx.y);
 }
 
 // The sums of the parts of f into one, in their order, and what follows a product.
@@ -623,17 +696,20 @@ __global__ __launch_bounds__(256) void k_join(Product a, int count) {
     const int64_t fours = (a.n + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int64_t i = at / fours, item = at % fours * 4;
     if (i >= a.m) return;
+    const int left = items_left(a, item);
     float v[1][4], offset[4] = {0.f, 0.f, 0.f, 0.f};
-    load4(a.parts + i * a.n + item, a.n - item, v[0]);
+    load4(a.parts + i * a.n + item, left, v[0]);
     for (int p = 1; p < count; ++p) {
         float w[4];
-        load4(a.parts + (p * a.m + i) * a.n + item, a.n - item, w);
+        load4(a.parts + (p * a.m + i) * a.n + item, left, w);
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[0][k] += w[k];
     }
-    if (a.end.item_offset) load4(a.end.item_offset + item, a.n - item, offset);
+    if (a.end.item_offset) load4(a.end.item_offset + item, left, offset);
     const float own = own_offset(a, i);
-    by_activation(a.end.activation, [&](auto act) { finish<1, act.value>(a, {i}, {a.n - item}, item, v, {own}, offset); });
+    by_activation(a.end, [&](auto act) {
+        finish<1, act.value>(a, i * a.end.ldo + item, i * a.end.ldr + item, {0}, {left}, v, {own}, offset);
+    });
 }
 
 // --------------------------------------------------------------------------- distribution --
@@ -1174,7 +1250,7 @@ __global__ __launch_bounds__(kGradThreads, COLUMNS ? 6 : 5) void k_gradient(
     int turn = 0;
     if (rated_ptr) {
         for (int w = threadIdx.x; w < 3 * kMarks; w += kGradThreads) marks[0][w] = 0;
-        __syncthreads();
+        lds_barrier();
     }
     // with the columns' sums a workgroup has several rows: the next one's values and the places after it are on their
     // way while a row is worked on
@@ -1203,7 +1279,7 @@ __global__ __launch_bounds__(kGradThreads, COLUMNS ? 6 : 5) void k_gradient(
                 for (int64_t k = p.rated + threadIdx.x + kGradThreads; k < p.rated_end; k += kGradThreads)
                     mark((uint32_t)rated_idx[k]);
             }
-            __syncthreads();
+            lds_barrier();
         }
         const uint32_t* marked = marks[turn];
         if (rated_ptr) {
@@ -1284,8 +1360,7 @@ __global__ __launch_bounds__(kGradThreads, COLUMNS ? 6 : 5) void k_gradient(
             for (int v = 0; v < E / V; ++v) {
                 const uint32_t c = position(v);
                 T w[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) from_float(d[v * V + i], &w[i]);
+                from_floats<V>(&d[v * V], w);
                 if (inside) {
                     __builtin_memcpy(to + c, w, sizeof w);
                 } else {
