@@ -66,8 +66,9 @@ struct Product {
     int64_t m;
     const void* theta;
     int64_t n, ldt;
-    int f;
+    int f, tail;             // values of a row, and those of them behind the last whole step (see k_product)
     uint32_t tu, ti;         // tiles of users and of items
+    uint32_t height;         // tiles of users that follow one another
     int steps;               // along f in one part of it
     Epilogue end;
     float* parts;            // where f is cut: parts x m x n sums; else NULL
@@ -259,13 +260,13 @@ __device__ __forceinline__ void finish(const Product& a, int64_t out_at, int64_t
 }
 
 // Tile t of a grid of tu x ti: the eight dies take workgroups in turn, so each gets a run of tiles of its own, and
-// runs go down eight tiles of users before the next of items (their rows stay in the die's L2).
-__device__ __forceinline__ void tile_of(uint32_t t, uint32_t tu, uint32_t ti, uint32_t* u, uint32_t* i) {
+// runs go down `height` tiles of users before the next of items (their rows stay in the die's L2).
+__device__ __forceinline__ void tile_of(uint32_t t, uint32_t tu, uint32_t ti, uint32_t height, uint32_t* u, uint32_t* i) {
     const uint32_t total = tu * ti, per = total / 8;
     if (t < per * 8) t = (t % 8) * per + t / 8;
-    const uint32_t band = 8 * ti, b = t / band, left = t % band;
-    const uint32_t high = tu - 8 * b < 8 ? tu - 8 * b : 8;
-    *u = 8 * b + left % high;
+    const uint32_t band = height * ti, b = t / band, left = t % band;
+    const uint32_t high = tu - height * b < height ? tu - height * b : height;
+    *u = height * b + left % high;
     *i = left / high;
 }
 
@@ -306,13 +307,15 @@ struct Parts<float> {
     using Part = BF16;
     static constexpr int kRaw = 2;
     static __device__ __forceinline__ void load(const float* p, int left, u4 (&v)[2]) {
-        if (left >= 8) {
-            __builtin_memcpy(v, p, 32);
-        } else {
-            float w[8];
+        using Vector = Vector4<float>::Type;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = i < left ? p[i] : 0.f;
-            __builtin_memcpy(v, w, 32);
+        for (int h = 0; h < 2; ++h) {
+            v[h] = u4{0, 0, 0, 0};
+            if (left >= 4 * h + 4) v[h] = *(const Vector*)(p + 4 * h);
+            else if (left > 4 * h)
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (4 * h + i < left) v[h][i] = __builtin_bit_cast(uint32_t, p[4 * h + i]);
         }
     }
     // x = high + mid + low: the upper 16 bits of x (cut off, so that the largest floats stay finite), then what is left
@@ -344,7 +347,8 @@ struct Staged {
     static constexpr int kUnits = kRows * kGroups, kLoads = (kUnits + kThreads - 1) / kThreads;
     // the way out: so many fragments of users at a time, rows of items four values apart from one bank
     static constexpr int kOut = FU < 2 ? 1 : 2, kOutRows = WU * kOut * 16, kOutStride = kItems + 4;
-    static constexpr int kLds = kStage > kOutRows * kOutStride * 4 ? kStage : kOutRows * kOutStride * 4;
+    static constexpr int kBoth = kStage + (P::kParts == 3 ? kRows * 32 : 0);      // with the values behind whole steps
+    static constexpr int kLds = kBoth > kOutRows * kOutStride * 4 ? kBoth : kOutRows * kOutStride * 4;
     static_assert(FU % kOut == 0, "whole passes");
     static_assert(kUsers * 4 <= kHead && kHead + kLds <= 160 * 1024, "LDS");
 };
@@ -422,7 +426,12 @@ __device__ __forceinline__ void write_tile(const Product& a, const f4 (&acc)[FU]
 // FU x FI fragments of 16 x 16, and walks f in steps of 32 fp32 or 64 16-bit values.  While a step is multiplied
 // from LDS the next one's rows arrive in registers; fp32 values are split there, once for all that they meet.
 // The 16-byte group c of a part of row r lies in slot c ^ s(r), so that the 16 rows of an operand read spread
-// over all banks: s is r / 4 % 4 for rows of 64 bytes, r / 2 % 8 for 128.
+// over all banks: s is r / 2 % 8 for rows of 128 bytes, and 0, 2, 3, 1 by r / 4 % 4 for 64 (with 0, 1, 2, 3 the sixteen
+// lanes that read at a time, which are not neighbours, met in pairs).
+// Of fp32, up to eight values behind whole steps are multiplied as they are, by fp32 matrix instructions, four at a time
+// from places of their own in LDS: a step for them would cost as much as any other (1,024 x 17,770 x 100: 44 us, 46 without).
+// (Rows whose stride is a multiple of 128 bytes are the fastest: a step of a row at 400 bytes lies in two lines, and f = 96
+// takes 34 us, f = 128 41.)
 template <typename T, int WU, int WI, int FU, int FI>
 __global__ __launch_bounds__(64 * WU * WI) void k_product(Product a) {
     using C = Staged<T, WU, WI, FU, FI>;
@@ -432,10 +441,18 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product(Product a) {
     unsigned char* lds = shared + kHead;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t tile_u, tile_i;
-    tile_of(blockIdx.x, a.tu, a.ti, &tile_u, &tile_i);
+    tile_of(blockIdx.x, a.tu, a.ti, a.height, &tile_u, &tile_i);
     const int64_t u0 = (int64_t)tile_u * C::kUsers, i0 = (int64_t)tile_i * C::kItems;
-    const auto slot = [](int r, int g) { return C::kRowBytes == 64 ? g ^ (r >> 2 & 3) : g ^ (r >> 1 & 7); };
+    const auto slot = [](int r, int g) { return C::kRowBytes == 64 ? g ^ (0x78 >> (r >> 1 & 6) & 3) : g ^ (r >> 1 & 7); };
 
+    const int whole = a.f - a.tail;
+    const auto row_of = [&](int r) -> const T* {      // of the tile's rows, users first
+        if (r < C::kUsers) {
+            const int64_t u = u0 + r < a.m ? a.user_of(u0 + r) : -1;
+            return u >= 0 ? (const T*)a.x + u * a.ldx : nullptr;
+        }
+        return i0 + r - C::kUsers < a.n ? (const T*)a.theta + (i0 + r - C::kUsers) * a.ldt : nullptr;
+    };
     // this thread's groups of eight values: a row each, at the same place in every step
     const T* from[C::kLoads];
     int to[C::kLoads];
@@ -443,22 +460,16 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product(Product a) {
 #pragma unroll
     for (int l = 0; l < C::kLoads; ++l) {
         const int unit = threadIdx.x + l * C::kThreads, r = unit / C::kGroups, g = unit % C::kGroups;
-        from[l] = nullptr;
         at[l] = 8 * g;
         to[l] = unit < C::kUnits ? r * C::kRowBytes + 16 * slot(r, g) : -1;
-        if (r < C::kUsers) {
-            const int64_t u = u0 + r < a.m ? a.user_of(u0 + r) : -1;
-            if (u >= 0) from[l] = (const T*)a.x + u * a.ldx;
-        } else if (unit < C::kUnits && i0 + r - C::kUsers < a.n) {
-            from[l] = (const T*)a.theta + (i0 + r - C::kUsers) * a.ldt;
-        }
+        from[l] = unit < C::kUnits ? row_of(r) : nullptr;
     }
     u4 raw[C::kLoads][P::kRaw];
     const auto fetch = [&](int step) {
 #pragma unroll
         for (int l = 0; l < C::kLoads; ++l) {
             const int k = step * P::kValues + at[l];
-            P::load(from[l] + k, from[l] ? a.f - k : 0, raw[l]);
+            P::load(from[l] + k, from[l] ? whole - k : 0, raw[l]);
         }
     };
     const auto stage = [&]() {
@@ -510,17 +521,47 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product(Product a) {
         }
     };
 
-    const int steps = (a.f + P::kValues - 1) / P::kValues, begin = blockIdx.y * a.steps;
+    const int steps = (whole + P::kValues - 1) / P::kValues, begin = blockIdx.y * a.steps;
     const int end = begin + a.steps < steps ? begin + a.steps : steps;
     fetch(begin);
     float offset[4];
     fetch_offsets<C>(a, own, offset, u0, i0);
+    float* tails = (float*)(lds + C::kStage);
+    const bool with_tail = P::kParts == 3 && a.tail > 0 && end == steps;
+    if (with_tail)
+        for (int r = threadIdx.x; r < C::kRows; r += C::kThreads) {
+            const float* p = (const float*)row_of(r) + whole;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float v[4];
+                load4(p + 4 * c, row_of(r) ? a.tail - 4 * c : 0, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] += v[i] - v[i];      // an infinity gives NaN, as it does in parts
+                *(f4*)(tails + (c * C::kRows + r) * 4) = f4{v[0], v[1], v[2], v[3]};
+            }
+        }
     for (int step = begin; step < end; ++step) {
         stage();
         lds_barrier();
         if (step + 1 < end) fetch(step + 1);
         multiply();
         if (step + 1 < end) lds_barrier();
+    }
+    if (with_tail) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            if (4 * c >= a.tail) continue;
+            const auto value = [&](int r) { return tails[(c * C::kRows + r) * 4 + group]; };
+            float t[FI];
+#pragma unroll
+            for (int i = 0; i < FI; ++i) t[i] = value(C::kUsers + (wi * FI + i) * 16 + row);
+#pragma unroll
+            for (int u = 0; u < FU; ++u) {
+                const float x = value((wu * FU + u) * 16 + row);
+#pragma unroll
+                for (int i = 0; i < FI; ++i) acc[u][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(t[i], x, acc[u][i], 0, 0, 0);
+            }
+        }
     }
     write_tile<C, WU, WI, FU, FI>(a, acc, (float*)lds, own, offset, u0, i0, wu, wi, blockIdx.y);
 }
@@ -590,7 +631,7 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
     unsigned char* lds = shared + kHead;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t tile_u, tile_i;
-    tile_of(blockIdx.x, a.tu, a.ti, &tile_u, &tile_i);
+    tile_of(blockIdx.x, a.tu, a.ti, a.height, &tile_u, &tile_i);
     const int64_t u0 = (int64_t)tile_u * C::kUsers, i0 = (int64_t)tile_i * C::kItems;
 
     // what the buffers hold: the tile's rows (all of X where users are taken by index), the last up to the end of its
@@ -1442,6 +1483,8 @@ void by_type(int dtype, Fn fn) {
 template <typename P>
 using Type = std::remove_cv_t<std::remove_pointer_t<P>>;
 
+constexpr int64_t kCache = 256 << 20;      // of the last level
+
 // The product's tiles in one launch, and where there are few of them f in parts of 4 steps at least, as many as give every CU
 // two workgroups and the workspace holds.
 template <typename Kernel>
@@ -1449,7 +1492,10 @@ void launch_product(const als_predict_ctx* ctx, Kernel kernel, Product a, int us
                     int lds, hipStream_t st) {
     a.tu = (uint32_t)((a.m + users - 1) / users);
     a.ti = (uint32_t)((a.n + items - 1) / items);
-    const int64_t steps = (a.f + values - 1) / values, tiles = (int64_t)a.tu * a.ti;
+    // Where the results' bytes count (f up to 128) and no cache holds them, rows of tiles next to one another write what lies
+    // side by side: 4,096 x 40,000 x 128 bf16 150 us at height 2, 159 at 4, 179 at 8; 1,024 x 17,770 21.7, 20.6, 20.8.
+    a.height = a.f <= 128 && a.m * a.n * (a.end.type == ALS_F32 ? 4 : 2) > kCache ? 2 : 8;
+    const int64_t steps = (a.f - a.tail + values - 1) / values, tiles = (int64_t)a.tu * a.ti;
     int64_t parts = 2 * ctx->cus / tiles;
     if (parts > steps / 4) parts = steps / 4;
     const int64_t fit = (int64_t)(ctx->ws_bytes / 4) / (a.m * a.n);
@@ -1466,11 +1512,12 @@ void launch_product(const als_predict_ctx* ctx, Kernel kernel, Product a, int us
 }
 
 template <typename T, int WU, int WI, int FU, int FI>
-void staged(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
+void staged(const als_predict_ctx* ctx, Product a, hipStream_t st) {
     using C = Staged<T, WU, WI, FU, FI>;
     static std::atomic<uint64_t> done{0};
     auto* kernel = k_product<T, WU, WI, FU, FI>;
     whole_lds(kernel, ctx->device, &done);
+    if (sizeof(T) == 4 && a.f > C::P::kValues && a.f % C::P::kValues <= 8) a.tail = a.f % C::P::kValues;
     launch_product(ctx, kernel, a, C::kUsers, C::kItems, C::P::kValues, C::kThreads, C::kLds, st);
 }
 
@@ -1494,7 +1541,7 @@ void product(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
         if (near(a.x, a.ldx) && near(a.theta, a.ldt) && (!a.users || a.of < (int64_t)(kPastEnd / 2) / a.ldx)) {
             if (a.m > 16) {
                 if (a.f >= 512 && tiles(256, 256) >= ctx->cus) return direct<T, 2, 4, 8, 4, 2>(ctx, a, st);
-                if (tiles(128, 128) >= 2 * ctx->cus) return direct<T, 2, 2, 4, 4, 2>(ctx, a, st);
+                if (a.f > 128 && tiles(128, 128) >= 2 * ctx->cus) return direct<T, 2, 2, 4, 4, 2>(ctx, a, st);
                 if (tiles(64, 128) >= 2 * ctx->cus) return direct<T, 2, 2, 2, 4, 2>(ctx, a, st);
                 return direct<T, 2, 2, 2, 2, 4>(ctx, a, st);
             }
@@ -1502,7 +1549,7 @@ void product(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
         }
     }
     if (a.m > 16) {
-        if (tiles(128, 128) >= 2 * ctx->cus) return staged<T, 2, 2, 4, 4>(ctx, a, st);
+        if (a.f > 128 && tiles(128, 128) >= 2 * ctx->cus) return staged<T, 2, 2, 4, 4>(ctx, a, st);
         if (tiles(64, 128) >= 2 * ctx->cus) return staged<T, 2, 2, 2, 4>(ctx, a, st);
         return staged<T, 2, 2, 2, 2>(ctx, a, st);
     }
