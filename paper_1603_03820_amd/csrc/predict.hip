@@ -880,8 +880,9 @@ struct RowShared {
 // `top`; the columns from it on are listed (random rows: hardly more than `top`, as the groups' best are mostly of
 // different groups) and each one's rank is counted among them.  Where the list does not hold them (the best columns stand
 // in few groups, or many are equal) they are taken one at a time.
-//   offer     before the barrier that the caller has anyway: each thread's best key (0: none)
-//   finish    after it; each(fn) calls fn(place) for all of a thread's places whose key is at least its argument
+//   offer     each thread's best key (0: none); then a barrier
+//   decide    by the first wave, while the others go on with something else; then a barrier
+//   finish    each(cut, fn) calls fn(place) for all of a thread's places whose key is at least the cut
 struct Top {
     RowShared* sh;
     int top;
@@ -900,8 +901,7 @@ struct Top {
         if (threadIdx.x == 0) sh->count = 0;
     }
 
-    template <typename Each, typename Below, typename Emit>
-    __device__ __forceinline__ int finish(uint32_t own, Each each, Below below, Emit emit) const {
+    __device__ __forceinline__ void decide() const {
         if (threadIdx.x < kWave) {
             const int d = blockDim.x > 2 * kGroups ? 2 : (blockDim.x > kGroups ? 1 : 0), groups = blockDim.x >> d;
             uint32_t key[kGroups / kWave];
@@ -920,14 +920,17 @@ struct Top {
             }
             if (threadIdx.x == 0) sh->cut = cut < 1 ? 1 : cut;
         }
-        __syncthreads();
+    }
+
+    template <typename Each, typename Below, typename Emit>
+    __device__ __forceinline__ int finish(uint32_t own, Each each, Below below, Emit emit) const {
         const uint32_t cut = sh->cut;
         if (own >= cut)
             each(cut, [&](uint64_t place) {
                 const uint32_t at = atomicAdd(&sh->count, 1u);
                 if (at < kList) sh->list[at] = place;
             });
-        __syncthreads();
+        lds_barrier();
         const int count = sh->count;
         if (count <= kList) {
             for (int i = threadIdx.x; i < count; i += blockDim.x) {
@@ -944,9 +947,9 @@ struct Top {
         int found = 0;
         for (; found < top; ++found) {
             uint64_t p = wave_max64(below(limit));
-            __syncthreads();
+            lds_barrier();
             if ((threadIdx.x & 63) == 0) sh->place[wave] = p;
-            __syncthreads();
+            lds_barrier();
             for (int w = 0; w < waves; ++w) p = sh->place[w] > p ? sh->place[w] : p;
             if (p == 0) break;
             if (threadIdx.x == 0) emit(found, p);
@@ -999,6 +1002,17 @@ __global__ __launch_bounds__(1024, E <= 16 ? 8 : (E <= 32 ? 7 : 5)) void k_row(R
     const T* row = a.z + r * a.ldz + base;
     const auto position = [&](int v) { return (uint32_t)(v * blockDim.x + threadIdx.x) * V; };
 
+    // the lists' first entries before the scores, as loads come back in their order
+    const int32_t* list;
+    int64_t listed, begin, end;
+    Law law;
+    law.there = a.rated.row(r, &list, &listed);
+    law.t = limit_of(a.temperature, a.temperature_all, r);
+    a.entries(r, &begin, &end);
+    const bool some = law.there && listed > 0;
+    const uint32_t out0 = some && threadIdx.x < listed ? (uint32_t)list[threadIdx.x] - base : ~0u;
+    const bool asked = begin + threadIdx.x < end;
+    const uint32_t column0 = asked ? (uint32_t)a.given.idx[begin + threadIdx.x] : ~0u;
     float z[E];
 #pragma unroll
     for (int v = 0; v < E / V; ++v) {
@@ -1013,22 +1027,18 @@ __global__ __launch_bounds__(1024, E <= 16 ? 8 : (E <= 32 ? 7 : 5)) void k_row(R
             for (int i = 0; i < V; ++i) z[v * V + i] = c + i < n ? to_float(row[c + i]) : -INFINITY;
         }
     }
-    const int32_t* list;
-    int64_t listed;
-    Law law;
-    law.there = a.rated.row(r, &list, &listed);
-    law.t = limit_of(a.temperature, a.temperature_all, r);
-    const bool some = law.there && listed > 0;
+    const float score0 = column0 - base < n ? to_float(row[column0 - base]) : 0.f;
     if (threadIdx.x == 0) sh.first = ~0u;
     if (some) {
         for (uint32_t w = threadIdx.x; w < (n + 31) / 32; w += blockDim.x) bits[w] = 0;
-        __syncthreads();
-        for (int64_t k = threadIdx.x; k < listed; k += blockDim.x) {
-            const uint32_t c = (uint32_t)list[k] - base;
+        lds_barrier();
+        const auto mark = [&](uint32_t c) {
             if (c < n) atomicOr(&bits[c >> 5], 1u << (c & 31));
-        }
+        };
+        mark(out0);
+        for (int64_t k = threadIdx.x + blockDim.x; k < listed; k += blockDim.x) mark((uint32_t)list[k] - base);
     }
-    __syncthreads();
+    lds_barrier();
     const auto left_out = [&](uint32_t c) { return some && (bits[c >> 5] >> (c & 31) & 1); };
     if (some) {
 #pragma unroll
@@ -1047,7 +1057,11 @@ __global__ __launch_bounds__(1024, E <= 16 ? 8 : (E <= 32 ? 7 : 5)) void k_row(R
     for (int e = 0; e < E; ++e) mass.best = fmaxf(mass.best, z[e]);
     const uint32_t own = mass.best > -INFINITY ? key_of(mass.best) : 0;
     const Top top{&sh, a.top};
-    if (a.top) top.offer(own);
+    if (a.top) {
+        top.offer(own);
+        lds_barrier();
+        top.decide();
+    }
     mass.best = wave_max(mass.best);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
@@ -1063,7 +1077,7 @@ __global__ __launch_bounds__(1024, E <= 16 ? 8 : (E <= 32 ? 7 : 5)) void k_row(R
     mass.sum = wave_sum(mass.sum);
     mass.spread = wave_sum(mass.spread);
     if (lane == 0) sh.mass[wave] = mass;
-    __syncthreads();
+    lds_barrier();
     mass = joined(lane < waves ? sh.mass[lane] : Mass{-INFINITY, 0.f, 0.f}, c);
     law.best = mass.best;
     law.size = logf(mass.sum);
@@ -1076,21 +1090,24 @@ __global__ __launch_bounds__(1024, E <= 16 ? 8 : (E <= 32 ? 7 : 5)) void k_row(R
                 first = at < first ? at : first;
             }
         if (first != ~0u) atomicMin(&sh.first, base + first);
-        __syncthreads();
+        lds_barrier();
     }
     law.first = sh.first;
 
     const bool whole = a.segments == 1;
-    int64_t begin, end;
-    a.entries(r, &begin, &end);
-    for (int64_t e = begin + threadIdx.x; e < end; e += blockDim.x) {
-        const uint32_t column = (uint32_t)a.given.idx[e], at = column - base;
+    const auto answer = [&](int64_t e, uint32_t column, float s) {
+        const uint32_t at = column - base;
         if (at < n) {
-            const float s = to_float(row[at]), v = left_out(at) ? -INFINITY : s;
+            const float v = left_out(at) ? -INFINITY : s;
             a.log[e] = whole ? law.log_of(v, column) : v;
         } else if (column >= (uint32_t)a.n && segment == 0) {
             a.log[e] = law.there ? -INFINITY : NAN;
         }
+    };
+    if (asked) answer(begin + threadIdx.x, column0, score0);
+    for (int64_t e = begin + threadIdx.x + blockDim.x; e < end; e += blockDim.x) {
+        const uint32_t column = (uint32_t)a.given.idx[e], at = column - base;
+        answer(e, column, at < n ? to_float(row[at]) : 0.f);
     }
     const auto below = [&](uint64_t limit) {      // (from memory, so that no key is kept in a register)
         uint64_t best = 0;
@@ -1102,9 +1119,17 @@ __global__ __launch_bounds__(1024, E <= 16 ? 8 : (E <= 32 ? 7 : 5)) void k_row(R
     };
     const auto each = [&](uint32_t cut, auto fn) {
         const float least = fmaxf(score_of(cut < 0x00800000u ? 0x00800000u : cut), -3.402823466e38f);
+        // (eight at a time: a branch for each score that is below the cut would take longer than the comparison)
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (z[e] >= least) fn(place_of(z[e], base + position(e / V) + e % V));
+        for (int g = 0; g < E / 8; ++g) {
+            float most = z[8 * g];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) most = fmaxf(most, z[8 * g + i]);
+            if (!__any(most >= least)) continue;
+#pragma unroll
+            for (int e = 8 * g; e < 8 * g + 8; ++e)
+                if (z[e] >= least) fn(place_of(z[e], base + position(e / V) + e % V));
+        }
     };
     if (whole) {
         write_law(a, r, law, mass);
@@ -1152,14 +1177,16 @@ __global__ __launch_bounds__(kJoinThreads) void k_row_join(RowArgs<T> a) {
     if (a.top) {
         for (uint32_t k = threadIdx.x; k < count; k += kJoinThreads) most = max(most, (uint32_t)(keys[k] >> 32));
         top.offer(most);
+        lds_barrier();
+        top.decide();
     }
-    __syncthreads();
+    lds_barrier();
     mass = joined(lane < kJoinThreads / 64 ? sh.mass[lane] : Mass{-INFINITY, 0.f, 0.f}, c);
     law.best = mass.best;
     law.size = logf(mass.sum);
     if (law.greedy()) {
         if (own == mass.best && first != ~0u) atomicMin(&sh.first, first);
-        __syncthreads();
+        lds_barrier();
     }
     law.first = sh.first;
     int64_t begin, end;
@@ -1558,7 +1585,7 @@ void product(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
 
 // A row's registers: as many scores a thread as E; longer rows in segments.
 constexpr int64_t kHeld = 32 * 1024;
-constexpr int64_t kSegment = 16384;
+constexpr int64_t kSegment = 20480;
 static_assert(ALS_PREDICT_N_MAX <= kSegment * kJoinThreads, "a thread a segment");
 
 int check_scores(const als_scores* s, const als_given* g) {
@@ -1750,7 +1777,7 @@ int als_log_prob(als_predict_ctx* ctx, const als_scores* scores, const als_given
             const int64_t some = s.rows - row0 < batch ? s.rows - row0 : batch;
             a.mass = (SegMass*)(ctx->ws + some * a.segments * a.top * sizeof(uint64_t));
             a.row0 = row0;
-            go(integral_constant<int, 32>(), some);
+            go(integral_constant<int, 40>(), some);
             hipLaunchKernelGGL(k_row_join<T>, dim3((unsigned)some), dim3(kJoinThreads), 0, (hipStream_t)stream, a);
         }
     });
