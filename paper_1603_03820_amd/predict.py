@@ -190,13 +190,16 @@ def _of_rows(ctx, scores, given, temperature, rated, users, other):
         g.entries, g.each = idx.numel(), 0
         shape = (idx.numel(),)
     else:
-        _use(ctx, given, "given", _I32)
-        shape, entries = given.shape, given.numel()
-        if given.dim() not in (1, 2) or shape[0] != rows:
+        try:
+            shape, entries = given.shape, given.numel()
+        except AttributeError:
+            _use(ctx, given, "given", _I32)
+        if len(shape) not in (1, 2) or shape[0] != rows:
             raise ValueError(f"given must be a value or a row of them for each of {rows} rows, has shape {tuple(shape)}")
-        if not given.is_contiguous():
-            raise ValueError("given must be contiguous")
-        given = given.view(-1)
+        if len(shape) == 2:
+            if not given.is_contiguous():
+                raise ValueError("given must be contiguous")
+            given = given.view(-1)
         g.ptr = None
         g.idx = _vector(ctx, given, "given", _I32, entries, other)
         g.entries, g.each = entries, entries // rows if rows else 0
@@ -313,10 +316,10 @@ class Predictor:
     def _left_out(self, users):
         return dict(rated=self.rated, users=None if self.rated is None else users)
 
-    def log_prob(self, users, given, temperature=1.0, top=0, stream=None):
+    def log_prob(self, users, given, temperature=1.0, top=0, log=None, stream=None):
         """LogProb of the items `given` (see als_log_prob) among those that `users` (int32) have not rated."""
         z = als_predict(self.ctx, self.x, self.theta, users, None, self.item_offset, stream=stream)
-        return als_log_prob(self.ctx, z, given, temperature, top, stream=stream, **self._left_out(users))
+        return als_log_prob(self.ctx, z, given, temperature, top, log=log, stream=stream, **self._left_out(users))
 
     def fit_offsets(self, users, given, temperature=1.0, steps=20, rate=1.0, batch=1024):
         """Raises the mean log probability of `given` (int32, an item for each of `users`) by the items' offsets, and
@@ -342,7 +345,7 @@ class Predictor:
                 counts.index_add_(0, g.clamp(0, n - 1), there.float())
                 total = total + torch.where(there, r.log, 0.0).double().sum()
                 used = used + there.sum()
-            means.append(total / used)
+            means.append(total / used.clamp(min=1))
             short *= temperature
             most = torch.maximum(counts, counts - short).clamp_(min=1e-6)
             self.item_offset = self.item_offset + (rate * temperature) * (short / most)

@@ -698,3 +698,53 @@ def test_refusals_of_the_library(ctx):
                 dict(columns=p(en)), dict(columns=p(small)), dict(grad=p(o), columns=p(o, 256)), dict(t=p(o))):
         assert gradient(**bad) == -6, bad
     torch.cuda.synchronize()
+
+
+def test_evaluate_command():
+    """The command's evaluation on the tiny workload against the 64-bit forms: means over the held-out items of every
+    second user."""
+    import synth
+    from paper_1603_03820_amd import als, driver, recommend
+    log("train, evaluate and fit, tiny workload")
+    before, after, means = recommend.evaluate("tiny", iters=3, batch=300, temperature=0.2, steps=4)
+    again = recommend.evaluate("tiny", iters=3, batch=1000, temperature=0.2, steps=0)[0]
+    assert len(means) == 4 and all(np.isfinite(means)) and all(np.isfinite(v) for v in after.values())
+    assert before["hits"] == again["hits"] and before["log_prob"] == pytest.approx(again["log_prob"], abs=1e-9)
+    p = synth.config("tiny")
+    train, test = synth.split(p.rowptr, p.colidx, p.vals, 0.1, p.recipe["seed"])
+    c = als.Context(0, p.f)
+    dp = driver.DeviceProblem.from_host_csr(c, p.m, p.n, p.f, p.lam, *train)
+    x, theta, _ = driver.train(c, dp, torch.from_numpy(p.theta0).to(D), 3)
+    z = (x @ theta.t()).float().cpu().numpy()
+    logs, hits, entropy = [], [], []
+    for u in range(1, p.m, 2):
+        row = predict_oracle.Row(z[u], np.float32(0.2).item(), train[1][train[0][u]:train[0][u + 1]])
+        items = test[1][test[0][u]:test[0][u + 1]]
+        logs += [row.log(i) for i in items]
+        hits += [i in row.top(20)[0] for i in items]
+        entropy.append(row.entropy)
+    # z from another product: 1e-6 of scores up to some units, five times that in y
+    assert before["log_prob"] == pytest.approx(np.mean(logs), abs=1e-4)
+    assert before["entropy"] == pytest.approx(np.mean(entropy), abs=1e-4)
+    assert abs(before["hits"] - np.mean(hits)) <= 3 / len(hits)
+
+
+def test_fit_leaves_out_what_is_rated(ctx):
+    """Given items that their users have rated, or that are no items, count for nothing in a fit."""
+    from paper_1603_03820_amd import predict
+    rng = np.random.default_rng(5)
+    x, t = dev(rng.standard_normal((40, 8)).astype(np.float32)), dev(rng.standard_normal((60, 8)).astype(np.float32))
+    rated = lists(rng, 40, 60, 20)
+    rd = tuple(dev(a) for a in rated)
+    who, what = rng.integers(0, 40, 200).astype(np.int32), rng.integers(0, 60, 200).astype(np.int32)
+    clean = np.array([w not in row_of(rated, u) for u, w in zip(who, what)])
+    log("fit with and without entries that do not count")
+    a, b = (predict.Predictor(ctx, x, t, rated=rd) for _ in range(2))
+    more = np.concatenate([what, [-1, 60, 2 ** 31 - 1]]).astype(np.int32)
+    with_all = a.fit_offsets(dev(np.concatenate([who, [0, 1, 2]]).astype(np.int32)), dev(more), 0.5, 3)
+    with_clean = b.fit_offsets(dev(who[clean]), dev(what[clean]), 0.5, 3)
+    # rows of nothing that counts still expect nothing: their weight is 0
+    assert np.allclose(with_all, with_clean, atol=1e-5)
+    assert torch.allclose(a.item_offset, b.item_offset, atol=1e-4)
+    nothing = predict.Predictor(ctx, x, t, rated=rd)
+    assert nothing.fit_offsets(dev(who[~clean][:3]), dev(what[~clean][:3]), 0.5, 1) == [0.0] and not nothing.item_offset.any()
