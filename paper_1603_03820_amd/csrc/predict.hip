@@ -602,19 +602,20 @@ __device__ __forceinline__ u4 keep_values(u4 v, int left) {
     return v;
 }
 
-constexpr int kStep = 64, kStepBytes = 128;
 constexpr int64_t kNear = 1 << 21;              // row strides below it (4 MiB) keep a tile's offsets below 2^30 ...
 constexpr uint32_t kPastEnd = 0x7FFFFFF0u;      // ... and this past every buffer's end
 
-template <int WU, int WI, int FU, int FI, int STAGES>
+template <int WU, int WI, int FU, int FI, int STEP, int STAGES>
 struct Direct {
+    static constexpr int kStep = STEP, kStepBytes = 2 * STEP, kGroups = STEP / 8;      // a row's in a step
     static constexpr int kWaves = WU * WI, kThreads = 64 * kWaves;
     static constexpr int kUsers = WU * FU * 16, kItems = WI * FI * 16, kRows = kUsers + kItems;
-    static constexpr int kUserLoads = kUsers / 8 / kWaves, kItemLoads = kItems / 8 / kWaves;   // 1 KB, a wave and step
+    static constexpr int kAtOnce = 64 / kGroups;      // rows that a wave's load of 1 KB takes
+    static constexpr int kUserLoads = kUsers / kAtOnce / kWaves, kItemLoads = kItems / kAtOnce / kWaves;
     static constexpr int kStage = kRows * kStepBytes;
     static constexpr int kOut = FU < 2 ? 1 : 2, kOutRows = WU * kOut * 16, kOutStride = kItems + 4;
     static constexpr int kOutBytes = kOutRows * kOutStride * 4;
-    static_assert(kUsers % (8 * kWaves) == 0 && kItems % (8 * kWaves) == 0, "whole loads");
+    static_assert(kUsers % (kAtOnce * kWaves) == 0 && kItems % (kAtOnce * kWaves) == 0, "whole loads");
     static_assert((STAGES - 2) * (kUserLoads + kItemLoads) < 64, "loads that can be counted");
     static_assert(kUsers * 4 <= kHead && kHead + STAGES * kStage <= 160 * 1024 && kHead + kOutBytes <= 160 * 1024, "LDS");
 };
@@ -623,9 +624,10 @@ struct Direct {
 // in LDS, 128 bytes a row, while the next steps' (STAGES - 1 of them) arrive straight from memory beside them
 // (buffer_load ... lds: no registers, no instructions but the load).  Items and users past the end read as zeros; in the
 // last step values past f are masked on both sides, as what lies in their place may be no number.
-template <typename T, int WU, int WI, int FU, int FI, int STAGES>
+template <typename T, int WU, int WI, int FU, int FI, int STEP, int STAGES>
 __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
-    using C = Direct<WU, WI, FU, FI, STAGES>;
+    using C = Direct<WU, WI, FU, FI, STEP, STAGES>;
+    constexpr int kStep = C::kStep, kStepBytes = C::kStepBytes, kAtOnce = C::kAtOnce;
     extern __shared__ __align__(1024) unsigned char shared[];
     float* own = (float*)shared;
     unsigned char* lds = shared + kHead;
@@ -642,18 +644,19 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
     const i4 from_u = buffer_of((const T*)a.x + from * a.ldx, rows > 0 ? (uint32_t)((rows - 1) * a.ldx * 2 + whole) : 0);
     const i4 from_i = buffer_of((const T*)a.theta + i0 * a.ldt, (uint32_t)((items - 1) * a.ldt * 2 + whole));
     buffer_settle(from_u, from_i);
-    const int first_u = wave * C::kUserLoads * 8, first_i = wave * C::kItemLoads * 8;   // this wave's rows
-    const auto group_of = [&](int r) { return 16 * ((lane & 7) ^ (r >> 1 & 7)); };
+    const int first_u = wave * C::kUserLoads * kAtOnce, first_i = wave * C::kItemLoads * kAtOnce;   // this wave's rows
+    const auto slot = [](int r, int g) { return kStepBytes == 64 ? g ^ (0x78 >> (r >> 1 & 6) & 3) : g ^ (r >> 1 & 7); };
+    const auto group_of = [&](int r) { return 16 * slot(r, lane % C::kGroups); };
     uint32_t of_u[C::kUserLoads], of_i[C::kItemLoads];
 #pragma unroll
     for (int l = 0; l < C::kUserLoads; ++l) {
-        const int r = first_u + 8 * l + (lane >> 3);
+        const int r = first_u + kAtOnce * l + lane / C::kGroups;
         const int64_t u = u0 + r < a.m ? a.user_of(u0 + r) : -1;
         of_u[l] = u < 0 ? kPastEnd : (uint32_t)((u - from) * a.ldx * 2) + group_of(r);
     }
 #pragma unroll
     for (int l = 0; l < C::kItemLoads; ++l) {
-        const int r = first_i + 8 * l + (lane >> 3);
+        const int r = first_i + kAtOnce * l + lane / C::kGroups;
         of_i[l] = (uint32_t)(r * a.ldt * 2) + group_of(r);
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
@@ -665,14 +668,14 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
         const int left = 2 * a.f - step * kStepBytes;
 #pragma unroll
         for (int l = 0; l < C::kUserLoads; ++l) {
-            const int r = first_u + 8 * l;
-            load_to_lds(from_u, group_of(r + (lane >> 3)) < left ? of_u[l] : kPastEnd, step * kStepBytes,
+            const int r = first_u + kAtOnce * l;
+            load_to_lds(from_u, group_of(r + lane / C::kGroups) < left ? of_u[l] : kPastEnd, step * kStepBytes,
                         __builtin_amdgcn_readfirstlane(to + r * kStepBytes));
         }
 #pragma unroll
         for (int l = 0; l < C::kItemLoads; ++l) {
-            const int r = first_i + 8 * l;
-            load_to_lds(from_i, group_of(r + (lane >> 3)) < left ? of_i[l] : kPastEnd, step * kStepBytes,
+            const int r = first_i + kAtOnce * l;
+            load_to_lds(from_i, group_of(r + lane / C::kGroups) < left ? of_i[l] : kPastEnd, step * kStepBytes,
                         __builtin_amdgcn_readfirstlane(to + (C::kUsers + r) * kStepBytes));
         }
     };
@@ -687,21 +690,23 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
     const auto multiply = [&](int step, int stage, auto tail) {
         const unsigned char* at = lds + stage * C::kStage;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kStep / 32; ++h) {
             u4 t[FI], x[FU];
             const int left = a.f - step * kStep - 32 * h - 8 * group;
             const auto read = [&](int r) {
-                const u4 v = *(const u4*)(at + r * kStepBytes + 16 * ((4 * h + group) ^ (r >> 1 & 7)));
+                const u4 v = *(const u4*)(at + r * kStepBytes + 16 * slot(r, 4 * h + group));
                 return tail.value ? keep_values(v, left) : v;
             };
 #pragma unroll
             for (int i = 0; i < FI; ++i) t[i] = read(C::kUsers + (wi * FI + i) * 16 + row);
 #pragma unroll
             for (int u = 0; u < FU; ++u) x[u] = read((wu * FU + u) * 16 + row);
+            __builtin_amdgcn_s_setprio(1);      // (these before another wave's reads: 1% at 4,096 x 8,192 x 8,192)
 #pragma unroll
             for (int u = 0; u < FU; ++u)
 #pragma unroll
                 for (int i = 0; i < FI; ++i) acc[u][i] = multiply8(t[i], x[u], acc[u][i], T());
+            __builtin_amdgcn_s_setprio(0);
         }
     };
 
@@ -1548,39 +1553,45 @@ void staged(const als_predict_ctx* ctx, Product a, hipStream_t st) {
     launch_product(ctx, kernel, a, C::kUsers, C::kItems, C::P::kValues, C::kThreads, C::kLds, st);
 }
 
-template <typename T, int WU, int WI, int FU, int FI, int STAGES>
+template <typename T, int WU, int WI, int FU, int FI, int STEP, int STAGES>
 void direct(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
-    using C = Direct<WU, WI, FU, FI, STAGES>;
+    using C = Direct<WU, WI, FU, FI, STEP, STAGES>;
     static std::atomic<uint64_t> done{0};
-    auto* kernel = k_product_lds<T, WU, WI, FU, FI, STAGES>;
+    auto* kernel = k_product_lds<T, WU, WI, FU, FI, STEP, STAGES>;
     whole_lds(kernel, ctx->device, &done);
-    const int steps = (a.f + kStep - 1) / kStep, rows = (steps < STAGES ? steps : STAGES) * C::kStage;
-    launch_product(ctx, kernel, a, C::kUsers, C::kItems, kStep, C::kThreads, rows > C::kOutBytes ? rows : C::kOutBytes, st);
+    const int steps = (a.f + STEP - 1) / STEP, rows = (steps < STAGES ? steps : STAGES) * C::kStage;
+    launch_product(ctx, kernel, a, C::kUsers, C::kItems, STEP, C::kThreads, rows > C::kOutBytes ? rows : C::kOutBytes, st);
 }
 
+// The tile: the largest that still gives every CU enough of them, and up to f = 128, where the results' way out counts, a
+// smaller one, of which a CU holds more at a time.  Measured (us, users x items x f):
+//   bf16   4,096 x 8,192 x 8,192      256 x 256 427 (the library's product 406)
+//          4,096 x 40,000 x 128       64 x 128 in steps of 32 values 139, of 64 153; 128 x 128 of 32 135, of 64 160
+//          1,024 x 17,770 x 128       64 x 128 in steps of 32 values 19.9, of 64 20.9; 128 x 128 of 32 20.6, of 64 24.5
+//          5 x 8,192 x 8,192          16 x 64 25.5 (the library's product 23)
+//   fp32   1,024 x 17,770 x 100       64 x 128 45, 64 x 64 46, 128 x 64 47, 128 x 128 51 (before the values behind steps)
+//          1,024 x 17,770 x 32        64 x 128 24, 64 x 64 23, 128 x 64 26, 128 x 128 29
 template <typename T>
 void product(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
     const auto tiles = [&](int64_t users, int64_t items) {
         return ((a.m + users - 1) / users) * ((a.n + items - 1) / items);
     };
+    const bool large = a.f > 128 && tiles(128, 128) >= 2 * ctx->cus, middle = tiles(64, 128) >= 2 * ctx->cus;
     if constexpr (sizeof(T) == 2) {
         const auto near = [](const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0 && ld < kNear; };
         if (near(a.x, a.ldx) && near(a.theta, a.ldt) && (!a.users || a.of < (int64_t)(kPastEnd / 2) / a.ldx)) {
-            if (a.m > 16) {
-                if (a.f >= 512 && tiles(256, 256) >= ctx->cus) return direct<T, 2, 4, 8, 4, 2>(ctx, a, st);
-                if (a.f > 128 && tiles(128, 128) >= 2 * ctx->cus) return direct<T, 2, 2, 4, 4, 2>(ctx, a, st);
-                if (tiles(64, 128) >= 2 * ctx->cus) return direct<T, 2, 2, 2, 4, 2>(ctx, a, st);
-                return direct<T, 2, 2, 2, 2, 4>(ctx, a, st);
-            }
-            return direct<T, 1, 2, 1, 2, 4>(ctx, a, st);
+            if (a.m <= 16) return direct<T, 1, 2, 1, 2, 64, 4>(ctx, a, st);
+            if (a.f >= 512 && tiles(256, 256) >= ctx->cus) return direct<T, 2, 4, 8, 4, 64, 2>(ctx, a, st);
+            if (large) return direct<T, 2, 2, 4, 4, 64, 2>(ctx, a, st);
+            if (middle && a.f <= 128) return direct<T, 2, 2, 2, 4, 32, 3>(ctx, a, st);
+            if (middle) return direct<T, 2, 2, 2, 4, 64, 2>(ctx, a, st);
+            return direct<T, 2, 2, 2, 2, 64, 4>(ctx, a, st);
         }
     }
-    if (a.m > 16) {
-        if (a.f > 128 && tiles(128, 128) >= 2 * ctx->cus) return staged<T, 2, 2, 4, 4>(ctx, a, st);
-        if (tiles(64, 128) >= 2 * ctx->cus) return staged<T, 2, 2, 2, 4>(ctx, a, st);
-        return staged<T, 2, 2, 2, 2>(ctx, a, st);
-    }
-    return staged<T, 1, 4, 1, 1>(ctx, a, st);
+    if (a.m <= 16) return staged<T, 1, 4, 1, 1>(ctx, a, st);
+    if (large) return staged<T, 2, 2, 4, 4>(ctx, a, st);
+    if (middle) return staged<T, 2, 2, 2, 4>(ctx, a, st);
+    return staged<T, 2, 2, 2, 2>(ctx, a, st);
 }
 
 // A row's registers: as many scores a thread as E; longer rows in segments.
