@@ -745,6 +745,7 @@ __global__ __launch_bounds__(256) void k_join(Product a, int count) {
     const int left = items_left(a, item);
     float v[1][4], offset[4] = {0.f, 0.f, 0.f, 0.f};
     load4(a.parts + i * a.n + item, left, v[0]);
+#pragma unroll 4
     for (int p = 1; p < count; ++p) {
         float w[4];
         load4(a.parts + (p * a.m + i) * a.n + item, left, w);
@@ -995,7 +996,7 @@ __device__ __forceinline__ void write_no_top(const RowArgs<T>& a, int64_t r, con
 
 // A row, or a segment of one, of up to E scores a thread, which stay in registers from their one read on.
 template <typename T, int E>
-__global__ __launch_bounds__(1024, E <= 16 ? 8 : (E <= 32 ? 7 : 5)) void k_row(RowArgs<T> a) {
+__global__ __launch_bounds__(1024, E <= 16 || sizeof(T) == 2 ? 8 : 5) void k_row(RowArgs<T> a) {
     constexpr int V = E * sizeof(T) < 16 ? E : 16 / sizeof(T);
     __shared__ RowShared sh;
     extern __shared__ uint32_t bits[];

@@ -109,6 +109,17 @@ class Context(serve.Context):
             self.handle = None
 
 
+# Results are allocated as other tensors' kin (new_empty), which takes half of torch.empty's time: a small call's allocations
+# take longer than its kernel.
+
+
+def _like(ctx: Context, t, shape, dtype, other):
+    """Allocated on the call's stream; t is a tensor on the context's device."""
+    if other is None:
+        return t.new_empty(shape) if t.dtype == dtype else t.new_empty(shape, dtype=dtype)
+    return _empty(ctx, shape, dtype, other)      # (a number is a vector's length)
+
+
 def als_predict(ctx: Context, x, theta, users=None, user_offset=None, item_offset=None, activation="none",
                 low=None, high=None, residual=None, out=None, dtype=torch.float32, stream=None):
     """out[i, j] = act(x[u] . theta[j] + user_offset[u] + item_offset[j]) + residual[i, j] with u = users[i] (int32), or
@@ -131,7 +142,7 @@ def als_predict(ctx: Context, x, theta, users=None, user_offset=None, item_offse
     if out is None:
         if dtype not in _DTYPES:
             raise TypeError(f"dtype must be {' or '.join(map(str, _DTYPES))}, got {dtype}")
-        out = _empty(ctx, (m, n), dtype, other)
+        out = _like(ctx, x, (m, n), dtype, other)
         po, ldo = out.data_ptr(), n
     else:
         dtype = out.dtype
@@ -237,17 +248,18 @@ def als_log_prob(ctx: Context, scores, given, temperature=1.0, top=0, rated=None
     top = int(top)
     if not 0 <= top <= ALS_PREDICT_TOP_MAX:
         raise ValueError(f"top must be 0 to {ALS_PREDICT_TOP_MAX}, is {top}")
+    stats = _like(ctx, scores, (rows, 2), torch.float32, other)
     if log is None:
-        log = _empty(ctx, shape, torch.float32, other)
+        log = _like(ctx, stats, shape, torch.float32, other)
         pl = log.data_ptr()
     else:
         pl = _shaped(ctx, log, "log", shape, other)
         _apart("als_log_prob", ((pl, log.numel()),), rated)
-    stats = _empty(ctx, (rows, 2), torch.float32, other)
-    entropy = _empty(ctx, (rows,), torch.float32, other)
+    entropy = _like(ctx, stats, rows, torch.float32, other)
     top_index = top_log = pi = pt = None
     if top:
-        top_index, top_log = _empty(ctx, (rows, top), torch.int32, other), _empty(ctx, (rows, top), torch.float32, other)
+        top_log = _like(ctx, stats, (rows, top), torch.float32, other)
+        top_index = _like(ctx, given[1] if isinstance(given, tuple) else given, (rows, top), torch.int32, other)
         pi, pt = top_index.data_ptr(), top_log.data_ptr()
     ctx._use_workspace(handle, other)
     rc = _lib.als_log_prob(ctx.handle, ctx._scores_ref, ctx._given_ref, pl, stats.data_ptr(), entropy.data_ptr(), top,
@@ -279,7 +291,7 @@ def als_log_prob_grad(ctx: Context, scores, given, forward: LogProb, grad_log, g
         if rows and n:
             _apart("als_log_prob_grad", ((po, (((rows - 1) * ldg + n) * grad.element_size() + 3) // 4),), rated)
     elif grad:
-        grad = _empty(ctx, (rows, n), scores.dtype, other)
+        grad = _like(ctx, scores, (rows, n), scores.dtype, other)
         po = grad.data_ptr()
     else:
         grad = None
@@ -287,7 +299,7 @@ def als_log_prob_grad(ctx: Context, scores, given, forward: LogProb, grad_log, g
         pc = _vector(ctx, columns, "columns", _F32, n, other)
         _apart("als_log_prob_grad", ((pc, n),), rated)
     elif columns:
-        columns = _empty(ctx, (n,), torch.float32, other)
+        columns = _like(ctx, forward.stats, n, torch.float32, other)
         pc = columns.data_ptr()
     else:
         columns = None
