@@ -589,10 +589,10 @@ __device__ __forceinline__ void load_to_lds(i4 buffer, uint32_t voffset, uint32_
 // A load reads a scalar register that a vector instruction wrote (readfirstlane) no sooner than five wait states
 // later; the compiler keeps them for the loads it knows.
 __device__ __forceinline__ void buffer_settle(i4 a, i4 b) { asm volatile("s_nop 4" : : "s"(a), "s"(b)); }
-// All of this wave's loads but the last LEFT have arrived, and its LDS reads are done.
+// All of each wave's loads but its last LEFT have arrived, and its LDS reads are done.
 template <int LEFT>
 __device__ __forceinline__ void settle() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(LEFT) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LEFT) : "memory");
 }
 
 // The values of a group of eight 16-bit ones of which `left` are there, zeros in the others' place.
@@ -621,7 +621,7 @@ struct Direct {
 };
 
 // The product in tiles as k_product has them, of 16-bit rows at multiples of 16 bytes: a step's rows of both sides lie
-// in LDS, 128 bytes a row, while the next steps' (STAGES - 1 of them) arrive straight from memory beside them
+// in LDS, 2 STEP bytes a row, while the next steps' (STAGES - 1 of them) arrive straight from memory beside them
 // (buffer_load ... lds: no registers, no instructions but the load).  Items and users past the end read as zeros; in the
 // last step values past f are masked on both sides, as what lies in their place may be no number.
 template <typename T, int WU, int WI, int FU, int FI, int STEP, int STAGES>
@@ -715,20 +715,18 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
         if (begin + p < end) fetch(begin + p, p);
     float offset[4];
     fetch_offsets<C>(a, own, offset, u0, i0);
-    // a step: its rows are there and the last step's are done with (one barrier for both), whose place the rows
+    // a step: its rows are there and the last step's are done with (settle says both), whose place the rows
     // STAGES - 1 steps on take
     int stage = 0;
     const auto after = [](int x) { return x + 1 == STAGES ? 0 : x + 1; };
     int step = begin;
     for (; step + STAGES - 1 < end; ++step) {
         settle<(STAGES - 2) * (C::kUserLoads + C::kItemLoads)>();
-        __builtin_amdgcn_s_barrier();
         fetch(step + STAGES - 1, stage == 0 ? STAGES - 1 : stage - 1);
         multiply(step, stage, std::false_type());
         stage = after(stage);
     }
     settle<0>();
-    __builtin_amdgcn_s_barrier();
     for (; step + 1 < end; ++step) {
         multiply(step, stage, std::false_type());
         stage = after(stage);
@@ -1253,7 +1251,7 @@ __global__ __launch_bounds__(kGradThreads, COLUMNS ? 6 : 5) void k_gradient(
     const float* __restrict__ entropy, const float* __restrict__ grad_log, const float* __restrict__ grad_entropy) {
     constexpr int E = Grad<COLUMNS>::kEach, V = 16 / sizeof(T), kMarks = Grad<COLUMNS>::kChunk / 32;
     constexpr uint32_t kRun = Grad<COLUMNS>::kRun, kChunk = Grad<COLUMNS>::kChunk;
-    __shared__ uint32_t marks[3][kMarks];
+    __shared__ uint32_t marks[3 * kMarks];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t chunk = blockIdx.x % a.chunks, group = blockIdx.x / a.chunks;
     const uint32_t start = chunk * kChunk, base = start + wave * kRun, n = (uint32_t)a.n;
@@ -1323,7 +1321,7 @@ __global__ __launch_bounds__(kGradThreads, COLUMNS ? 6 : 5) void k_gradient(
     for (int e = 0; e < E; ++e) total[e] = 0.f;
     int turn = 0;
     if (rated_ptr) {
-        for (int w = threadIdx.x; w < 3 * kMarks; w += kGradThreads) marks[0][w] = 0;
+        for (int w = threadIdx.x; w < 3 * kMarks; w += kGradThreads) marks[w] = 0;
         lds_barrier();
     }
     // with the columns' sums a workgroup has several rows: the next one's values and the places after it are on their
@@ -1347,7 +1345,7 @@ __global__ __launch_bounds__(kGradThreads, COLUMNS ? 6 : 5) void k_gradient(
             if (some) {
                 const auto mark = [&](uint32_t column) {
                     const uint32_t at = column - start;
-                    if (at < kChunk) atomicOr(&marks[turn][at >> 5], 1u << (at & 31));
+                    if (at < kChunk) atomicOr(&marks[turn * kMarks + (at >> 5)], 1u << (at & 31));
                 };
                 mark(f.rated);
                 for (int64_t k = p.rated + threadIdx.x + kGradThreads; k < p.rated_end; k += kGradThreads)
@@ -1355,11 +1353,11 @@ __global__ __launch_bounds__(kGradThreads, COLUMNS ? 6 : 5) void k_gradient(
             }
             lds_barrier();
         }
-        const uint32_t* marked = marks[turn];
+        const uint32_t* marked = marks + turn * kMarks;
         if (rated_ptr) {
             turn = turn == 2 ? 0 : turn + 1;
             const int clear = turn == 2 ? 0 : turn + 1;
-            for (int w = threadIdx.x; w < kMarks; w += kGradThreads) marks[clear][w] = 0;
+            for (int w = threadIdx.x; w < kMarks; w += kGradThreads) marks[clear * kMarks + w] = 0;
         }
         float d[E];
         if (some) {

@@ -424,6 +424,46 @@ def test_gradient_against_differences(ctx):
             assert abs(d[i, j] - (up - down) / (2 * step)) <= 1e-5 * (1 + abs(d[i, j]))
 
 
+def test_offsets_past_32_bits(ctx):
+    """Rows that lie billions of elements apart, users far into a large factor, results past 4 GiB."""
+    from paper_1603_03820_amd import predict
+    rng = np.random.default_rng(1)
+    far = 2 ** 31 + 8
+    memory = torch.zeros(2 * far + 40_000, dtype=torch.bfloat16, device=D)
+    z = torch.as_strided(memory, (3, 33_000), (far, 1))
+    z.copy_(scores(rng, 3, 33_000, "bf16"))
+    given = rng.integers(0, 33_000, 3).astype(np.int32)
+    check(ctx, z, given, 0.8, 5, what="rows far apart")
+    check(ctx, z[:, :900], given % 900, 0.8, 5, what="short rows far apart")
+    r = predict.als_log_prob(ctx, z, dev(given))
+    want, _ = predict.als_log_prob_grad(ctx, z, dev(given), r, torch.ones(3, device=D))
+    predict.als_log_prob_grad(ctx, z, dev(given), r, torch.ones(3, device=D), grad=z)
+    assert torch.equal(z, want)
+    del memory, z
+    for dtype in ("f32", "bf16"):
+        log(f"predict of far users, {dtype}")
+        f = 104
+        x = torch.zeros(11_000_000, f, dtype=TYPES[dtype], device=D)
+        users = torch.tensor([10_999_999, 0, 5_500_000, 11_000_000, 10_999_999] * 8, dtype=torch.int32, device=D)
+        x[users[:3].long()] = dev(rng.integers(-9, 10, (3, f)).astype(np.float32), TYPES[dtype])
+        t = dev(rng.integers(-9, 10, (200, f)).astype(np.float32), TYPES[dtype])
+        got = predict.als_predict(ctx, x, t, users=users)
+        there = users < 11_000_000
+        assert torch.equal(got[there].double(), x[users[there].long()].double() @ t.double().t())
+        assert bool(torch.isnan(got[~there]).all())
+        del x
+    log("predict to rows past 4 GiB")
+    x, t = (torch.randint(-3, 4, (r, 8), device=D).float() for r in (40_000, 40_000))
+    got = predict.als_predict(ctx, x, t)
+    for rows in (slice(0, 3), slice(20_000, 20_003), slice(39_997, 40_000)):
+        assert torch.equal(got[rows].double(), x[rows].double() @ t.double().t())
+    del got
+    wide = torch.zeros(2 * far + 300, device=D, dtype=torch.float16)
+    out = torch.as_strided(wide, (3, 300), (far, 1))
+    predict.als_predict(ctx, x[:3], t[:300], out=out)
+    assert torch.equal(out.double(), x[:3].double() @ t[:300].double().t()) and int((wide != 0).sum()) == int((out != 0).sum())
+
+
 def test_log_prob_shapes(ctx):
     """No rows, no columns, no given columns; a batch's part of a CSR; entries past the list's end."""
     from paper_1603_03820_amd import predict

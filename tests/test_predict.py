@@ -73,6 +73,26 @@ def test_device_code_shape():
     assert "v_mfma_f32_16x16x32_bf16" in text and "v_mfma_f32_16x16x32_f16" in text
 
 
+def test_loads_to_lds():
+    """The loads to LDS, which are inline assembly: their wait states, M0 to themselves in their kernels, and no assembly
+    that writes a register."""
+    if not os.path.exists("/opt/rocm/llvm/bin/clang-offload-bundler"):
+        pytest.skip("ROCm LLVM tools not installed")
+    from paper_1603_03820_amd import build
+    from tests.test_serve import lds_load_violations
+    text = _device_disassembly(build.PREDICT_LIB)
+    assert lds_load_violations(text) == []
+    loading = [k for k in re.split(r"\n(?=[0-9a-f]+ <)", text) if re.search(r"buffer_load_dwordx4 .* lds", k)]
+    assert len(loading) == 12       # six shapes of tiles, two types
+    for k in loading:
+        assert not re.search(r"gpr_idx|v_movrel|s_movrel|s_sendmsg\b", k)
+        uses = [line.split("//")[0].strip() for line in k.splitlines() if re.search(r"\bm0\b", line.split("//")[0])]
+        assert uses and all(u.startswith("s_mov_b32 m0,") for u in uses), set(uses)
+    for b in re.findall(r"\basm volatile\((.*?)\);", open(build.PREDICT_SRC).read(), flags=re.S):
+        outputs = b.split(":")[1] if ":" in b else ""
+        assert "=" not in outputs and "+v" not in outputs, b
+
+
 def test_refusals_without_a_device():
     """Null contexts and a device that does not exist."""
     from paper_1603_03820_amd import predict
