@@ -196,10 +196,11 @@ def _of_rows(ctx, scores, given, temperature, rated, users, other):
         raise ValueError("users without rated")
     if isinstance(given, tuple):
         ptr, idx = given
+        entries = idx.numel()
+        shape = (entries,)
         g.ptr = _vector(ctx, ptr, "given[0]", _I64, rows + 1, other)
-        g.idx = _vector(ctx, idx, "given[1]", _I32, idx.numel(), other)
-        g.entries, g.each = idx.numel(), 0
-        shape = (idx.numel(),)
+        g.idx = _vector(ctx, idx, "given[1]", _I32, entries, other)
+        g.entries, g.each = entries, 0
     else:
         try:
             shape, entries = given.shape, given.numel()
@@ -207,24 +208,25 @@ def _of_rows(ctx, scores, given, temperature, rated, users, other):
             _use(ctx, given, "given", _I32)
         if len(shape) not in (1, 2) or shape[0] != rows:
             raise ValueError(f"given must be a value or a row of them for each of {rows} rows, has shape {tuple(shape)}")
-        if len(shape) == 2:
-            if not given.is_contiguous():
-                raise ValueError("given must be contiguous")
-            given = given.view(-1)
         g.ptr = None
-        g.idx = _vector(ctx, given, "given", _I32, entries, other)
+        g.idx = _shaped(ctx, given, "given", shape, other, _I32)
         g.entries, g.each = entries, entries // rows if rows else 0
-    return rows, n, tuple(shape)
+    return rows, n, shape
 
 
-def _shaped(ctx, t, name, shape, other):
-    """Pointer of a contiguous float32 tensor of that shape."""
-    if isinstance(t, torch.Tensor) and tuple(t.shape) != shape:
-        raise ValueError(f"{name} must have shape {shape}, has {tuple(t.shape)}")
-    if isinstance(t, torch.Tensor) and t.dim() != 1 and t.is_contiguous():
-        flat = t.view(-1)
-        return _vector(ctx, flat, name, _F32, flat.numel(), other)
-    return _vector(ctx, t, name, _F32, shape[0], other)
+def _shaped(ctx, t, name, shape, other, dtypes=_F32):
+    """Pointer of a contiguous tensor of that shape."""
+    try:
+        if t.dtype in dtypes and t.get_device() == ctx.index and t.shape == shape and t.is_contiguous():
+            if other is not None:
+                t.record_stream(other)
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _use(ctx, t, name, dtypes)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, has {tuple(t.shape)}")
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _apart(fn, results, rated):
