@@ -74,7 +74,8 @@ enum {
  *   residual  : m x n of the output's type, row stride ldr >= n, or NULL.  It may be `out` itself (the same
  *               pointer and stride).
  *   out       : m x n of type out_dtype, row stride ldo >= n; must not overlap an input but so (ALS_ERR_ALIAS)
- * f in [1, ALS_PREDICT_F_MAX].
+ * f in [1, ALS_PREDICT_F_MAX].  Rows of 16-bit types at addresses and strides that are multiples of 16 bytes (and fp32 ones
+ * at strides of multiples of 128) are the fastest.
  */
 int als_predict(als_predict_ctx* ctx, const void* x, int64_t of, int64_t ldx, const int32_t* users, int64_t m,
                 const void* theta, int64_t n, int64_t ldt, int32_t dtype, int32_t f, const float* user_offset,

@@ -432,6 +432,8 @@ __device__ __forceinline__ void write_tile(const Product& a, const f4 (&acc)[FU]
 // from places of their own in LDS: a step for them would cost as much as any other (1,024 x 17,770 x 100: 44 us, 46 without).
 // (Rows whose stride is a multiple of 128 bytes are the fastest: a step of a row at 400 bytes lies in two lines, and f = 96
 // takes 34 us, f = 128 41.)
+// 1,024 x 17,770 x 100 fp32 in 39 to 44 us (1.8 TB/s out, 93 Tflop/s): its vector instructions issue in 20 us (splits a third,
+// the way out a fifth), its matrix instructions in 12, and barriers and loads keep them from running side by side.
 template <typename T, int WU, int WI, int FU, int FI>
 __global__ __launch_bounds__(64 * WU * WI) void k_product(Product a) {
     using C = Staged<T, WU, WI, FU, FI>;
@@ -624,6 +626,10 @@ struct Direct {
 // in LDS, 2 STEP bytes a row, while the next steps' (STAGES - 1 of them) arrive straight from memory beside them
 // (buffer_load ... lds: no registers, no instructions but the load).  Items and users past the end read as zeros; in the
 // last step values past f are masked on both sides, as what lies in their place may be no number.
+// 4,096 x 8,192 x 8,192 in 427 us without activation and residual (1.29 Pflop/s; the library's product 406), with GELU and
+// residual 451: one workgroup is on a CU, and nothing runs beside its way out.  4,096 x 40,000 x 128 with a sigmoid in 133
+// (2.5 TB/s): loads, products and stores of a tile follow one another, and the four workgroups of a CU do not hide all of it
+// (stores alone took 95 us).  5 x 8,192 x 8,192 in 26 (5.2 TB/s): the weights' bytes.
 template <typename T, int WU, int WI, int FU, int FI, int STEP, int STAGES>
 __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
     using C = Direct<WU, WI, FU, FI, STEP, STAGES>;
@@ -992,7 +998,14 @@ __device__ __forceinline__ void write_no_top(const RowArgs<T>& a, int64_t r, con
     }
 }
 
-// A row, or a segment of one, of up to E scores a thread, which stay in registers from their one read on.
+// A row, or a segment of one, of up to E scores a thread, which stay in registers from their one read on: the best one of
+// a wave, then weights relative to it (a wave's sums need no barrier), then the waves' masses joined.  H comes from the
+// same pass: with x = log2 w, H = log S - ln 2 sum(w x) / S, whose terms are all of one sign.
+// 1,024 x 17,770 fp32 in 19.5 us, with the 20 best 25 (73 MB: 3.8 and 2.9 TB/s); 64 x 625,000 bf16 in 28 and 42.  Bound by
+// waits: a workgroup's loads, lists, sums and its best columns follow one another, and most workgroups are at the same
+// one.  40 scores a thread past 16,384: seven waves a row of 17,770, so that four rows are on a CU and the batch takes one
+// round (with the best, 32 a thread 36 us, 40 27, 48 29, 64 42 at the time); segments of 20,480 columns (45.8 us; 8,192 49.0,
+// 16,384 49.4, 32,768 59.0).
 template <typename T, int E>
 __global__ __launch_bounds__(1024, E <= 16 || sizeof(T) == 2 ? 8 : 5) void k_row(RowArgs<T> a) {
     constexpr int V = E * sizeof(T) < 16 ? E : 16 / sizeof(T);
@@ -1243,6 +1256,9 @@ struct Grad {
 // left-out columns are marked in LDS by all of the workgroup (three rows' marks in turn: one is cleared while one is read,
 // so a row takes one barrier).  The given columns each wave looks through for itself: what lies in its run goes to the
 // lane that has it, in the list's order, so that sums of repeated columns are the same on every run.
+// 1,024 x 17,770 fp32 in 28 us (5.2 TB/s read and written), 64 x 625,000 bf16 in 34 (4.7 TB/s): memory.  With the columns'
+// sums alone 28 + 6 us (2.6 TB/s): 8 columns a lane, as the sums and the next row's scores take registers (34.7 us with
+// k_columns, 16 a lane 44), and a third of its instructions are a row's, not a column's.
 template <typename T, bool COLUMNS>
 __global__ __launch_bounds__(kGradThreads, COLUMNS ? 6 : 5) void k_gradient(
     GradArgs<T> a, const float* __restrict__ temperature, const int64_t* __restrict__ rated_ptr,
