@@ -1170,6 +1170,25 @@ __global__ __launch_bounds__(kJoinThreads) void k_row_join(RowArgs<T> a) {
     __shared__ RowShared sh;
     const int64_t local = blockIdx.x, r = a.row0 + local;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // all that can be asked for at once: the segments' best places (the first four a thread), masses, and given columns
+    const uint64_t* keys = a.keys + local * a.segments * a.top;
+    const uint32_t count = a.segments * a.top;
+    uint64_t held[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t k = j * kJoinThreads + threadIdx.x;
+        held[j] = k < count ? keys[k] : 0;
+    }
+    const auto each_key = [&](auto fn) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) fn(held[j]);
+        for (uint32_t k = 4 * kJoinThreads + threadIdx.x; k < count; k += kJoinThreads) fn(keys[k]);
+    };
+    int64_t begin, end;
+    a.entries(r, &begin, &end);
+    const bool asked = begin + threadIdx.x < end;
+    const uint32_t column0 = asked ? (uint32_t)a.given.idx[begin + threadIdx.x] : ~0u;
+    const float log0 = asked ? a.log[begin + threadIdx.x] : 0.f;
     const int32_t* list;
     int64_t listed;
     Law law;
@@ -1187,12 +1206,10 @@ __global__ __launch_bounds__(kJoinThreads) void k_row_join(RowArgs<T> a) {
     const float own = mass.best;
     mass = joined(mass, c);
     if (lane == 0) sh.mass[wave] = mass;
-    const uint64_t* keys = a.keys + local * a.segments * a.top;
-    const uint32_t count = a.segments * a.top;
     const Top top{&sh, a.top};
     uint32_t most = 0;
     if (a.top) {
-        for (uint32_t k = threadIdx.x; k < count; k += kJoinThreads) most = max(most, (uint32_t)(keys[k] >> 32));
+        each_key([&](uint64_t p) { most = max(most, (uint32_t)(p >> 32)); });
         top.offer(most);
         lds_barrier();
         top.decide();
@@ -1206,24 +1223,21 @@ __global__ __launch_bounds__(kJoinThreads) void k_row_join(RowArgs<T> a) {
         lds_barrier();
     }
     law.first = sh.first;
-    int64_t begin, end;
-    a.entries(r, &begin, &end);
-    for (int64_t e = begin + threadIdx.x; e < end; e += blockDim.x) {
+    if (asked && column0 < (uint32_t)a.n) a.log[begin + threadIdx.x] = law.log_of(log0, column0);
+    for (int64_t e = begin + threadIdx.x + kJoinThreads; e < end; e += kJoinThreads) {
         const uint32_t column = (uint32_t)a.given.idx[e];
         if (column < (uint32_t)a.n) a.log[e] = law.log_of(a.log[e], column);
     }
     write_law(a, r, law, mass);
     if (a.top == 0) return;
     const auto each = [&](uint32_t cut, auto fn) {
-        for (uint32_t k = threadIdx.x; k < count; k += kJoinThreads)
-            if ((uint32_t)(keys[k] >> 32) >= cut) fn(keys[k]);
+        each_key([&](uint64_t p) {
+            if ((uint32_t)(p >> 32) >= cut) fn(p);
+        });
     };
     const auto below = [&](uint64_t limit) {
         uint64_t best = 0;
-        for (uint32_t k = threadIdx.x; k < count; k += kJoinThreads) {
-            const uint64_t p = keys[k];
-            best = p < limit && p > best ? p : best;
-        }
+        each_key([&](uint64_t p) { best = p < limit && p > best ? p : best; });
         return best;
     };
     const int found = top.finish(most, each, below, [&](int k, uint64_t p) { write_top(a, r, law, k, p); });
