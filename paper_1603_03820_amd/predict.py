@@ -342,6 +342,8 @@ class Predictor:
         at most by T.  Users are taken `batch` at a time.  Items that a user has rated are left out for them; given
         ones among those count for nothing."""
         n, count = self.theta.shape[0], users.numel()
+        if count == 0 or given.shape != users.shape:
+            raise ValueError(f"given must have an item for each of {count} users (one at least), has shape {tuple(given.shape)}")
         if self.item_offset is None:
             self.item_offset = torch.zeros(n, dtype=torch.float32, device=self.theta.device)
         means = []

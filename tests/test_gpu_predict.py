@@ -568,6 +568,38 @@ def test_scores_and_draws_agree(ctx):
     sctx.close()
 
 
+def test_captured_in_the_workspace(ctx):
+    """Calls that work in the workspace, captured: a product that is cut along its rows, rows in segments, columns' sums.
+    Replays on other inputs, with eager calls between them, against the eager results."""
+    from paper_1603_03820_amd import predict
+    rng = np.random.default_rng(7)
+    x, t = dev(rng.standard_normal((4, 3000)).astype(np.float32), torch.bfloat16), dev(rng.standard_normal((50_000, 3000)).astype(np.float32), torch.bfloat16)
+    few = t[:200].contiguous()
+    given = dev(rng.integers(0, 50_000, (4, 3)).astype(np.int32))
+
+    def step():
+        y = predict.als_predict(ctx, x, few, activation="silu")
+        z = predict.als_predict(ctx, x, t, dtype=torch.float32)
+        r = predict.als_log_prob(ctx, z, given, 40.0, 12)
+        d, c = predict.als_log_prob_grad(ctx, z, given, r, r.log, r.entropy, 40.0, columns=True)
+        return [y, z, *r, d, c]
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for k in range(3):
+        x.copy_(dev(rng.standard_normal((4, 3000)).astype(np.float32), torch.bfloat16))
+        given.copy_(dev(rng.integers(0, 50_000, (4, 3)).astype(np.int32)))
+        log(f"replay {k}")
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [v.clone() for v in held]
+        for a, w in zip(got, step()):
+            assert torch.equal(a, w)
+        torch.cuda.synchronize()
+
+
 def test_other_streams(ctx):
     """Calls on a stream that is not the current one, whose tensors are dropped at once; two streams in turn."""
     from paper_1603_03820_amd import predict
@@ -787,4 +819,7 @@ def test_fit_leaves_out_what_is_rated(ctx):
     assert np.allclose(with_all, with_clean, atol=1e-5)
     assert torch.allclose(a.item_offset, b.item_offset, atol=1e-4)
     nothing = predict.Predictor(ctx, x, t, rated=rd)
+    for bad in (what[:0], what[:5]):
+        with pytest.raises(ValueError):
+            a.fit_offsets(dev(who[:bad.size // 2]), dev(bad))
     assert nothing.fit_offsets(dev(who[~clean][:3]), dev(what[~clean][:3]), 0.5, 1) == [0.0] and not nothing.item_offset.any()
