@@ -1592,34 +1592,56 @@ void direct(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
     launch_product(ctx, kernel, a, C::kUsers, C::kItems, STEP, C::kThreads, rows > C::kOutBytes ? rows : C::kOutBytes, st);
 }
 
-// The tile: the largest that still gives every CU enough of them, and up to f = 128, where the results' way out counts, a
-// smaller one, of which a CU holds more at a time.  Measured (us, users x items x f):
+// The tile.  Few users: as few rows for them as hold them.  Otherwise the largest that still gives every CU enough of them, and
+// up to f = 128, where the results' way out counts, a smaller one, of which a CU holds more at a time.  Tiles come in rounds of
+// as many as the CUs hold at once, so what a shape costs goes by its rounds' whole area (`rounds`), filled or not.  Measured (us,
+// users x items x f):
 //   bf16   4,096 x 8,192 x 8,192      256 x 256 427 (the library's product 406)
+//          310 x 38,418 x 2,568       256 x 256 155 (two rounds, the second all but empty), 128 x 128 119, 64 x 128 133
+//          1,024 x 8,192 x 8,192      256 x 256 153, 128 x 128 135, 64 x 128 198
+//          1,000 x 9,000 x 1,000      256 x 256 69, 128 x 128 41, 64 x 128 37, 64 x 64 45
+//          600 x 5,000 x 2,000        128 x 128 29, 64 x 128 28, 64 x 64 36
+//          2,048 x 2,048 x 1,024      128 x 128 24, 64 x 128 14, 64 x 64 18
 //          4,096 x 40,000 x 128       64 x 128 in steps of 32 values 139, of 64 153; 128 x 128 of 32 135, of 64 160
 //          1,024 x 17,770 x 128       64 x 128 in steps of 32 values 19.9, of 64 20.9; 128 x 128 of 32 20.6, of 64 24.5
+//          25 x 100,000 x 1,000       128 x 128 78, 64 x 128 54, 64 x 64 49, 32 x 128 50
 //          5 x 8,192 x 8,192          16 x 64 25.5 (the library's product 23)
 //   fp32   1,024 x 17,770 x 100       64 x 128 45, 64 x 64 46, 128 x 64 47, 128 x 128 51 (before the values behind steps)
-//          1,024 x 17,770 x 32        64 x 128 24, 64 x 64 23, 128 x 64 26, 128 x 128 29
+//          2,000 x 9,000 x 500        64 x 128 122, 64 x 64 134, 128 x 128 128
+//          500 x 9,000 x 1,000        64 x 128 78, 64 x 64 85, 128 x 128 93
+//          100 x 50,000 x 200         64 x 128 33 (14 of 782 tiles are left for a second round), 64 x 64 27, 128 x 128 27
+//          25 x 221,853 x 80          64 x 128 33, 64 x 64 31, 32 x 128 26, 32 x 64 24
 template <typename T>
 void product(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
     const auto tiles = [&](int64_t users, int64_t items) {
         return ((a.m + users - 1) / users) * ((a.n + items - 1) / items);
     };
-    const bool large = a.f > 128 && tiles(128, 128) >= 2 * ctx->cus, middle = tiles(64, 128) >= 2 * ctx->cus;
+    const auto rounds = [&](int64_t users, int64_t items, int64_t on_a_cu) {
+        const int64_t at_once = ctx->cus * on_a_cu;
+        return (double)((tiles(users, items) + at_once - 1) / at_once * at_once) * (double)(users * items);
+    };
     if constexpr (sizeof(T) == 2) {
         const auto near = [](const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0 && ld < kNear; };
         if (near(a.x, a.ldx) && near(a.theta, a.ldt) && (!a.users || a.of < (int64_t)(kPastEnd / 2) / a.ldx)) {
             if (a.m <= 16) return direct<T, 1, 2, 1, 2, 64, 4>(ctx, a, st);
-            if (a.f >= 512 && tiles(256, 256) >= ctx->cus) return direct<T, 2, 4, 8, 4, 64, 2>(ctx, a, st);
-            if (large) return direct<T, 2, 2, 4, 4, 64, 2>(ctx, a, st);
-            if (middle && a.f <= 128) return direct<T, 2, 2, 2, 4, 32, 3>(ctx, a, st);
-            if (middle) return direct<T, 2, 2, 2, 4, 64, 2>(ctx, a, st);
+            if (a.f > 128) {
+                if (a.m <= 32) return direct<T, 1, 4, 2, 2, 64, 3>(ctx, a, st);
+                if (a.f >= 512 && tiles(256, 256) >= ctx->cus && rounds(256, 256, 1) <= 1.4 * rounds(128, 128, 2))
+                    return direct<T, 2, 4, 8, 4, 64, 2>(ctx, a, st);
+                if (a.m > 64 && tiles(128, 128) >= 2 * ctx->cus) return direct<T, 2, 2, 4, 4, 64, 2>(ctx, a, st);
+                if (2 * tiles(64, 128) >= 3 * ctx->cus) return direct<T, 2, 2, 2, 4, 64, 2>(ctx, a, st);
+            } else if (tiles(64, 128) >= 2 * ctx->cus) {
+                return direct<T, 2, 2, 2, 4, 32, 3>(ctx, a, st);
+            }
             return direct<T, 2, 2, 2, 2, 64, 4>(ctx, a, st);
         }
     }
     if (a.m <= 16) return staged<T, 1, 4, 1, 1>(ctx, a, st);
-    if (large) return staged<T, 2, 2, 4, 4>(ctx, a, st);
-    if (middle) return staged<T, 2, 2, 2, 4>(ctx, a, st);
+    if (a.m <= 32) return staged<T, 1, 4, 2, 1>(ctx, a, st);
+    const double wide = 1.2 * rounds(64, 128, 3), narrow = 1.15 * rounds(64, 64, 4);
+    if (a.f > 128 && a.m > 64 && rounds(128, 128, 2) <= wide && rounds(128, 128, 2) <= narrow)
+        return staged<T, 2, 2, 4, 4>(ctx, a, st);
+    if (wide <= narrow) return staged<T, 2, 2, 2, 4>(ctx, a, st);
     return staged<T, 2, 2, 2, 2>(ctx, a, st);
 }
 

@@ -68,7 +68,8 @@ def test_predict_whole_numbers(ctx, dtype, m, n, f):
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("m,n,f", [(4101, 4105, 520), (4101, 4105, 515), (2300, 2100, 64), (2300, 2100, 200), (1100, 2100, 1000),
-                                   (1500, 1400, 72), (600, 900, 4100), (20, 300, 9000), (16, 8192, 2048), (4096, 4097, 512)])
+                                   (1500, 1400, 72), (600, 900, 4100), (20, 300, 9000), (16, 8192, 2048), (4096, 4097, 512),
+                                   (31, 9000, 200), (32, 5000, 96), (310, 20_000, 520), (100, 20_000, 136)])
 def test_predict_large(ctx, dtype, m, n, f):
     """Enough tiles for every shape of them, and few that are cut along f: whole numbers against 64-bit products, rows taken
     by index and in order."""

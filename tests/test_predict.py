@@ -83,7 +83,7 @@ def test_loads_to_lds():
     text = _device_disassembly(build.PREDICT_LIB)
     assert lds_load_violations(text) == []
     loading = [k for k in re.split(r"\n(?=[0-9a-f]+ <)", text) if re.search(r"buffer_load_dwordx4 .* lds", k)]
-    assert len(loading) == 12       # six shapes of tiles, two types
+    assert len(loading) == 14       # seven shapes of tiles, two types
     for k in loading:
         assert not re.search(r"gpr_idx|v_movrel|s_movrel|s_sendmsg\b", k)
         uses = [line.split("//")[0].strip() for line in k.splitlines() if re.search(r"\bm0\b", line.split("//")[0])]
