@@ -523,6 +523,39 @@ def test_one_of_many_rows(ctx):
             assert torch.equal(one.top_index[0], r.top_index[i]) and torch.equal(one.log[0], r.log[i])
 
 
+def test_the_most_columns(ctx):
+    """Rows of ALS_PREDICT_N_MAX columns, against the 64-bit forms, and more of them than the workspace holds at a time,
+    against the same rows alone; the offsets' gradient in as few groups as the workspace holds."""
+    from paper_1603_03820_amd import predict
+    rng = np.random.default_rng(11)
+    n = predict.ALS_PREDICT_N_MAX
+    check(ctx, scores(rng, 2, n, "f32"), rng.integers(0, n, (2, 5)).astype(np.int32), 0.9, 128, lists(rng, 2, n, 300), what="the most columns")
+    rows = 700
+    gen = torch.Generator(device=D).manual_seed(3)
+    z = torch.empty(rows, n, dtype=torch.bfloat16, device=D)
+    for r in range(0, rows, 100):
+        z[r:r + 100] = torch.randn(100, n, device=D, generator=gen)
+    given = torch.randint(0, n, (rows,), device=D, generator=gen, dtype=torch.int32)
+    log(f"log_prob {rows}x{n}")
+    r = predict.als_log_prob(ctx, z, given, top=128)
+    for i in (0, 314, 628, 629, 630, 699):
+        one = predict.als_log_prob(ctx, z[i:i + 1], given[i:i + 1], top=128)
+        for a, b in zip(one, r):
+            assert torch.equal(a[0], b[i])
+    log("and its gradient")
+    some = z[:40]
+    part = predict.LogProb(r.log[:40], r.stats[:40], r.entropy[:40], None, None)
+    g = torch.rand(40, device=D, generator=gen)
+    d, c = predict.als_log_prob_grad(ctx, some, given[:40], part, g, columns=True)
+    p = torch.softmax(some.double(), 1)
+    want = -(p * g.double()[:, None])
+    want[torch.arange(40, device=D), given[:40].long()] += g.double()
+    size = want.abs().sum(0)
+    # of p: the sum's error (as in tests/predict_oracle.py, below 2^-17 here), of 40 rows' sum as many roundings
+    assert bool(((c.double() - want.sum(0)).abs() <= size * (2.0 ** -17 + 44 * 2.0 ** -24) + 2.0 ** -126).all())
+    assert bool(((d.double() - want).abs() <= want.abs() * (2.0 ** -8 + 2.0 ** -17) + 2.0 ** -126).all())
+
+
 def test_scores_and_draws_agree(ctx):
     """The log probability of what als_sample draws is the one that it gives: predictions, draw and log probability
     together, as a recommender uses them, captured into a graph and replayed on other users."""
