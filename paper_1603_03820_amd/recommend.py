@@ -17,7 +17,7 @@ import time
 
 import torch
 
-from . import als, driver, predict, serve
+from . import als, driver, serve
 
 
 def run(workload: str = "tiny", iters: int = 5, batch: int = 256, temperature: float = 0.2, top_k: int = 50,
@@ -49,6 +49,7 @@ def evaluate(workload: str = "tiny", iters: int = 5, batch: int = 256, temperatu
     and after `steps` steps of fitting the items' offsets to the other users' held-out items, and the mean log probability
     of those before each step."""
     import synth
+    from . import predict
     p = synth.config(workload)
     train, test = synth.split(p.rowptr, p.colidx, p.vals, held, p.recipe["seed"])
     ctx = als.Context(device, p.f)

@@ -116,6 +116,26 @@ def test_refusals_without_a_device():
     assert lib.als_predict_destroy(None) == 0 and lib.als_predict_last_hip_error(None) == 0
 
 
+def test_training_and_serving_do_without_the_library(tmp_path):
+    """The package where libals_predict.so is not built: the rest imports, and the prediction names say what is missing."""
+    import shutil
+    from tests.test_import import PACKAGE, run
+    shutil.copytree(os.path.join(ROOT, PACKAGE), tmp_path / PACKAGE,
+                    ignore=shutil.ignore_patterns("libals_predict.so", "__pycache__", "csrc"))
+    r = run(tmp_path, f"import {PACKAGE} as p; from {PACKAGE} import driver, serve, recommend; print(p.als_score.__name__)")
+    assert r.returncode == 0 and r.stdout.split() == ["als_score"], r.stderr
+    for code in (f"from {PACKAGE} import predict", f"from {PACKAGE} import Predictor", f"import {PACKAGE}; {PACKAGE}.als_log_prob"):
+        r = run(tmp_path, code)
+        assert r.returncode != 0 and "libals_predict.so is not built" in r.stderr, r.stderr
+
+
+def test_the_names_are_the_packages():
+    import paper_1603_03820_amd as p
+    from paper_1603_03820_amd import predict
+    for name in ("Predictor", "als_predict", "als_log_prob", "als_log_prob_grad", "als_predict_workspace_bytes"):
+        assert getattr(p, name) is getattr(predict, name) and name in dir(p)
+
+
 def test_oracle_by_hand():
     row = predict_oracle.Row(np.log([0.5, 0.25, 0.125, 0.125]))
     assert np.allclose(np.exp(row.log_p), [0.5, 0.25, 0.125, 0.125])
