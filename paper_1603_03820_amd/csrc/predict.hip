@@ -642,12 +642,13 @@ __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
     tile_of(blockIdx.x, a.tu, a.ti, a.height, &tile_u, &tile_i);
     const int64_t u0 = (int64_t)tile_u * C::kUsers, i0 = (int64_t)tile_i * C::kItems;
 
-    // what the buffers hold: the tile's rows (all of X where users are taken by index), the last up to the end of its
-    // last group
+    // what the buffers hold: the tile's rows (all of X where users are taken by index; one at least), the last up to the
+    // end of its last group.  A load's offset is compared with the bytes less the scalar offset, which a buffer
+    // without rows would take below 0 and so past kPastEnd.
     const int64_t users = a.m - u0 < C::kUsers ? a.m - u0 : C::kUsers, items = a.n - i0 < C::kItems ? a.n - i0 : C::kItems;
     const int64_t from = a.users ? 0 : u0, rows = a.users ? a.of : users;
     const int whole = (a.f + 7) / 8 * 16;
-    const i4 from_u = buffer_of((const T*)a.x + from * a.ldx, rows > 0 ? (uint32_t)((rows - 1) * a.ldx * 2 + whole) : 0);
+    const i4 from_u = buffer_of((const T*)a.x + from * a.ldx, (uint32_t)((rows - 1) * a.ldx * 2 + whole));
     const i4 from_i = buffer_of((const T*)a.theta + i0 * a.ldt, (uint32_t)((items - 1) * a.ldt * 2 + whole));
     buffer_settle(from_u, from_i);
     const int first_u = wave * C::kUserLoads * kAtOnce, first_i = wave * C::kItemLoads * kAtOnce;   // this wave's rows
@@ -1622,7 +1623,8 @@ void product(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
     };
     if constexpr (sizeof(T) == 2) {
         const auto near = [](const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0 && ld < kNear; };
-        if (near(a.x, a.ldx) && near(a.theta, a.ldt) && (!a.users || a.of < (int64_t)(kPastEnd / 2) / a.ldx)) {
+        // (an X without rows, whose users all do not exist, is k_product's, which loads nothing for them)
+        if (a.of > 0 && near(a.x, a.ldx) && near(a.theta, a.ldt) && (!a.users || a.of < (int64_t)(kPastEnd / 2) / a.ldx)) {
             if (a.m <= 16) return direct<T, 1, 2, 1, 2, 64, 4>(ctx, a, st);
             if (a.f > 128) {
                 if (a.m <= 32) return direct<T, 1, 4, 2, 2, 64, 3>(ctx, a, st);
