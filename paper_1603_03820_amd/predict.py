@@ -340,16 +340,23 @@ class Predictor:
         returns that mean before each of `steps` steps.  A step compares how often an item is given (c) with how often
         the model expects it (e), whose difference is T times the gradient, and moves its offset by rate T (c - e) / max(c, e):
         at most by T.  Users are taken `batch` at a time.  Items that a user has rated are left out for them; given
-        ones among those count for nothing."""
+        ones among those count for nothing, and so does what is given for a user that there is not (no row of x, or none of
+        `rated`)."""
         n, count = self.theta.shape[0], users.numel()
-        if count == 0 or given.shape != users.shape:
+        if users.dim() != 1 or count == 0 or given.shape != users.shape:
             raise ValueError(f"given must have an item for each of {count} users (one at least), has shape {tuple(given.shape)}")
+        # (a row of a user that there is not has NaN in every column of its gradient)
+        of = self.x.shape[0] if self.rated is None else min(self.x.shape[0], self.rated[0].numel() - 1)
+        there = (users >= 0) & (users < of)
+        users, given = users[there], given[there]
+        count = users.numel()
         if self.item_offset is None:
             self.item_offset = torch.zeros(n, dtype=torch.float32, device=self.theta.device)
         means = []
         for _ in range(steps):
             short, counts = torch.zeros_like(self.item_offset), torch.zeros_like(self.item_offset)
-            total, used = 0.0, 0
+            total = torch.zeros((), dtype=torch.float64, device=users.device)
+            used = torch.zeros((), dtype=torch.int64, device=users.device)
             for k in range(0, count, batch):
                 u, g = users[k:k + batch], given[k:k + batch]
                 z = als_predict(self.ctx, self.x, self.theta, u, None, self.item_offset)

@@ -22,3 +22,21 @@ def test_users_of_a_model_without_any(ctx, dtype, m, n, f):  # noqa: F811
         got = predict.als_predict(ctx, x, t, users=users, user_offset=torch.empty(0, device=D), item_offset=torch.ones(n, device=D),
                                   activation=activation, residual=torch.ones(m, n, device=D))
         assert got.shape == (m, n) and bool(torch.isnan(got).all())
+
+
+@pytest.mark.parametrize("with_rated", [False, True])
+def test_fit_with_users_that_do_not_exist(ctx, with_rated):  # noqa: F811
+    """They count for nothing, with and without a CSR of rated items."""
+    from paper_1603_03820_amd import predict
+    rng = np.random.default_rng(14)
+    x, t = dev(rng.standard_normal((40, 8)).astype(np.float32)), dev(rng.standard_normal((60, 8)).astype(np.float32))
+    rated = tuple(dev(a) for a in lists(rng, 40, 60, 20)) if with_rated else None
+    who, what = rng.integers(0, 40, 200).astype(np.int32), rng.integers(0, 60, 200).astype(np.int32)
+    bad = np.array([-1, 40, 2 ** 31 - 1, -2 ** 31], np.int32)
+    log(f"fit with users that do not exist, rated {with_rated}")
+    a, b, c = (predict.Predictor(ctx, x, t, rated=rated) for _ in range(3))
+    got = a.fit_offsets(dev(np.concatenate([bad[:2], who, bad[2:]])), dev(np.concatenate([what[:2], what, what[:2]])), 0.5, 3)
+    want = b.fit_offsets(dev(who), dev(what), 0.5, 3)
+    assert bool(torch.isfinite(a.item_offset).all()) and torch.allclose(a.item_offset, b.item_offset, atol=1e-5)
+    assert got == pytest.approx(want, abs=4e-5)
+    assert c.fit_offsets(dev(bad), dev(what[:4]), 0.5, 2) == [0.0, 0.0] and not c.item_offset.any()
