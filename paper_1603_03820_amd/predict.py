@@ -10,6 +10,7 @@ there is no fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import NamedTuple
 
@@ -341,7 +342,9 @@ class Predictor:
         the model expects it (e), whose difference is T times the gradient, and moves its offset by rate T (c - e) / max(c, e):
         at most by T.  Users are taken `batch` at a time.  Items that a user has rated are left out for them; given
         ones among those count for nothing, and so does what is given for a user that there is not (no row of x, or none of
-        `rated`)."""
+        `rated`).  The temperature is one number; one that is not above 0 leaves the offsets as they are."""
+        if isinstance(temperature, torch.Tensor):
+            raise TypeError("temperature must be a number")
         n, count = self.theta.shape[0], users.numel()
         if users.dim() != 1 or count == 0 or given.shape != users.shape:
             raise ValueError(f"given must have an item for each of {count} users (one at least), has shape {tuple(given.shape)}")
@@ -350,6 +353,10 @@ class Predictor:
         there = (users >= 0) & (users < of)
         users, given = users[there], given[there]
         count = users.numel()
+        # the gradient of an offset is up to count / T, a step up to rate T
+        largest = torch.finfo(torch.float32).max
+        if not (abs(temperature) * max(1.0, abs(rate)) <= largest and (temperature <= 0 or count <= temperature * largest)):
+            raise ValueError(f"temperature, rate times it and {count} / temperature must be in float32's range, is {temperature}")
         if self.item_offset is None:
             self.item_offset = torch.zeros(n, dtype=torch.float32, device=self.theta.device)
         means = []

@@ -82,3 +82,35 @@ def test_lists_that_are_no_vectors_are_refused(predict):
         with pytest.raises(ValueError):
             model.fit_offsets(w, g)
     assert model.item_offset is None
+
+
+@pytest.mark.parametrize("temperature", [float("nan"), float("inf"), float("-inf"), 1e-42, 1e-37, 1e39])
+def test_temperatures_without_a_gradient_are_refused(predict, temperature):
+    """Those of no finite gradient: its product with T would be no number, and the offsets with it."""
+    x, theta, rated, who, what = problem(4)
+    for offset in (None, torch.ones(12)):
+        model = predict.Predictor(None, x, theta, item_offset=offset, rated=rated)
+        with pytest.raises(ValueError):
+            model.fit_offsets(who, what, temperature, 2)
+        assert model.item_offset is offset
+
+
+def test_a_temperature_for_each_user_is_refused(predict):
+    x, theta, rated, who, what = problem(5, n=1, count=30)
+    with pytest.raises(TypeError):
+        predict.Predictor(None, x, theta).fit_offsets(who, what, torch.ones(30), 2)
+
+
+@pytest.mark.parametrize("temperature", [0.0, -1.0])
+def test_a_greedy_fit_moves_nothing(predict, temperature):
+    x, theta, rated, who, what = problem(6)
+    model = predict.Predictor(None, x, theta)
+    model.fit_offsets(who, what, temperature, 2)
+    assert not model.item_offset.any()
+
+
+def test_a_cold_fit_is_finite(predict):
+    x, theta, rated, who, what = problem(7)
+    model = predict.Predictor(None, x, theta, rated=rated)
+    model.fit_offsets(who, what, 1e-30, 2)
+    assert torch.isfinite(model.item_offset).all()
