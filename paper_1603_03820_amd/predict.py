@@ -114,6 +114,14 @@ class Context(serve.Context):
 # take longer than its kernel.
 
 
+def _count(ctx: Context, t, name, dtypes):
+    """A tensor's elements; what is no tensor is refused."""
+    try:
+        return t.numel()
+    except AttributeError:
+        _use(ctx, t, name, dtypes)
+
+
 def _like(ctx: Context, t, shape, dtype, other):
     """Allocated on the call's stream; t is a tensor on the context's device."""
     if other is None:
@@ -132,7 +140,7 @@ def als_predict(ctx: Context, x, theta, users=None, user_offset=None, item_offse
     pt, ldt, n, _ = _matrix(ctx, theta, "theta", (x.dtype,), None, f, other)
     m, pu = of, None
     if users is not None:
-        m = users.numel()
+        m = _count(ctx, users, "users", _I32)
         pu = _vector(ctx, users, "users", _I32, m, other)
     pa = None if user_offset is None else _vector(ctx, user_offset, "user_offset", _F32, of, other)
     pb = None if item_offset is None else _vector(ctx, item_offset, "item_offset", _F32, n, other)
@@ -146,8 +154,8 @@ def als_predict(ctx: Context, x, theta, users=None, user_offset=None, item_offse
         out = _like(ctx, x, (m, n), dtype, other)
         po, ldo = out.data_ptr(), n
     else:
-        dtype = out.dtype
         po, ldo, _, _ = _matrix(ctx, out, "out", _FLOATS, m, n, other)
+        dtype = out.dtype
     pr, ldr = None, n
     if residual is not None:
         pr, ldr, _, _ = _matrix(ctx, residual, "residual", (dtype,), m, n, other)
@@ -184,11 +192,11 @@ def _of_rows(ctx, scores, given, temperature, rated, users, other):
     s.of = 0
     if rated is not None:
         rowptr, colidx = rated
-        of = rowptr.numel() - 1
+        of = _count(ctx, rowptr, "rated[0]", _I64) - 1
         s.of = of
         s.rated_ptr = _vector(ctx, rowptr, "rated[0]", _I64, of + 1, other)
         # (of a CSR without entries nothing is read)
-        s.rated_idx = _vector(ctx, colidx, "rated[1]", _I32, colidx.numel(), other) or s.rated_ptr
+        s.rated_idx = _vector(ctx, colidx, "rated[1]", _I32, _count(ctx, colidx, "rated[1]", _I32), other) or s.rated_ptr
         if users is not None:
             s.users = _vector(ctx, users, "users", _I32, rows, other)
         elif of < rows:
@@ -197,7 +205,7 @@ def _of_rows(ctx, scores, given, temperature, rated, users, other):
         raise ValueError("users without rated")
     if isinstance(given, tuple):
         ptr, idx = given
-        entries = idx.numel()
+        entries = _count(ctx, idx, "given[1]", _I32)
         shape = (entries,)
         g.ptr = _vector(ctx, ptr, "given[0]", _I64, rows + 1, other)
         g.idx = _vector(ctx, idx, "given[1]", _I32, entries, other)
@@ -345,7 +353,8 @@ class Predictor:
         `rated`).  The temperature is one number; one that is not above 0 leaves the offsets as they are."""
         if isinstance(temperature, torch.Tensor):
             raise TypeError("temperature must be a number")
-        n, count = self.theta.shape[0], users.numel()
+        n, count = self.theta.shape[0], _count(self.ctx, users, "users", _I32)
+        _count(self.ctx, given, "given", _I32)
         if users.dim() != 1 or count == 0 or given.shape != users.shape:
             raise ValueError(f"given must have an item for each of {count} users (one at least), has shape {tuple(given.shape)}")
         # (a row of a user that there is not has NaN in every column of its gradient)

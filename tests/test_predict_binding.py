@@ -170,3 +170,23 @@ def test_refusals(lib, monkeypatch, call, error):
     with pytest.raises(error):
         call(HostContext(), torch.zeros(2, 9), torch.zeros(2, dtype=torch.int32))
     assert not lib.calls
+
+
+@pytest.mark.parametrize("call,name", [
+    (lambda c, z, g: predict.als_predict(c, z, z, users=[0, 1]), "users"),
+    (lambda c, z, g: predict.als_predict(c, z, z, out=[0.0]), "out"),
+    (lambda c, z, g: predict.als_predict(c, [[0.0]], z), "x"),
+    (lambda c, z, g: predict.als_predict(c, z, z, residual=[0.0]), "residual"),
+    (lambda c, z, g: predict.als_predict(c, z, z, item_offset=[0.0] * 2), "item_offset"),
+    (lambda c, z, g: predict.als_log_prob(c, z, [0, 0]), "given"),
+    (lambda c, z, g: predict.als_log_prob(c, z, ([0, 1, 2], g)), "given[0]"),
+    (lambda c, z, g: predict.als_log_prob(c, z, (torch.zeros(3, dtype=torch.int64), [0, 0])), "given[1]"),
+    (lambda c, z, g: predict.als_log_prob(c, z, g, rated=([0, 0, 0], g)), "rated[0]"),
+    (lambda c, z, g: predict.als_log_prob(c, z, g, rated=(torch.zeros(3, dtype=torch.int64), [0])), "rated[1]"),
+    (lambda c, z, g: predict.als_log_prob(c, z, g, rated=(torch.zeros(3, dtype=torch.int64), g), users=[0, 1]), "users"),
+    (lambda c, z, g: predict.als_log_prob(c, z, g, log=[0.0, 0.0]), "log"),
+])
+def test_lists_in_place_of_tensors_are_refused_by_name(lib, call, name):
+    with pytest.raises(TypeError, match=name.replace("[", r"\[").replace("]", r"\]") + " must be a device tensor"):
+        call(HostContext(), torch.zeros(2, 9), torch.zeros(2, dtype=torch.int32))
+    assert not lib.calls

@@ -114,3 +114,11 @@ def test_a_cold_fit_is_finite(predict):
     model = predict.Predictor(None, x, theta, rated=rated)
     model.fit_offsets(who, what, 1e-30, 2)
     assert torch.isfinite(model.item_offset).all()
+
+
+def test_lists_in_place_of_tensors_are_refused(predict):
+    x, theta, rated, who, what = problem(8)
+    model = predict.Predictor(None, x, theta)
+    for w, g, name in (([0, 1], what, "users"), (who, [0, 1], "given")):
+        with pytest.raises(TypeError, match=name + " must be a device tensor"):
+            model.fit_offsets(w, g)
