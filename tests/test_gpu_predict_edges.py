@@ -40,3 +40,46 @@ def test_fit_with_users_that_do_not_exist(ctx, with_rated):  # noqa: F811
     assert bool(torch.isfinite(a.item_offset).all()) and torch.allclose(a.item_offset, b.item_offset, atol=1e-5)
     assert got == pytest.approx(want, abs=4e-5)
     assert c.fit_offsets(dev(bad), dev(what[:4]), 0.5, 2) == [0.0, 0.0] and not c.item_offset.any()
+
+
+def fit64(x, t, who, what, temperature, steps, rate, rated=None):
+    """fit_offsets in 64 bits: (the means before each step, the offsets after each)."""
+    n, b, means, offsets = t.shape[0], np.zeros(t.shape[0]), [], []
+    for _ in range(steps):
+        expected, counts, total = np.zeros(n), np.zeros(n), []
+        for u, g in zip(who, what):
+            row = predict_oracle.Row(x[u].astype(np.float64) @ t.T.astype(np.float64) + b, temperature,
+                                     () if rated is None else row_of(rated, u))
+            if row.log(g) > -np.inf:
+                total.append(row.log(g))
+                expected += np.exp(row.log_p)
+                counts[g] += 1
+        means.append(np.mean(total))
+        b = b + rate * temperature * (counts - expected) / np.maximum(np.maximum(counts, expected), 1e-6)
+        offsets.append(b)
+    return means, offsets
+
+
+@pytest.mark.parametrize("with_rated", [False, True])
+@pytest.mark.parametrize("batch", [1000, 150])
+def test_fit_offsets_against_64_bits(ctx, with_rated, batch):  # noqa: F811
+    """Each step's mean, which rises (a step is no longer than iterative scaling's, T log(c / e)), and the offsets."""
+    from paper_1603_03820_amd import predict
+    rng = np.random.default_rng(21)
+    users, n, count, t = 100, 50, 400, 0.7
+    x, theta = (0.3 * rng.standard_normal((users, 8))).astype(np.float32), rng.standard_normal((n, 8)).astype(np.float32)
+    rated = lists(rng, users, n, 10) if with_rated else None
+    who, what = rng.integers(0, users, count).astype(np.int32), (rng.zipf(1.5, count) % n).astype(np.int32)
+    want, offsets = fit64(x, theta, who, what, t, 8, 0.5, rated)
+    assert all(b > a + 1e-4 for a, b in zip(want, want[1:]))
+    log(f"fit against 64 bits, rated {with_rated}, batch {batch}")
+    rd = None if rated is None else tuple(dev(a) for a in rated)
+    short, whole = (predict.Predictor(ctx, dev(x), dev(theta), rated=rd) for _ in range(2))
+    means = short.fit_offsets(dev(who), dev(what), t, 3, 0.5, batch)
+    # a score is off by at most 2.2e-5 (predict_bound at sizes up to 3.5), log p and the share of an expected count by 2 / T
+    # of that; the sums over 400 rows by 400 units: 1.2e-4 of a step of at most rate T, which each later step doubles at most
+    off = 0.5 * t * 1.2e-4 * 7
+    assert np.abs(f64(short.item_offset) - offsets[2]).max() <= off
+    assert means == pytest.approx(want[:3], abs=2 * off / t + 1e-4)
+    means = whole.fit_offsets(dev(who), dev(what), t, 8, 0.5, batch)
+    assert all(b > a for a, b in zip(means, means[1:]))

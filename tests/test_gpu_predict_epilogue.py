@@ -17,7 +17,7 @@ LEAST = 2.0 ** -126      # exponentials below it are 0
 # product rounds), a reciprocal by 1.1 after its Newton step.
 #   sigmoid, silu  1 + e: half of the exponential's, and 1; reciprocal; product with e; with y: 3.1 + 2.6 + 1.1 + 1 + 1
 #   gelu           t by 3.1 (constant, sum, reciprocal), which moves t q(t) by at most 3.8 times as much; Horner's steps and
-#                  coefficients 6.7; the exponential 3.1 and the rounding of its fit 0.4; three products: 25
+#                  coefficients 6.7; the exponential 3.1; the polynomial's own 0.7; three products: 25.3
 #   tanh           the library's, 5 units of 2
 OFF = {"none": 0, "clip": 0, "relu": 0, "sigmoid": 9, "silu": 9, "gelu": 26, "tanh": 10}
 # of 16-bit results: an exponent's three roundings count |y| (or y^2 / 2, up to 85) times: 2^-16 up to |y| = 87, and with
