@@ -47,7 +47,8 @@ int als_predict_destroy(als_predict_ctx* ctx);
 /* HIP error code of the most recent ALS_ERR_HIP on this context (0 if none). */
 int als_predict_last_hip_error(const als_predict_ctx* ctx);
 
-/* Activations; y is the product with its offsets.  Where y is -inf, GELU and SILU are -0, their limit.  A NaN stays. */
+/* Activations; y is the product with its offsets.  Where y is -inf, GELU and SILU are -0, their limit.  A NaN stays.
+   Exponentials below 2^-126 are 0: so are SIGMOID and SILU where y is below -87.3, and GELU where y is below -13.2. */
 enum {
     ALS_ACT_NONE = 0,
     ALS_ACT_CLIP = 1,       /* min(max(y, low), high), low <= high (infinities allowed) */
@@ -75,7 +76,8 @@ enum {
  *               pointer and stride).
  *   out       : m x n of type out_dtype, row stride ldo >= n; must not overlap an input but so (ALS_ERR_ALIAS)
  * f in [1, ALS_PREDICT_F_MAX].  Rows of 16-bit types at addresses and strides that are multiples of 16 bytes (and fp32 ones
- * at strides of multiples of 128) are the fastest.
+ * at strides of multiples of 128) are the fastest; of such a 16-bit row the last 16 bytes that hold a value are read whole,
+ * up to 14 bytes past it (within the same 16 bytes), and what lies there does not count.
  */
 int als_predict(als_predict_ctx* ctx, const void* x, int64_t of, int64_t ldx, const int32_t* users, int64_t m,
                 const void* theta, int64_t n, int64_t ldt, int32_t dtype, int32_t f, const float* user_offset,

@@ -93,14 +93,17 @@ __device__ __forceinline__ float inverse_of(float d) {
     const float r = __builtin_amdgcn_rcpf(d);
     return fmaf(fmaf(-d, r, 1.f), r, r);
 }
-// 1 / (1 + exp(-y)) by exp(-|y|), which neither overflows nor loses the small values.
+// 1 / (1 + exp(-y)) by exp(-|y|), which does not overflow and keeps the small values down to 2^-126, below which an
+// exponential is 0 (y < -87.3).
 __device__ __forceinline__ float sigmoid(float y) {
     const float e = exp_of(-fminf(fabsf(y), 126.f), 0.f), r = inverse_of(1.f + e);
     return y != y ? y : (y < 0.f ? e * r : r);
 }
-// y erfc(-y / sqrt 2) / 2.  With a = |y| / sqrt 2 and t = 1 / (1 + 0.3 a), erfc(a) exp(a^2) / t is a polynomial in t to
-// 2.1e-8 of its value for a up to 12 (fitted by least squares, weighted towards the largest error, to scipy's
-// erfcx); in fp32 GELU is off by at most 5e-7 of its value, also where it is small: 1 + erf(y / sqrt 2) would lose it.
+// y erfc(-y / sqrt 2) / 2.  With a = |y| / sqrt 2 and t = 1 / (1 + 0.3 a), erfc(a) exp(a^2) / t is a polynomial in t
+// (fitted by least squares, weighted towards the largest error, to scipy's erfcx); with these coefficients it is off by
+// 4.3e-8 of its value up to |y| = 13.  In fp32 GELU was off by at most 5.3e-7 of its value (2 million arguments each in
+// [-13.1, -12], [-12, -0.001], [-1, -0.001], [-0.001, 0] and [0, 12]), also where it is small: 1 + erf(y / sqrt 2) would lose
+// it.  Below y = -13.2, where the exponential is below 2^-126, it is -0.
 __device__ __forceinline__ float gelu(float y) {
     const float a = fminf(fabsf(y), 18.f), t = inverse_of(fmaf(a, 0.212132034f, 1.f));
     float q = -0.12925273f;
@@ -118,7 +121,8 @@ __device__ __forceinline__ float gelu(float y) {
 }
 
 // For results of 16 bits, whose half a unit is 2^-11 or more of them: exponentials of arguments rounded to fp32 (a few
-// units of 2^-24, times the exponent's size), and for GELU a polynomial (in t = 1 / (1 + 0.44 a)) to 5e-06.
+// units of 2^-24, times the exponent's size), and for GELU a polynomial (in t = 1 / (1 + 0.44 a)) to 5.2e-6 of its value
+// up to |y| = 13 (7.5e-6 at 18, where the value is 0 in every type).
 __device__ __forceinline__ float sigmoid16(float y) {
     return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y * -0x1.715476p+0f));
 }
@@ -626,10 +630,12 @@ struct Direct {
 // in LDS, 2 STEP bytes a row, while the next steps' (STAGES - 1 of them) arrive straight from memory beside them
 // (buffer_load ... lds: no registers, no instructions but the load).  Items and users past the end read as zeros; in the
 // last step values past f are masked on both sides, as what lies in their place may be no number.
-// 4,096 x 8,192 x 8,192 in 427 us without activation and residual (1.29 Pflop/s; the library's product 406), with GELU and
-// residual 451: one workgroup is on a CU, and nothing runs beside its way out.  4,096 x 40,000 x 128 with a sigmoid in 133
-// (2.5 TB/s): loads, products and stores of a tile follow one another, and the four workgroups of a CU do not hide all of it
-// (stores alone took 95 us).  5 x 8,192 x 8,192 in 26 (5.2 TB/s): the weights' bytes.
+// 4,096 x 8,192 x 8,192 in 425 us without activation and residual (1.29 Pflop/s; the library's product 406), with GELU and
+// residual 456 to 484 by card: one workgroup is on a CU, and nothing runs beside its way out.  4,096 x 40,000 x 128 in 124 us
+// without activation, with a sigmoid in 132 to 140 (2.5 TB/s): loads, products and stores of a tile follow one another, and
+// the four workgroups of a CU do not hide all of it (stores alone took 95 us, where a fill of as many bytes takes 48).
+// 5 x 8,192 x 8,192 with its join in 24.5 us where the last level of cache holds the weights (5.5 TB/s), in 35 where they come
+// from memory (3.8 TB/s).
 template <typename T, int WU, int WI, int FU, int FI, int STEP, int STAGES>
 __global__ __launch_bounds__(64 * WU * WI) void k_product_lds(Product a) {
     using C = Direct<WU, WI, FU, FI, STEP, STAGES>;
@@ -1002,11 +1008,13 @@ __device__ __forceinline__ void write_no_top(const RowArgs<T>& a, int64_t r, con
 // A row, or a segment of one, of up to E scores a thread, which stay in registers from their one read on: the best one of
 // a wave, then weights relative to it (a wave's sums need no barrier), then the waves' masses joined.  H comes from the
 // same pass: with x = log2 w, H = log S - ln 2 sum(w x) / S, whose terms are all of one sign.
-// 1,024 x 17,770 fp32 in 19.5 us, with the 20 best 25 (73 MB: 3.8 and 2.9 TB/s); 64 x 625,000 bf16 in 28 and 42.  Bound by
-// waits: a workgroup's loads, lists, sums and its best columns follow one another, and most workgroups are at the same
-// one.  40 scores a thread past 16,384: seven waves a row of 17,770, so that four rows are on a CU and the batch takes one
-// round (with the best, 32 a thread 36 us, 40 27, 48 29, 64 42 at the time); segments of 20,480 columns (45.8 us; 8,192 49.0,
-// 16,384 49.4, 32,768 59.0).
+// 1,024 x 17,770 fp32 in 19.5 us, with the 20 best 25 to 26 (73 MB: 3.8 and 2.9 TB/s); 64 x 625,000 bf16 with the join in 29
+// and 41 where the last level of cache holds the rows, in 33 and 46 where not.  Bound by waits: a workgroup's loads, lists, sums
+// and its best columns follow one another, and most workgroups are at the same one.  40 scores a thread past 16,384 took the
+// least time (1,024 x 17,770 with the best: 32 a thread 36 us, 40 27, 48 29, 64 42 at the time).  At 78 registers a SIMD has
+// six of its waves, so a CU three rows of 17,770 (seven waves each), and 1,024 rows take two rounds, the second a third full.
+// Segments of 20,480 columns (64 x 625,000 bf16: 45.8 us; 8,192 49.0, 16,384 49.4, 32,768 59.0); fewer rows have segments as
+// long, and leave CUs idle: one row of 625,000 is 31 workgroups.
 template <typename T, int E>
 __global__ __launch_bounds__(1024, E <= 16 || sizeof(T) == 2 ? 8 : 5) void k_row(RowArgs<T> a) {
     constexpr int V = E * sizeof(T) < 16 ? E : 16 / sizeof(T);
@@ -1271,9 +1279,10 @@ struct Grad {
 // left-out columns are marked in LDS by all of the workgroup (three rows' marks in turn: one is cleared while one is read,
 // so a row takes one barrier).  The given columns each wave looks through for itself: what lies in its run goes to the
 // lane that has it, in the list's order, so that sums of repeated columns are the same on every run.
-// 1,024 x 17,770 fp32 in 28 us (5.2 TB/s read and written), 64 x 625,000 bf16 in 34 (4.7 TB/s): memory.  With the columns'
-// sums alone 28 + 6 us (2.6 TB/s): 8 columns a lane, as the sums and the next row's scores take registers (34.7 us with
-// k_columns, 16 a lane 44), and a third of its instructions are a row's, not a column's.
+// 1,024 x 17,770 fp32 in 29 us (5.0 TB/s read and written), 64 x 625,000 bf16 in 40 to 42 (3.9 TB/s): memory.  Where the last
+// level of cache holds the rows, 27 (5.5 TB/s) and 33 (4.9).  With the columns' sums alone 28 + 6 us (2.1 TB/s): 8 columns a
+// lane, as the sums and the next row's scores take registers (34.7 us with k_columns, 16 a lane 44), and a third of its
+// instructions are a row's, not a column's.
 template <typename T, bool COLUMNS>
 __global__ __launch_bounds__(kGradThreads, COLUMNS ? 6 : 5) void k_gradient(
     GradArgs<T> a, const float* __restrict__ temperature, const int64_t* __restrict__ rated_ptr,
@@ -1606,7 +1615,7 @@ void direct(const als_predict_ctx* ctx, const Product& a, hipStream_t st) {
 //          4,096 x 40,000 x 128       64 x 128 in steps of 32 values 139, of 64 153; 128 x 128 of 32 135, of 64 160
 //          1,024 x 17,770 x 128       64 x 128 in steps of 32 values 19.9, of 64 20.9; 128 x 128 of 32 20.6, of 64 24.5
 //          25 x 100,000 x 1,000       128 x 128 78, 64 x 128 54, 64 x 64 49, 32 x 128 50
-//          5 x 8,192 x 8,192          16 x 64 25.5 (the library's product 23)
+//          5 x 8,192 x 8,192          16 x 64 25.5 (the library's product 23; both with the weights in the last-level cache)
 //   fp32   1,024 x 17,770 x 100       64 x 128 45, 64 x 64 46, 128 x 64 47, 128 x 128 51 (before the values behind steps)
 //          2,000 x 9,000 x 500        64 x 128 122, 64 x 64 134, 128 x 128 128
 //          500 x 9,000 x 1,000        64 x 128 78, 64 x 64 85, 128 x 128 93
@@ -1875,7 +1884,8 @@ int als_log_prob_grad(als_predict_ctx* ctx, const als_scores* scores, const als_
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return ALS_ERR_DEVICE;
     const hipStream_t st = (hipStream_t)stream;
-    // a workgroup takes one row's chunk, or with the columns' sums as many rows as leave every CU eight workgroups
+    // a workgroup takes one row's chunk, or with the columns' sums as many rows as leave every CU eight workgroups (it has six
+    // of them at a time, at 80 registers, so that at 1,024 x 17,770 the last quarter is a round of its own)
     int64_t groups = 0;
     by_type(s.dtype, [&](auto* p) {
         using T = Type<decltype(p)>;

@@ -4,8 +4,8 @@ marshalling torch tensors, and a model that evaluates and fits its offsets with 
 ``als_predict`` gives predictions at the factors' own precision, with offsets, an activation and a residual;
 ``als_log_prob`` takes rows of scores as distributions and gives the log probabilities of items in them, their entropy
 and best items; ``als_log_prob_grad`` is its gradient.  ``Predictor`` holds a model's factors and offsets.  All
-arithmetic runs in the library's kernels; importing this module fails loudly when libals_predict.so is not built:
-there is no fallback implementation.
+arithmetic runs in the library's kernels; importing this module fails loudly when libals_predict.so is not built, or
+libals_serve.so, with whose binding it shares the handling of tensors: there is no fallback implementation.
 """
 from __future__ import annotations
 
@@ -324,14 +324,17 @@ def als_log_prob_grad(ctx: Context, scores, given, forward: LogProb, grad_log, g
 
 class Predictor:
     """A trained model's predictions and what they say of items: factors x and theta, an offset for each user and item
-    (float32, or None), and `rated`, the CSR of the training ratings, which its users are not recommended again."""
+    (float32, or None), and `rated`, the CSR of the training ratings, which its users are not recommended again.  The offsets
+    belong to the scores whatever they are for: those that fit_offsets leaves are part of what predict gives from then on."""
 
     def __init__(self, ctx: Context, x, theta, user_offset=None, item_offset=None, rated=None):
         self.ctx, self.x, self.theta, self.rated = ctx, x, theta, rated
         self.user_offset, self.item_offset = user_offset, item_offset
 
     def predict(self, users=None, low=None, high=None, dtype=torch.float32, stream=None):
-        """The predicted ratings of `users` (int32 rows of X; all of them) for every item, between `low` and `high`."""
+        """The predicted ratings of `users` (int32 rows of X; all of them) for every item, between `low` and `high`.  (Where the
+        items' offsets were fitted to choices, by fit_offsets, these are scores of choice and no longer ratings: predict ratings
+        with a Predictor of the offsets before.)"""
         clip = low is not None or high is not None
         return als_predict(self.ctx, self.x, self.theta, users, self.user_offset, self.item_offset,
                            "clip" if clip else "none", low, high, dtype=dtype, stream=stream)
@@ -340,7 +343,8 @@ class Predictor:
         return dict(rated=self.rated, users=None if self.rated is None else users)
 
     def log_prob(self, users, given, temperature=1.0, top=0, log=None, stream=None):
-        """LogProb of the items `given` (see als_log_prob) among those that `users` (int32) have not rated."""
+        """LogProb of the items `given` (see als_log_prob) among those that `users` (int32) have not rated.  For a user that is
+        no row of x no item is allowed (log p -inf); for one that `rated` has no row of, all results are NaN."""
         z = als_predict(self.ctx, self.x, self.theta, users, None, self.item_offset, stream=stream)
         return als_log_prob(self.ctx, z, given, temperature, top, log=log, stream=stream, **self._left_out(users))
 
