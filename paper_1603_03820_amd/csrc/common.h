@@ -30,6 +30,9 @@ __device__ __forceinline__ float to_float(F16 v) {
 __device__ __forceinline__ float to_float(BF16 v) {
     return __builtin_bit_cast(float, (uint32_t)v.bits << 16);
 }
+// A score that fmaxf may meet: of a signalling NaN it may make NaN, and lose the other operand; a quiet one it leaves out.
+// (f16 scores are quiet from their conversion on.)
+__device__ __forceinline__ float quiet(float v) { return __builtin_canonicalizef(v); }
 // The nearest value of the type, ties to even.
 __device__ __forceinline__ void from_float(float v, float* out) { *out = v; }
 __device__ __forceinline__ void from_float(float v, F16* out) {

@@ -1011,12 +1011,12 @@ __device__ __forceinline__ void write_no_top(const RowArgs<T>& a, int64_t r, con
 // 1,024 x 17,770 fp32 in 19.5 us, with the 20 best 25 to 26 (73 MB: 3.8 and 2.9 TB/s); 64 x 625,000 bf16 with the join in 29
 // and 41 where the last level of cache holds the rows, in 33 and 46 where not.  Bound by waits: a workgroup's loads, lists, sums
 // and its best columns follow one another, and most workgroups are at the same one.  40 scores a thread past 16,384 took the
-// least time (1,024 x 17,770 with the best: 32 a thread 36 us, 40 27, 48 29, 64 42 at the time).  At 78 registers a SIMD has
+// least time (1,024 x 17,770 with the best: 32 a thread 36 us, 40 27, 48 29, 64 42 at the time).  At 80 registers a SIMD has
 // six of its waves, so a CU three rows of 17,770 (seven waves each), and 1,024 rows take two rounds, the second a third full.
 // Segments of 20,480 columns (64 x 625,000 bf16: 45.8 us; 8,192 49.0, 16,384 49.4, 32,768 59.0); fewer rows have segments as
 // long, and leave CUs idle: one row of 625,000 is 31 workgroups.
 template <typename T, int E>
-__global__ __launch_bounds__(1024, E <= 16 || sizeof(T) == 2 ? 8 : 5) void k_row(RowArgs<T> a) {
+__global__ __launch_bounds__(1024, E <= 16 || sizeof(T) == 2 ? 8 : 6) void k_row(RowArgs<T> a) {
     constexpr int V = E * sizeof(T) < 16 ? E : 16 / sizeof(T);
     __shared__ RowShared sh;
     extern __shared__ uint32_t bits[];
@@ -1039,6 +1039,8 @@ __global__ __launch_bounds__(1024, E <= 16 || sizeof(T) == 2 ? 8 : 5) void k_row
     const uint32_t out0 = some && threadIdx.x < listed ? (uint32_t)list[threadIdx.x] - base : ~0u;
     const bool asked = begin + threadIdx.x < end;
     const uint32_t column0 = asked ? (uint32_t)a.given.idx[begin + threadIdx.x] : ~0u;
+    // (scores of 16 bits are quiet from here on, fp32 ones once they have arrived: a loop here would wait for each load)
+    const auto score = [](T t) { return sizeof(T) == 2 ? quiet(to_float(t)) : to_float(t); };
     float z[E];
 #pragma unroll
     for (int v = 0; v < E / V; ++v) {
@@ -1047,10 +1049,10 @@ __global__ __launch_bounds__(1024, E <= 16 || sizeof(T) == 2 ? 8 : 5) void k_row
         if (c + V <= n) {
             __builtin_memcpy(t, row + c, sizeof t);
 #pragma unroll
-            for (int i = 0; i < V; ++i) z[v * V + i] = to_float(t[i]);
+            for (int i = 0; i < V; ++i) z[v * V + i] = score(t[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < V; ++i) z[v * V + i] = c + i < n ? to_float(row[c + i]) : -INFINITY;
+            for (int i = 0; i < V; ++i) z[v * V + i] = c + i < n ? score(row[c + i]) : -INFINITY;
         }
     }
     const float score0 = column0 - base < n ? to_float(row[column0 - base]) : 0.f;
@@ -1079,6 +1081,10 @@ __global__ __launch_bounds__(1024, E <= 16 || sizeof(T) == 2 ? 8 : 5) void k_row
 
     const float c = law.greedy() ? 1.f : rate_of(law.t);
     Mass mass{-INFINITY, 0.f, 0.f};
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) z[e] = quiet(z[e]);
+    }
 #pragma unroll
     for (int e = 0; e < E; ++e) mass.best = fmaxf(mass.best, z[e]);
     const uint32_t own = mass.best > -INFINITY ? key_of(mass.best) : 0;

@@ -83,3 +83,30 @@ def test_fit_offsets_against_64_bits(ctx, with_rated, batch):  # noqa: F811
     assert means == pytest.approx(want[:3], abs=2 * off / t + 1e-4)
     means = whole.fit_offsets(dev(who), dev(what), t, 8, 0.5, batch)
     assert all(b > a for a, b in zip(means, means[1:]))
+
+
+@pytest.mark.parametrize("dtype,nans", [("f32", [0x7F800001, 0x7FC00000, 0x7F80FFFF, -1, -0x7FFFFF, -0x400000]),
+                                        ("f16", [0x7C01, 0x7E00, 0x7FFF, -1, -0x3FF]), ("bf16", [0x7F81, 0x7FC0, 0x7FFF, -1, -0x7F])])
+@pytest.mark.parametrize("n", [300, 20_000, 40_000])
+def test_every_kind_of_nan_is_left_out(ctx, dtype, nans, n):  # noqa: F811
+    """Quiet and signalling ones of both signs, at the best columns of a row and in most of another, give the bits that
+    -inf gives in their places."""
+    from paper_1603_03820_amd import predict
+    rng = np.random.default_rng(n)
+    z = dev((2 * rng.standard_normal((3, n))).astype(np.float32), TYPES[dtype])
+    least = z.clone()
+    bits = z.view(torch.int32 if dtype == "f32" else torch.int16)
+    values = torch.tensor(nans, dtype=bits.dtype, device=D)
+    at = [torch.topk(z[0].float(), 40).indices, torch.arange(n - 5, device=D), torch.arange(0, n, 2, device=D)]
+    for row, columns in enumerate(at):
+        bits[row, columns] = values[torch.arange(columns.numel(), device=D) % values.numel()]
+        least[row, columns] = float("-inf")
+    given = dev(rng.integers(0, n, (3, 5)).astype(np.int32))
+    given[:, 0] = torch.stack([c[0] for c in at]).int()
+    log(f"NaN of every kind, {dtype}, {n} columns")
+    got, want = (predict.als_log_prob(ctx, s, given, 0.7, 9) for s in (z, least))
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    ones, h = torch.ones(3, 5, device=D), torch.ones(3, device=D)
+    got, want = (predict.als_log_prob_grad(ctx, s, given, want, ones, h, 0.7, columns=True) for s in (z, least))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
