@@ -606,7 +606,8 @@ struct Held {
     // A thread's largest score, and the workgroup's.
     __device__ __forceinline__ float largest(float* best) {
         float mine = -INFINITY;
-        each_at_once([&](float k, uint32_t) { mine = fmaxf(mine, k); });
+        // (scores may be signalling NaN; everything else compares them, or takes sums of them)
+        each_at_once([&](float k, uint32_t) { mine = fmaxf(mine, quiet(k)); });
         float hi = wave_max(mine);
         if (waves > 1) {
             if (lane() == 0) sh->wave_a[wave()] = hi;
